@@ -480,6 +480,97 @@ int trimmoe_train_exit_head(int32_t dtype, int32_t d_model, int32_t n_rows, cons
                             const uint8_t* labels, int32_t epochs, float lr, float* w, float* c,
                             float* loss, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Training losses.  Device memory, caller-owned; work is enqueued on `stream`;
+ * arguments are checked before anything is enqueued.  dtype is that of the
+ * weights, the rows and their gradients (bf16: d_model a multiple of 64, those
+ * arrays 16-byte aligned; fp32: any d_model); everything else is fp32 or an
+ * integer.  Arrays of n_rows rows may be NULL when n_rows is 0; a gradient
+ * that is NULL is not computed.  Workspaces are 256-byte aligned, of the size
+ * that the call's _workspace_size function gives for the same dimensions.
+ * n_rows <= TRIMMOE_LOSS_MAX_ROWS, vocab <= TRIMMOE_LOSS_MAX_VOCAB, d_model <=
+ * TRIMMOE_LOSS_MAX_D.  Sums run in a fixed order: repeated calls give identical
+ * results.  A NaN (or infinite) logit makes its row's results NaN.
+ */
+#define TRIMMOE_LOSS_MAX_ROWS (1 << 22)
+#define TRIMMOE_LOSS_MAX_VOCAB (1 << 28)
+#define TRIMMOE_LOSS_MAX_D (1 << 20)
+
+/*
+ * Cross entropy of a vocabulary head (a softmax exit head of Eq. (7), or the
+ * output head): z = w_head h + b_head (b_head fp32 [V] or NULL),
+ *   lse[q]  = log sum_v exp z[q][v],
+ *   loss[q] = lse[q] - z[q][target[q]].
+ * target int32 [n_rows] (trimmoe_head_argmax's predictions, or token ids); a
+ * row whose target lies outside [0, V) takes no part: its loss is 0 and its
+ * lse is written all the same.  A bias of -inf leaves a vocabulary row out; a
+ * row q with no logit above -inf (lse -inf) takes no part either.  The logits
+ * are never kept.
+ */
+int trimmoe_head_cross_entropy_workspace_size(int32_t dtype, int32_t vocab, int32_t d_model,
+                                              int32_t n_rows, size_t* bytes);
+int trimmoe_head_cross_entropy(int32_t dtype, int32_t vocab, int32_t d_model, int32_t n_rows,
+                               const void* w_head, const float* b_head, const void* h,
+                               const int32_t* target, float* loss, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum_q dloss[q] loss[q] (dloss fp32 [n_rows]: the weight of each
+ * row, as 1 / n of a mean): with D[q][v] = dloss[q] (exp(z[q][v] - lse[q]) -
+ * (v == target[q])), zero in rows that take no part,
+ *   dh [n_rows, d] = D w_head,  dw_head [V, d] = D^T h,  db_head [V] = sum_q D.
+ * lse as trimmoe_head_cross_entropy wrote it for the same inputs.  The logits
+ * are computed again in pieces of the vocabulary; the workspace holds D of one
+ * piece.  Gradients are written, not added to what is there; dh and dw_head may
+ * not overlap any input.  bf16: D is rounded to bf16 before the two products
+ * (by at most 2^-8 of each entry, as the results are), db_head sums it before.
+ */
+int trimmoe_head_cross_entropy_backward_workspace_size(int32_t dtype, int32_t vocab, int32_t d_model,
+                                                       int32_t n_rows, size_t* bytes);
+int trimmoe_head_cross_entropy_backward(int32_t dtype, int32_t vocab, int32_t d_model,
+                                        int32_t n_rows, const void* w_head, const float* b_head,
+                                        const void* h, const int32_t* target, const float* lse,
+                                        const float* dloss, void* dh, void* dw_head, float* db_head,
+                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Balance loss of a router, with the load of its experts.  target int16
+ * [n_rows, top_k] holds the routed experts as a trace records them
+ * (trace->target or trace->exec; an entry outside [0, E) is no slot, as the -1
+ * of inactive tokens and skipped layers):
+ *   prob[q]      = softmax(w_router h[q] + b_router)             [n_rows, E]
+ *   counts[e]    = slots that hold expert e; counts[E] = n, the rows with a
+ *                  slot                                          int32 [E + 1]
+ *   prob_sum[e]  = sum of prob[q][e] over those rows             [E]
+ *   loss         = E / (S n) sum_e counts[e] prob_sum[e],  S = sum_e counts[e]
+ * (1 for an even load, 0 for no slots).  prob is written for every row; a row
+ * without a logit above -inf has prob 0.
+ */
+int trimmoe_balance_loss_workspace_size(int32_t dtype, int32_t n_experts, int32_t top_k,
+                                        int32_t d_model, int32_t n_rows, size_t* bytes);
+int trimmoe_balance_loss(int32_t dtype, int32_t n_experts, int32_t top_k, int32_t d_model,
+                         int32_t n_rows, const void* w_router, const float* b_router, const void* h,
+                         const int16_t* target, float* loss, int32_t* counts, float* prob_sum,
+                         float* prob, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of dloss[0] * loss with the counts held constant (they have no
+ * derivative): with dz[q][e] = dloss[0] E / (S n) prob[q][e] (counts[e] - sum_j
+ * prob[q][j] counts[j]), zero in rows without a slot,
+ *   dh [n_rows, d] = dz w_router,  dw_router [E, d] = dz^T h,  db_router [E] =
+ *   sum_q dz.
+ * prob and counts as trimmoe_balance_loss wrote them.  counts summed over
+ * several ranks' batches give this batch's share of the gradient of their
+ * joint loss.  Gradients are written, not added to what is there.
+ */
+int trimmoe_balance_loss_backward_workspace_size(int32_t dtype, int32_t n_experts, int32_t top_k,
+                                                 int32_t d_model, int32_t n_rows, size_t* bytes);
+int trimmoe_balance_loss_backward(int32_t dtype, int32_t n_experts, int32_t top_k, int32_t d_model,
+                                  int32_t n_rows, const void* w_router, const void* h,
+                                  const int16_t* target, const float* prob, const int32_t* counts,
+                                  const float* dloss, void* dh, void* dw_router, float* db_router,
+                                  void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -76,7 +76,12 @@ EXPORTS = ["trimmoe_abi_version", "trimmoe_status_str", "trimmoe_workspace_size"
            "trimmoe_place_replicas", "trimmoe_head_argmax_workspace_size",
            "trimmoe_head_argmax", "trimmoe_consistency_labels",
            "trimmoe_train_exit_head_workspace_size",
-           "trimmoe_train_exit_head"]
+           "trimmoe_train_exit_head",
+           "trimmoe_head_cross_entropy_workspace_size", "trimmoe_head_cross_entropy",
+           "trimmoe_head_cross_entropy_backward_workspace_size",
+           "trimmoe_head_cross_entropy_backward",
+           "trimmoe_balance_loss_workspace_size", "trimmoe_balance_loss",
+           "trimmoe_balance_loss_backward_workspace_size", "trimmoe_balance_loss_backward"]
 TIMED_CLASSES = ["route", "bucket", "up", "down", "shared", "combine", "exit", "gate"]
 
 _lib = None
@@ -144,6 +149,21 @@ def lib():
         L.trimmoe_train_exit_head.restype = C.c_int
         L.trimmoe_train_exit_head.argtypes = [i32, i32, i32, p, p, i32, f32, p, p, p, p,
                                               C.c_size_t, p]
+        size, out = C.c_size_t, C.POINTER(C.c_size_t)
+        for name in ("trimmoe_head_cross_entropy", "trimmoe_head_cross_entropy_backward"):
+            getattr(L, name + "_workspace_size").restype = C.c_int
+            getattr(L, name + "_workspace_size").argtypes = [i32, i32, i32, i32, out]
+        L.trimmoe_head_cross_entropy.restype = C.c_int
+        L.trimmoe_head_cross_entropy.argtypes = [i32] * 4 + [p] * 7 + [size, p]
+        L.trimmoe_head_cross_entropy_backward.restype = C.c_int
+        L.trimmoe_head_cross_entropy_backward.argtypes = [i32] * 4 + [p] * 10 + [size, p]
+        for name in ("trimmoe_balance_loss", "trimmoe_balance_loss_backward"):
+            getattr(L, name + "_workspace_size").restype = C.c_int
+            getattr(L, name + "_workspace_size").argtypes = [i32, i32, i32, i32, i32, out]
+        L.trimmoe_balance_loss.restype = C.c_int
+        L.trimmoe_balance_loss.argtypes = [i32] * 5 + [p] * 9 + [size, p]
+        L.trimmoe_balance_loss_backward.restype = C.c_int
+        L.trimmoe_balance_loss_backward.argtypes = [i32] * 5 + [p] * 10 + [size, p]
         if L.trimmoe_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} has ABI version {L.trimmoe_abi_version()}, the "
                                f"binding expects {ABI_VERSION}: rebuild it")
@@ -389,6 +409,137 @@ def trimmoe_train_exit_head(h: torch.Tensor, labels: torch.Tensor, epochs: int, 
            lib().trimmoe_train_exit_head(_dtype_code(h), d, Q, _ptr(h), _ptr(labels), int(epochs),
                                          float(lr), _ptr(w), _ptr(c), _ptr(loss), _ptr(ws),
                                          ws.numel(), _stream_handle(stream)))
+
+
+# ------------------------------------------------------- training losses ---
+def _on_stream(t: torch.Tensor, stream):
+    """Context in which outputs and workspaces belong to the stream that the
+    call runs on (`stream`, or the current one of t's device)."""
+    if not t.is_cuda:
+        raise ValueError("the training losses run on GPU tensors")
+    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(t.device))
+
+
+def _take(name: str, t: torch.Tensor, shape, dtype, device):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device \
+            or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} "
+                         f"is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t
+
+
+def _rows_and_weights(w: torch.Tensor, h: torch.Tensor):
+    code = _dtype_code(h)
+    if w.dim() != 2 or h.dim() != 2:
+        raise ValueError("the weights are [V, d] (or [E, d]) and the rows [n, d]")
+    _take("weights", w, (w.shape[0], h.shape[1]), h.dtype, h.device)
+    _take("rows", h, h.shape, h.dtype, h.device)
+    return code, w.shape[0], h.shape[1], h.shape[0]
+
+
+def _loss_ws(name: str, dims, device) -> torch.Tensor:
+    n = C.c_size_t(0)
+    _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(*dims, C.byref(n)))
+    return _aligned_ws(max(n.value, 256), device)
+
+
+def trimmoe_head_cross_entropy(w_head: torch.Tensor, h: torch.Tensor, target: torch.Tensor,
+                               b_head=None, stream=None):
+    """(loss fp32 [Q], lse fp32 [Q]) of the head w_head [V, d] (bias fp32 [V])
+    on rows h [Q, d] against target int32 [Q]; a target outside [0, V) is
+    ignored (loss 0)."""
+    dt, V, d, Q = _rows_and_weights(w_head, h)
+    dev = h.device
+    _take("target", target, (Q,), torch.int32, dev)
+    if b_head is not None:
+        _take("b_head", b_head, (V,), torch.float32, dev)
+    with _on_stream(h, stream):
+        loss = torch.empty(Q, dtype=torch.float32, device=dev)
+        lse = torch.empty(Q, dtype=torch.float32, device=dev)
+        ws = _loss_ws("trimmoe_head_cross_entropy", (dt, V, d, Q), dev)
+        _check("trimmoe_head_cross_entropy",
+               lib().trimmoe_head_cross_entropy(dt, V, d, Q, _ptr(w_head), _ptr(b_head), _ptr(h),
+                                                _ptr(target), _ptr(loss), _ptr(lse), _ptr(ws),
+                                                ws.numel(), _stream_handle(None)))
+    return loss, lse
+
+
+def trimmoe_head_cross_entropy_backward(w_head: torch.Tensor, h: torch.Tensor,
+                                        target: torch.Tensor, lse: torch.Tensor,
+                                        dloss: torch.Tensor, b_head=None, want_dh=True,
+                                        want_dw=True, stream=None):
+    """Gradients (dh [Q, d], dw [V, d], db fp32 [V]) of sum(dloss * loss), dloss
+    fp32 [Q], lse from trimmoe_head_cross_entropy; None for one that is not
+    wanted (db: without a bias)."""
+    dt, V, d, Q = _rows_and_weights(w_head, h)
+    dev = h.device
+    _take("target", target, (Q,), torch.int32, dev)
+    _take("lse", lse, (Q,), torch.float32, dev)
+    _take("dloss", dloss, (Q,), torch.float32, dev)
+    if b_head is not None:
+        _take("b_head", b_head, (V,), torch.float32, dev)
+    with _on_stream(h, stream):
+        dh = torch.empty_like(h) if want_dh else None
+        dw = torch.empty_like(w_head) if want_dw else None
+        db = None if b_head is None else torch.empty_like(b_head)
+        ws = _loss_ws("trimmoe_head_cross_entropy_backward", (dt, V, d, Q), dev)
+        _check("trimmoe_head_cross_entropy_backward",
+               lib().trimmoe_head_cross_entropy_backward(
+                   dt, V, d, Q, _ptr(w_head), _ptr(b_head), _ptr(h), _ptr(target), _ptr(lse),
+                   _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(db), _ptr(ws), ws.numel(),
+                   _stream_handle(None)))
+    return dh, dw, db
+
+
+def trimmoe_balance_loss(w_router: torch.Tensor, h: torch.Tensor, target: torch.Tensor,
+                         b_router=None, stream=None):
+    """(loss fp32 [1], counts int32 [E + 1], prob_sum fp32 [E], prob fp32
+    [Q, E]) of the router w_router [E, d] (bias fp32 [E]) on rows h [Q, d] with
+    the routed experts target int16 [Q, k] (-1: none); counts[E] is the number
+    of rows with a routed slot."""
+    dt, E, d, Q = _rows_and_weights(w_router, h)
+    dev = h.device
+    k = target.shape[1] if target.dim() == 2 else 0
+    _take("target", target, (Q, k), torch.int16, dev)
+    if b_router is not None:
+        _take("b_router", b_router, (E,), torch.float32, dev)
+    with _on_stream(h, stream):
+        f = dict(dtype=torch.float32, device=dev)
+        loss, prob_sum = torch.empty(1, **f), torch.empty(E, **f)
+        prob = torch.empty(Q, E, **f)
+        counts = torch.empty(E + 1, dtype=torch.int32, device=dev)
+        ws = _loss_ws("trimmoe_balance_loss", (dt, E, k, d, Q), dev)
+        _check("trimmoe_balance_loss",
+               lib().trimmoe_balance_loss(dt, E, k, d, Q, _ptr(w_router), _ptr(b_router), _ptr(h),
+                                          _ptr(target), _ptr(loss), _ptr(counts), _ptr(prob_sum),
+                                          _ptr(prob), _ptr(ws), ws.numel(), _stream_handle(None)))
+    return loss, counts, prob_sum, prob
+
+
+def trimmoe_balance_loss_backward(w_router: torch.Tensor, h: torch.Tensor, target: torch.Tensor,
+                                  prob: torch.Tensor, counts: torch.Tensor, dloss: torch.Tensor,
+                                  want_dh=True, want_dw=True, want_db=True, stream=None):
+    """Gradients (dh [Q, d], dw [E, d], db fp32 [E]) of dloss * loss (dloss fp32
+    [1]) with prob and counts from trimmoe_balance_loss (counts may be summed
+    over ranks); None for one that is not wanted."""
+    dt, E, d, Q = _rows_and_weights(w_router, h)
+    dev = h.device
+    k = target.shape[1] if target.dim() == 2 else 0
+    _take("target", target, (Q, k), torch.int16, dev)
+    _take("prob", prob, (Q, E), torch.float32, dev)
+    _take("counts", counts, (E + 1,), torch.int32, dev)
+    _take("dloss", dloss, (1,), torch.float32, dev)
+    with _on_stream(h, stream):
+        dh = torch.empty_like(h) if want_dh else None
+        dw = torch.empty_like(w_router) if want_dw else None
+        db = torch.empty(E, dtype=torch.float32, device=dev) if want_db else None
+        ws = _loss_ws("trimmoe_balance_loss_backward", (dt, E, k, d, Q), dev)
+        _check("trimmoe_balance_loss_backward",
+               lib().trimmoe_balance_loss_backward(
+                   dt, E, k, d, Q, _ptr(w_router), _ptr(h), _ptr(target), _ptr(prob), _ptr(counts),
+                   _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(db), _ptr(ws), ws.numel(),
+                   _stream_handle(None)))
+    return dh, dw, db
 
 
 # ------------------------------------------------ struct construction ------

@@ -16,6 +16,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "loss.h"
 
 using namespace trimmoe;
 
@@ -665,6 +666,213 @@ int trimmoe_train_exit_head(int32_t dtype, int32_t d_model, int32_t n_rows, cons
                         loss ? loss + e : nullptr, st) != hipSuccess)
       return TRIMMOE_ERR_HIP;
   return TRIMMOE_OK;
+}
+
+// -------------------------------------------------------- training losses --
+namespace {
+bool aligned_rows(bool bf16, const void* p) {
+  return (reinterpret_cast<uintptr_t>(p) & (bf16 ? 15 : 3)) == 0;
+}
+int loss_dims(int dtype, int d, int n_rows) {
+  if (dtype != TRIMMOE_F32 && dtype != TRIMMOE_BF16) return TRIMMOE_ERR_DTYPE;
+  if (n_rows < 0 || n_rows > TRIMMOE_LOSS_MAX_ROWS || d > TRIMMOE_LOSS_MAX_D ||
+      !head_dims_ok(dtype, d))
+    return TRIMMOE_ERR_SHAPE;
+  return TRIMMOE_OK;
+}
+int head_loss_dims(int dtype, int vocab, int d, int n_rows) {
+  const int rc = loss_dims(dtype, d, n_rows);
+  if (rc) return rc;
+  return vocab < 1 || vocab > TRIMMOE_LOSS_MAX_VOCAB ? TRIMMOE_ERR_SHAPE : TRIMMOE_OK;
+}
+int balance_dims(int dtype, int E, int k, int d, int n_rows) {
+  const int rc = loss_dims(dtype, d, n_rows);
+  if (rc) return rc;
+  return E < 1 || E > TRIMMOE_MAX_EXPERTS || k < 1 || k > TRIMMOE_MAX_TOPK || k > E
+             ? TRIMMOE_ERR_SHAPE
+             : TRIMMOE_OK;
+}
+int check_ws(const void* ws, size_t bytes, size_t need) {
+  return (reinterpret_cast<uintptr_t>(ws) & 255) || bytes < need ? TRIMMOE_ERR_WORKSPACE
+                                                                 : TRIMMOE_OK;
+}
+// compute units of the current device (persistent grids)
+int device_cus(int* n_cu) {
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(n_cu, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess)
+    return TRIMMOE_ERR_HIP;
+  return TRIMMOE_OK;
+}
+}  // namespace
+
+int trimmoe_head_cross_entropy_workspace_size(int32_t dtype, int32_t vocab, int32_t d_model,
+                                              int32_t n_rows, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  const int rc = head_loss_dims(dtype, vocab, d_model, n_rows);
+  if (rc) return rc;
+  *bytes = head_loss_ws(dtype == TRIMMOE_BF16, vocab, d_model, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_head_cross_entropy(int32_t dtype, int32_t vocab, int32_t d_model, int32_t n_rows,
+                               const void* w_head, const float* b_head, const void* h,
+                               const int32_t* target, float* loss, float* lse, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (!w_head || !workspace) return TRIMMOE_ERR_NULL;
+  if (n_rows != 0 && (!h || !target || !loss || !lse)) return TRIMMOE_ERR_NULL;
+  int rc = head_loss_dims(dtype, vocab, d_model, n_rows);
+  if (rc) return rc;
+  const bool bf16 = dtype == TRIMMOE_BF16;
+  if (!aligned_rows(bf16, w_head) || !aligned_rows(bf16, h)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes, head_loss_ws(bf16, vocab, d_model, n_rows))))
+    return rc;
+  if (n_rows == 0) return TRIMMOE_OK;
+  HeadLossArgs a{};
+  if ((rc = device_cus(&a.n_cu))) return rc;
+  a.bf16 = bf16;
+  a.V = vocab;
+  a.d = d_model;
+  a.T = n_rows;
+  a.w = w_head;
+  a.b = b_head;
+  a.h = h;
+  a.target = target;
+  a.loss = loss;
+  a.lse = lse;
+  a.ws = static_cast<char*>(workspace);
+  return launch_head_loss(a, static_cast<hipStream_t>(stream)) == hipSuccess ? TRIMMOE_OK
+                                                                             : TRIMMOE_ERR_HIP;
+}
+
+int trimmoe_head_cross_entropy_backward_workspace_size(int32_t dtype, int32_t vocab, int32_t d_model,
+                                                       int32_t n_rows, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  const int rc = head_loss_dims(dtype, vocab, d_model, n_rows);
+  if (rc) return rc;
+  *bytes = head_loss_backward_ws(dtype == TRIMMOE_BF16, vocab, d_model, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_head_cross_entropy_backward(int32_t dtype, int32_t vocab, int32_t d_model,
+                                        int32_t n_rows, const void* w_head, const float* b_head,
+                                        const void* h, const int32_t* target, const float* lse,
+                                        const float* dloss, void* dh, void* dw_head, float* db_head,
+                                        void* workspace, size_t workspace_bytes, void* stream) {
+  if (!w_head || !workspace) return TRIMMOE_ERR_NULL;
+  if (n_rows != 0 && (!h || !target || !lse || !dloss)) return TRIMMOE_ERR_NULL;
+  int rc = head_loss_dims(dtype, vocab, d_model, n_rows);
+  if (rc) return rc;
+  const bool bf16 = dtype == TRIMMOE_BF16;
+  for (const void* p : {w_head, h, static_cast<const void*>(dh), static_cast<const void*>(dw_head)})
+    if (!aligned_rows(bf16, p)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes,
+                     head_loss_backward_ws(bf16, vocab, d_model, n_rows))))
+    return rc;
+  if (!dh && !dw_head && !db_head) return TRIMMOE_OK;
+  HeadLossArgs a{};
+  if ((rc = device_cus(&a.n_cu))) return rc;
+  a.bf16 = bf16;
+  a.V = vocab;
+  a.d = d_model;
+  a.T = n_rows;
+  a.w = w_head;
+  a.b = b_head;
+  a.h = h;
+  a.target = target;
+  a.lse = const_cast<float*>(lse);
+  a.dloss = dloss;
+  a.dh = n_rows > 0 ? dh : nullptr;
+  a.dw = dw_head;
+  a.db = db_head;
+  a.ws = static_cast<char*>(workspace);
+  return launch_head_loss_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? TRIMMOE_OK
+             : TRIMMOE_ERR_HIP;
+}
+
+int trimmoe_balance_loss_workspace_size(int32_t dtype, int32_t n_experts, int32_t top_k,
+                                        int32_t d_model, int32_t n_rows, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  const int rc = balance_dims(dtype, n_experts, top_k, d_model, n_rows);
+  if (rc) return rc;
+  *bytes = balance_ws(n_experts, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_balance_loss(int32_t dtype, int32_t n_experts, int32_t top_k, int32_t d_model,
+                         int32_t n_rows, const void* w_router, const float* b_router, const void* h,
+                         const int16_t* target, float* loss, int32_t* counts, float* prob_sum,
+                         float* prob, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!w_router || !loss || !counts || !prob_sum || !workspace) return TRIMMOE_ERR_NULL;
+  if (n_rows != 0 && (!h || !target || !prob)) return TRIMMOE_ERR_NULL;
+  int rc = balance_dims(dtype, n_experts, top_k, d_model, n_rows);
+  if (rc) return rc;
+  const bool bf16 = dtype == TRIMMOE_BF16;
+  if (!aligned_rows(bf16, w_router) || !aligned_rows(bf16, h)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes, balance_ws(n_experts, n_rows)))) return rc;
+  BalanceArgs a{};
+  a.bf16 = bf16;
+  a.E = n_experts;
+  a.k = top_k;
+  a.d = d_model;
+  a.T = n_rows;
+  a.w = w_router;
+  a.b = b_router;
+  a.h = h;
+  a.target = target;
+  a.prob = prob;
+  a.counts = counts;
+  a.prob_sum = prob_sum;
+  a.loss = loss;
+  a.ws = static_cast<char*>(workspace);
+  return launch_balance(a, static_cast<hipStream_t>(stream)) == hipSuccess ? TRIMMOE_OK
+                                                                           : TRIMMOE_ERR_HIP;
+}
+
+int trimmoe_balance_loss_backward_workspace_size(int32_t dtype, int32_t n_experts, int32_t top_k,
+                                                 int32_t d_model, int32_t n_rows, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  const int rc = balance_dims(dtype, n_experts, top_k, d_model, n_rows);
+  if (rc) return rc;
+  *bytes = balance_backward_ws(n_experts, d_model, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_balance_loss_backward(int32_t dtype, int32_t n_experts, int32_t top_k, int32_t d_model,
+                                  int32_t n_rows, const void* w_router, const void* h,
+                                  const int16_t* target, const float* prob, const int32_t* counts,
+                                  const float* dloss, void* dh, void* dw_router, float* db_router,
+                                  void* workspace, size_t workspace_bytes, void* stream) {
+  if (!w_router || !counts || !dloss || !workspace) return TRIMMOE_ERR_NULL;
+  if (n_rows != 0 && (!h || !target || !prob)) return TRIMMOE_ERR_NULL;
+  int rc = balance_dims(dtype, n_experts, top_k, d_model, n_rows);
+  if (rc) return rc;
+  const bool bf16 = dtype == TRIMMOE_BF16;
+  for (const void* p : {w_router, h, static_cast<const void*>(dh), static_cast<const void*>(dw_router)})
+    if (!aligned_rows(bf16, p)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes, balance_backward_ws(n_experts, d_model, n_rows))))
+    return rc;
+  if (!dh && !dw_router && !db_router) return TRIMMOE_OK;
+  BalanceArgs a{};
+  a.bf16 = bf16;
+  a.E = n_experts;
+  a.k = top_k;
+  a.d = d_model;
+  a.T = n_rows;
+  a.w = w_router;
+  a.h = h;
+  a.target = target;
+  a.prob = const_cast<float*>(prob);
+  a.counts = const_cast<int32_t*>(counts);
+  a.dloss = dloss;
+  a.dh = n_rows > 0 ? dh : nullptr;
+  a.dw = dw_router;
+  a.db = db_router;
+  a.ws = static_cast<char*>(workspace);
+  return launch_balance_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess
+             ? TRIMMOE_OK
+             : TRIMMOE_ERR_HIP;
 }
 
 }  // extern "C"

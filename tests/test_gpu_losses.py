@@ -1,0 +1,618 @@
+"""GPU parity of the training losses through the C ABI: the cross entropy of a
+vocabulary head and the balance loss of a router, each with its gradients,
+against the fp64 oracle on the same stored values.
+
+Every tolerance is an error bound of the stated arithmetic, element by element:
+u = 2^-24 is half a step of fp32, and a sum of K products in any order is off by
+at most (K + 8) u times the sum of their magnitudes.  Outputs in bf16 add half a
+step of bf16, 2^-8 of the value, and so does every entry of D that the bf16
+path rounds before its products.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import losses as X
+from paper_2608_00573_amd import abi
+from synthgen import make_inputs, workload
+from synthgen.rng import normal_f32
+
+from gpu_harness import GpuRun, gpu_trace_np, log
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TINY = 1e-30
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _mat(seed, tid, shape, sigma, dtype):
+    t = normal_f32(seed, tid, shape, sigma, "cpu").to(dtype)
+    return t, t.double().numpy()
+
+
+def _within(got, want, bound, what):
+    got = got.double().cpu().numpy() if isinstance(got, torch.Tensor) else np.asarray(got)
+    want = np.asarray(want, np.float64)
+    assert got.shape == want.shape, what
+    with np.errstate(invalid="ignore"):  # (equal infinities)
+        bad = ~(np.abs(got - want) <= bound)
+    bad &= ~(np.isnan(got) & np.isnan(want)) & ~(got == want)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(),
+                           got[bad][:4], want[bad][:4])
+
+
+def _logit_bound(W, H, b):
+    """Largest error of a logit of each row."""
+    d = W.shape[1]
+    mag = np.abs(H) @ np.abs(W).T
+    if b is not None:
+        mag = mag + np.where(np.isfinite(b), np.abs(b), 0.0)
+    return ((d + 9) * U * mag).max(axis=1)
+
+
+def _lse_bound(W, H, b, lse):
+    """... and of its log-sum-exp: the logits' error, exponentials of arguments
+    up to the row's spread R (argument rounding, in base 2 a product more, and
+    4 u of the function), the longest chain of the sum (V / 64 + 300 terms of one
+    thread or of a join) and the log's own rounding."""
+    z = X.logits(W, H, b)
+    R = np.where(np.isfinite(z), np.abs(z), 0.0).max(axis=1) * 2
+    lse = np.where(np.isfinite(lse), np.abs(lse), 0.0)
+    return _logit_bound(W, H, b) + U * (W.shape[0] / 64 + 308 + 4 * R + 4 * lse)
+
+
+class Head:
+    """One call's inputs, on the GPU and as fp64."""
+
+    def __init__(self, seed, dtype, V, d, Q, bias=True, ignored=0.2, sigma=None):
+        r = np.random.default_rng(seed)
+        self.W, self.Wn = _mat(seed, 1, (V, d), d ** -0.5 if sigma is None else sigma, dtype)
+        self.H, self.Hn = _mat(seed, 2, (Q, d), 2.0, dtype)
+        self.b = r.normal(size=V).astype(np.float32) if bias else None
+        self.y = r.integers(0, V, size=Q).astype(np.int32)
+        off = r.random(Q) < ignored
+        self.y[off] = r.choice([-1, V, -2 ** 31, 2 ** 31 - 1], size=int(off.sum()))
+        self.g = (r.normal(size=Q) * r.choice([1e-3, 1.0, 0.0], size=Q)).astype(np.float32)
+
+    def dev(self):
+        self.Wd, self.Hd = self.W.to(DEV), self.H.to(DEV)
+        self.bd = None if self.b is None else torch.from_numpy(self.b).to(DEV)
+        self.yd, self.gd = torch.from_numpy(self.y).to(DEV), torch.from_numpy(self.g).to(DEV)
+        return self
+
+    def forward(self, stream=None):
+        return abi.trimmoe_head_cross_entropy(self.Wd, self.Hd, self.yd, self.bd, stream=stream)
+
+    def backward(self, lse, **kw):
+        return abi.trimmoe_head_cross_entropy_backward(self.Wd, self.Hd, self.yd, lse, self.gd,
+                                                       self.bd, **kw)
+
+    def check_forward(self, loss, lse, what=""):
+        want, wl = X.head_loss(self.Wn, self.Hn, self.y, self.b)
+        e = _lse_bound(self.Wn, self.Hn, self.b, wl)
+        _within(lse, wl, e, what + "lse")
+        _within(loss, want, e + _logit_bound(self.Wn, self.Hn, self.b) + 4 * U * np.abs(want),
+                what + "loss")
+
+    def check_backward(self, got, what=""):
+        """D is off by |g| p times the error of the exponent (logit, lse, the
+        exponential), and in the bf16 path by half a step; the products add their
+        sums' rounding and half a step of the output's type."""
+        dh, dw, db = got
+        D, p, live = X.head_loss_d(self.Wn, self.Hn, self.y, self.g, self.b)
+        Hl = np.where(live[:, None], self.Hn, 0.0)
+        _, lse = X.head_loss(self.Wn, self.Hn, self.y, self.b)
+        z = X.logits(self.Wn, self.Hn, self.b)
+        R = np.where(np.isfinite(z), np.abs(z), 0.0).max(axis=1)
+        lse0 = np.where(np.isfinite(lse), np.abs(lse), 0.0)
+        ex = 2 * _lse_bound(self.Wn, self.Hn, self.b, lse) + U * (16 + 4 * R + 4 * lse0)
+        g = np.abs(np.where(live, self.g, 0.0))[:, None]
+        eD = g * p * ex[:, None] * 1.01 + 8 * U * np.abs(D) + 2 * U * g
+        half = torch.finfo(self.W.dtype).eps / 2
+        rD = half * (1 + half) if self.W.dtype == BF16 else 0.0
+        V, Q = D.shape[1], D.shape[0]
+        aD = np.abs(D)
+        if dh is not None:
+            want = D @ self.Wn
+            e = (eD + (rD + (V + 80) * U) * aD) @ np.abs(self.Wn) * 1.01
+            _within(dh, want, e + half * (np.abs(want) + e) + TINY, what + "dh")
+        if dw is not None:
+            want = D.T @ Hl
+            # (row weights are relative to the largest one here: an entry is a product more)
+            e = (eD + (rD + (Q + 80) * U) * aD).T @ np.abs(Hl) * 1.01
+            _within(dw, want, e + half * (np.abs(want) + e) + TINY, what + "dw")
+        if db is not None:
+            _within(db, D.sum(axis=0), (eD + (Q + 80) * U * aD).sum(axis=0) * 1.01 + TINY, what + "db")
+
+
+# (dtype, V, d, Q, bias)
+HEADS = [
+    (F32, 512, 64, 64, True),       # the tiny model
+    (F32, 1, 40, 3, True),          # one vocabulary row: the loss is 0
+    (F32, 2, 1, 1, False),          # the smallest head
+    (F32, 1003, 41, 129, True),     # rows that are not whole vectors
+    (F32, 300, 97, 1000, False),
+    (F32, 5000, 264, 17, True),
+    (BF16, 512, 64, 37, True),
+    (BF16, 1, 64, 5, True),
+    (BF16, 2, 64, 1, False),
+    (BF16, 1003, 128, 1, True),     # one row
+    (BF16, 1003, 192, 16, False),
+    (BF16, 4001, 2112, 33, True),
+    (BF16, 1003, 64, 64, True),     # the last decode-sized batch
+    (BF16, 1003, 64, 65, True),     # the first one beyond
+    (BF16, 5000, 128, 300, True),
+    (BF16, 777, 768, 513, True),    # ragged tiles in every direction
+    (BF16, 255, 2048, 1030, False),
+    (BF16, 2049, 64, 2050, True),
+    (BF16, 32000, 256, 256, False),
+]
+
+
+@pytest.mark.parametrize("dtype,V,d,Q,bias", HEADS)
+def test_head_loss_matches_oracle(dtype, V, d, Q, bias):
+    log(f"[losses] head forward {dtype} V={V} d={d} Q={Q}")
+    c = Head(31, dtype, V, d, Q, bias).dev()
+    c.check_forward(*c.forward())
+
+
+@pytest.mark.parametrize("dtype,V,d,Q,bias", HEADS)
+def test_head_gradients_match_oracle(dtype, V, d, Q, bias):
+    log(f"[losses] head backward {dtype} V={V} d={d} Q={Q}")
+    c = Head(32, dtype, V, d, Q, bias).dev()
+    _, lse = c.forward()
+    c.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(F32, 20001, 64, 4100), (BF16, 40001, 64, 4100)])
+def test_head_gradients_over_several_pieces(dtype, V, d, Q):
+    # more of D than a piece holds: dh is summed over the pieces
+    log(f"[losses] head pieces {dtype}")
+    c = Head(33, dtype, V, d, Q).dev()
+    loss, lse = c.forward()
+    c.check_forward(loss, lse)
+    c.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(F32, 300, 96, 40), (BF16, 300, 128, 40),
+                                         (BF16, 700, 128, 200)])
+def test_head_gradient_is_the_difference_quotient(dtype, V, d, Q):
+    # along a random direction of stored values: W moves by s * E with entries
+    # of E in {-1, 0, 1} steps that bf16 holds exactly.  The central difference
+    # of the fp64 loss is compared with the kernel's gradient.
+    c = Head(34, dtype, V, d, Q).dev()
+    _, lse = c.forward()
+    dh, dw, db = (t.double().cpu().numpy() for t in c.backward(lse))
+    r = np.random.default_rng(5)
+    live = X.head_loss_d(c.Wn, c.Hn, c.y, c.g, c.b)[2]
+    for arr, grad, which in ((c.Wn, dw, "W"), (c.Hn, dh, "H")):
+        E = r.choice([-1.0, 0.0, 1.0], size=arr.shape)
+
+        def total(s):
+            W_ = c.Wn + s * E if which == "W" else c.Wn
+            H_ = c.Hn + s * E if which == "H" else c.Hn
+            return float(c.g.astype(np.float64) @ X.head_loss(W_, H_, c.y, c.b)[0])
+
+        s = 1e-5
+        num = (total(s) - total(-s)) / (2 * s)
+        # the difference's own error is below 1e-6 here; the gradient's entries are off by
+        # at most a step of their type (2^-7 for bf16: D's rounding and the output's, with
+        # the magnitudes of the terms in D's place), summed over the direction
+        D = X.head_loss_d(c.Wn, c.Hn, c.y, c.g, c.b)[0]
+        Hl = np.where(live[:, None], c.Hn, 0.0)
+        mag = np.abs(D).T @ np.abs(Hl) if which == "W" else np.abs(D) @ np.abs(c.Wn)
+        step = 2.0 ** -7 if dtype == BF16 else (V + d + Q + 700) * U * 4
+        bound = step * float((mag * np.abs(E)).sum()) + 1e-6 * (1 + abs(num))
+        assert abs(float((grad * E).sum()) - num) <= bound, which
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(F32, 300, 96, 40), (BF16, 1003, 64, 20),
+                                         (BF16, 1003, 128, 300)])
+def test_head_with_rows_left_out(dtype, V, d, Q):
+    # vocabulary rows of bias -inf have no probability; with all of them left
+    # out no row takes part
+    c = Head(35, dtype, V, d, Q)
+    c.b[::3] = -np.inf
+    c.y[1:4] = [0, 1, 2]
+    c.g[:] = 1.0
+    c.y[1] = 1  # (a target that is left out has an infinite loss)
+    c.dev()
+    loss, lse = c.forward()
+    keep = (c.y < 0) | (c.y >= V) | (c.y % 3 != 0)
+    want, wl = X.head_loss(c.Wn, c.Hn, c.y, c.b)
+    assert np.isposinf(loss.cpu().numpy()[~keep]).all() and np.isposinf(want[~keep]).all()
+    c.check_forward(loss, lse)
+    got = c.backward(lse)
+    c.check_backward(got)
+    left = got[1].double().cpu().numpy()[::3]
+    hit = np.isin(np.arange(0, V, 3), c.y)
+    assert (left[~hit] == 0).all()
+    c.b[:] = -np.inf
+    c.dev()
+    loss, lse = c.forward()
+    assert (loss == 0).all() and torch.isneginf(lse).all()
+    for t in c.backward(lse):
+        assert (t == 0).all()
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(F32, 300, 96, 40), (BF16, 1003, 64, 20),
+                                         (BF16, 1003, 128, 300)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_head_with_rows_of_anything(dtype, V, d, Q, bad):
+    # an ignored row's h may hold anything; a row that takes part passes it on
+    c = Head(36, dtype, V, d, Q, ignored=0.0)
+    c.y[[0, 7, Q - 1]] = [-1, V, -1]
+    c.g[:] = 1.0
+    clean = Head(36, dtype, V, d, Q, ignored=0.0)
+    clean.y, clean.g = c.y, c.g
+    c.H[[0, 7, Q - 1]] = bad
+    c.dev()
+    loss, lse = c.forward()
+    assert (loss[[0, 7, Q - 1]] == 0).all() and torch.isfinite(loss).all()
+    clean.check_backward(c.backward(lse))
+    c.Hd[3] = bad
+    loss, lse = c.forward()
+    assert torch.isnan(loss[3]) and torch.isfinite(loss[4])
+    dh, dw, db = c.backward(lse)
+    assert torch.isnan(dh[3]).all() and torch.isfinite(dh[4]).all()
+    assert torch.isnan(dw).any() and torch.isnan(db).all()
+    # a NaN weight is in every row's sum
+    c.Hd[3] = c.Hd[4]
+    c.Wd[V - 1, d - 1] = float("nan")
+    loss, lse = c.forward()
+    live = torch.from_numpy((c.y >= 0) & (c.y < V)).to(DEV)
+    assert torch.isnan(loss[live]).all() and torch.isnan(lse[live]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_head_weights_of_zero_and_wanted_gradients(dtype):
+    c = Head(37, dtype, 700, 128, 200).dev()
+    _, lse = c.forward()
+    full = c.backward(lse)
+    for kw, none in ((dict(want_dh=False), 0), (dict(want_dw=False), 1)):
+        got = c.backward(lse, **kw)
+        assert got[none] is None
+        for i in (0, 1, 2):
+            if i != none:
+                assert torch.equal(got[i], full[i])
+    c.gd.zero_()
+    for t in c.backward(lse):
+        assert (t == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_head_without_rows(dtype):
+    c = Head(38, dtype, 100, 64, 0).dev()
+    loss, lse = c.forward()
+    assert loss.shape == (0,)
+    dh, dw, db = c.backward(lse)
+    assert dh.shape == (0, 64) and (dw == 0).all() and (db == 0).all()
+
+
+def test_head_with_extreme_logits():
+    # logits of several hundred: the largest one carries the sum
+    for dtype in (F32, BF16):
+        c = Head(39, dtype, 600, 64, 70, sigma=8.0).dev()
+        loss, lse = c.forward()
+        assert float(lse.max()) > 50
+        c.check_forward(loss, lse)
+        c.check_backward(c.backward(lse))
+
+
+def test_head_with_row_weights_far_apart():
+    # one row a million times the others: dw keeps both
+    for dtype in (F32, BF16):
+        c = Head(40, dtype, 500, 128, 90, ignored=0.0)
+        c.g[:] = 1e-6
+        c.g[11] = 1.0
+        c.dev()
+        _, lse = c.forward()
+        c.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_head_with_unaligned_fp32_operands(offset):
+    c = Head(41, F32, 203, 52, 33).dev()
+
+    def moved(t):
+        buf = torch.empty(t.numel() + offset, dtype=F32, device=DEV)
+        out = buf[offset:].view(t.shape)
+        out.copy_(t)
+        assert out.data_ptr() % 16 != 0
+        return out
+
+    c.Wd, c.Hd = moved(c.Wd), moved(c.Hd)
+    loss, lse = c.forward()
+    c.check_forward(loss, lse)
+    c.check_backward(c.backward(lse))
+
+
+# ------------------------------------------------------------- balance -----
+class Router:
+    def __init__(self, seed, dtype, E, k, d, Q, bias=True, inactive=0.3, sigma=None):
+        r = np.random.default_rng(seed)
+        self.W, self.Wn = _mat(seed, 1, (E, d), 2 * d ** -0.5 if sigma is None else sigma, dtype)
+        self.H, self.Hn = _mat(seed, 2, (Q, d), 1.0, dtype)
+        self.b = r.normal(size=E).astype(np.float32) if bias else None
+        t = r.integers(0, E, size=(Q, k))
+        t[r.random((Q, k)) < 0.1] = -1                    # single slots without an expert
+        t[r.random(Q) < inactive] = -1                    # inactive rows
+        if Q > 2:
+            t[1] = E                                      # out of range: no slot either
+        self.t = t.astype(np.int16)
+        self.g = np.float32(0.37)
+
+    def dev(self):
+        self.Wd, self.Hd = self.W.to(DEV), self.H.to(DEV)
+        self.bd = None if self.b is None else torch.from_numpy(self.b).to(DEV)
+        self.td = torch.from_numpy(self.t).to(DEV)
+        self.gd = torch.full((1,), float(self.g), device=DEV)
+        return self
+
+    def forward(self, stream=None):
+        return abi.trimmoe_balance_loss(self.Wd, self.Hd, self.td, self.bd, stream=stream)
+
+    def backward(self, prob, counts, **kw):
+        return abi.trimmoe_balance_loss_backward(self.Wd, self.Hd, self.td, prob, counts, self.gd,
+                                                 **kw)
+
+    def _prob_bound(self):
+        z = X.logits(self.Wn, self.Hn, self.b)
+        R = 2 * np.where(np.isfinite(z), np.abs(z), 0.0).max(axis=1)
+        # numerator and denominator: logits, exponentials, a sum of E terms, the quotient
+        return 2 * _logit_bound(self.Wn, self.Hn, self.b) + U * (2 * (8 + 4 * R) + z.shape[1] + 4)
+
+    def check_forward(self, loss, counts, prob_sum, prob):
+        wl, wc, ws, wp = X.balance_loss(self.Wn, self.Hn, self.t, self.b)
+        assert np.array_equal(counts.cpu().numpy(), wc)
+        ep = self._prob_bound()[:, None] * wp * 1.01
+        _within(prob, wp, ep + TINY, "prob")
+        live = ((self.t >= 0) & (self.t < wp.shape[1])).any(axis=1)
+        Q = max(int(live.sum()), 1)
+        es = ep[live].sum(axis=0) + (Q + 8) * U * ws
+        _within(prob_sum, ws, es + TINY, "prob_sum")
+        E = wp.shape[1]
+        S = max(int(wc[:E].sum()), 1)
+        _within(loss, [wl], E / (S * Q) * float(wc[:E] @ es) + 8 * U * abs(wl) + TINY, "loss")
+
+    def check_backward(self, got, counts=None):
+        """dz = k p (c - s), c taken against the mean count: the error of p in the
+        factor and in s, the rounding of the sum of E terms and of three products;
+        dz enters the bf16 products within 2^-16 of its value."""
+        dh, dw, db = got
+        wh, ww, wb, dz = X.balance_grad(self.Wn, self.Hn, self.t, float(self.g), self.b, counts)
+        _, own, _, p = X.balance_loss(self.Wn, self.Hn, self.t, self.b)
+        cn = own if counts is None else np.asarray(counts)
+        E = p.shape[1]
+        c, n = cn[:E].astype(np.float64), int(cn[E])
+        if n == 0:
+            for t in got:
+                assert (t == 0).all()
+            return
+        cm = c - c.mean()
+        kk = abs(float(self.g)) * E / (c.sum() * n)
+        live = ((self.t >= 0) & (self.t < E)).any(axis=1)[:, None]
+        rp = self._prob_bound()[:, None]
+        ac = (p * np.abs(cm)).sum(axis=1, keepdims=True)       # magnitude of s
+        e_c = 2 * U * c.max()                                  # rounding of c - mean
+        ez = kk * p * (rp * (np.abs(cm - (p @ cm)[:, None]) + ac) + (E + 8) * U * ac + e_c
+                       + 8 * U * np.abs(cm)) * 1.01
+        ez = np.where(live, ez, 0.0)
+        half = torch.finfo(self.W.dtype).eps / 2
+        rz = 2.0 ** -16 if self.W.dtype == BF16 else 0.0
+        az = np.abs(dz)
+        Hl = np.where(live, self.Hn, 0.0)
+        Q = p.shape[0]
+        if dh is not None:
+            e = (ez + (rz + (2 * E + 16) * U) * (az + ez)) @ np.abs(self.Wn)
+            _within(dh, wh, e + half * (np.abs(wh) + e) + TINY, "dh")
+        if dw is not None:
+            e = (ez + (rz + (2 * Q + 80) * U) * (az + ez)).T @ np.abs(Hl)
+            _within(dw, ww, e + half * (np.abs(ww) + e) + TINY, "dw")
+        if db is not None:
+            _within(db, wb, (ez + (Q + 80) * U * (az + ez)).sum(axis=0) + TINY, "db")
+
+
+# (dtype, E, k, d, Q)
+ROUTERS = [
+    (F32, 8, 1, 64, 64), (F32, 1, 1, 1, 1), (F32, 2, 2, 3, 5), (F32, 60, 4, 100, 333),
+    (F32, 256, 8, 41, 129), (F32, 17, 3, 2048, 40), (F32, 8, 2, 4096, 300),
+    (BF16, 8, 1, 64, 1), (BF16, 8, 2, 128, 37), (BF16, 1, 1, 64, 3), (BF16, 2, 1, 64, 17),
+    (BF16, 60, 4, 2048, 500), (BF16, 256, 8, 192, 129), (BF16, 16, 8, 4096, 33),
+    (BF16, 33, 2, 832, 2049), (BF16, 128, 4, 64, 1000), (BF16, 8, 2, 4096, 1001),
+    (BF16, 64, 6, 64, 20000),
+]
+
+
+@pytest.mark.parametrize("dtype,E,k,d,Q", ROUTERS)
+@pytest.mark.parametrize("bias", [True, False])
+def test_balance_matches_oracle(dtype, E, k, d, Q, bias):
+    log(f"[losses] balance {dtype} E={E} k={k} d={d} Q={Q} bias={bias}")
+    c = Router(51, dtype, E, k, d, Q, bias).dev()
+    loss, counts, prob_sum, prob = c.forward()
+    c.check_forward(loss, counts, prob_sum, prob)
+    c.check_backward(c.backward(prob, counts))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_balance_without_slots_and_without_rows(dtype):
+    c = Router(52, dtype, 8, 2, 64, 50)
+    c.t[:] = -1
+    c.dev()
+    loss, counts, prob_sum, prob = c.forward()
+    assert loss.item() == 0 and (counts == 0).all() and (prob_sum == 0).all()
+    c.check_forward(loss, counts, prob_sum, prob)
+    for t in c.backward(prob, counts):
+        assert (t == 0).all()
+    c = Router(53, dtype, 8, 2, 64, 0).dev()
+    loss, counts, prob_sum, prob = c.forward()
+    assert loss.item() == 0 and (counts == 0).all() and prob.shape == (0, 8)
+    dh, dw, db = c.backward(prob, counts)
+    assert dh.shape == (0, 64) and (dw == 0).all() and (db == 0).all()
+
+
+@pytest.mark.parametrize("dtype,E,d,Q", [(F32, 8, 96, 40), (BF16, 60, 128, 40), (BF16, 8, 64, 700)])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_balance_with_inactive_rows_of_anything(dtype, E, d, Q, bad):
+    c = Router(54, dtype, E, 2, d, Q)
+    rows = np.nonzero(~((c.t >= 0) & (c.t < E)).any(axis=1))[0]
+    assert len(rows) > 2
+    clean = Router(54, dtype, E, 2, d, Q)
+    c.H[rows] = bad
+    c.dev()
+    loss, counts, prob_sum, prob = c.forward()
+    keep = np.setdiff1d(np.arange(Q), rows)
+    wl, wc, ws, wp = X.balance_loss(clean.Wn, clean.Hn, clean.t, clean.b)
+    assert np.array_equal(counts.cpu().numpy(), wc)
+    prob = prob.clone()
+    prob[torch.from_numpy(rows).to(DEV)] = torch.from_numpy(wp[rows]).float().to(DEV)
+    clean.check_forward(loss, counts, prob_sum, prob)
+    clean.check_backward(c.backward(c.forward()[3], counts))
+    # a row that takes part passes it on
+    c.Hd[int(keep[0])] = bad
+    loss, counts, prob_sum, prob = c.forward()
+    assert torch.isnan(loss).all()
+
+
+def test_balance_with_experts_left_out():
+    for dtype in (F32, BF16):
+        c = Router(55, dtype, 12, 2, 64, 100)
+        c.b[::4] = -np.inf
+        c.dev()
+        loss, counts, prob_sum, prob = c.forward()
+        assert (prob[:, ::4] == 0).all()
+        c.check_forward(loss, counts, prob_sum, prob)
+        c.check_backward(c.backward(prob, counts))
+        c.b[:] = -np.inf
+        c.dev()
+        loss, counts, prob_sum, prob = c.forward()
+        assert (prob == 0).all() and loss.item() == 0
+        for t in c.backward(prob, counts):
+            assert (t == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_balance_of_two_ranks(dtype):
+    # counts summed over two batches: the two gradients of the weights add up to
+    # the gradient over the joint batch
+    a, b = Router(56, dtype, 16, 2, 128, 300).dev(), Router(57, dtype, 16, 2, 128, 200).dev()
+    b.W, b.Wn, b.Wd, b.b, b.bd = a.W, a.Wn, a.Wd, a.b, a.bd
+    ra, rb = a.forward(), b.forward()
+    counts = ra[1] + rb[1]
+    cn = counts.cpu().numpy()
+    a.check_backward(a.backward(ra[3], counts), cn)
+    b.check_backward(b.backward(rb[3], counts), cn)
+    joint = X.balance_grad(a.Wn, np.concatenate([a.Hn, b.Hn]), np.concatenate([a.t, b.t]),
+                           float(a.g), a.b)
+    split = [X.balance_grad(r.Wn, r.Hn, r.t, float(r.g), r.b, cn) for r in (a, b)]
+    # fp64 sums in another order
+    assert np.allclose(joint[1], split[0][1] + split[1][1], rtol=0, atol=1e-12)
+
+
+def test_balance_wanted_gradients():
+    c = Router(58, BF16, 60, 4, 256, 300).dev()
+    _, counts, _, prob = c.forward()
+    full = c.backward(prob, counts)
+    for i, kw in enumerate((dict(want_dh=False), dict(want_dw=False), dict(want_db=False))):
+        got = c.backward(prob, counts, **kw)
+        for j in range(3):
+            assert got[j] is None if j == i else torch.equal(got[j], full[j])
+
+
+# ------------------------------------------------- streams, graphs, use ----
+def _all(c, r):
+    loss, lse = c.forward()
+    bl = r.forward()
+    return (loss, lse, *c.backward(lse), *bl, *r.backward(bl[3], bl[1]))
+
+
+CALLS = [(F32, 300, 96, 40, 8), (BF16, 1003, 128, 16, 8), (BF16, 2003, 128, 700, 60)]
+
+
+@pytest.mark.parametrize("dtype,V,d,Q,E", CALLS)
+def test_losses_repeat_on_another_stream(dtype, V, d, Q, E):
+    c, r = Head(61, dtype, V, d, Q).dev(), Router(62, dtype, E, 2, d, Q).dev()
+    first = _all(c, r)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    loss, lse = c.forward(stream=s)
+    got = (loss, lse, *c.backward(lse, stream=s))
+    bl = r.forward(stream=s)
+    got += (*bl, *r.backward(bl[3], bl[1], stream=s))
+    second = _all(c, r)          # at the same time on the current stream
+    torch.cuda.synchronize()
+    for x, y, z in zip(first, got, second):
+        assert torch.equal(x, y) and torch.equal(x, z)
+
+
+@pytest.mark.parametrize("dtype,V,d,Q,E", CALLS)
+def test_losses_captured_and_replayed(dtype, V, d, Q, E):
+    c, r = Head(63, dtype, V, d, Q).dev(), Router(64, dtype, E, 2, d, Q).dev()
+    _all(c, r)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = _all(c, r)
+    for k in range(3):
+        c.Hd.copy_(torch.randn(c.Hd.shape, device=DEV).to(dtype))
+        r.td.copy_(torch.randint(-1, E, r.td.shape, device=DEV).to(torch.int16))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = _all(c, r)
+        torch.cuda.synchronize()
+        for x, y in zip(got, want):
+            assert torch.equal(x, y), k
+
+
+def test_outputs_stop_at_their_last_row():
+    # rows behind the last one of every output stay as they were
+    for dtype in (F32, BF16):
+        for V, d, Q in ((1003, 128, 20), (1003, 128, 300)):
+            c = Head(65, dtype, V, d, Q).dev()
+            _, lse = c.forward()
+            want = c.backward(lse)
+            dims = (abi._dtype_code(c.Hd), V, d, Q)
+            ws = abi._loss_ws("trimmoe_head_cross_entropy_backward", dims, c.Hd.device)
+            ws.fill_(0x5a)
+            dh = torch.full((Q + 2, d), 7.0, dtype=dtype, device=DEV)
+            dw = torch.full((V + 2, d), 7.0, dtype=dtype, device=DEV)
+            db = torch.full((V + 2,), 7.0, device=DEV)
+            rc = abi.lib().trimmoe_head_cross_entropy_backward(
+                *dims, c.Wd.data_ptr(), c.bd.data_ptr(), c.Hd.data_ptr(), c.yd.data_ptr(),
+                lse.data_ptr(), c.gd.data_ptr(), dh.data_ptr(), dw.data_ptr(), db.data_ptr(),
+                ws.data_ptr(), ws.numel(), None)
+            assert rc == 0
+            torch.cuda.synchronize()
+            for got, ref, n in ((dh, want[0], Q), (dw, want[1], V), (db, want[2], V)):
+                assert torch.equal(got[:n], ref) and (got[n:] == 7).all()
+
+
+def test_training_objective_over_a_traced_stack():
+    # as they are used together: a stack runs, its trace gives the routed
+    # experts and the output head the targets; both losses and every gradient
+    cfg = workload("tiny_fp32", dtype="bf16", n_tokens=200)
+    inp = make_inputs(cfg)
+    g = GpuRun(inp)
+    st = abi.StateBuffers(inp["h0"].to(DEV).clone())
+    tr = abi.TraceBuffers(cfg["n_layers"], 200, cfg["top_k"], DEV)
+    abi.trimmoe_stack_forward(g.mh.model, g.policy(), st.state, tr.trace, g.ws)
+    L = inp["layers"][1]
+    r = Router(66, BF16, cfg["n_experts"], cfg["top_k"], cfg["d_model"], 200)
+    r.W = L["w_router"].cpu()
+    r.Wn, r.b = r.W.double().numpy(), None if L["b_router"] is None else L["b_router"].cpu().numpy()
+    r.H, r.t = st.h.cpu(), tr.target[1].cpu().numpy()
+    r.Hn = r.H.double().numpy()
+    assert (r.t < 0).any() or (gpu_trace_np(tr)["action"][1] != 0).all()
+    r.dev()
+    bl = r.forward()
+    r.check_forward(*bl)
+    r.check_backward(r.backward(bl[3], bl[1]))
+    c = Head(67, BF16, cfg["vocab_exit"], cfg["d_model"], 200, bias=False)
+    c.H, c.Hn = r.H, r.Hn
+    c.dev()
+    c.yd = abi.trimmoe_head_argmax(c.Wd, c.Hd)
+    c.y = c.yd.cpu().numpy()
+    loss, lse = c.forward()
+    c.check_forward(loss, lse)
+    c.check_backward(c.backward(lse))
