@@ -8,6 +8,7 @@ namespace trimmoe {
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 
 static inline int cdiv(int a, int b) { return (a + b - 1) / b; }
 

@@ -8,8 +8,6 @@
 
 namespace trimmoe {
 
-typedef float f32x16_t __attribute__((ext_vector_type(16)));
-
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // ------------------------------------------------------------ fp32 products --
