@@ -120,5 +120,6 @@ struct ExitArgs {
 // decode-sized batches (skinny.hip)
 hipError_t launch_ffn_skinny(const FfnArgs& a, bool up, bool dual, int n_cu, hipStream_t st);
 hipError_t launch_exit_skinny(const ExitArgs& a, bool argmax, hipStream_t st);
+hipError_t launch_loss_skinny(const ExitArgs& a, int n_rows, hipStream_t st);
 
 }  // namespace trimmoe

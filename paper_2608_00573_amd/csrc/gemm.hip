@@ -30,6 +30,7 @@
 // not a whole number of slices.
 #include <math.h>
 
+#include "loss.h"
 #include "mfma_core.h"
 
 namespace trimmoe {
@@ -530,7 +531,8 @@ using ExitWide = Tile<kExitTileBF16, 256, 1, 4, 2>;
 // columns, 128 vocabulary rows, so that the MFMA work is not 4x padding
 using ExitSmall = Tile<kExitTileBF16Small, 32, 1, 4, 1>;
 
-template <class T, bool ARGMAX = false>
+// LOSS: a NaN logit, which the confidence leaves out, makes the tile's sum NaN
+template <class T, bool ARGMAX = false, bool LOSS = false>
 struct ExitSrc {
   struct Desc {
     int mt, nt;
@@ -724,11 +726,12 @@ struct ExitSrc {
         m = fmaxf(pm.a, pm.b);
       }
       float sum = 0.f;
-      if (m != ninf) {
+      if (LOSS || m != ninf) {
+        const float ms = LOSS && m == ninf ? 0.f : m;
 #pragma unroll
         for (int i = 0; i < T::TM; ++i)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(acc[i][jj][r] - m);
+          for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(acc[i][jj][r] - ms);
       }
       {
         const LanePair ps = lanes_xor32(sum);
@@ -743,10 +746,11 @@ struct ExitSrc {
 #pragma unroll
       for (int g = 1; g < T::GM; ++g) M = fmaxf(M, s_part[g][c].x);
       float S2 = 0.f;
+      const float Ms = LOSS && M == ninf ? 0.f : M;
 #pragma unroll
       for (int g = 0; g < T::GM; ++g) {
         const float2 v = s_part[g][c];
-        if (v.y > 0.f) S2 += v.y * __builtin_amdgcn_exp2f(v.x - M);
+        if (LOSS || v.y > 0.f) S2 += v.y * __builtin_amdgcn_exp2f(v.x - Ms);
       }
       a.partials[(size_t)(j0 + c) * a.n_vtiles + d.mt] = make_float2(M, S2);
     }
@@ -765,6 +769,17 @@ __global__ __launch_bounds__(T::THREADS) void k_exit_mma(ExitArgs a) {
   const ExitSrc<T, ARGMAX> src{a, S, n_x, s_part};
   dma_gemm_stream<T>(lds, ntiles, a.K / BK, src);
   clock_mark(a.clk, false);
+}
+
+template <class T>
+__global__ __launch_bounds__(T::THREADS) void k_loss_mma(ExitArgs a, int n_rows) {
+  __shared__ __align__(16) char lds[DmaTile<T>::LDS];
+  __shared__ float2 s_part[T::GM][T::BN];
+  TileSched S;
+  int ntiles;
+  if (!S.init(a.n_vtiles, (n_rows + T::BN - 1) / T::BN, 1, ntiles)) return;
+  const ExitSrc<T, false, true> src{a, S, n_rows, s_part};
+  dma_gemm_stream<T>(lds, ntiles, a.K / BK, src);
 }
 
 // Exit head on the large-group core (large d): 256 vocabulary rows x 256
@@ -799,6 +814,7 @@ __device__ __forceinline__ void exit_big_rows(BigRows& q, const ExitArgs& a, con
 // vocabulary tile, or a bias) take the bias and row mask in both passes.
 // The tile's loads have all landed by now, so the LDS exchange waits for LDS
 // work only.
+template <bool LOSS>
 __device__ __forceinline__ void exit_big_epilogue(const ExitArgs& a, const TileSched& S, int n_x,
                                                   int jt, const AccBig& acc,
                                                   float2 (*s_part)[big::BN], int wm, int wn,
@@ -841,12 +857,13 @@ __device__ __forceinline__ void exit_big_epilogue(const ExitArgs& a, const TileS
     }
     const float m = mz * kLog2e;
     float sum = 0.f;
-    if (mz != ninf) {
+    if (LOSS || mz != ninf) {
+      const float ms = LOSS && mz == ninf ? 0.f : m;
       if (full) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, -m));
+          for (int r = 0; r < 4; ++r) sum += __builtin_amdgcn_exp2f(fmaf(acc[i][j][r], kLog2e, -ms));
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -854,7 +871,7 @@ __device__ __forceinline__ void exit_big_epilogue(const ExitArgs& a, const TileS
           for (int r = 0; r < 4; ++r) {
             const int o = 16 * i + r;
             const float b = bias ? bias[min(o, lim - 1)] : 0.f;
-            const float e = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r] + b, kLog2e, -m));
+            const float e = __builtin_amdgcn_exp2f(fmaf(acc[i][j][r] + b, kLog2e, -ms));
             sum += o < lim ? e : 0.f;
           }
       }
@@ -872,9 +889,10 @@ __device__ __forceinline__ void exit_big_epilogue(const ExitArgs& a, const TileS
   if (c < b_valid) {
     const float2 p0 = s_part[0][c], p1 = s_part[1][c];
     const float M = fmaxf(p0.x, p1.x);
+    const float Ms = LOSS && M == ninf ? 0.f : M;
     float S2 = 0.f;
-    if (p0.y > 0.f) S2 += p0.y * __builtin_amdgcn_exp2f(p0.x - M);
-    if (p1.y > 0.f) S2 += p1.y * __builtin_amdgcn_exp2f(p1.x - M);
+    if (LOSS || p0.y > 0.f) S2 += p0.y * __builtin_amdgcn_exp2f(p0.x - Ms);
+    if (LOSS || p1.y > 0.f) S2 += p1.y * __builtin_amdgcn_exp2f(p1.x - Ms);
     a.partials[(size_t)(c0 + c) * a.n_vtiles + vt] = make_float2(M, S2);
   }
   // s_part is rewritten by the next epilogue only after the next tile's
@@ -952,8 +970,8 @@ __device__ __forceinline__ void exit_big_argmax(const ExitArgs& a, const TileSch
   }
 }
 
-template <bool ARGMAX>
-__device__ __forceinline__ void exit_big(const ExitArgs& a, char* lds) {
+template <bool ARGMAX, bool LOSS = false>
+__device__ __forceinline__ void exit_big(const ExitArgs& a, char* lds, int n_rows = 0) {
   // per row half: (max y, sum) per token column, in the last B stage (free
   // while the epilogue runs; the next tile writes it only after its first
   // slice barrier)
@@ -961,7 +979,7 @@ __device__ __forceinline__ void exit_big(const ExitArgs& a, char* lds) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
-  const int n_x = *a.n_exec;
+  const int n_x = LOSS ? n_rows : *a.n_exec;
   TileSched S;
   int ntiles;
   if (!S.init(a.n_vtiles, (n_x + big::BN - 1) / big::BN, 1, ntiles)) return;
@@ -991,7 +1009,7 @@ __device__ __forceinline__ void exit_big(const ExitArgs& a, char* lds) {
     if constexpr (ARGMAX)
       exit_big_argmax(a, S, n_x, jt, acc, s_part, wm, wn, lane);
     else
-      exit_big_epilogue(a, S, n_x, jt, acc, s_part, wm, wn, lane);
+      exit_big_epilogue<LOSS>(a, S, n_x, jt, acc, s_part, wm, wn, lane);
   }
   clock_mark(a.clk, false);
 }
@@ -1004,6 +1022,11 @@ __global__ __launch_bounds__(big::THREADS) void k_exit_big(ExitArgs a) {
 __global__ __launch_bounds__(big::THREADS) void k_argmax_big(ExitArgs a) {
   __shared__ __align__(16) char lds[big::LDS];
   exit_big<true>(a, lds);
+}
+
+__global__ __launch_bounds__(big::THREADS) void k_loss_big(ExitArgs a, int n_rows) {
+  __shared__ __align__(16) char lds[big::LDS];
+  exit_big<false, true>(a, lds, n_rows);
 }
 
 // ------------------------------------------------------------- fp32 path --
@@ -1354,6 +1377,28 @@ hipError_t launch_head_argmax_partials(bool bf16, const void* W, const float* bi
     hipLaunchKernelGGL(k_exit_f32<true>, grid, dim3(256), 0, st, static_cast<const float*>(W),
                        static_cast<const float*>(H), nullptr, bias, n_rows_dev, V, K, n_vtiles,
                        partials);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_head_loss_partials(const void* W, const float* bias, const void* H, int n_rows,
+                                     int V, int K, int n_vtiles, float2* partials, int n_cu,
+                                     hipStream_t st) {
+  ExitArgs a{static_cast<const bf16_t*>(W), static_cast<const bf16_t*>(H), bias, nullptr, V, K,
+             n_vtiles, partials, nullptr};
+  if (exit_streams(true, true, n_rows, V, K)) return launch_loss_skinny(a, n_rows, st);
+  if (big_argmax(n_rows, V, K, n_cu)) {
+    const dim3 grid(min(n_vtiles * cdiv(n_rows, big::BN), n_cu));
+    hipLaunchKernelGGL(k_loss_big, grid, dim3(big::THREADS), 0, st, a, n_rows);
+  } else if (n_rows <= kSkinnyTokens) {
+    const dim3 grid(min(n_vtiles * cdiv(n_rows, ExitSmall::BN), n_cu));
+    hipLaunchKernelGGL(k_loss_mma<ExitSmall>, grid, dim3(ExitSmall::THREADS), 0, st, a, n_rows);
+  } else if (n_rows >= kWideTokens) {
+    const dim3 grid(min(n_vtiles * cdiv(n_rows, ExitWide::BN), n_cu));
+    hipLaunchKernelGGL(k_loss_mma<ExitWide>, grid, dim3(ExitWide::THREADS), 0, st, a, n_rows);
+  } else {
+    const dim3 grid(min(n_vtiles * cdiv(n_rows, ExitTile::BN), n_cu));
+    hipLaunchKernelGGL(k_loss_mma<ExitTile>, grid, dim3(ExitTile::THREADS), 0, st, a, n_rows);
   }
   return hipGetLastError();
 }

@@ -26,6 +26,12 @@ struct HeadLossArgs {
   int n_cu;
 };
 
+// softmax pairs (max z log2 e, sum exp(z - max z)) of a bf16 head per row and
+// vocabulary tile, NaN logits kept (gemm.hip)
+hipError_t launch_head_loss_partials(const void* W, const float* bias, const void* H, int n_rows,
+                                     int V, int K, int n_vtiles, float2* partials, int n_cu,
+                                     hipStream_t st);
+
 size_t head_loss_ws(bool bf16, int V, int d, int T);
 size_t head_loss_backward_ws(bool bf16, int V, int d, int T);
 hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t st);

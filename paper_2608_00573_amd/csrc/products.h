@@ -18,7 +18,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 // loads in flight under the MFMAs), so a fragment read is 32 consecutive floats
 // and the order of the operand in memory only changes how a slice is written.
 namespace f32p {
-constexpr int BM = 128, BN = 128, BK = 16, THREADS = 256;
+constexpr int BM = 128, BN = 128, KS = 16, THREADS = 256;
 constexpr int LS = 132;  // floats of an LDS row: four lanes of one row, 4 k apart, hit distinct banks
 }  // namespace f32p
 
@@ -97,7 +97,7 @@ __device__ __forceinline__ void f32_tile(const Operand<TA, AK>& A, const Operand
   using namespace f32p;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int ra = (wave >> 1) * 64 + (lane & 31), rb = (wave & 1) * 64 + (lane & 31), kk = lane >> 5;
-  constexpr int BUF = 2 * BK * LS;
+  constexpr int BUF = 2 * KS * LS;
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -106,19 +106,19 @@ __device__ __forceinline__ void f32_tile(const Operand<TA, AK>& A, const Operand
   load_slice(A, r0, k0, k_end, xa);
   load_slice(B, n0, k0, k_end, xb);
   store_slice<AK>(lds, xa);
-  store_slice<BKC>(lds + BK * LS, xb);
+  store_slice<BKC>(lds + KS * LS, xb);
   __syncthreads();
   int buf = 0;
-  for (int k = k0; k < k_end; k += BK) {
-    const bool more = k + BK < k_end;
+  for (int k = k0; k < k_end; k += KS) {
+    const bool more = k + KS < k_end;
     if (more) {
-      load_slice(A, r0, k + BK, k_end, xa);
-      load_slice(B, n0, k + BK, k_end, xb);
+      load_slice(A, r0, k + KS, k_end, xa);
+      load_slice(B, n0, k + KS, k_end, xb);
     }
     const float* sa = lds + buf * BUF;
-    const float* sb = sa + BK * LS;
+    const float* sb = sa + KS * LS;
 #pragma unroll
-    for (int s = 0; s < BK; s += 2) {
+    for (int s = 0; s < KS; s += 2) {
       float fa[2], fb[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -133,7 +133,7 @@ __device__ __forceinline__ void f32_tile(const Operand<TA, AK>& A, const Operand
     }
     if (more) {
       store_slice<AK>(lds + (buf ^ 1) * BUF, xa);
-      store_slice<BKC>(lds + (buf ^ 1) * BUF + BK * LS, xb);
+      store_slice<BKC>(lds + (buf ^ 1) * BUF + KS * LS, xb);
     }
     __syncthreads();
     buf ^= 1;

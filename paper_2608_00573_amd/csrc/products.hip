@@ -10,7 +10,7 @@ template <typename TO, typename TA, bool AK, typename TB, bool BKC>
 __global__ __launch_bounds__(f32p::THREADS) void k_prod_f32(Operand<TA, AK> A, Operand<TB, BKC> B,
                                                             int k_per, TO* out, int add) {
   using namespace f32p;
-  __shared__ __align__(16) float lds[4 * BK * LS];
+  __shared__ __align__(16) float lds[4 * KS * LS];
   const int nt = blockIdx.y, mt = blockIdx.x;
   const int k0 = min((int)blockIdx.z * k_per, A.K), k1 = min(k0 + k_per, A.K);
   F32Acc acc;
@@ -47,7 +47,7 @@ template <typename TO, typename TA, bool AK, typename TB, bool BKC>
 hipError_t launch_product(const Operand<TA, AK>& A, const Operand<TB, BKC>& B, int splits, bool add,
                           TO* out, hipStream_t st) {
   using namespace f32p;
-  const int k_per = cdiv(cdiv(A.K, splits), BK) * BK;
+  const int k_per = cdiv(cdiv(A.K, splits), KS) * KS;
   const dim3 grid(cdiv(A.rows, BM), cdiv(B.rows, BN), splits);
   hipLaunchKernelGGL((k_prod_f32<TO, TA, AK, TB, BKC>), grid, dim3(THREADS), 0, st, A, B, k_per, out,
                      add ? 1 : 0);

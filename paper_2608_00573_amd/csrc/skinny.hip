@@ -449,7 +449,8 @@ __global__ __launch_bounds__(skinny::THREADS) void k_ffn_skinny(FfnArgs a) {
 // or, ARGMAX, the largest logit and its row, per token; one partial per token
 // and block (n_vtiles is the grid).  The softmax reads hx in operand order,
 // the argmax a caller's rows.
-template <bool ARGMAX, class T>
+// LOSS: a softmax of a caller's rows that keeps NaN logits.
+template <bool ARGMAX, class T, bool LOSS = false>
 __device__ __forceinline__ void skinny_exit_rows(const ExitArgs& a, char* lds, int n_x, int v0,
                                                  int v1) {
   constexpr int MT = T::MT, UC = T::G * skinny::COLS;
@@ -458,7 +459,7 @@ __device__ __forceinline__ void skinny_exit_rows(const ExitArgs& a, char* lds, i
   XSrc<MT> xs;
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
-    if constexpr (ARGMAX) {
+    if constexpr (ARGMAX || LOSS) {
       xs.p[m] = a.H + (size_t)min(16 * m + fr, n_x - 1) * a.K + 8 * q;
       xs.step[m] = skinny::KSTEP;
     } else {
@@ -493,7 +494,13 @@ __device__ __forceinline__ void skinny_exit_rows(const ExitArgs& a, char* lds, i
         }
     } else {
       const float m = fmaxf(M, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
-      if (m != ninf) {
+      if constexpr (LOSS) {
+        const float ms = m == ninf ? 0.f : m;
+        S *= __builtin_amdgcn_exp2f(M - ms);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S += __builtin_amdgcn_exp2f(y[r] - ms);
+        M = m;
+      } else if (m != ninf) {
         float t = M != ninf ? S * __builtin_amdgcn_exp2f(M - m) : 0.f;
 #pragma unroll
         for (int r = 0; r < 4; ++r) t += __builtin_amdgcn_exp2f(y[r] - m);
@@ -522,9 +529,10 @@ __device__ __forceinline__ void skinny_exit_rows(const ExitArgs& a, char* lds, i
       R = take ? r1 : r0;
     } else {
       M = fmaxf(m0, m1);
+      const float ms = LOSS && M == ninf ? 0.f : M;
       S = 0.f;
-      if (s0 > 0.f) S += s0 * __builtin_amdgcn_exp2f(m0 - M);
-      if (s1 > 0.f) S += s1 * __builtin_amdgcn_exp2f(m1 - M);
+      if (LOSS || s0 > 0.f) S += s0 * __builtin_amdgcn_exp2f(m0 - ms);
+      if (LOSS || s1 > 0.f) S += s1 * __builtin_amdgcn_exp2f(m1 - ms);
     }
   };
 #pragma unroll
@@ -566,6 +574,20 @@ __global__ __launch_bounds__(skinny::THREADS) void k_exit_skinny(ExitArgs a) {
   clock_mark(a.clk, false);
 }
 
+template <int KIND>
+__global__ __launch_bounds__(skinny::THREADS) void k_loss_skinny(ExitArgs a, int n_x) {
+  __shared__ __align__(16) char lds[skinny::LDS];
+  const long n_u = (a.V + skinny::COLS - 1) / skinny::COLS;
+  const int u0 = (int)(n_u * blockIdx.x / gridDim.x), u1 = (int)(n_u * (blockIdx.x + 1) / gridDim.x);
+  const int v0 = u0 * skinny::COLS, v1 = min(u1 * skinny::COLS, a.V);
+  if (n_x <= 16)
+    skinny_exit_rows<false, Stream<1, 1, KIND>, true>(a, lds, n_x, v0, v1);
+  else if (n_x <= 32)
+    skinny_exit_rows<false, Stream<1, 2, KIND>, true>(a, lds, n_x, v0, v1);
+  else
+    skinny_exit_rows<false, Stream<1, 4, wide_kind(KIND)>, true>(a, lds, n_x, v0, v1);
+}
+
 // -------------------------------------------------------------- launchers --
 // set shape for a K of ks k-steps: sets must fit K
 static int stream_kind(int ks) { return ks < 8 ? kShort : kLong; }
@@ -603,6 +625,15 @@ hipError_t launch_exit_skinny(const ExitArgs& a, bool argmax, hipStream_t st) {
     launch_exit<true>(a, st);
   else
     launch_exit<false>(a, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_loss_skinny(const ExitArgs& a, int n_rows, hipStream_t st) {
+  const dim3 grid(a.n_vtiles), block(skinny::THREADS);
+  if (stream_kind(a.K / skinny::KSTEP) == kShort)
+    hipLaunchKernelGGL(k_loss_skinny<kShort>, grid, block, 0, st, a, n_rows);
+  else
+    hipLaunchKernelGGL(k_loss_skinny<kLong>, grid, block, 0, st, a, n_rows);
   return hipGetLastError();
 }
 
