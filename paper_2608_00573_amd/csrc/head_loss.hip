@@ -190,102 +190,94 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 }
 
 // ------------------------------------------------------ backward, bf16 --
-// Three products on the large-group core, whose operands are both K-contiguous,
-// so whatever runs the other way is laid out once: h^T for dw (zeros in the rows
-// that take no part, whose h may hold anything) and w^T of the piece for dh; D
-// is written in both orders by its own epilogue.
-//   * D enters the products in bf16.  Its order for dh holds softmax - onehot
-//     without the row's weight g (applied to the fp32 sums), its order for dw
-//     g / G times that, G the largest |g| (applied to the fp32 sums): weights
-//     that are all alike are exact, and so is the -1 of an unlikely target,
-//     which carries most of an untrained row's gradient.
+// Three products on the large-group core.  D of a piece is written once, [T, Vp],
+// and read in both orders: as it lies for dh, transposed out of LDS for dw (as
+// are w for dh and h for dw: nothing is laid out again in memory).
+//   * D enters the products in bf16, once rounded.  A row's weight g is G m 2^-e
+//     with G the largest |g| and |m| in [1, 2): D holds m (softmax - onehot), dh
+//     takes g / m on its fp32 sums, dw G on its own and 2^-e on the rows of h,
+//     where it is exact.  So weights that are all alike (m = 1) add no rounding
+//     to the -1 of an unlikely target, which carries most of an untrained row's
+//     gradient.
+//   * The scaled copy of h has zeros in the rows that take no part: their h may
+//     hold anything, and 0 * NaN is NaN.
 //   * dh is summed in fp32 over pieces and K splits, then rounded once.
+// A tile's A rows are the columns of its result (4 consecutive ones a lane), so
+// that results leave the registers in 16-byte pieces without a turn through LDS.
 
-// row t's part in the backward: its target, or -1 where it takes no part; its
-// weight and weight / G (0 there); lse log2 e.  One block.
+// a row's part in the backward
+struct RowPart {
+  int32_t* y;  // its target, or -1 where it takes no part
+  float* l2;   // lse log2 e
+  float* m;    // m, 2^-e (0 for a weight of 0) and g / m (0 where it takes no part)
+  float* e;
+  float* gm;
+  float* G;    // [1]
+};
+
 __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const float* lse,
-                                                   const float* dloss, int V, int T, int Tp,
-                                                   int32_t* ys, float* gl, float* gs, float* l2,
-                                                   float* G) {
+                                                   const float* dloss, int V, int T, RowPart p) {
   __shared__ float s_m[16];
-  float m = 0.f;
-  for (int t = threadIdx.x; t < Tp; t += 1024) {
-    const int y = t < T ? target[t] : -1;
-    const float L = t < T ? lse[t] : 0.f;
+  float G = 0.f;
+  for (int t = threadIdx.x; t < T; t += 1024) {
+    const int y = target[t];
+    const float L = lse[t];
     const bool live = y >= 0 && y < V && L != -__builtin_inff();
     const float g = live ? dloss[t] : 0.f;
-    ys[t] = live ? y : -1;
-    gl[t] = g;
-    l2[t] = live ? L * kLog2e : 0.f;
-    m = fmaxf(m, fabsf(g));
+    p.y[t] = live ? y : -1;
+    p.gm[t] = g;
+    p.l2[t] = live ? L * kLog2e : 0.f;
+    G = fmaxf(G, fabsf(g));
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = m;
+  for (int o = 32; o > 0; o >>= 1) G = fmaxf(G, __shfl_xor(G, o));
+  if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = G;
   __syncthreads();
-  m = s_m[0];
+  G = s_m[0];
 #pragma unroll
-  for (int i = 1; i < 16; ++i) m = fmaxf(m, s_m[i]);
-  if (threadIdx.x == 0) *G = m;
+  for (int i = 1; i < 16; ++i) G = fmaxf(G, s_m[i]);
+  if (threadIdx.x == 0) *p.G = G;
   // (each thread reads back its own rows)
-  for (int t = threadIdx.x; t < Tp; t += 1024) {
-    const float g = gl[t];
-    gs[t] = g == 0.f ? 0.f : g / m;
+  for (int t = threadIdx.x; t < T; t += 1024) {
+    const float g = p.gm[t];
+    int e = 0;
+    const float f = g == 0.f ? 0.5f : frexpf(g / G, &e);  // (NaN stays NaN)
+    const float m = f == 0.f ? 1.f : 2.f * f;
+    p.m[t] = m;
+    p.e[t] = g == 0.f || f == 0.f ? 0.f : ldexpf(1.f, e - 1);
+    p.gm[t] = g / m;
   }
 }
 
-// out [C, Rp] = in [R, C] transposed, columns past R zero; rows with ys < 0 are
-// zeros (ys may be NULL).  64 x 64 tiles: 128-byte runs on both sides.
-__global__ __launch_bounds__(256) void k_transpose(const bf16_t* in, const int32_t* ys, int R, int C,
-                                                   int Rp, bf16_t* out) {
-  __shared__ __align__(16) bf16_t s[64][72];
-  const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64;
-  const int row = threadIdx.x >> 3, ch = 8 * (threadIdx.x & 7);
-#pragma unroll
-  for (int i = 0; i < 64; i += 32) {
-    const int r = r0 + row + i;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (r < R && (!ys || ys[r] >= 0)) v = *reinterpret_cast<const uint4*>(in + (size_t)r * C + c0 + ch);
-    *reinterpret_cast<uint4*>(&s[row + i][ch]) = v;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < 64; i += 32) {
-    const int c = row + i;
+// hw = 2^-e h_t, zeros in the rows that take no part; 8 elements a thread
+__global__ __launch_bounds__(256) void k_scale_rows(const bf16_t* h, RowPart p, int T, int d,
+                                                    bf16_t* hw) {
+  const size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x);
+  if (i >= (size_t)T * d) return;
+  const int t = (int)(i / d);
+  union {
+    uint4 v;
+    bf16_t e[8];
     uint32_t w[4];
+  } x;
+  x.v = make_uint4(0, 0, 0, 0);
+  if (p.y[t] >= 0) {
+    x.v = *reinterpret_cast<const uint4*>(h + i);
+    const float s = p.e[t];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      w[u] = (uint32_t)s[ch + 2 * u][c] | (uint32_t)s[ch + 2 * u + 1][c] << 16;
-    *reinterpret_cast<uint4*>(out + (size_t)(c0 + c) * Rp + r0 + ch) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int u = 0; u < 4; ++u) x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * s, bf2f(x.e[2 * u + 1]) * s);
   }
+  *reinterpret_cast<uint4*>(hw + i) = x.v;
 }
 
 }  // namespace
 
 __device__ __forceinline__ int cdiv_d(int a, int b) { return (a + b - 1) / b; }
 
-// operand rows of a tile of the large-group core: A rows from m0 (m of them
-// valid), B rows from n0, both K-contiguous with leading dimension ld, from
-// column k0
-__device__ __forceinline__ void big_rows(BigRows& q, const bf16_t* A, int m0, int m_valid,
-                                         const bf16_t* B, int n0, int n_valid, int ld, int k0, int r0,
-                                         int cc) {
-  q.ra = buf_rsrc(A + (size_t)m0 * ld);
-  q.rb0 = buf_rsrc(B + (size_t)n0 * ld);
-  q.rb1 = q.rb0;
-  q.none = buf_rsrc_empty(A);
-#pragma unroll
-  for (int u = 0; u < 8; ++u) {
-    const int r = r0 + big::RPP * u;
-    q.off[u] = ((uint32_t)min(r, m_valid - 1) * ld + k0 + cc) * 2;
-    q.off[8 + u] = ((uint32_t)min(r, n_valid - 1) * ld + k0 + cc) * 2;
-  }
-}
-
-// the block's lane constants on that core
+// the block's lane constants on the large-group core: LDS offsets of fragments
+// of a K-contiguous (a, b) and of a transposed operand (at, bt), fetch rows
 struct BigLane {
   int lane, wave, wm, wn, r0, cc;
-  uint32_t a[2], b[2];
   __device__ __forceinline__ BigLane() {
     const int tid = threadIdx.x;
     lane = tid & 63;
@@ -294,15 +286,33 @@ struct BigLane {
     wn = wave & 1;
     r0 = tid >> 3;
     cc = 8 * ((tid & 7) ^ swz16(r0));
+  }
+  // fragment offsets of the operand whose half `half` of the tile this wavefront reads
+  __device__ __forceinline__ void rows(uint32_t (&o)[2], int half) const {
     const int fr = lane & 15, hk = lane >> 4;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const uint32_t ch = ((4 * ks + hk) ^ swz16(fr)) << 4;
-      a[ks] = (wm * 128 + fr) * big::RB + ch;
-      b[ks] = (wn * 128 + fr) * big::RB + ch;
-    }
+    for (int ks = 0; ks < 2; ++ks)
+      o[ks] = (half * 128 + fr) * big::RB + (((4 * ks + hk) ^ swz16(fr)) << 4);
+  }
+  __device__ __forceinline__ void cols(uint32_t (&o)[2], int half) const {
+    const int i = lane & 15, hk = lane >> 4, k = 8 * hk + (i >> 2);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+      o[ks] = (32 * ks + k) * 512 + half * 256 + (tr_swz(k) << 5) + 8 * (i & 3);
+  }
+  // fetch offset u of a transposed operand with leading dimension ld
+  __device__ __forceinline__ uint32_t fetch(int u, int ld) const {
+    const int k = 2 * wave + 8 * u + (lane >> 5), p = lane & 31;
+    return (uint32_t)((k * ld + 16 * ((p >> 1) ^ tr_swz(k)) + 8 * (p & 1)) * 2);
   }
 };
+
+// an operand of `rows` rows along K from row k0 and column c0
+__device__ __forceinline__ BigLong big_long(const bf16_t* p, int ld, int rows, int k0, int c0) {
+  const long long o = ((long long)k0 * ld + c0) * 2;
+  return BigLong{reinterpret_cast<const char*>(p) + o, (long long)rows * ld * 2 - o,
+                 (long long)ld * 128};
+}
 
 __device__ __forceinline__ void big_zero(AccBig& acc) {
 #pragma unroll
@@ -311,44 +321,53 @@ __device__ __forceinline__ void big_zero(AccBig& acc) {
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{};
 }
 
-// LDS image of a 256 x 256 bf16 tile: rows padded by 16 bytes
-constexpr int kImgRow = 2 * 256 + 16;
-static_assert(256 * kImgRow <= big::LDS, "tile image fits the stages");
+// Two accumulators' values of one row (columns 16 i .. and 16 (i + 1) ..; a lane
+// holds 4 consecutive ones) as bf16, 8 consecutive columns a lane: lanes of even
+// groups of 16 get the first block's pieces, those of odd groups the second's
+__device__ __forceinline__ u32x4_t pack_rows(const float (&x)[4], const float (&y)[4]) {
+  const unsigned x0 = pack_bf16x2(x[0], x[1]), x1 = pack_bf16x2(x[2], x[3]);
+  const unsigned y0 = pack_bf16x2(y[0], y[1]), y1 = pack_bf16x2(y[2], y[3]);
+  const auto p = __builtin_amdgcn_permlane16_swap(x0, y0, false, false);
+  const auto q = __builtin_amdgcn_permlane16_swap(x1, y1, false, false);
+  const unsigned p0 = p[0], p1 = p[1], q0 = q[0], q1 = q[1];
+  return u32x4_t{p0, q0, p1, q1};
+}
+// ... and where they go: column of the lane's piece within the two blocks
+__device__ __forceinline__ int pack_col(int lane) {
+  return 16 * (lane >> 4 & 1) + 8 * (lane >> 5);
+}
 
-// the image's valid rows and columns (a multiple of 8) to out, rows ld apart
-__device__ __forceinline__ void big_image_out(const char* lds, bf16_t* out, size_t ld, int rows,
-                                              int cols) {
-  lds_barrier();
-#pragma unroll 4
-  for (int idx = threadIdx.x; idx < 256 * 32; idx += big::THREADS) {
-    const int r = idx >> 5, ch = idx & 31;
-    if (r < rows && ch * 8 < cols)
-      *reinterpret_cast<uint4*>(out + (size_t)r * ld + ch * 8) =
-          *reinterpret_cast<const uint4*>(lds + r * kImgRow + ch * 16);
-  }
-  lds_barrier();
+__device__ __forceinline__ float row16_sum(float v) {
+  // over the 16 lanes of a row (rotations by 8, 4, 2, 1)
+  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x124, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x122, 0xf, 0xf, false));
+  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x121, 0xf, 0xf, false));
+  return v;
 }
 
 struct DzArgs {
   const bf16_t* w;    // the piece's first row
   const bf16_t* h;
   const float* bias;  // the piece's first row, or NULL
-  const int32_t* ys;
-  const float *gs, *l2;
+  RowPart rows;
   int nv, v0, d, T;
-  int Vp, Tp;         // leading dimensions of D and D^T
-  bf16_t *D, *DT;
+  int Vp;             // leading dimension of D
+  bf16_t* D;
   float* db_part;     // [token tiles][Vp] or NULL
 };
 
-// D of a piece: A = w (vocabulary rows), B = h, so that a lane holds 4
-// consecutive vocabulary rows of one row t per accumulator
+// D of a piece: A = w (vocabulary rows), B = h.  BIAS: with a bias, db or both
+template <bool BIAS>
 __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
   __shared__ __align__(16) char lds[big::LDS];
   const BigLane L;
   TileSched S;
   int ntiles;
   if (!S.init(a.Vp / big::BM, cdiv_d(a.T, big::BN), 1, ntiles)) return;
+  uint32_t la[2], lb[2];
+  L.rows(la, L.wm);
+  L.rows(lb, L.wn);
   const int nk = a.d / BK;
   AccBig acc;
   for (int jt = 0; jt < ntiles; ++jt) {
@@ -358,72 +377,70 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
     const int v_valid = min(big::BM, a.nv - c0), t_valid = min(big::BN, a.T - t0);
     {
       BigRows q;
-      big_rows(q, a.w, c0, v_valid, a.h, t0, t_valid, a.d, 0, L.r0, L.cc);
-      big_zero(acc);
-      big_tile<false>(lds, q, nk, acc, L.a, L.b);
-    }
-    const int c = L.lane & 15, hq = L.lane >> 4;
-    const int rl = L.wm * 128 + 4 * hq;  // the lane's first vocabulary row
-    const float* bias = a.bias ? a.bias + c0 : nullptr;
+      q.ra = buf_rsrc(a.w + (size_t)c0 * a.d);
+      q.rb0 = q.rb1 = buf_rsrc(a.h + (size_t)t0 * a.d);
+      q.none = buf_rsrc_empty(a.w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int tl = L.wn * 128 + 16 * j + c, t = min(t0 + tl, a.T - 1);
-      const float l2 = a.l2[t];
-      const int y = tl < t_valid ? a.ys[t] : -1;
-      const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        f32x4_t x = acc[i][j];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float z = x[r];
-          if (bias) z += bias[min(rl + 16 * i + r, v_valid - 1)];
-          const float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -l2));
-          const bool in = y >= 0 && rl + 16 * i + r < v_valid;
-          x[r] = in ? p - (16 * i + r == yr ? 1.f : 0.f) : 0.f;
-        }
-        acc[i][j] = x;
-        uint2 w;
-        w.x = pack_bf16x2(x[0], x[1]);
-        w.y = pack_bf16x2(x[2], x[3]);
-        *reinterpret_cast<uint2*>(lds + tl * kImgRow + (rl + 16 * i) * 2) = w;
+      for (int u = 0; u < 8; ++u) {
+        const int r = L.r0 + big::RPP * u;
+        q.off[u] = ((uint32_t)min(r, v_valid - 1) * a.d + L.cc) * 2;
+        q.off[8 + u] = ((uint32_t)min(r, t_valid - 1) * a.d + L.cc) * 2;
       }
+      big_zero(acc);
+      big_tile<false, true>(lds, q, nk, acc, la, lb);
     }
-    big_image_out(lds, a.D + (size_t)t0 * a.Vp + c0, a.Vp, t_valid, 256);
-    // the other order, weighted; column sums for db
-    float sum[8][4];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) sum[i][r] = 0.f;
-    const bool odd = c & 1;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int tl = L.wn * 128 + 16 * j + c;
-      const float g = a.gs[min(t0 + tl, a.T - 1)];
+    const int c = L.lane & 15, rl = L.wm * 128 + 4 * (L.lane >> 4);  // the lane's first row
+    const int lim = v_valid - rl;  // its row o (16 i + r) is valid for o < lim
+    float b[BIAS ? 8 : 1][4], sum[BIAS ? 8 : 1][4];
+    if constexpr (BIAS)
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; r += 2) {
-          const float v0 = acc[i][j][r] * g, v1 = acc[i][j][r + 1] * g;
-          sum[i][r] += v0;
-          sum[i][r + 1] += v1;
-          const float got = swap_pair(odd ? v0 : v1);
-          const uint32_t w = odd ? pack_bf16x2(got, v1) : pack_bf16x2(v0, got);
-          *reinterpret_cast<uint32_t*>(lds + (rl + 16 * i + r + (odd ? 1 : 0)) * kImgRow +
-                                       (L.wn * 128 + 16 * j + (c & ~1)) * 2) = w;
+        for (int r = 0; r < 4; ++r) {
+          b[i][r] = a.bias ? a.bias[c0 + min(rl + 16 * i + r, v_valid - 1)] * kLog2e : 0.f;
+          sum[i][r] = 0.f;
         }
+    // rows of D past the last one lie behind the buffer's end and are dropped
+    int Vp = a.Vp;
+    asm volatile("" : "+s"(Vp));  // per-tile value: keeps the offsets below inside the tile loop
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
+        a.D + (size_t)t0 * Vp + c0, (short)0, (int)((uint32_t)t_valid * Vp * 2), 0x00020000);
+    const uint32_t col = (uint32_t)(L.wm * 128 + pack_col(L.lane));
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tl = L.wn * 128 + 16 * j + c, t = min(t0 + tl, a.T - 1);
+      const int y = a.rows.y[t];
+      const float l2 = a.rows.l2[t], m = a.rows.m[t], g = BIAS ? m * a.rows.e[t] : 0.f;
+      const bool live = y >= 0 && tl < t_valid;
+      const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
+      const int l = live ? lim : 0;
+      const uint32_t off = ((uint32_t)tl * Vp + col) * 2;
+#pragma unroll
+      for (int i = 0; i < 8; i += 2) {
+        float x[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int o = 16 * (i + k) + r;
+            const float s = BIAS ? b[i + k][r] - l2 : -l2;
+            float p = __builtin_amdgcn_exp2f(fmaf(acc[i + k][j][r], kLog2e, s));
+            p = o == yr ? p - 1.f : p;
+            p = o < l ? p : 0.f;
+            x[k][r] = p * m;
+            if constexpr (BIAS) sum[i + k][r] = fmaf(g, p, sum[i + k][r]);
+          }
+        __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, off, 32 * i, 0);
+      }
     }
-    big_image_out(lds, a.DT + (size_t)c0 * a.Tp + t0, a.Tp, 256, min(big::BN, a.Tp - t0));
-    if (a.db_part) {
+    if constexpr (BIAS) {
+      if (!a.db_part) continue;
       float* s_db = reinterpret_cast<float*>(lds);  // [2][256]
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float v = sum[i][r];
-#pragma unroll
-          for (int o = 8; o > 0; o >>= 1) v += __shfl_xor(v, o);
+          const float v = row16_sum(sum[i][r]);
           if (c == 0) s_db[L.wn * 256 + rl + 16 * i + r] = v;
         }
       lds_barrier();
@@ -434,78 +451,111 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
 }
 
 struct BigProdArgs {
-  const bf16_t* A;  // [M, K]
-  const bf16_t* B;  // [N, K]
+  const bf16_t* A;  // [K, M]
+  const bf16_t* B;  // [K, N] (DW) or [N, K] with rows ldb apart
   int M, N, K;
-  const float* scale;  // PARTIAL: not read
-  void* out;           // bf16 [M, N] times *scale, or fp32 slices [splits][M, N]
+  int lda, ldb;
+  const float* scale;  // DW
+  void* out;           // DW: bf16 [N, M] times *scale; else fp32 slices [splits][N, M]
   int splits;
-  int add;             // PARTIAL: added to what the slices hold
+  int add;             // not DW: added to what the slices hold
 };
 
-// A B^T on the large-group core
-template <bool PARTIAL>
+// out = B' A with the sums over K: dw (DW: A = scaled h, B = D, both transposed)
+// or partials of dh (A = w transposed, B = D)
+template <bool DW>
 __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
   __shared__ __align__(16) char lds[big::LDS];
   const BigLane L;
   TileSched S;
   int ntiles;
-  if (!S.init(cdiv_d(a.M, big::BM), cdiv_d(a.N, big::BN), a.splits, ntiles)) return;
-  const int nk = a.K / BK;
+  if (!S.init(cdiv_d(a.N, big::BN), cdiv_d(a.M, big::BM), a.splits, ntiles)) return;
+  uint32_t la[2], lb[2];
+  L.cols(la, L.wm);
+  if constexpr (DW)
+    L.cols(lb, L.wn);
+  else
+    L.rows(lb, L.wn);
+  const int nk = cdiv_d(a.K, BK);
   AccBig acc;
   for (int jt = 0; jt < ntiles; ++jt) {
-    int mt, nt, sp;
-    S.decode(jt, mt, nt, sp);
+    int nt, mt, sp;
+    S.decode(jt, nt, mt, sp);
     const int m0 = mt * big::BM, n0 = nt * big::BN;
     const int m_valid = min(big::BM, a.M - m0), n_valid = min(big::BN, a.N - n0);
     const int ka = (int)((long)sp * nk / a.splits), kb = (int)((long)(sp + 1) * nk / a.splits);
     {
-      BigRows q;
-      big_rows(q, a.A, m0, m_valid, a.B, n0, n_valid, a.K, ka * BK, L.r0, L.cc);
-      big_zero(acc);
-      big_tile<false>(lds, q, kb - ka, acc, L.a, L.b);
+      BigRowsT<DW> q;
+      q.la = big_long(a.A, a.lda, a.K, ka * BK, m0);
+      q.none = buf_rsrc_empty(a.A);
+      if constexpr (DW)
+        q.lb = big_long(a.B, a.ldb, a.K, ka * BK, n0);
+      else
+        q.rb0 = buf_rsrc(a.B + (size_t)n0 * a.ldb + ka * BK);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        q.off[u] = L.fetch(u, a.lda);
+        q.off[8 + u] = DW ? L.fetch(u, a.ldb)
+                          : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * a.ldb + L.cc) * 2;
+      }
+      if (!DW && a.add) {
+        // the sums so far in place of zeros
+        const int c = L.lane & 15, m = L.wm * 128 + 4 * (L.lane >> 4);
+        const float* was = static_cast<const float*>(a.out) + ((size_t)sp * a.N + n0) * a.M + m0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float* p = was + (size_t)min(L.wn * 128 + 16 * j + c, n_valid - 1) * a.M;
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            acc[i][j] = *reinterpret_cast<const f32x4_t*>(p + (m + 16 * i < m_valid ? m + 16 * i : 0));
+        }
+      } else {
+        big_zero(acc);
+      }
+      big_tile<false, true>(lds, q, kb - ka, acc, la, lb);
     }
-    const int c = L.lane & 15, hq = L.lane >> 4;
-    const int rl = L.wm * 128 + 4 * hq;
-    if constexpr (PARTIAL) {
-      float* out = static_cast<float*>(a.out) + (size_t)sp * a.M * a.N + (size_t)m0 * a.N + n0;
-      const int cl = L.wn * 128 + c;
+    const int c = L.lane & 15;
+    int M = a.M;
+    asm volatile("" : "+s"(M));  // per-tile value: keeps the offsets below inside the tile loop
+    constexpr int ES = DW ? 2 : 4;
+    const size_t o = ((size_t)(DW ? 0 : sp) * a.N + n0) * M + m0;
+    // rows past the last one lie behind the buffer's end
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<char*>(a.out) + o * ES, (short)0, (int)((uint32_t)n_valid * M * ES), 0x00020000);
+    const float g = DW ? *a.scale : 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t row = (uint32_t)(L.wn * 128 + 16 * j + c) * M;
+      const uint32_t off = (row + L.wm * 128 + (DW ? pack_col(L.lane) : 4 * (L.lane >> 4))) * ES;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (cl + 16 * j < n_valid)
+      for (int i = 0; i < 8; i += 2) {
+        if (L.wm * 128 + 16 * i >= m_valid) continue;  // (M is a multiple of 64)
+        if constexpr (DW) {
+          float x[2][4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (rl + 16 * i + r < m_valid) {
-                float* o = out + (size_t)(rl + 16 * i + r) * a.N + cl + 16 * j;
-                *o = a.add ? *o + acc[i][j][r] : acc[i][j][r];
-              }
-    } else {
-      const float g = *a.scale;
-      const bool odd = c & 1;
+          for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
+            for (int r = 0; r < 4; ++r) x[k][r] = acc[i + k][j][r] * g;
+          __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, off, 32 * i, 0);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-          for (int r = 0; r < 4; r += 2) {
-            const float v0 = acc[i][j][r] * g, v1 = acc[i][j][r + 1] * g;
-            const float got = swap_pair(odd ? v0 : v1);
-            const uint32_t w = odd ? pack_bf16x2(got, v1) : pack_bf16x2(v0, got);
-            *reinterpret_cast<uint32_t*>(lds + (rl + 16 * i + r + (odd ? 1 : 0)) * kImgRow +
-                                         (L.wn * 128 + 16 * j + (c & ~1)) * 2) = w;
+          for (int k = 0; k < 2; ++k) {
+            f32x4_t x = acc[i + k][j];
+            asm volatile("" : "+v"(x));  // through VGPRs (see big_store_partial_rows)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), ro, off,
+                                                   64 * (i + k), 0);
           }
-      big_image_out(lds, static_cast<bf16_t*>(a.out) + (size_t)m0 * a.N + n0, a.N, m_valid, n_valid);
+        }
+      }
     }
   }
 }
 
 namespace {
 
-// dh = g_t times the sum of the S slices, rounded once; 4 elements a thread (d
+// dh = g_t / m_t times the sum of the S slices, rounded once; 4 elements a thread (d
 // is a multiple of 64)
-__global__ __launch_bounds__(256) void k_dh_finish(const float* part, int S, const float* gl, int T,
+__global__ __launch_bounds__(256) void k_dh_finish(const float* part, int S, const float* gm, int T,
                                                    int d, bf16_t* dh) {
   const size_t n = (size_t)T * d, i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
   if (i >= n) return;
@@ -517,7 +567,7 @@ __global__ __launch_bounds__(256) void k_dh_finish(const float* part, int S, con
     s.z += x.z;
     s.w += x.w;
   }
-  const float g = gl[i / d];
+  const float g = gm[i / d];
   uint2 w;
   w.x = pack_bf16x2(s.x * g, s.y * g);
   w.y = pack_bf16x2(s.z * g, s.w * g);
@@ -636,10 +686,9 @@ hipError_t backward_f32(const HeadLossArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
-// bf16: a piece's D in both orders
 struct BackPlanBf16 {
-  int Vp, Tp, s_dh;  // columns of a piece, rows rounded up to a K slice, splits of dh
-  size_t o_rows, o_ht, o_wt, o_d, o_dt, o_dh, o_db, total;
+  int Vp, s_dh;  // columns of a piece (a multiple of the tile), splits of dh
+  size_t o_rows, o_hw, o_d, o_dh, o_db, total;
 };
 
 // K splits of an m x n product of nk slices on the large-group core: the fewest
@@ -661,8 +710,7 @@ int big_splits(int m, int n, int nk) {
 BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   BackPlanBf16 p;
   const size_t rows = T > 0 ? T : 1;
-  p.Tp = (int)((rows + 63) / 64 * 64);
-  const size_t fit = kPieceBytes / (4 * (size_t)p.Tp) / big::BM * big::BM;
+  const size_t fit = kPieceBytes / (2 * rows) / big::BM * big::BM;
   const int most = (int)std::min<size_t>(std::max<size_t>(fit, big::BM), (size_t)1 << 22);
   const int n_pieces = cdiv(V, most);
   p.Vp = cdiv(cdiv(V, n_pieces), big::BM) * big::BM;
@@ -673,11 +721,9 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
     o += align256(bytes);
     return at;
   };
-  p.o_rows = take(4 * (size_t)p.Tp * 4 + 256);
-  p.o_ht = take((size_t)d * p.Tp * 2);
-  p.o_wt = take((size_t)d * p.Vp * 2);
+  p.o_rows = take(5 * rows * 4 + 4);
+  p.o_hw = take(rows * d * 2);
   p.o_d = take(rows * p.Vp * 2);
-  p.o_dt = take((size_t)p.Vp * p.Tp * 2);
   p.o_dh = take((size_t)p.s_dh * rows * d * 4);
   p.o_db = take((size_t)cdiv((int)rows, big::BN) * p.Vp * 4);
   p.total = o;
@@ -698,53 +744,53 @@ hipError_t loss_bf16(const HeadLossArgs& a, hipStream_t st) {
 
 hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   const BackPlanBf16 p = back_plan_bf16(a.V, a.d, a.T);
-  int32_t* ys = reinterpret_cast<int32_t*>(a.ws + p.o_rows);
-  float* gl = reinterpret_cast<float*>(ys) + p.Tp;
-  float *gs = gl + p.Tp, *l2 = gs + p.Tp, *G = l2 + p.Tp;
-  bf16_t* ht = reinterpret_cast<bf16_t*>(a.ws + p.o_ht);
-  bf16_t* wt = reinterpret_cast<bf16_t*>(a.ws + p.o_wt);
+  const size_t rows = a.T > 0 ? a.T : 1;
+  float* f = reinterpret_cast<float*>(a.ws + p.o_rows);
+  const RowPart part{reinterpret_cast<int32_t*>(f), f + rows,     f + 2 * rows,
+                     f + 3 * rows,                  f + 4 * rows, f + 5 * rows};
+  bf16_t* hw = reinterpret_cast<bf16_t*>(a.ws + p.o_hw);
   bf16_t* D = reinterpret_cast<bf16_t*>(a.ws + p.o_d);
-  bf16_t* DT = reinterpret_cast<bf16_t*>(a.ws + p.o_dt);
   float* dh = reinterpret_cast<float*>(a.ws + p.o_dh);
   float* db = reinterpret_cast<float*>(a.ws + p.o_db);
   const bf16_t* w = static_cast<const bf16_t*>(a.w);
   const bf16_t* h = static_cast<const bf16_t*>(a.h);
-  const int n_tt = cdiv(a.T, big::BN);
+  const int n_tt = cdiv(a.T, big::BN), n_dt = cdiv(a.d, big::BM);
   const auto grid = [&](long tiles) { return dim3((unsigned)std::min<long>(tiles, a.n_cu)); };
-  hipLaunchKernelGGL(k_row_prep, dim3(1), dim3(1024), 0, st, a.target, a.lse, a.dloss, a.V, a.T, p.Tp,
-                     ys, gl, gs, l2, G);
-  if (a.dw)
-    hipLaunchKernelGGL(k_transpose, dim3(p.Tp / 64, a.d / 64), dim3(256), 0, st, h, ys, a.T, a.d,
-                       p.Tp, ht);
+  const auto threads = [](size_t n) { return dim3((unsigned)((n + 255) / 256)); };
+  const dim3 block(256);
+  static_assert(big::THREADS == 256, "one block shape");
+  hipLaunchKernelGGL(k_row_prep, dim3(1), dim3(1024), 0, st, a.target, a.lse, a.dloss, a.V, a.T,
+                     part);
+  if (a.dw && a.T > 0)
+    hipLaunchKernelGGL(k_scale_rows, threads((size_t)a.T * a.d / 8), block, 0, st, h, part, a.T, a.d,
+                       hw);
   for (int v0 = 0; v0 < a.V; v0 += p.Vp) {
     const int nv = std::min(p.Vp, a.V - v0), Vp = cdiv(nv, big::BM) * big::BM;
     const bf16_t* wp = w + (size_t)v0 * a.d;
-    DzArgs z{wp, h, a.b ? a.b + v0 : nullptr, ys, gs, l2, nv, v0, a.d, a.T, Vp, p.Tp, D, DT,
-             a.db ? db : nullptr};
-    if (a.T > 0)
-      hipLaunchKernelGGL(k_dz_big, grid((long)(Vp / big::BM) * n_tt), dim3(big::THREADS), 0, st, z);
+    if (a.T > 0) {
+      const DzArgs z{wp, h, a.b ? a.b + v0 : nullptr, part, nv, v0, a.d, a.T, Vp, D,
+                     a.db ? db : nullptr};
+      const dim3 g = grid((long)(Vp / big::BM) * n_tt);
+      if (a.b || a.db)
+        hipLaunchKernelGGL(k_dz_big<true>, g, block, 0, st, z);
+      else
+        hipLaunchKernelGGL(k_dz_big<false>, g, block, 0, st, z);
+    }
     if (a.db)
-      hipLaunchKernelGGL(k_db_finish, dim3(cdiv(nv, 256)), dim3(256), 0, st, db, n_tt, Vp, nv, G,
-                         a.db + v0);
+      hipLaunchKernelGGL(k_db_finish, threads(nv), block, 0, st, db, n_tt, Vp, nv, part.G, a.db + v0);
     if (a.dw) {
-      BigProdArgs q{DT, ht, nv, a.d, a.T > 0 ? p.Tp : 0, G, static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d,
-                    1, 0};
-      hipLaunchKernelGGL(k_prod_big<false>, grid((long)cdiv(nv, big::BM) * cdiv(a.d, big::BN)),
-                         dim3(big::THREADS), 0, st, q);
+      const BigProdArgs q{hw, D, a.d, nv, a.T, a.d, Vp, part.G,
+                          static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d, 1, 0};
+      hipLaunchKernelGGL(k_prod_big<true>, grid((long)cdiv(nv, big::BN) * n_dt), block, 0, st, q);
     }
     if (a.dh) {
-      hipLaunchKernelGGL(k_transpose, dim3(Vp / 64, a.d / 64), dim3(256), 0, st, wp, nullptr, nv, a.d,
-                         Vp, wt);
-      BigProdArgs q{D, wt, a.T, a.d, Vp, nullptr, dh, p.s_dh, v0 > 0};
-      hipLaunchKernelGGL(k_prod_big<true>, grid((long)n_tt * cdiv(a.d, big::BN) * p.s_dh),
-                         dim3(big::THREADS), 0, st, q);
+      const BigProdArgs q{wp, D, a.d, a.T, nv, a.d, Vp, nullptr, dh, p.s_dh, v0 > 0};
+      hipLaunchKernelGGL(k_prod_big<false>, grid((long)n_tt * n_dt * p.s_dh), block, 0, st, q);
     }
   }
-  if (a.dh) {
-    const size_t n = (size_t)a.T * a.d / 4;
-    hipLaunchKernelGGL(k_dh_finish, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, dh, p.s_dh,
-                       gl, a.T, a.d, static_cast<bf16_t*>(a.dh));
-  }
+  if (a.dh)
+    hipLaunchKernelGGL(k_dh_finish, threads((size_t)a.T * a.d / 4), block, 0, st, dh, p.s_dh, part.gm,
+                       a.T, a.d, static_cast<bf16_t*>(a.dh));
   return hipGetLastError();
 }
 

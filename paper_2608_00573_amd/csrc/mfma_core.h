@@ -481,34 +481,10 @@ typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 // A 32-wide k-step issues its 64 MFMAs row by row (tile (i, j) = (T / 8,
 // T % 8)): a_i is last used by MFMA 8 i + 7, so the next k-step's a_i is read
 // into the same registers right after it, while the b fragments alternate
-// between two sets.  Per MFMA slot T: the lgkmcnt wait before it (-1: none;
-// the value counts the LDS reads issued after the ones it needs, capped at
-// the counter's 15, which only waits longer), and the fragment read after it
-// (q = 2 n for a_n, 2 n + 1 for b_n; -1: none; the first k-step also reads
-// the next a_0 after MFMA 7), for the first k-step of a slice (0) and the
-// last (1: its reads, of the next slice, follow the slice barrier before
-// MFMA 32).  The first k-step waits on the last k-step's read order and the
-// last k-step on the first's.
-constexpr int kWait0[64] = {
-    14, 13, 12, 11, 10, 10, 10, 10,  // MFMAs 0..7
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 8..15
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 16..23
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 24..31
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 32..39
-    15, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 40..47
-    15, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 48..55
-    15, -1, -1, -1, -1, -1, -1, -1   // MFMAs 56..63
-};
-constexpr int kWait1[64] = {
-     7, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 0..7
-     6, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 8..15
-     5, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 16..23
-     4, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 24..31
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 32..39
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 40..47
-    -1, -1, -1, -1, -1, -1, -1, -1,  // MFMAs 48..55
-    -1, -1, -1, -1, -1, -1, -1, -1   // MFMAs 56..63
-};
+// between two sets.  Per MFMA slot T: the fragment read after it (q = 2 n for
+// a_n, 2 n + 1 for b_n; -1: none; the first k-step also reads the next a_0
+// after MFMA 7), for the first k-step of a slice (0) and the last (1: its
+// reads, of the next slice, follow the slice barrier before MFMA 32).
 constexpr int kRead0[64] = {
      1,  3,  5,  7,  9, 11, 13, 15,  // MFMAs 0..7
     -1, -1, -1, -1, -1, -1, -1,  2,  // MFMAs 8..15
@@ -530,6 +506,48 @@ constexpr int kRead1[64] = {
     12, -1, -1, -1, -1, -1, -1, 14   // MFMAs 56..63
 };
 
+// The lgkmcnt wait before each MFMA slot (-1: none): the LDS operations issued
+// after the ones the slot needs, at most the counter's 15 (which only waits
+// longer), where an earlier wait has not shown them landed.  The first k-step
+// waits on the last k-step's read order and the last on the first's.  A
+// fragment that is read transposed (BigRowsT) takes two operations.
+struct BigWaits {
+  int w[2][64];
+};
+constexpr BigWaits big_waits(bool atr, bool btr) {
+  BigWaits out{};
+  const int ops_a = atr ? 2 : 1, ops_b = btr ? 2 : 1;
+  int end[2][16] = {};  // per k-step: operations issued up to the end of read q
+  int issued = 0, landed = 0;
+  for (int t = 0; t < 64; ++t)  // what is in flight when a slice begins
+    if (kRead1[t] >= 0) {
+      issued += kRead1[t] & 1 ? ops_b : ops_a;
+      end[0][kRead1[t]] = issued;
+    }
+  for (int ks = 0; ks < 2; ++ks)
+    for (int t = 0; t < 64; ++t) {
+      if (ks == 1 && t == 32) landed = issued;  // the slice barrier
+      const int ea = end[ks][2 * (t / 8)], eb = end[ks][2 * (t % 8) + 1];
+      const int need = ea > eb ? ea : eb;
+      out.w[ks][t] = -1;
+      if (need > landed) {
+        const int n = issued - need < 15 ? issued - need : 15;
+        out.w[ks][t] = n;
+        landed = issued - n;
+      }
+      const int q = ks ? kRead1[t] : kRead0[t];
+      if (q >= 0) {
+        issued += q & 1 ? ops_b : ops_a;
+        end[1 - ks][q] = issued;
+      }
+      if (ks == 0 && t == 7) {
+        issued += ops_a;
+        end[1][0] = issued;
+      }
+    }
+  return out;
+}
+
 // B fragment j of a wavefront: LDS row offset from its first B row.  DUAL:
 // columns j = 0..3 of the up operand (rows 0..127 of the B stage), j = 4..7
 // the same columns of the gate operand (rows 128..255).
@@ -538,14 +556,39 @@ constexpr int big_brow(int j) {
   return DUAL ? (j < 4 ? 16 * j : 128 + 16 * (j - 4)) : 16 * j;
 }
 
+// Transposed fragment read, of an operand that lies row by row along K: a slice
+// is 64 rows (K) of 256 columns, 512 bytes each.  ds_read_b64_tr_b16 gives lane
+// l of each 16 the 4 rows of column l out of what the 16 lanes address (lane i:
+// 4 columns from 4 (i % 4) of row i / 4), so two of them, 4 rows apart, fill a
+// fragment.  The 32-byte pieces of a row sit at piece n ^ (k % 4 + 4 (k / 8 % 2)):
+// the rows that 32 lanes read together touch distinct banks, and fragment n's
+// address is the lane's base ^ 32 n.
+__device__ __forceinline__ bf16x8_t lds_read_tr(uint32_t a) {
+  typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+  u32x2_t lo, hi;
+  asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(a));
+  asm volatile("ds_read_b64_tr_b16 %0, %1 offset:2048" : "=v"(hi) : "v"(a));
+  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
+}
+// piece of a transposed operand's row k
+__device__ __forceinline__ int tr_swz(int k) { return (k & 3) | ((k >> 3 & 1) << 2); }
+
 // fragment read Q of a k-step: a_{Q/2} for even Q, b_{Q/2} for odd Q
-template <bool DUAL, int Q>
+template <bool DUAL, bool ATR, bool BTR, int Q>
 __device__ __forceinline__ void big_read(FragA& fa, FragB& fb, uint32_t pa, uint32_t pb) {
   if constexpr (Q >= 0) {
-    if constexpr (Q & 1)
-      fb.b[Q >> 1] = lds_read_at<big_brow<DUAL>(Q >> 1) * big::RB>(pb);
-    else
-      fa.a[Q >> 1] = lds_read_at<(Q >> 1) * 16 * big::RB>(pa);
+    constexpr int n = Q >> 1;
+    if constexpr (Q & 1) {
+      if constexpr (BTR)
+        fb.b[n] = lds_read_tr(pb ^ (n << 5));
+      else
+        fb.b[n] = lds_read_at<big_brow<DUAL>(n) * big::RB>(pb);
+    } else {
+      if constexpr (ATR)
+        fa.a[n] = lds_read_tr(pa ^ (n << 5));
+      else
+        fa.a[n] = lds_read_at<n * 16 * big::RB>(pa);
+    }
     sched_fence();
   }
 }
@@ -554,6 +597,7 @@ __device__ __forceinline__ void big_read(FragA& fa, FragB& fb, uint32_t pa, uint
 // clamped), u >= 8 B row r0 + 32 (u - 8) (clamped to the valid columns); byte
 // offsets of the thread's 16-byte chunk within their buffers at K = k0
 struct BigRows {
+  static constexpr bool ATR = false, BTR = false;
   __amdgpu_buffer_rsrc_t ra, rb0, rb1, none;
   uint32_t off[16];
 };
@@ -572,23 +616,71 @@ struct BigSrc {
   }
 };
 
-// B row group u (0..7) of the wave straight into B stage `bst` (LDS address):
-// lane l lands at bst + (8 w + 32 u) * 128 + 16 l, which is row 8 w + 32 u +
-// l / 8, chunk slot l % 8 (the thread's fetch chunk is the swizzled one)
-template <bool DUAL>
-__device__ __forceinline__ void big_dma(uint32_t bst, int wave, const BigRows& q, const BigSrc& b,
-                                        int u) {
-  const __amdgpu_buffer_rsrc_t& rs = DUAL && u >= 4 ? b.rb1 : b.rb0;
-  const uint32_t dst = bst + (uint32_t)((8 * wave + big::RPP * u) * big::RB);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_byte*)(uintptr_t)dst, 16, q.off[8 + u], b.ko, 0,
-                                           0);
-}
+// An operand that lies row by row along K is fetched 64 rows a slice: the
+// buffer starts at the slice's first row (so its offsets stay within one slice)
+// and ends with the operand, whose missing rows land as zeros.  Thread offsets:
+// row 2 w + 8 u + l / 32, 16-byte chunk l % 32 of the swizzled LDS row.
+struct BigLong {
+  const char* p;      // row 0 of the tile's K range, column 0 of the tile
+  long long bytes;    // from there to the operand's end
+  long long slice;    // 64 rows
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int kt, int nk) const {
+    const long long o = kt * slice, left = bytes - o;
+    const bool live = kt < nk && left > 0;
+    const int n = live ? (int)(unsigned)(left < 0xffffffffll ? left : 0xffffffffll) : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p) + (live ? o : 0), (short)0, n,
+                                             0x00020000);
+  }
+};
+// A such an operand, B one too (BTR) or K-contiguous
+template <bool BTR_>
+struct BigRowsT {
+  static constexpr bool ATR = true, BTR = BTR_;
+  __amdgpu_buffer_rsrc_t rb0, none;  // B, unless BTR
+  BigLong la, lb;
+  uint32_t off[16];
+};
+template <bool BTR>
+struct BigSrcT {
+  __amdgpu_buffer_rsrc_t ra, rb0;
+  uint32_t ko;
+  __device__ __forceinline__ BigSrcT(const BigRowsT<BTR>& q, int kt, int nk) {
+    const bool live = kt < nk;
+    ra = q.la.at(kt, nk);
+    if constexpr (BTR)
+      rb0 = q.lb.at(kt, nk);
+    else
+      rb0 = live ? q.rb0 : q.none;
+    ko = live && !BTR ? kt * big::RB : 0;
+  }
+};
+template <class R>
+struct BigSrcOf {
+  using type = BigSrcT<R::BTR>;
+};
+template <>
+struct BigSrcOf<BigRows> {
+  using type = BigSrc;
+};
 
-// A row group u (0..7) of the wave straight into A stage `ast`
-__device__ __forceinline__ void big_dma_a(uint32_t ast, int wave, const BigRows& q, const BigSrc& b,
-                                          int u) {
-  const uint32_t dst = ast + (uint32_t)((8 * wave + big::RPP * u) * big::RB);
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(b.ra, (lds_byte*)(uintptr_t)dst, 16, q.off[u], b.ko, 0, 0);
+// Row group u (0..7) of the wave straight into an LDS stage: lane l lands at
+// stage + (8 w + 32 u) * 128 + 16 l, which is row 8 w + 32 u + l / 8, chunk slot
+// l % 8 (the thread's fetch chunk is the swizzled one)
+__device__ __forceinline__ void big_dma_group(uint32_t stage, int wave, __amdgpu_buffer_rsrc_t rs,
+                                              uint32_t off, uint32_t ko, int u) {
+  const uint32_t dst = stage + (uint32_t)((8 * wave + big::RPP * u) * big::RB);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_byte*)(uintptr_t)dst, 16, off, ko, 0, 0);
+}
+template <bool DUAL, class R, class Src>
+__device__ __forceinline__ void big_dma(uint32_t bst, int wave, const R& q, const Src& b, int u) {
+  if constexpr (DUAL)
+    big_dma_group(bst, wave, u >= 4 ? b.rb1 : b.rb0, q.off[8 + u], b.ko, u);
+  else
+    big_dma_group(bst, wave, b.rb0, q.off[8 + u], b.ko, u);
+}
+template <class R, class Src>
+__device__ __forceinline__ void big_dma_a(uint32_t ast, int wave, const R& q, const Src& b, int u) {
+  big_dma_group(ast, wave, b.ra, q.off[u], R::ATR ? 0 : b.ko, u);
 }
 
 // MFMA slot T of a k-step (LAST: the second of the slice) from fragments fa,
@@ -601,11 +693,11 @@ __device__ __forceinline__ void big_dma_a(uint32_t ast, int wave, const BigRows&
 // in the first, 4..7 in the last).  The barrier waits for the next slice's
 // A DMAs (the last issued at MFMA 28 of the first k-step, followed by 4 B
 // DMAs) and its B DMAs (issued a slice earlier).
-template <int T, bool LAST, bool DUAL, class DmaA, class DmaB>
+template <int T, bool LAST, bool DUAL, class R, class DmaA, class DmaB>
 __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig& acc,
                                          uint32_t pa, uint32_t pb, DmaA& dma_a, DmaB& dma_b) {
   constexpr int i = T / 8, j = T % 8;
-  constexpr int w = LAST ? kWait1[T] : kWait0[T];
+  constexpr int w = big_waits(R::ATR, R::BTR).w[LAST ? 1 : 0][T];
   if constexpr (w >= 0) {
     lgkm_le<w>();
     asm volatile("" : "+v"(fa.a[i]), "+v"(fb.b[j]));
@@ -622,9 +714,9 @@ __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig
                : "+a"(acc[i][j])
                : "v"(fa.a[i]), "v"(fb.b[j]));
   sched_fence();
-  big_read<DUAL, LAST ? kRead1[T] : kRead0[T]>(fa, fn, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, LAST ? kRead1[T] : kRead0[T]>(fa, fn, pa, pb);
   // the first k-step's a_0 for the next k-step, after its last use
-  if constexpr (!LAST && T == 7) big_read<DUAL, 0>(fa, fn, pa, pb);
+  if constexpr (!LAST && T == 7) big_read<DUAL, R::ATR, R::BTR, 0>(fa, fn, pa, pb);
   if constexpr (!LAST && (T == 16 || T == 20 || T == 24 || T == 28)) {
     dma_a(4 + (T - 16) / 4);
     sched_fence();
@@ -637,7 +729,7 @@ __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig
     dma_b((LAST ? 4 : 0) + (T == 18 ? 0 : T == 26 ? 1 : T == 50 ? 2 : 3));
     sched_fence();
   }
-  if constexpr (T < 63) big_slot<T + 1, LAST, DUAL>(fa, fb, fn, acc, pa, pb, dma_a, dma_b);
+  if constexpr (T < 63) big_slot<T + 1, LAST, DUAL, R>(fa, fb, fn, acc, pa, pb, dma_a, dma_b);
 }
 
 // LDS of the large-group core: A stages at s0 and s0 + AB (slice parity), B
@@ -650,30 +742,32 @@ struct BigLds {
 
 // One 64-wide slice g: two k-steps of 32 from A stage g & 1 and B stage
 // g mod 3
-template <bool DUAL>
-__device__ __forceinline__ void big_half(const BigLds& L, int g, int wave, const BigRows& q,
+template <bool DUAL, class R>
+__device__ __forceinline__ void big_half(const BigLds& L, int g, int wave, const R& q,
                                          int nk, AccBig& acc, const uint32_t (&a_lane)[2],
                                          const uint32_t (&b_lane)[2], FragA& fa, FragB& fb0,
                                          FragB& fb1) {
   const uint32_t ca = L.a(g), cb = L.b(g), na = L.a(g + 1), nb = L.b(g + 1), db = L.b(g + 2);
-  const BigSrc sa(q, g + 1, nk), sb(q, g + 2, nk);
+  const typename BigSrcOf<R>::type sa(q, g + 1, nk), sb(q, g + 2, nk);
   auto dma_a = [&](int u) { big_dma_a(na, wave, q, sa, u); };
   auto dma_a2 = [&](int u) { big_dma_a(ca, wave, q, sb, u); };
   auto dma_b = [&](int u) { big_dma<DUAL>(db, wave, q, sb, u); };
-  big_slot<0, false, DUAL>(fa, fb0, fb1, acc, ca + a_lane[1], cb + b_lane[1], dma_a, dma_b);
-  big_slot<0, true, DUAL>(fa, fb1, fb0, acc, na + a_lane[0], nb + b_lane[0], dma_a2, dma_b);
+  big_slot<0, false, DUAL, R>(fa, fb0, fb1, acc, ca + a_lane[1], cb + b_lane[1], dma_a, dma_b);
+  big_slot<0, true, DUAL, R>(fa, fb1, fb0, acc, na + a_lane[0], nb + b_lane[0], dma_a2, dma_b);
 }
 
 // C tile += A rows x B rows over nk slices from the rows' K origin; returns
 // with every load landed and every wave past its last LDS access
-template <bool DUAL>
-__device__ __forceinline__ void big_tile(char* lds, const BigRows& q, int nk, AccBig& acc,
+// (SETTLE: the last row's wait states come inside the loop, after its last slice,
+// for kernels in which the compiler copies accumulators on the way out of it).
+template <bool DUAL, bool SETTLE = false, class R>
+__device__ __forceinline__ void big_tile(char* lds, const R& q, int nk, AccBig& acc,
                                          const uint32_t (&a_lane)[2],
                                          const uint32_t (&b_lane)[2]) {
   const BigLds L{lds_addr(lds)};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   {
-    const BigSrc s0(q, 0, nk), s1(q, 1, nk);
+    const typename BigSrcOf<R>::type s0(q, 0, nk), s1(q, 1, nk);
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       big_dma_a(L.a(0), wave, q, s0, u);
@@ -703,24 +797,29 @@ __device__ __forceinline__ void big_tile(char* lds, const BigRows& q, int nk, Ac
   FragA fa;
   FragB fb0, fb1;
   const uint32_t pa = L.a(0) + a_lane[0], pb = L.b(0) + b_lane[0];
-  big_read<DUAL, 0>(fa, fb0, pa, pb);
-  big_read<DUAL, 1>(fa, fb0, pa, pb);
-  big_read<DUAL, 2>(fa, fb0, pa, pb);
-  big_read<DUAL, 3>(fa, fb0, pa, pb);
-  big_read<DUAL, 4>(fa, fb0, pa, pb);
-  big_read<DUAL, 5>(fa, fb0, pa, pb);
-  big_read<DUAL, 6>(fa, fb0, pa, pb);
-  big_read<DUAL, 7>(fa, fb0, pa, pb);
-  big_read<DUAL, 8>(fa, fb0, pa, pb);
-  big_read<DUAL, 9>(fa, fb0, pa, pb);
-  big_read<DUAL, 11>(fa, fb0, pa, pb);
-  big_read<DUAL, 13>(fa, fb0, pa, pb);
-  big_read<DUAL, 15>(fa, fb0, pa, pb);
-  big_read<DUAL, 10>(fa, fb0, pa, pb);
-  big_read<DUAL, 12>(fa, fb0, pa, pb);
-  big_read<DUAL, 14>(fa, fb0, pa, pb);
-  for (int g = 0; g < nk; ++g)
-    big_half<DUAL>(L, g, wave, q, nk, acc, a_lane, b_lane, fa, fb0, fb1);
+  big_read<DUAL, R::ATR, R::BTR, 0>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 1>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 2>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 3>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 4>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 5>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 6>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 7>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 8>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 9>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 11>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 13>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 15>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 10>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 12>(fa, fb0, pa, pb);
+  big_read<DUAL, R::ATR, R::BTR, 14>(fa, fb0, pa, pb);
+  for (int g = 0; g < nk; ++g) {
+    big_half<DUAL, R>(L, g, wave, q, nk, acc, a_lane, b_lane, fa, fb0, fb1);
+    if (SETTLE && g + 1 == nk)
+      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 3"
+                   : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]),
+                     "+a"(acc[7][4]), "+a"(acc[7][5]), "+a"(acc[7][6]), "+a"(acc[7][7]));
+  }
   // The last k-step read the first fragments of the slice past the end
   // (never used).  Those reads land whenever the LDS returns them, which the
   // compiler cannot see: the wait for them takes their registers as inputs,
