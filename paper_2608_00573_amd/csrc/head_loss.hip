@@ -190,9 +190,11 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 }
 
 // ------------------------------------------------------ backward, bf16 --
-// Three products on the large-group core.  D of a piece is written once, [T, Vp],
-// and read in both orders: as it lies for dh, transposed out of LDS for dw (as
-// are w for dh and h for dw: nothing is laid out again in memory).
+// Three products on the large-group core.  D of a piece is written once and read
+// in both orders: as it lies for dh, transposed out of LDS for dw (as are w for
+// dh and h for dw: nothing is turned in memory).
+//   * D and the scaled copy of h lie in panels of 256 columns, [panel][row][256]:
+//     a 64-row slice of a tile is then one run of 32 KB.
 //   * D enters the products in bf16, once rounded.  A row's weight g is G m 2^-e
 //     with G the largest |g| and |m| in [1, 2): D holds m (softmax - onehot), dh
 //     takes g / m on its fp32 sums, dw G on its own and 2^-e on the rows of h,
@@ -249,7 +251,7 @@ __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const 
   }
 }
 
-// hw = 2^-e h_t, zeros in the rows that take no part; 8 elements a thread
+// hw = 2^-e h_t in panels, zeros in the rows that take no part; 8 elements a thread
 __global__ __launch_bounds__(256) void k_scale_rows(const bf16_t* h, RowPart p, int T, int d,
                                                     bf16_t* hw) {
   const size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x);
@@ -267,7 +269,8 @@ __global__ __launch_bounds__(256) void k_scale_rows(const bf16_t* h, RowPart p, 
 #pragma unroll
     for (int u = 0; u < 4; ++u) x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * s, bf2f(x.e[2 * u + 1]) * s);
   }
-  *reinterpret_cast<uint4*>(hw + i) = x.v;
+  const int c = (int)(i - (size_t)t * d);
+  *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t) * 256 + (c & 255)) = x.v;
 }
 
 }  // namespace
@@ -307,11 +310,15 @@ struct BigLane {
   }
 };
 
-// an operand of `rows` rows along K from row k0 and column c0
+// an operand of `rows` rows along K from row k0 and column c0, or panel c0 / 256
+// of one in panels
 __device__ __forceinline__ BigLong big_long(const bf16_t* p, int ld, int rows, int k0, int c0) {
   const long long o = ((long long)k0 * ld + c0) * 2;
   return BigLong{reinterpret_cast<const char*>(p) + o, (long long)rows * ld * 2 - o,
                  (long long)ld * 128};
+}
+__device__ __forceinline__ BigLong big_panel(const bf16_t* p, int rows, int k0, int c0) {
+  return big_long(p + (size_t)c0 * rows, 256, rows, k0, 0);
 }
 
 __device__ __forceinline__ void big_zero(AccBig& acc) {
@@ -352,8 +359,8 @@ struct DzArgs {
   const float* bias;  // the piece's first row, or NULL
   RowPart rows;
   int nv, v0, d, T;
-  int Vp;             // leading dimension of D
-  bf16_t* D;
+  int Vp;             // columns of D
+  bf16_t* D;          // [Vp / 256][T][256]
   float* db_part;     // [token tiles][Vp] or NULL
 };
 
@@ -401,10 +408,8 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
           sum[i][r] = 0.f;
         }
     // rows of D past the last one lie behind the buffer's end and are dropped
-    int Vp = a.Vp;
-    asm volatile("" : "+s"(Vp));  // per-tile value: keeps the offsets below inside the tile loop
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
-        a.D + (size_t)t0 * Vp + c0, (short)0, (int)((uint32_t)t_valid * Vp * 2), 0x00020000);
+        a.D + ((size_t)vt * a.T + t0) * 256, (short)0, t_valid * 512, 0x00020000);
     const uint32_t col = (uint32_t)(L.wm * 128 + pack_col(L.lane));
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -414,7 +419,7 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
       const bool live = y >= 0 && tl < t_valid;
       const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
       const int l = live ? lim : 0;
-      const uint32_t off = ((uint32_t)tl * Vp + col) * 2;
+      const uint32_t off = ((uint32_t)tl * 256 + col) * 2;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         float x[2][4];
@@ -451,10 +456,9 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
 }
 
 struct BigProdArgs {
-  const bf16_t* A;  // [K, M]
-  const bf16_t* B;  // [K, N] (DW) or [N, K] with rows ldb apart
+  const bf16_t* A;  // [K, M], DW: in panels
+  const bf16_t* B;  // D in panels: [K, N] (DW) or [N, K]
   int M, N, K;
-  int lda, ldb;
   const float* scale;  // DW
   void* out;           // DW: bf16 [N, M] times *scale; else fp32 slices [splits][N, M]
   int splits;
@@ -486,17 +490,21 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
     const int ka = (int)((long)sp * nk / a.splits), kb = (int)((long)(sp + 1) * nk / a.splits);
     {
       BigRowsT<DW> q;
-      q.la = big_long(a.A, a.lda, a.K, ka * BK, m0);
       q.none = buf_rsrc_empty(a.A);
-      if constexpr (DW)
-        q.lb = big_long(a.B, a.ldb, a.K, ka * BK, n0);
-      else
-        q.rb0 = buf_rsrc(a.B + (size_t)n0 * a.ldb + ka * BK);
+      if constexpr (DW) {
+        q.la = big_panel(a.A, a.K, ka * BK, m0);
+        q.lb = big_panel(a.B, a.K, ka * BK, n0);
+      } else {
+        q.la = big_long(a.A, a.M, a.K, ka * BK, m0);
+        q.rb0 = buf_rsrc(a.B + (size_t)n0 * 256);
+        q.panel = (uint32_t)a.N * 512;
+        q.k0 = ka;
+      }
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
-        q.off[u] = L.fetch(u, a.lda);
-        q.off[8 + u] = DW ? L.fetch(u, a.ldb)
-                          : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * a.ldb + L.cc) * 2;
+        q.off[u] = L.fetch(u, DW ? 256 : a.M);
+        q.off[8 + u] = DW ? L.fetch(u, 256)
+                          : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * 256 + L.cc) * 2;
       }
       if (!DW && a.add) {
         // the sums so far in place of zeros
@@ -722,7 +730,7 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
     return at;
   };
   p.o_rows = take(5 * rows * 4 + 4);
-  p.o_hw = take(rows * d * 2);
+  p.o_hw = take(rows * cdiv(d, 256) * 512);
   p.o_d = take(rows * p.Vp * 2);
   p.o_dh = take((size_t)p.s_dh * rows * d * 4);
   p.o_db = take((size_t)cdiv((int)rows, big::BN) * p.Vp * 4);
@@ -779,12 +787,12 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
     if (a.db)
       hipLaunchKernelGGL(k_db_finish, threads(nv), block, 0, st, db, n_tt, Vp, nv, part.G, a.db + v0);
     if (a.dw) {
-      const BigProdArgs q{hw, D, a.d, nv, a.T, a.d, Vp, part.G,
+      const BigProdArgs q{hw, D, a.d, nv, a.T, part.G,
                           static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d, 1, 0};
       hipLaunchKernelGGL(k_prod_big<true>, grid((long)cdiv(nv, big::BN) * n_dt), block, 0, st, q);
     }
     if (a.dh) {
-      const BigProdArgs q{wp, D, a.d, a.T, nv, a.d, Vp, nullptr, dh, p.s_dh, v0 > 0};
+      const BigProdArgs q{wp, D, a.d, a.T, nv, nullptr, dh, p.s_dh, v0 > 0};
       hipLaunchKernelGGL(k_prod_big<false>, grid((long)n_tt * n_dt * p.s_dh), block, 0, st, q);
     }
   }

@@ -632,12 +632,15 @@ struct BigLong {
                                              0x00020000);
   }
 };
-// A such an operand, B one too (BTR) or K-contiguous
+// A such an operand, B one too (BTR) or K-contiguous in panels of 256 columns
+// (K), `panel` bytes each, from slice k0
 template <bool BTR_>
 struct BigRowsT {
   static constexpr bool ATR = true, BTR = BTR_;
   __amdgpu_buffer_rsrc_t rb0, none;  // B, unless BTR
   BigLong la, lb;
+  uint32_t panel;
+  int k0;
   uint32_t off[16];
 };
 template <bool BTR>
@@ -651,7 +654,8 @@ struct BigSrcT {
       rb0 = q.lb.at(kt, nk);
     else
       rb0 = live ? q.rb0 : q.none;
-    ko = live && !BTR ? kt * big::RB : 0;
+    const int k = q.k0 + kt;
+    ko = live && !BTR ? (uint32_t)(k >> 2) * q.panel + (uint32_t)(k & 3) * big::RB : 0;
   }
 };
 template <class R>
