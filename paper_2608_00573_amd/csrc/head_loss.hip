@@ -328,22 +328,6 @@ __device__ __forceinline__ void big_zero(AccBig& acc) {
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{};
 }
 
-// Two accumulators' values of one row (columns 16 i .. and 16 (i + 1) ..; a lane
-// holds 4 consecutive ones) as bf16, 8 consecutive columns a lane: lanes of even
-// groups of 16 get the first block's pieces, those of odd groups the second's
-__device__ __forceinline__ u32x4_t pack_rows(const float (&x)[4], const float (&y)[4]) {
-  const unsigned x0 = pack_bf16x2(x[0], x[1]), x1 = pack_bf16x2(x[2], x[3]);
-  const unsigned y0 = pack_bf16x2(y[0], y[1]), y1 = pack_bf16x2(y[2], y[3]);
-  const auto p = __builtin_amdgcn_permlane16_swap(x0, y0, false, false);
-  const auto q = __builtin_amdgcn_permlane16_swap(x1, y1, false, false);
-  const unsigned p0 = p[0], p1 = p[1], q0 = q[0], q1 = q[1];
-  return u32x4_t{p0, q0, p1, q1};
-}
-// ... and where they go: column of the lane's piece within the two blocks
-__device__ __forceinline__ int pack_col(int lane) {
-  return 16 * (lane >> 4 & 1) + 8 * (lane >> 5);
-}
-
 __device__ __forceinline__ float row16_sum(float v) {
   // over the 16 lanes of a row (rotations by 8, 4, 2, 1)
   v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));

@@ -58,8 +58,8 @@ struct BalanceArgs {
   char* ws;
 };
 
-size_t balance_ws(int E, int T);
-size_t balance_backward_ws(int E, int d, int T);
+size_t balance_ws(bool bf16, int E, int d, int T);
+size_t balance_backward_ws(bool bf16, int E, int d, int T);
 hipError_t launch_balance(const BalanceArgs& a, hipStream_t st);
 hipError_t launch_balance_backward(const BalanceArgs& a, hipStream_t st);
 
