@@ -9,6 +9,7 @@ the import of ``lib()`` raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -412,35 +413,58 @@ def trimmoe_train_exit_head(h: torch.Tensor, labels: torch.Tensor, epochs: int, 
 
 
 # ------------------------------------------------------- training losses ---
+class _NoContext:
+    def __enter__(self):
+        return None
+
+    def __exit__(self, *exc):
+        return False
+
+
+_NO_CONTEXT = _NoContext()
+
+
 def _on_stream(t: torch.Tensor, stream):
     """Context in which outputs and workspaces belong to the stream that the
     call runs on (`stream`, or the current one of t's device)."""
     if not t.is_cuda:
         raise ValueError("the training losses run on GPU tensors")
-    return torch.cuda.stream(stream if stream is not None else torch.cuda.current_stream(t.device))
+    if stream is not None:
+        return torch.cuda.stream(stream)
+    if t.device.index == torch.cuda.current_device():
+        return _NO_CONTEXT
+    return torch.cuda.device(t.device)
 
 
 def _take(name: str, t: torch.Tensor, shape, dtype, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device \
-            or not t.is_contiguous():
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} "
                          f"is needed, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t
 
 
 def _rows_and_weights(w: torch.Tensor, h: torch.Tensor):
     code = _dtype_code(h)
     if w.dim() != 2 or h.dim() != 2:
         raise ValueError("the weights are [V, d] (or [E, d]) and the rows [n, d]")
-    _take("weights", w, (w.shape[0], h.shape[1]), h.dtype, h.device)
-    _take("rows", h, h.shape, h.dtype, h.device)
-    return code, w.shape[0], h.shape[1], h.shape[0]
+    (n, d), v = h.shape, w.shape[0]
+    _take("weights", w, (v, d), h.dtype, h.device)
+    if not h.is_contiguous():
+        raise ValueError("rows: a contiguous tensor is needed")
+    return code, v, d, n
+
+
+@functools.lru_cache(maxsize=1024)
+def _loss_ws_bytes(name: str, dims) -> int:
+    n = C.c_size_t(0)
+    _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(*dims, C.byref(n)))
+    return max(n.value, 256)
 
 
 def _loss_ws(name: str, dims, device) -> torch.Tensor:
-    n = C.c_size_t(0)
-    _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(*dims, C.byref(n)))
-    return _aligned_ws(max(n.value, 256), device)
+    n = _loss_ws_bytes(name, dims)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    # (torch's allocator aligns its blocks further than the library asks)
+    return ws if ws.data_ptr() % 256 == 0 else _aligned_ws(n, device)
 
 
 def trimmoe_head_cross_entropy(w_head: torch.Tensor, h: torch.Tensor, target: torch.Tensor,

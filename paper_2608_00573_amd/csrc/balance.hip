@@ -6,15 +6,17 @@
 //   dh = dz w,  dw = dz^T h,  db_e = sum_t dz_te        (counts held constant)
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "loss.h"
 #include "mfma_core.h"
-#include "products.h"
 
 namespace trimmoe {
 
 namespace {
+
+inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Rows are handled 16 lanes a row (experts l, l + 16, ...: ET of them a lane) and
 // 64 a tile.
@@ -77,58 +79,121 @@ __device__ __forceinline__ bool row_forward(float (&z)[ET], size_t t, const int1
   return live;
 }
 
-// fp32: the rows' logits lie in S slices of partial sums
-template <int ET>
-__global__ __launch_bounds__(256) void k_balance_rows(const float* logits, int S, const float* b,
-                                                      const int16_t* target, int T, int E, int k,
-                                                      float* prob, float* part_p, int32_t* part_c) {
-  __shared__ float s_p[16][16 * ET + 1];
-  __shared__ int32_t s_c[TRIMMOE_MAX_EXPERTS + 1];
-  const int row = threadIdx.x >> 4, l = threadIdx.x & 15;
-  for (int e = threadIdx.x; e <= E; e += 256) s_c[e] = 0;
-  __syncthreads();
-  float sum[ET] = {};
-  for (int t0 = blockIdx.x * 16; t0 < T; t0 += 16 * gridDim.x) {
-    const int t = t0 + row;
-    if (t >= T) break;  // (whole groups of 16 lanes)
-    float z[ET];
-#pragma unroll
-    for (int i = 0; i < ET; ++i) {
-      const int e = l + 16 * i;
-      z[i] = 0.f;
-      if (e < E) {
-        for (int j = 0; j < S; ++j) z[i] += logits[((size_t)j * T + t) * E + e];
-        if (b) z[i] += b[e];
-      }
-    }
-    const bool live = row_forward<ET>(z, t, target, E, k, prob, s_c);
-#pragma unroll
-    for (int i = 0; i < ET; ++i)
-      if (live) sum[i] += z[i];
+// Operand fragments straight from memory.  bf16: 8 of a row's elements a lane,
+// one v_mfma_f32_16x16x32_bf16 a k-step of 32.  fp32: 4 a lane, four
+// v_mfma_f32_16x16x4_f32 a k-step of 16 (the MFMA u takes element u of every
+// lane, on both sides); rows of any length and alignment (vec: all of them start
+// on 16 bytes).
+template <typename T>
+struct Frag;
+template <>
+struct Frag<bf16_t> {
+  static constexpr int K = 32;
+  typedef bf16x8_t V;
+  static __device__ __forceinline__ V load(const bf16_t* row, int k, int q, int, bool) {
+    return *reinterpret_cast<const V*>(row + k + 8 * q);
   }
+  static __device__ __forceinline__ void mma(const V& a, const V& b, f32x4_t& c) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Frag<float> {
+  static constexpr int K = 16;
+  typedef f32x4_t V;
+  static __device__ __forceinline__ V load(const float* row, int k, int q, int d, bool vec) {
+    const int at = k + 4 * q;
+    if (vec && at + 4 <= d) return *reinterpret_cast<const V*>(row + at);
+    V v;
 #pragma unroll
-  for (int i = 0; i < ET; ++i) s_p[row][l + 16 * i] = sum[i];
+    for (int u = 0; u < 4; ++u) v[u] = at + u < d ? row[at + u] : 0.f;
+    return v;
+  }
+  static __device__ __forceinline__ void mma(const V& a, const V& b, f32x4_t& c) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[u], b[u], c, 0, 0, 0);
+  }
+};
+
+struct LossOut {
+  int32_t* counts;
+  float* prob_sum;
+  float* loss;
+};
+
+// sums over the nb blocks, and the loss: by one block of N threads.  Groups of EP
+// threads (a power of two from E up) take every N / EP-th block's sums.
+template <int N>
+__device__ void balance_loss(const float* part_p, const int32_t* part_c, int nb, int E, int EP,
+                             const LossOut& o) {
+  __shared__ double s_p[N];
+  __shared__ int32_t s_c[N];
+  __shared__ int32_t s_n;
+  const int e = threadIdx.x & (EP - 1), g0 = threadIdx.x / EP, ng = N / EP;
+  if (threadIdx.x == 0) s_n = 0;
   __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += 256) {
-    part_c[(size_t)blockIdx.x * (E + 1) + e] = s_c[e];
-    float p = 0.f;
-    if (e < E) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) p += s_p[r][e];
-      part_p[(size_t)blockIdx.x * E + e] = p;
+  double p = 0.0;
+  int c = 0, n = 0;
+  if (e < E) {
+#pragma unroll 8
+    for (int i = g0; i < nb; i += ng) {
+      p += part_p[(size_t)i * E + e];
+      c += part_c[(size_t)i * (E + 1) + e];
     }
+  }
+  for (int i = threadIdx.x; i < nb; i += N) n += part_c[(size_t)i * (E + 1) + E];
+  if (n) atomicAdd(&s_n, n);
+  s_p[threadIdx.x] = p;
+  s_c[threadIdx.x] = c;
+  __syncthreads();
+  for (int r = N / 2; r >= EP; r >>= 1) {
+    if ((int)threadIdx.x < r) {
+      s_p[threadIdx.x] += s_p[threadIdx.x + r];
+      s_c[threadIdx.x] += s_c[threadIdx.x + r];
+    }
+    __syncthreads();
+  }
+  double l = 0.0;
+  if ((int)threadIdx.x < E) {
+    p = s_p[threadIdx.x];
+    c = s_c[threadIdx.x];
+    o.counts[threadIdx.x] = c;
+    o.prob_sum[threadIdx.x] = (float)p;
+    l = p * c;
+  }
+  __syncthreads();
+  // the loss: sum of p c over the experts, and the slots
+  if ((int)threadIdx.x < EP) s_p[threadIdx.x] = l;
+  __syncthreads();
+  for (int r = EP / 2; r > 0; r >>= 1) {
+    if ((int)threadIdx.x < r) {
+      s_p[threadIdx.x] += s_p[threadIdx.x + r];
+      s_c[threadIdx.x] += s_c[threadIdx.x + r];
+    }
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) {
+    o.counts[E] = s_n;
+    *o.loss = s_n > 0 ? (float)(E * s_p[0] / ((double)s_c[0] * s_n)) : 0.f;
   }
 }
 
-// bf16: logits of RT x 16 rows a block in 16 x 16 x 32 MFMAs, K split over the
-// four wavefronts, operands straight from memory (h is read once; w, at most 2
-// MB, comes from L2), then the rows' softmax and sums.  Bound by reading h:
-// a block keeps 4 wavefronts' loads of several k-steps in flight.
-template <int ET, int RT>
-__global__ __launch_bounds__(256) void k_balance_forward(const bf16_t* w, const float* b,
-                                                         const bf16_t* h, const int16_t* target,
-                                                         int T, int E, int k, int d, float* prob,
-                                                         float* part_p, int32_t* part_c) {
+__global__ __launch_bounds__(1024) void k_balance_loss(const float* part_p, const int32_t* part_c,
+                                                       int nb, int E, int EP, LossOut o) {
+  balance_loss<1024>(part_p, part_c, nb, E, EP, o);
+}
+
+// Logits of RT x 16 rows a block in MFMAs, K split over the four wavefronts (h is
+// read once; w comes from L2), then the rows' softmax and sums.  Bound by reading
+// h: a block keeps 4 wavefronts' loads of several k-steps in flight.  A single
+// block goes on to the loss itself.
+template <typename TT, int ET, int RT>
+__global__ __launch_bounds__(256) void k_balance_forward(const TT* w, const float* b, const TT* h,
+                                                         const int16_t* target, int T, int E, int EP2,
+                                                         int k, int d, bool vec, float* prob,
+                                                         float* part_p, int32_t* part_c, LossOut out) {
+  using F = Frag<TT>;
+  using V = typename F::V;
   constexpr int U = ET <= 2 ? 8 : ET == 4 ? 4 : ET == 8 ? 2 : 1;  // k-steps in flight
   constexpr int EP = 16 * ET, ZS = EP + 4;  // floats of an LDS row
   // K parts, then probabilities
@@ -136,48 +201,44 @@ __global__ __launch_bounds__(256) void k_balance_forward(const bf16_t* w, const 
   __shared__ int32_t s_c[TRIMMOE_MAX_EXPERTS + 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
   for (int e = threadIdx.x; e <= E; e += 256) s_c[e] = 0;
-  const int steps = d / 32, ks0 = steps * wave / 4, ks1 = steps * (wave + 1) / 4;
-  const bf16_t* wp[ET];
+  const int steps = (d + F::K - 1) / F::K, ks0 = steps * wave / 4, ks1 = steps * (wave + 1) / 4;
+  const TT* wp[ET];
 #pragma unroll
-  for (int i = 0; i < ET; ++i) wp[i] = w + (size_t)min(16 * i + fr, E - 1) * d + 8 * q;
+  for (int i = 0; i < ET; ++i) wp[i] = w + (size_t)min(16 * i + fr, E - 1) * d;
   float sum = 0.f;  // of expert threadIdx.x
   for (int t0 = blockIdx.x * 16 * RT; t0 < T; t0 += 16 * RT * gridDim.x) {
     f32x4_t acc[RT][ET];
-    const bf16_t* hp[RT];
+    const TT* hp[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-      hp[r] = h + (size_t)min(t0 + 16 * r + fr, T - 1) * d + 8 * q;
+      hp[r] = h + (size_t)min(t0 + 16 * r + fr, T - 1) * d;
 #pragma unroll
       for (int i = 0; i < ET; ++i) acc[r][i] = f32x4_t{};
     }
     int s = ks0;
     for (; s + U <= ks1; s += U) {
-      bf16x8_t fh[U][RT], fw[U][ET];
+      V fh[U][RT], fw[U][ET];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
 #pragma unroll
-        for (int r = 0; r < RT; ++r)
-          fh[u][r] = *reinterpret_cast<const bf16x8_t*>(hp[r] + 32 * (s + u));
+        for (int r = 0; r < RT; ++r) fh[u][r] = F::load(hp[r], F::K * (s + u), q, d, vec);
 #pragma unroll
-        for (int i = 0; i < ET; ++i)
-          fw[u][i] = *reinterpret_cast<const bf16x8_t*>(wp[i] + 32 * (s + u));
+        for (int i = 0; i < ET; ++i) fw[u][i] = F::load(wp[i], F::K * (s + u), q, d, vec);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
         for (int r = 0; r < RT; ++r)
 #pragma unroll
-          for (int i = 0; i < ET; ++i)
-            acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh[u][r], fw[u][i], acc[r][i], 0, 0, 0);
+          for (int i = 0; i < ET; ++i) F::mma(fh[u][r], fw[u][i], acc[r][i]);
     }
     for (; s < ks1; ++s)
 #pragma unroll
       for (int r = 0; r < RT; ++r) {
-        const bf16x8_t fh = *reinterpret_cast<const bf16x8_t*>(hp[r] + 32 * s);
+        const V fh = F::load(hp[r], F::K * s, q, d, vec);
 #pragma unroll
         for (int i = 0; i < ET; ++i)
-          acc[r][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              fh, *reinterpret_cast<const bf16x8_t*>(wp[i] + 32 * s), acc[r][i], 0, 0, 0);
+          F::mma(fh, F::load(wp[i], F::K * s, q, d, vec), acc[r][i]);
       }
     __syncthreads();  // the last rows' probabilities are summed
 #pragma unroll
@@ -215,126 +276,67 @@ __global__ __launch_bounds__(256) void k_balance_forward(const bf16_t* w, const 
   __syncthreads();
   for (int e = threadIdx.x; e <= E; e += 256) part_c[(size_t)blockIdx.x * (E + 1) + e] = s_c[e];
   if ((int)threadIdx.x < E) part_p[(size_t)blockIdx.x * E + threadIdx.x] = sum;
-}
-
-// sums over the blocks, and the loss.  One block: groups of threads of EP (a
-// power of two from E up) experts take every 1024 / EP-th block's sums.
-__global__ __launch_bounds__(1024) void k_balance_loss(const float* part_p, const int32_t* part_c,
-                                                       int nb, int E, int EP, int32_t* counts,
-                                                       float* prob_sum, float* loss) {
-  __shared__ double s_p[1024];
-  __shared__ int32_t s_c[1024];
-  __shared__ int32_t s_n;
-  const int e = threadIdx.x & (EP - 1), g0 = threadIdx.x / EP, ng = 1024 / EP;
-  if (threadIdx.x == 0) s_n = 0;
-  __syncthreads();
-  double p = 0.0;
-  int c = 0, n = 0;
-  if (e < E) {
-#pragma unroll 4
-    for (int i = g0; i < nb; i += ng) {
-      p += part_p[(size_t)i * E + e];
-      c += part_c[(size_t)i * (E + 1) + e];
-    }
-  }
-  for (int i = threadIdx.x; i < nb; i += 1024) n += part_c[(size_t)i * (E + 1) + E];
-  if (n) atomicAdd(&s_n, n);
-  s_p[threadIdx.x] = p;
-  s_c[threadIdx.x] = c;
-  __syncthreads();
-  for (int o = 512; o >= EP; o >>= 1) {
-    if ((int)threadIdx.x < o) {
-      s_p[threadIdx.x] += s_p[threadIdx.x + o];
-      s_c[threadIdx.x] += s_c[threadIdx.x + o];
-    }
+  if (gridDim.x == 1) {
     __syncthreads();
-  }
-  double l = 0.0;
-  if ((int)threadIdx.x < E) {
-    p = s_p[threadIdx.x];
-    c = s_c[threadIdx.x];
-    counts[threadIdx.x] = c;
-    prob_sum[threadIdx.x] = (float)p;
-    l = p * c;
-  }
-  __syncthreads();
-  // the loss: sum of p c over the experts, and the slots
-  if ((int)threadIdx.x < EP) s_p[threadIdx.x] = l;
-  __syncthreads();
-  for (int o = EP / 2; o > 0; o >>= 1) {
-    if ((int)threadIdx.x < o) {
-      s_p[threadIdx.x] += s_p[threadIdx.x + o];
-      s_c[threadIdx.x] += s_c[threadIdx.x + o];
-    }
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) {
-    counts[E] = s_n;
-    *loss = s_n > 0 ? (float)(E * s_p[0] / ((double)s_c[0] * s_n)) : 0.f;
+    balance_loss<256>(part_p, part_c, 1, E, EP2, out);
   }
 }
 
-// dz of a tile of 64 rows a block and its column sums (db).  fp32: as it is.
-// bf16: in two parts, the value rounded to bf16 and what that leaves rounded
-// again (together within 2^-16 of dz), as [row][part][16 ET] with zeros past E
-// and in rows past T; and the tile's rows with a slot as a bit mask.
+// dz of 16 rows a block, with zeros past E and in rows past T, its column sums
+// and its rows with a slot as a bit mask.  fp32: [row][16
+// ET].  bf16: [row][part][16 ET] in two parts, the value rounded to bf16 and what
+// that leaves rounded again (together within 2^-16 of dz).
 template <int ET, bool BF16>
 __global__ __launch_bounds__(256) void k_balance_dz(const float* prob, const int16_t* target,
                                                     const int32_t* counts, const float* dloss, int T,
-                                                    int E, int k, void* dz, unsigned long long* mask,
+                                                    int E, int k, void* dz, uint16_t* mask,
                                                     float* part_db) {
   __shared__ float s_p[16][16 * ET + 1];
-  __shared__ uint8_t s_live[kTile];
+  __shared__ uint8_t s_live[16];
   const int row = threadIdx.x >> 4, l = threadIdx.x & 15;
-  // counts against their mean: sum_j p_tj = 1, so the mean drops out of
-  // c_e - sum_j p_tj c_j and would only cost digits
-  float c[ET], total = 0.f;
+  const size_t t = (size_t)blockIdx.x * 16 + row;
+  bool live = false;
+  if (t < (size_t)T) row_slot(target, t, k, E, l, live);
+  float c[ET], p[ET], total = 0.f;
 #pragma unroll
   for (int i = 0; i < ET; ++i) {
-    c[i] = l + 16 * i < E ? (float)counts[l + 16 * i] : 0.f;
+    const bool in = l + 16 * i < E;
+    c[i] = in ? (float)counts[l + 16 * i] : 0.f;
+    p[i] = in && t < (size_t)T ? prob[t * E + l + 16 * i] : 0.f;
     total += c[i];
   }
+  // counts against their mean: sum_j p_tj = 1, so the mean drops out of
+  // c_e - sum_j p_tj c_j and would only cost digits
   total = sum16(total);
   const int n = counts[E];
   const float scale = n > 0 ? *dloss * (float)((double)E / ((double)total * n)) : 0.f;
   const float mean = total / E;
+  float s = 0.f;
 #pragma unroll
-  for (int i = 0; i < ET; ++i) c[i] -= mean;
-  float sum[ET] = {};
-#pragma unroll
-  for (int r = 0; r < kTile; r += 16) {
-    const size_t t = (size_t)blockIdx.x * kTile + r + row;
-    bool live = false;
-    float p[ET], s = 0.f;
-    if (t < (size_t)T) row_slot(target, t, k, E, l, live);
-#pragma unroll
-    for (int i = 0; i < ET; ++i) {
-      p[i] = live && l + 16 * i < E ? prob[t * E + l + 16 * i] : 0.f;
-      s = fmaf(p[i], c[i], s);
-    }
-    s = sum16(s);
-    if (l == 0) s_live[r + row] = live;
-#pragma unroll
-    for (int i = 0; i < ET; ++i) {
-      const int e = l + 16 * i;
-      const float x = live && e < E ? scale * p[i] * (c[i] - s) : 0.f;
-      sum[i] += x;
-      if constexpr (BF16) {
-        bf16_t* o = static_cast<bf16_t*>(dz) + t * (32 * ET) + e;
-        const bf16_t hi = f2bf(x);
-        o[0] = hi;
-        o[16 * ET] = f2bf(x - bf2f(hi));
-      } else if (t < (size_t)T && e < E) {
-        static_cast<float*>(dz)[t * E + e] = x;
-      }
-    }
+  for (int i = 0; i < ET; ++i) {
+    c[i] -= mean;
+    s = fmaf(p[i], c[i], s);
   }
+  s = sum16(s);
+  if (l == 0) s_live[row] = live;
 #pragma unroll
-  for (int i = 0; i < ET; ++i) s_p[row][l + 16 * i] = sum[i];
+  for (int i = 0; i < ET; ++i) {
+    const int e = l + 16 * i;
+    const float x = live && e < E ? scale * p[i] * (c[i] - s) : 0.f;
+    if constexpr (BF16) {
+      bf16_t* o = static_cast<bf16_t*>(dz) + t * (32 * ET) + e;
+      const bf16_t hi = f2bf(x);
+      o[0] = hi;
+      o[16 * ET] = f2bf(x - bf2f(hi));
+    } else {
+      static_cast<float*>(dz)[t * (16 * ET) + e] = x;
+    }
+    s_p[row][e] = x;
+  }
   __syncthreads();
-  if (BF16 && threadIdx.x < 64) {
-    const unsigned long long m = __ballot(s_live[threadIdx.x]);
-    if (threadIdx.x == 0) mask[blockIdx.x] = m;
+  if (threadIdx.x < 64) {
+    const unsigned long long m = __ballot(threadIdx.x < 16 && s_live[threadIdx.x & 15]);
+    if (threadIdx.x == 0) mask[blockIdx.x] = (uint16_t)m;
   }
   if ((int)threadIdx.x < E) {
     float x = 0.f;
@@ -379,8 +381,8 @@ template <int ET, int CW>
 __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf16_t* h,
                                                       const bf16_t* dz,
                                                       const unsigned long long* mask, int T, int E,
-                                                      int d, bf16_t* dh, float* part_dw,
-                                                      bf16_t* dw) {
+                                                      int d, bf16_t* dh, float* part_dw, bf16_t* dw,
+                                                      const float* part_db, float* db) {
   using G = Grad<ET, CW>;
   __shared__ __align__(16) char lds[G::LDS];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
@@ -500,6 +502,12 @@ __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf1
       }
     }
   }
+  if (db && blockIdx.x == 0 && (int)threadIdx.x < E) {  // of a single tile
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) s += part_db[i * E + threadIdx.x];
+    db[threadIdx.x] = s;
+  }
   if (!part_dw && !dw) return;
   // lane: columns 4 q .. + 4 of its 16, expert fr
 #pragma unroll
@@ -519,44 +527,178 @@ __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf1
     }
 }
 
-// dw from its R slices (4 elements a thread), then db from the tiles' sums (one
+// The same in fp32, 16 x 16 x 4 MFMAs: a lane holds single elements, so both
+// orders of an operand are plain LDS reads; d and the alignment of rows are any
+// (vec: four columns at a time).
+template <int ET, int CW>
+struct GradF32 {
+  static constexpr int BC = 64 * CW, EP = 16 * ET;
+  static constexpr int HS = BC + 4, ZS = EP + 4;  // floats of an LDS row
+  static constexpr int HL = kTile * BC / 4 / 256, ZL = kTile * EP / 4 / 256;  // loads a thread
+};
+
+template <int ET, int CW>
+__global__ __launch_bounds__(256) void k_balance_grad_f32(const float* w, const float* h,
+                                                          const float* dz,
+                                                          const unsigned long long* mask, int T,
+                                                          int E, int d, bool vec, float* dh,
+                                                          float* part_dw, float* dw,
+                                                          const float* part_db, float* db) {
+  using G = GradF32<ET, CW>;
+  __shared__ __align__(16) float s_h[kTile * G::HS];
+  __shared__ __align__(16) float s_z[kTile * G::ZS];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
+  const int c0 = blockIdx.x * G::BC, cw = 16 * CW * wave, c_valid = min(G::BC, d - c0);
+  const int n_t = (T + kTile - 1) / kTile;
+  // w: column cw + 16 j + fr, expert 4 s + q
+  float fw[4 * ET][CW];
+#pragma unroll
+  for (int s = 0; s < 4 * ET; ++s)
+#pragma unroll
+    for (int j = 0; j < CW; ++j) {
+      const int c = cw + 16 * j + fr, e = 4 * s + q;
+      fw[s][j] = e < E && c < c_valid ? w[(size_t)e * d + c0 + c] : 0.f;
+    }
+  f32x4_t acc[ET][CW];
+#pragma unroll
+  for (int i = 0; i < ET; ++i)
+#pragma unroll
+    for (int j = 0; j < CW; ++j) acc[i][j] = f32x4_t{};
+  f32x4_t xh[G::HL], xz[G::ZL];
+  auto load = [&](int tile) {
+    const unsigned long long live = mask[tile];
+#pragma unroll
+    for (int u = 0; u < G::HL; ++u) {
+      const int i = threadIdx.x + 256 * u, r = i / (G::BC / 4), c = 4 * (i % (G::BC / 4));
+      const float* p = h + ((size_t)tile * kTile + r) * d + c0 + c;
+      const int lim = live >> r & 1 ? c_valid - c : 0;  // (see k_balance_grad)
+      xh[u] = f32x4_t{};
+      if (vec && lim >= 4) {
+        xh[u] = *reinterpret_cast<const f32x4_t*>(p);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k < lim) xh[u][k] = p[k];
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < G::ZL; ++u) {
+      const int i = threadIdx.x + 256 * u;
+      xz[u] = *reinterpret_cast<const f32x4_t*>(dz + (size_t)tile * kTile * G::EP + 4 * i);
+    }
+  };
+  int tile = blockIdx.y;
+  if (tile < n_t) load(tile);
+  for (; tile < n_t; tile += gridDim.y) {
+    __syncthreads();  // the last tile is read
+#pragma unroll
+    for (int u = 0; u < G::HL; ++u) {
+      const int i = threadIdx.x + 256 * u, r = i / (G::BC / 4), c = 4 * (i % (G::BC / 4));
+      *reinterpret_cast<f32x4_t*>(s_h + r * G::HS + c) = xh[u];
+    }
+#pragma unroll
+    for (int u = 0; u < G::ZL; ++u) {
+      const int i = threadIdx.x + 256 * u, r = i / (G::EP / 4), c = 4 * (i % (G::EP / 4));
+      *reinterpret_cast<f32x4_t*>(s_z + r * G::ZS + c) = xz[u];
+    }
+    __syncthreads();
+    if (tile + (int)gridDim.y < n_t) load(tile + gridDim.y);
+    // dw += dz^T h: 16 k-steps of 4 rows
+#pragma unroll 4
+    for (int s = 0; s < kTile / 4; ++s) {
+      const int r = 4 * s + q;
+      float fh[CW], fz[ET];
+#pragma unroll
+      for (int j = 0; j < CW; ++j) fh[j] = s_h[r * G::HS + cw + 16 * j + fr];
+#pragma unroll
+      for (int i = 0; i < ET; ++i) fz[i] = s_z[r * G::ZS + 16 * i + fr];
+#pragma unroll
+      for (int i = 0; i < ET; ++i)
+#pragma unroll
+        for (int j = 0; j < CW; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fh[j], fz[i], acc[i][j], 0, 0, 0);
+    }
+    // dh = dz w: 4 tiles of 16 rows
+    if (dh) {
+#pragma unroll
+      for (int rt = 0; rt < 4; ++rt) {
+        f32x4_t o[CW];
+#pragma unroll
+        for (int j = 0; j < CW; ++j) o[j] = f32x4_t{};
+#pragma unroll
+        for (int s = 0; s < 4 * ET; ++s) {
+          const float fz = s_z[(16 * rt + fr) * G::ZS + 4 * s + q];
+#pragma unroll
+          for (int j = 0; j < CW; ++j)
+            o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[s][j], fz, o[j], 0, 0, 0);
+        }
+        const size_t t = (size_t)tile * kTile + 16 * rt + fr;
+#pragma unroll
+        for (int j = 0; j < CW; ++j) {
+          const int c = cw + 16 * j + 4 * q;
+          float* p = dh + t * d + c0 + c;
+          if (t >= (size_t)T) continue;
+          if (vec && c + 4 <= c_valid) {
+            *reinterpret_cast<f32x4_t*>(p) = o[j];
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (c + k < c_valid) p[k] = o[j][k];
+          }
+        }
+      }
+    }
+  }
+  if (db && blockIdx.x == 0 && (int)threadIdx.x < E) {  // of a single tile
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kTile / 16; ++i) s += part_db[i * E + threadIdx.x];
+    db[threadIdx.x] = s;
+  }
+  if (!part_dw && !dw) return;
+  float* out = dw ? dw : part_dw + (size_t)blockIdx.y * E * d;
+#pragma unroll
+  for (int i = 0; i < ET; ++i)
+#pragma unroll
+    for (int j = 0; j < CW; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = 16 * i + fr, c = cw + 16 * j + 4 * q + k;
+        if (e < E && c < c_valid) out[(size_t)e * d + c0 + c] = acc[i][j][k];
+      }
+}
+
+// dw from its R slices (4 elements a thread), then db from the blocks' sums (one
 // wavefront an expert)
+template <typename TT>
 __global__ __launch_bounds__(256) void k_balance_finish(const float* part_dw, int R, size_t n,
-                                                        int dw_blocks, bf16_t* dw,
-                                                        const float* part_db, int n_t, int E,
-                                                        float* db) {
+                                                        int dw_blocks, TT* dw, const float* part_db,
+                                                        int nb, int E, float* db) {
   if ((int)blockIdx.x < dw_blocks) {
     const size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
-    if (i >= n) return;
-    f32x4_t s = *reinterpret_cast<const f32x4_t*>(part_dw + i);
+    if (n % 4 == 0) {
+      if (i >= n) return;
+      f32x4_t s = *reinterpret_cast<const f32x4_t*>(part_dw + i);
 #pragma unroll 4
-    for (int r = 1; r < R; ++r) s += *reinterpret_cast<const f32x4_t*>(part_dw + (size_t)r * n + i);
-    uint2 v;
-    v.x = pack_bf16x2(s[0], s[1]);
-    v.y = pack_bf16x2(s[2], s[3]);
-    *reinterpret_cast<uint2*>(dw + i) = v;
+      for (int r = 1; r < R; ++r) s += *reinterpret_cast<const f32x4_t*>(part_dw + (size_t)r * n + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) dw[i + k] = from_f32<TT>(s[k]);
+    } else {
+      for (size_t k = i; k < min(i + 4, n); ++k) {
+        float s = part_dw[k];
+        for (int r = 1; r < R; ++r) s += part_dw[(size_t)r * n + k];
+        dw[k] = from_f32<TT>(s);
+      }
+    }
     return;
   }
   const int e = ((int)blockIdx.x - dw_blocks) * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (e >= E) return;
   float s = 0.f;
-  for (int i = lane; i < n_t; i += 64) s += part_db[(size_t)i * E + e];
+  for (int i = lane; i < nb; i += 64) s += part_db[(size_t)i * E + e];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
   if (lane == 0) db[e] = s;
-}
-
-// rows with a slot, zeros for the others: an inactive row's h may hold
-// anything, and 0 * NaN is NaN
-__global__ __launch_bounds__(256) void k_live_rows(const float* h, const int16_t* target, int E,
-                                                   int k, int d, float* out) {
-  const size_t t = blockIdx.x;
-  bool live = false;
-  for (int s = 0; s < k; ++s) {
-    const int e = target[t * k + s];
-    live |= e >= 0 && e < E;
-  }
-  for (int i = threadIdx.x; i < d; i += 256) out[t * d + i] = live ? h[t * d + i] : 0.f;
 }
 
 // ------------------------------------------------------------------ plan --
@@ -579,136 +721,94 @@ void with_tiles(int E, F f) {
 // rows / 16 a forward block takes at once: w passes the block once for them
 constexpr int row_tiles(int et) { return et >= 8 ? 2 : 1; }
 // columns / 64 of a gradient block: accumulators of dw and fragments of w in registers
-constexpr int col_tiles(int et) { return et == 16 ? 2 : 4; }
+template <typename TT>
+constexpr int col_tiles(int et) {
+  return sizeof(TT) == 2 ? (et == 16 ? 2 : 4) : (et >= 8 ? 1 : 2);
+}
+
+// fp32 rows that start on 16 bytes
+bool rows_aligned(int d, const void* p, const void* q) {
+  return d % 4 == 0 && ((reinterpret_cast<uintptr_t>(p) | reinterpret_cast<uintptr_t>(q)) & 15) == 0;
+}
 
 struct Plan {
-  bool bf16;
-  int E, d, T, et;
-  int nb;     // forward blocks
-  int s_z;    // fp32: K splits of the logits
-  size_t f_c, f_z, f_total;  // forward: counts, logits
-  int n_t;    // tiles of 64 rows
-  int R;      // bf16: slices of dw; fp32: K splits of dw
-  size_t b_mask, b_db, b_dw, b_h, b_total;
-  Plan(bool bf, int E_, int d_, int T_) : bf16(bf), E(E_), d(d_), T(T_), et(expert_tiles(E_)) {
-    const int rows = std::max(T, 1), per = bf16 ? 16 * row_tiles(et) : 16;
-    nb = std::min(kRowBlocks, cdiv(rows, per));
-    s_z = bf16 ? 1 : product_splits(rows, E, d);
+  int et, nb;  // expert tiles, forward blocks
+  size_t f_c, f_total;
+  int n_t, R;  // tiles of 64 rows, slices of dw
+  size_t b_mask, b_db, b_dw, b_total;
+  Plan(bool bf16, int E, int d, int T) : et(expert_tiles(E)) {
+    const int rows = std::max(T, 1);
+    nb = std::min(kRowBlocks, cdiv(rows, 16 * row_tiles(et)));
     f_c = align256((size_t)nb * E * 4);
-    f_z = f_c + align256((size_t)nb * (E + 1) * 4);
-    f_total = f_z + (bf16 ? 0 : align256((size_t)s_z * rows * E * 4));
+    f_total = f_c + align256((size_t)nb * (E + 1) * 4);
     n_t = cdiv(rows, kTile);
-    size_t dz;
-    if (bf16) {
-      // two blocks a CU, and slices of dw no larger than 32 MB together
-      const int n_c = cdiv(d, 64 * col_tiles(et));
-      const size_t most = ((size_t)32 << 20) / ((size_t)E * d * 4);
-      R = std::max(1, std::min(std::min(n_t, cdiv(512, n_c)), (int)std::min<size_t>(most, 1 << 20)));
-      dz = (size_t)n_t * kTile * 64 * et;
-    } else {
-      R = product_splits(E, d, rows);
-      dz = (size_t)rows * E * 4;
-    }
-    b_mask = align256(dz);
+    // blocks for every CU, and slices of dw no larger than 32 MB together
+    const int n_c = cdiv(d, 64 * (bf16 ? col_tiles<bf16_t>(et) : col_tiles<float>(et)));
+    const size_t most = ((size_t)32 << 20) / ((size_t)E * d * 4);
+    R = std::max(1, std::min(std::min(n_t, cdiv(256, n_c)), (int)std::min<size_t>(most, 1 << 20)));
+    b_mask = align256((size_t)n_t * kTile * 64 * et);  // (dz: 4 bytes, or two parts of 2)
     b_db = b_mask + align256((size_t)n_t * 8);
-    b_dw = b_db + align256((size_t)n_t * E * 4);
-    b_h = b_dw + (R > 1 ? align256((size_t)R * E * d * 4) : 0);
-    b_total = b_h + (bf16 ? 0 : align256((size_t)rows * d * 4));
+    b_dw = b_db + align256((size_t)n_t * (kTile / 16) * E * 4);
+    b_total = b_dw + (R > 1 ? align256((size_t)R * E * d * 4) : 0);
   }
 };
 
+template <typename TT>
 hipError_t forward(const BalanceArgs& a, hipStream_t st) {
   const Plan p(a.bf16, a.E, a.d, a.T);
   float* part_p = reinterpret_cast<float*>(a.ws);
   int32_t* part_c = reinterpret_cast<int32_t*>(a.ws + p.f_c);
-  float* z = reinterpret_cast<float*>(a.ws + p.f_z);
-  if (a.T > 0 && !a.bf16) {
-    const hipError_t e = launch_product(operand<float, true>(a.h, a.d, a.T, a.d),
-                                        operand<float, true>(a.w, a.d, a.E, a.d), p.s_z, false, z, st);
-    if (e != hipSuccess) return e;
-  }
-  if (a.T > 0)
-    with_tiles(a.E, [&](auto c) {
-      constexpr int ET = c;
-      constexpr int RT = row_tiles(ET);
-      if (a.bf16)
-        hipLaunchKernelGGL((k_balance_forward<ET, RT>), dim3(p.nb), dim3(256), 0, st,
-                           static_cast<const bf16_t*>(a.w), a.b,
-                           static_cast<const bf16_t*>(a.h), a.target, a.T, a.E, a.k, a.d, a.prob,
-                           part_p, part_c);
-      else
-        hipLaunchKernelGGL(k_balance_rows<ET>, dim3(p.nb), dim3(256), 0, st, z, p.s_z, a.b, a.target,
-                           a.T, a.E, a.k, a.prob, part_p, part_c);
-    });
+  const LossOut out{a.counts, a.prob_sum, a.loss};
   int EP = 1;
   while (EP < a.E) EP *= 2;
-  hipLaunchKernelGGL(k_balance_loss, dim3(1), dim3(1024), 0, st, part_p, part_c, a.T > 0 ? p.nb : 0,
-                     a.E, EP, a.counts, a.prob_sum, a.loss);
+  const int nb = a.T > 0 ? p.nb : 0;
+  if (nb > 0)
+    with_tiles(a.E, [&](auto c) {
+      constexpr int ET = c;
+      hipLaunchKernelGGL((k_balance_forward<TT, ET, row_tiles(ET)>), dim3(nb), dim3(256), 0, st,
+                         static_cast<const TT*>(a.w), a.b, static_cast<const TT*>(a.h), a.target, a.T,
+                         a.E, EP, a.k, a.d, rows_aligned(a.d, a.w, a.h), a.prob, part_p, part_c, out);
+    });
+  if (nb != 1)
+    hipLaunchKernelGGL(k_balance_loss, dim3(1), dim3(1024), 0, st, part_p, part_c, nb, a.E, EP, out);
   return hipGetLastError();
 }
 
+template <typename TT>
 hipError_t backward(const BalanceArgs& a, hipStream_t st) {
+  constexpr bool BF16 = sizeof(TT) == 2;
   const Plan p(a.bf16, a.E, a.d, a.T);
   unsigned long long* mask = reinterpret_cast<unsigned long long*>(a.ws + p.b_mask);
   float* part_db = reinterpret_cast<float*>(a.ws + p.b_db);
-  float* part_dw = reinterpret_cast<float*>(a.ws + p.b_dw);
+  float* part_dw = a.dw && p.R > 1 ? reinterpret_cast<float*>(a.ws + p.b_dw) : nullptr;
+  TT *dh = static_cast<TT*>(a.dh), *dw = static_cast<TT*>(a.dw), *whole = p.R > 1 ? nullptr : dw;
+  const TT *w = static_cast<const TT*>(a.w), *h = static_cast<const TT*>(a.h);
+  const int nb = p.n_t * (kTile / 16);
+  // a single tile's gradient kernel sums db as well
+  float* one_db = p.n_t == 1 && (dh || dw) ? a.db : nullptr;
   with_tiles(a.E, [&](auto c) {
-    constexpr int ET = c;
-    if (a.bf16)
-      hipLaunchKernelGGL((k_balance_dz<ET, true>), dim3(p.n_t), dim3(256), 0, st, a.prob, a.target,
-                         a.counts, a.dloss, a.T, a.E, a.k, a.ws, mask, part_db);
+    constexpr int ET = c, CW = col_tiles<TT>(ET);
+    hipLaunchKernelGGL((k_balance_dz<ET, BF16>), dim3(nb), dim3(256), 0, st, a.prob, a.target,
+                       a.counts, a.dloss, a.T, a.E, a.k, a.ws, reinterpret_cast<uint16_t*>(mask),
+                       part_db);
+    if (!dh && !dw) return;
+    const dim3 grid(cdiv(a.d, 64 * CW), p.R);
+    if constexpr (BF16)
+      hipLaunchKernelGGL((k_balance_grad<ET, CW>), grid, dim3(256), 0, st, w, h,
+                         reinterpret_cast<const bf16_t*>(a.ws), mask, a.T, a.E, a.d, dh, part_dw,
+                         whole, part_db, one_db);
     else
-      hipLaunchKernelGGL((k_balance_dz<ET, false>), dim3(p.n_t), dim3(256), 0, st, a.prob, a.target,
-                         a.counts, a.dloss, a.T, a.E, a.k, a.ws, nullptr, part_db);
+      hipLaunchKernelGGL((k_balance_grad_f32<ET, CW>), grid, dim3(256), 0, st, w, h,
+                         reinterpret_cast<const float*>(a.ws), mask, a.T, a.E, a.d,
+                         rows_aligned(a.d, a.h, a.dh), dh, part_dw, whole, part_db, one_db);
   });
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (a.bf16) {
-    bf16_t* dw = static_cast<bf16_t*>(a.dw);
-    const bool whole = p.R == 1;
-    if (a.dh || a.dw)
-      with_tiles(a.E, [&](auto c) {
-        constexpr int ET = c;
-        using G = Grad<ET, col_tiles(ET)>;
-        hipLaunchKernelGGL((k_balance_grad<ET, col_tiles(ET)>), dim3(cdiv(a.d, G::BC), p.R), dim3(256),
-                           0, st, static_cast<const bf16_t*>(a.w),
-                           static_cast<const bf16_t*>(a.h), reinterpret_cast<const bf16_t*>(a.ws),
-                           mask, a.T, a.E, a.d, static_cast<bf16_t*>(a.dh),
-                           a.dw && !whole ? part_dw : nullptr, whole ? dw : nullptr);
-      });
-    const size_t n = (size_t)a.E * a.d;
-    const int dw_blocks = a.dw && !whole ? (int)((n / 4 + 255) / 256) : 0;
-    const int db_blocks = a.db ? cdiv(a.E, 4) : 0;
-    if (dw_blocks + db_blocks > 0)
-      hipLaunchKernelGGL(k_balance_finish, dim3(dw_blocks + db_blocks), dim3(256), 0, st, part_dw, p.R,
-                         n, dw_blocks, dw, part_db, p.n_t, a.E, a.db);
-    return hipGetLastError();
-  }
-  const float* dz = reinterpret_cast<const float*>(a.ws);
-  if (a.db)
-    hipLaunchKernelGGL(k_balance_finish, dim3(cdiv(a.E, 4)), dim3(256), 0, st, nullptr, 0, (size_t)0, 0,
-                       nullptr, part_db, p.n_t, a.E, a.db);
-  e = hipGetLastError();
-  if (e == hipSuccess && a.dh)
-    e = launch_product(operand<float, true>(dz, a.E, a.T, a.E),
-                       operand<float, false>(a.w, a.d, a.d, a.E), 1, false,
-                       static_cast<float*>(a.dh), st);
-  if (e == hipSuccess && a.dw) {
-    float* hl = reinterpret_cast<float*>(a.ws + p.b_h);
-    if (a.T > 0)
-      hipLaunchKernelGGL(k_live_rows, dim3(a.T), dim3(256), 0, st, static_cast<const float*>(a.h),
-                         a.target, a.E, a.k, a.d, hl);
-    const auto D = operand<float, false>(dz, a.E, a.E, a.T);
-    const auto H = operand<float, false>(hl, a.d, a.d, a.T);
-    float* dw = static_cast<float*>(a.dw);
-    if (p.R == 1) {
-      e = launch_product(D, H, 1, false, dw, st);
-    } else {
-      e = launch_product(D, H, p.R, false, part_dw, st);
-      if (e == hipSuccess) e = launch_sum_parts(part_dw, p.R, (size_t)a.E * a.d, dw, st);
-    }
-  }
-  return e;
+  const size_t n = (size_t)a.E * a.d;
+  const int dw_blocks = part_dw ? (int)((n + 1023) / 1024) : 0;
+  const int db_blocks = a.db && !one_db ? cdiv(a.E, 4) : 0;
+  if (dw_blocks + db_blocks > 0)
+    hipLaunchKernelGGL(k_balance_finish<TT>, dim3(dw_blocks + db_blocks), dim3(256), 0, st, part_dw,
+                       p.R, n, dw_blocks, dw, part_db, nb, a.E, a.db);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -716,7 +816,11 @@ hipError_t backward(const BalanceArgs& a, hipStream_t st) {
 size_t balance_ws(bool bf16, int E, int d, int T) { return Plan(bf16, E, d, T).f_total; }
 size_t balance_backward_ws(bool bf16, int E, int d, int T) { return Plan(bf16, E, d, T).b_total; }
 
-hipError_t launch_balance(const BalanceArgs& a, hipStream_t st) { return forward(a, st); }
-hipError_t launch_balance_backward(const BalanceArgs& a, hipStream_t st) { return backward(a, st); }
+hipError_t launch_balance(const BalanceArgs& a, hipStream_t st) {
+  return a.bf16 ? forward<bf16_t>(a, st) : forward<float>(a, st);
+}
+hipError_t launch_balance_backward(const BalanceArgs& a, hipStream_t st) {
+  return a.bf16 ? backward<bf16_t>(a, st) : backward<float>(a, st);
+}
 
 }  // namespace trimmoe
