@@ -183,25 +183,26 @@ __global__ __launch_bounds__(1024) void k_balance_loss(const float* part_p, cons
   balance_loss<1024>(part_p, part_c, nb, E, EP, o);
 }
 
-// Logits of RT x 16 rows a block in MFMAs, K split over the four wavefronts (h is
+// Logits of RT x 16 rows a block in MFMAs, K split over the NW wavefronts (h is
 // read once; w comes from L2), then the rows' softmax and sums.  Bound by reading
-// h: a block keeps 4 wavefronts' loads of several k-steps in flight.  A single
+// h: a block keeps its wavefronts' loads of several k-steps in flight.  A single
 // block goes on to the loss itself.
-template <typename TT, int ET, int RT>
-__global__ __launch_bounds__(256) void k_balance_forward(const TT* w, const float* b, const TT* h,
+template <typename TT, int ET, int RT, int NW>
+__global__ __launch_bounds__(64 * NW) void k_balance_forward(const TT* w, const float* b, const TT* h,
                                                          const int16_t* target, int T, int E, int EP2,
                                                          int k, int d, bool vec, float* prob,
                                                          float* part_p, int32_t* part_c, LossOut out) {
   using F = Frag<TT>;
   using V = typename F::V;
-  constexpr int U = ET <= 2 ? 8 : ET == 4 ? 4 : ET == 8 ? 2 : 1;  // k-steps in flight
+  constexpr int U = ET <= 2 ? 4 : ET <= 8 ? 2 : 1;  // k-steps in flight
   constexpr int EP = 16 * ET, ZS = EP + 4;  // floats of an LDS row
   // K parts, then probabilities
-  __shared__ __align__(16) float s_z[4 * 16 * RT * ZS];
+  __shared__ __align__(16) float s_z[NW * 16 * RT * ZS];
   __shared__ int32_t s_c[TRIMMOE_MAX_EXPERTS + 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
-  for (int e = threadIdx.x; e <= E; e += 256) s_c[e] = 0;
-  const int steps = (d + F::K - 1) / F::K, ks0 = steps * wave / 4, ks1 = steps * (wave + 1) / 4;
+  for (int e = threadIdx.x; e <= E; e += 64 * NW) s_c[e] = 0;
+  const int steps = (d + F::K - 1) / F::K;
+  const int ks0 = steps * wave / NW, ks1 = steps * (wave + 1) / NW;
   const TT* wp[ET];
 #pragma unroll
   for (int i = 0; i < ET; ++i) wp[i] = w + (size_t)min(16 * i + fr, E - 1) * d;
@@ -250,14 +251,21 @@ __global__ __launch_bounds__(256) void k_balance_forward(const TT* w, const floa
           s_z[(wave * 16 * RT + 16 * r + 4 * q + j) * ZS + 16 * i + fr] = acc[r][i][j];
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      const int row = 16 * r + (threadIdx.x >> 4), t = t0 + row, l = threadIdx.x & 15;
+    for (int r0 = 0; r0 < 16 * RT; r0 += 4 * NW) {
+      const int row = r0 + (threadIdx.x >> 4), t = t0 + row, l = threadIdx.x & 15;
+      if (row >= 16 * RT) break;  // (whole wavefronts)
       float* zr = s_z + row * ZS + l;
       float z[ET];
 #pragma unroll
       for (int i = 0; i < ET; ++i) {
-        z[i] = (zr[16 * i] + zr[16 * i + 16 * RT * ZS]) +
-               (zr[16 * i + 32 * RT * ZS] + zr[16 * i + 48 * RT * ZS]);
+        float x[NW];
+#pragma unroll
+        for (int n = 0; n < NW; ++n) x[n] = zr[16 * i + n * 16 * RT * ZS];
+#pragma unroll
+        for (int n = NW / 2; n > 0; n >>= 1)
+#pragma unroll
+          for (int m = 0; m < n; ++m) x[m] += x[m + n];
+        z[i] = x[0];
         if (b) z[i] += b[min(l + 16 * i, E - 1)];
       }
       bool live = false;
@@ -274,11 +282,11 @@ __global__ __launch_bounds__(256) void k_balance_forward(const TT* w, const floa
     }
   }
   __syncthreads();
-  for (int e = threadIdx.x; e <= E; e += 256) part_c[(size_t)blockIdx.x * (E + 1) + e] = s_c[e];
+  for (int e = threadIdx.x; e <= E; e += 64 * NW) part_c[(size_t)blockIdx.x * (E + 1) + e] = s_c[e];
   if ((int)threadIdx.x < E) part_p[(size_t)blockIdx.x * E + threadIdx.x] = sum;
   if (gridDim.x == 1) {
     __syncthreads();
-    balance_loss<256>(part_p, part_c, 1, E, EP2, out);
+    balance_loss<64 * NW>(part_p, part_c, 1, E, EP2, out);
   }
 }
 
@@ -719,7 +727,9 @@ void with_tiles(int E, F f) {
   }
 }
 // rows / 16 a forward block takes at once: w passes the block once for them
-constexpr int row_tiles(int et) { return et >= 8 ? 2 : 1; }
+constexpr int kRowTiles = 2;
+// wavefronts of a forward block: its K parts fit LDS
+constexpr int wavefronts(int et) { return et == 16 ? 4 : 8; }
 // columns / 64 of a gradient block: accumulators of dw and fragments of w in registers
 template <typename TT>
 constexpr int col_tiles(int et) {
@@ -738,7 +748,7 @@ struct Plan {
   size_t b_mask, b_db, b_dw, b_total;
   Plan(bool bf16, int E, int d, int T) : et(expert_tiles(E)) {
     const int rows = std::max(T, 1);
-    nb = std::min(kRowBlocks, cdiv(rows, 16 * row_tiles(et)));
+    nb = std::min(kRowBlocks, cdiv(rows, 16 * kRowTiles));
     f_c = align256((size_t)nb * E * 4);
     f_total = f_c + align256((size_t)nb * (E + 1) * 4);
     n_t = cdiv(rows, kTile);
@@ -765,7 +775,8 @@ hipError_t forward(const BalanceArgs& a, hipStream_t st) {
   if (nb > 0)
     with_tiles(a.E, [&](auto c) {
       constexpr int ET = c;
-      hipLaunchKernelGGL((k_balance_forward<TT, ET, row_tiles(ET)>), dim3(nb), dim3(256), 0, st,
+      hipLaunchKernelGGL((k_balance_forward<TT, ET, kRowTiles, wavefronts(ET)>), dim3(nb),
+                         dim3(64 * wavefronts(ET)), 0, st,
                          static_cast<const TT*>(a.w), a.b, static_cast<const TT*>(a.h), a.target, a.T,
                          a.E, EP, a.k, a.d, rows_aligned(a.d, a.w, a.h), a.prob, part_p, part_c, out);
     });
