@@ -10,7 +10,7 @@
 #include <type_traits>
 
 #include "loss.h"
-#include "mfma_core.h"
+#include "rows_grad.h"
 
 namespace trimmoe {
 
@@ -20,7 +20,7 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Rows are handled 16 lanes a row (experts l, l + 16, ...: ET of them a lane) and
 // 64 a tile.
-constexpr int kTile = 64;
+constexpr int kTile = kRowTile;
 constexpr int kRowBlocks = 512;
 
 __device__ __forceinline__ float sum16(float x) {
@@ -354,36 +354,18 @@ __global__ __launch_bounds__(256) void k_balance_dz(const float* prob, const int
   }
 }
 
-// dh = dz w and the block's part of dw = dz^T h, for 64 CW columns and every
-// gridDim.y-th tile of 64 rows, in 16 x 16 x 32 MFMAs whose A rows are the
-// columns.  h is read once and dh written once; w's fragments stay in
-// registers (a lane's 8 experts of a column), those of h (8 rows of a column)
-// come transposed out of LDS, as do dz's for dw.  The next tile's loads are in
-// flight under a tile's products.
-//   ET = 1: the two parts of dz are one k-step of 32 (16 experts each, w's
-// fragment twice); else a k-step is 32 experts of a part.
-template <int ET, int CW>
-struct Grad {
-  static constexpr int BC = 64 * CW;               // columns of a block
-  static constexpr int HR = 2 * BC;                // LDS bytes of a row of h
-  static constexpr int ZB = 64 * ET;               // bytes of a row of dz
-  static constexpr int ZR = ZB + 32;               // ... in LDS: rows on distinct banks
-  static constexpr int KS = ET == 1 ? 1 : ET / 2;  // fragments of w
-  static constexpr int LDS = kTile * (HR + ZR);
-  static constexpr int HL = kTile * HR / 16 / 256, ZL = kTile * ZB / 16 / 256;  // loads a thread
+// dh = dz w and dw = dz^T h (rows_grad.h).  A row without a slot is not read: its h
+// may hold anything, and 0 * NaN is NaN.
+struct RouterRows {
+  const bf16_t* wp;
+  const unsigned long long* m;
+  int E, d;
+  float scale;
+  __device__ __forceinline__ bf16_t w(int e, int c) const {
+    return e < E ? wp[(size_t)e * d + c] : bf16_t(0);
+  }
+  __device__ __forceinline__ unsigned long long mask(int tile) const { return m[tile]; }
 };
-
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
-
-// fragment of an operand that lies row by row along K (see lds_read_tr): rows
-// k .. k + 8 of this lane's column; a: LDS byte address of row k + i / 4, piece
-// i % 4, of the 16 lanes' columns, and of the row 4 further on
-__device__ __forceinline__ bf16x8_t read_tr(uint32_t a0, uint32_t a1) {
-  const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a0);
-  const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)a1);
-  return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
 
 template <int ET, int CW>
 __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf16_t* h,
@@ -391,148 +373,14 @@ __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf1
                                                       const unsigned long long* mask, int T, int E,
                                                       int d, bf16_t* dh, float* part_dw, bf16_t* dw,
                                                       const float* part_db, float* db) {
-  using G = Grad<ET, CW>;
-  __shared__ __align__(16) char lds[G::LDS];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
-  const int c0 = blockIdx.x * G::BC, cw = 16 * CW * wave;  // the block's and the wavefront's columns
-  const int c_valid = min(G::BC, d - c0);
-  const int n_t = (T + kTile - 1) / kTile;
-  char* s_h = lds;
-  char* s_z = lds + kTile * G::HR;
-  const uint32_t ah = lds_addr(s_h), az = lds_addr(s_z);
-  // fragments of w: column cw + 16 j + fr, experts 32 s + 8 q .. (ET = 1: 8 (q % 2) ..)
-  bf16x8_t fw[G::KS][CW];
-#pragma unroll
-  for (int s = 0; s < G::KS; ++s)
-#pragma unroll
-    for (int j = 0; j < CW; ++j) {
-      union {
-        bf16x8_t v;
-        bf16_t e[8];
-      } f;
-      const int c = c0 + min(cw + 16 * j + fr, c_valid - 1);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int e = ET == 1 ? 8 * (q & 1) + u : 32 * s + 8 * q + u;
-        f.e[u] = e < E ? w[(size_t)e * d + c] : bf16_t(0);
-      }
-      fw[s][j] = f.v;
-    }
-  f32x4_t acc[ET][CW];
-#pragma unroll
-  for (int i = 0; i < ET; ++i)
-#pragma unroll
-    for (int j = 0; j < CW; ++j) acc[i][j] = f32x4_t{};
-
-  constexpr int HC = G::HR / 16;  // 16-byte chunks of a row of h
-  u32x4_t xh[G::HL], xz[G::ZL];
-  auto load = [&](int tile) {
-    const unsigned long long live = mask[tile];
-#pragma unroll
-    for (int u = 0; u < G::HL; ++u) {
-      const int i = threadIdx.x + 256 * u, r = i / HC, ch = i % HC;
-      const size_t t = (size_t)tile * kTile + r;
-      // a row without a slot may hold anything, and 0 * NaN is NaN (its bit is
-      // off in rows past T too)
-      xh[u] = u32x4_t{};
-      if ((live >> r & 1) && 8 * ch < c_valid)
-        xh[u] = *reinterpret_cast<const u32x4_t*>(h + t * d + c0 + 8 * ch);
-    }
-#pragma unroll
-    for (int u = 0; u < G::ZL; ++u) {
-      const int i = threadIdx.x + 256 * u;
-      xz[u] = *reinterpret_cast<const u32x4_t*>(dz + (size_t)tile * kTile * (32 * ET) + 8 * i);
-    }
-  };
-  int tile = blockIdx.y;
-  if (tile < n_t) load(tile);
-  for (; tile < n_t; tile += gridDim.y) {
-    __syncthreads();  // the last tile is read
-#pragma unroll
-    for (int u = 0; u < G::HL; ++u) {
-      const int i = threadIdx.x + 256 * u, r = i / HC, ch = i % HC;
-      const int at = r * G::HR + (((ch >> 1) ^ tr_swz(r)) << 5) + 16 * (ch & 1);
-      *reinterpret_cast<u32x4_t*>(s_h + at) = xh[u];
-    }
-#pragma unroll
-    for (int u = 0; u < G::ZL; ++u) {
-      const int i = threadIdx.x + 256 * u, r = i / (4 * ET), ch = i % (4 * ET);
-      *reinterpret_cast<u32x4_t*>(s_z + r * G::ZR + 16 * ch) = xz[u];
-    }
-    __syncthreads();
-    if (tile + (int)gridDim.y < n_t) load(tile + gridDim.y);
-    // dw += dz^T h: two k-steps of 32 rows
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int k = 32 * s + 8 * q + (fr >> 2);
-      bf16x8_t fh[CW];
-#pragma unroll
-      for (int j = 0; j < CW; ++j) {
-        const int piece = wave * CW + j;  // of 16 columns
-        const uint32_t a = ah + k * G::HR + ((piece ^ tr_swz(k)) << 5) + 8 * (fr & 3);
-        fh[j] = read_tr(a, a + 4 * G::HR);
-      }
-#pragma unroll
-      for (int i = 0; i < ET; ++i)
-#pragma unroll
-        for (int part = 0; part < 2; ++part) {
-          const uint32_t a = az + k * G::ZR + (part * ET + i) * 32 + 8 * (fr & 3);
-          const bf16x8_t fz = read_tr(a, a + 4 * G::ZR);
-#pragma unroll
-          for (int j = 0; j < CW; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fh[j], fz, acc[i][j], 0, 0, 0);
-        }
-    }
-    // dh = dz w: 4 tiles of 16 rows
-    if (dh) {
-#pragma unroll
-      for (int rt = 0; rt < 4; ++rt) {
-        f32x4_t o[CW];
-#pragma unroll
-        for (int j = 0; j < CW; ++j) o[j] = f32x4_t{};
-        const char* zr = s_z + (16 * rt + fr) * G::ZR + 16 * q;
-#pragma unroll
-        for (int s = 0; s < (ET == 1 ? 1 : ET); ++s) {
-          const bf16x8_t fz = *reinterpret_cast<const bf16x8_t*>(zr + 64 * s);
-#pragma unroll
-          for (int j = 0; j < CW; ++j)
-            o[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fw[s % G::KS][j], fz, o[j], 0, 0, 0);
-        }
-        const size_t t = (size_t)tile * kTile + 16 * rt + fr;
-#pragma unroll
-        for (int j = 0; j < CW; j += 2) {
-          const float x[4] = {o[j][0], o[j][1], o[j][2], o[j][3]};
-          const float y[4] = {o[j + 1][0], o[j + 1][1], o[j + 1][2], o[j + 1][3]};
-          const u32x4_t v = pack_rows(x, y);
-          const int c = cw + 16 * j + pack_col(lane);
-          if (t < (size_t)T && c < c_valid) *reinterpret_cast<u32x4_t*>(dh + t * d + c0 + c) = v;
-        }
-      }
-    }
-  }
+  __shared__ __align__(16) char lds[RowsGrad<ET, CW, 2>::LDS];
   if (db && blockIdx.x == 0 && (int)threadIdx.x < E) {  // of a single tile
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < kTile / 16; ++i) s += part_db[i * E + threadIdx.x];
     db[threadIdx.x] = s;
   }
-  if (!part_dw && !dw) return;
-  // lane: columns 4 q .. + 4 of its 16, expert fr
-#pragma unroll
-  for (int i = 0; i < ET; ++i)
-#pragma unroll
-    for (int j = 0; j < CW; ++j) {
-      const int e = 16 * i + fr, c = cw + 16 * j + 4 * q;
-      if (e >= E || c >= c_valid) continue;
-      if (dw) {
-        uint2 v;
-        v.x = pack_bf16x2(acc[i][j][0], acc[i][j][1]);
-        v.y = pack_bf16x2(acc[i][j][2], acc[i][j][3]);
-        *reinterpret_cast<uint2*>(dw + (size_t)e * d + c0 + c) = v;
-      } else {
-        *reinterpret_cast<f32x4_t*>(part_dw + ((size_t)blockIdx.y * E + e) * d + c0 + c) = acc[i][j];
-      }
-    }
+  rows_grad<ET, CW, 2>(lds, RouterRows{w, mask, E, d, 1.f}, h, dz, T, E, d, dh, part_dw, dw);
 }
 
 // The same in fp32, 16 x 16 x 4 MFMAs: a lane holds single elements, so both

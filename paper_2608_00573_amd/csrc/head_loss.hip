@@ -17,8 +17,8 @@
 
 #include "gemm.h"
 #include "loss.h"
-#include "mfma_core.h"
 #include "products.h"
+#include "rows_grad.h"
 
 namespace trimmoe {
 
@@ -89,7 +89,7 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // BASE2: the pairs' maxima are in base 2 (z log2 e).
 template <typename T, bool BASE2>
 __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt, int V, int d, int T_,
-                                                   const T* w, const float* b, const T* h,
+                                                   bool vec, const T* w, const float* b, const T* h,
                                                    const int32_t* target, float* loss, float* lse) {
   const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= T_) return;
@@ -108,9 +108,23 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt,
   const int y = target[t];
   const bool live = y >= 0 && y < V;
   float z = 0.f;
-  if (live)
-    for (int k = lane; k < d; k += 64)
-      z = fmaf(to_f32<T>(h[(size_t)t * d + k]), to_f32<T>(w[(size_t)y * d + k]), z);
+  if (live) {
+    const T *hr = h + (size_t)t * d, *wr = w + (size_t)y * d;
+    constexpr int N = 16 / sizeof(T);  // elements of a 16-byte load
+    struct alignas(16) Vec {
+      T e[N];
+    };
+    if (vec) {
+#pragma unroll 4
+      for (int k = N * lane; k < d; k += 64 * N) {
+        const Vec x = *reinterpret_cast<const Vec*>(hr + k), u = *reinterpret_cast<const Vec*>(wr + k);
+#pragma unroll
+        for (int i = 0; i < N; ++i) z = fmaf(to_f32<T>(x.e[i]), to_f32<T>(u.e[i]), z);
+      }
+    } else {
+      for (int k = lane; k < d; k += 64) z = fmaf(to_f32<T>(hr[k]), to_f32<T>(wr[k]), z);
+    }
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
     sum += __shfl_xor(sum, o);
@@ -217,6 +231,15 @@ struct RowPart {
   float* G;    // [1]
 };
 
+// m, 2^-e and g / m of a weight g
+__device__ __forceinline__ void row_weight(float g, float G, float& m, float& e, float& gm) {
+  int x = 0;
+  const float f = g == 0.f ? 0.5f : frexpf(g / G, &x);  // (NaN stays NaN)
+  m = f == 0.f ? 1.f : 2.f * f;
+  e = g == 0.f || f == 0.f ? 0.f : ldexpf(1.f, x - 1);
+  gm = g / m;
+}
+
 __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const float* lse,
                                                    const float* dloss, int V, int T, RowPart p) {
   __shared__ float s_m[16];
@@ -241,13 +264,11 @@ __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const 
   if (threadIdx.x == 0) *p.G = G;
   // (each thread reads back its own rows)
   for (int t = threadIdx.x; t < T; t += 1024) {
-    const float g = p.gm[t];
-    int e = 0;
-    const float f = g == 0.f ? 0.5f : frexpf(g / G, &e);  // (NaN stays NaN)
-    const float m = f == 0.f ? 1.f : 2.f * f;
+    float m, e, gm;
+    row_weight(p.gm[t], G, m, e, gm);
     p.m[t] = m;
-    p.e[t] = g == 0.f || f == 0.f ? 0.f : ldexpf(1.f, e - 1);
-    p.gm[t] = g / m;
+    p.e[t] = e;
+    p.gm[t] = gm;
   }
 }
 
@@ -576,6 +597,194 @@ __global__ __launch_bounds__(256) void k_db_finish(const float* part, int n_tt, 
   db[c] = s * *G;
 }
 
+// ------------------------------------ backward, bf16, a few tokens --
+// Up to kSkinnyTokens rows every weight is used once per product, so w is read
+// twice (for z and for dh; past the last-level cache both come from HBM) and dw
+// written once, whatever the rows: three kernels, the second of them both
+// products in one pass over w (rows_grad.h; its rows are the vocabulary's, its
+// experts the tokens).  D lies [vocabulary row][token], in two bf16 parts where
+// the products' k-step leaves room for them (up to 16 rows).
+template <int ET>
+constexpr int few_parts() {
+  return ET == 1 ? 2 : 1;
+}
+
+// the rows' parts (see RowPart), by the lanes of a wavefront; G by all of them
+struct FewRow {
+  int y;
+  float l2, m, e, gm, G;
+  __device__ __forceinline__ FewRow(const int32_t* target, const float* lse, const float* dloss,
+                                    int V, int T, int t) {
+    const bool in = t < T;
+    const float L = in ? lse[t] : 0.f;
+    y = in ? target[t] : -1;
+    const bool live = y >= 0 && y < V && L != -__builtin_inff();
+    if (!live) y = -1;
+    l2 = live ? L * kLog2e : 0.f;
+    const float g = live ? dloss[t] : 0.f;
+    G = fabsf(g);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) G = fmaxf(G, __shfl_xor(G, o));
+    row_weight(g, G, m, e, gm);
+  }
+};
+
+struct FewArgs {
+  const bf16_t *w, *h;
+  const float* b;
+  const int32_t* target;
+  const float *lse, *dloss;
+  int V, d, T;
+  bf16_t* D;
+  float* db;
+};
+
+// D: the first core's tiles of 128 vocabulary rows x 16 ET tokens (32 at least)
+template <class T, int ET>
+struct FewSrc {
+  struct Desc {
+    int mt;
+    static __device__ __forceinline__ Desc pick(bool c, const Desc& x, const Desc& y) {
+      return Desc{c ? x.mt : y.mt};
+    }
+  };
+  const FewArgs& a;
+  const TileSched& S;
+  const int* s_y;
+  const float *s_l2, *s_m, *s_e;
+  float G;
+
+  __device__ __forceinline__ Desc desc(int j) const {
+    int mt, nt, sp;
+    S.decode(j, mt, nt, sp);
+    return Desc{mt};
+  }
+  __device__ __forceinline__ void rows(const Desc& d, int (&src)[T::A_PT]) const {
+    const int v0 = d.mt * T::BM, valid = min(T::BM, a.V - v0);
+#pragma unroll
+    for (int i = 0; i < T::A_PT; ++i) src[i] = v0 + min(dma_row(i, T::ROWS_PER_PASS), valid - 1);
+  }
+  __device__ __forceinline__ void ptrs(DPtrs<T>& q, const Desc&, const int (&src)[T::A_PT]) const {
+    make_dptrs<T>(q, a.w, src, a.h, nullptr, 0, min(T::BN, a.T), a.d, 0);
+  }
+  __device__ __forceinline__ void epilogue(const Desc& d, Acc<T>& acc) const {
+    constexpr int PARTS = few_parts<ET>(), W = 16 * ET * PARTS;
+    const int lane = threadIdx.x & 63, wm = threadIdx.x >> 6;
+    const int v0 = d.mt * T::BM;
+    float sum[T::TM][16];
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[i][r] = 0.f;
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = acc_col<T>(0, j, lane);
+      const int y = s_y[t];
+      const float l2 = s_l2[t], m = s_m[t], e = m * s_e[t];
+#pragma unroll
+      for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int v = v0 + acc_row<T>(wm, i, r, lane);
+          float z = acc[i][j][r];
+          if (a.b) z += a.b[min(v, a.V - 1)];
+          float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -l2));
+          p = v == y ? p - 1.f : p;
+          p = y >= 0 && v < a.V ? p : 0.f;
+          sum[i][r] = fmaf(e, p, sum[i][r]);
+          const float x = p * m;
+          bf16_t* o = a.D + (size_t)v * W + t;
+          if (16 * ET >= T::BN || t < 16 * ET) {
+            const bf16_t hi = f2bf(x);
+            o[0] = hi;
+            if constexpr (PARTS == 2) o[16 * ET] = f2bf(x - bf2f(hi));
+          }
+        }
+    }
+    if (!a.db) return;
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float s = row16_sum(sum[i][r]);
+        const LanePair p = lanes_xor16(s);
+        const int v = v0 + acc_row<T>(wm, i, r, lane);
+        if ((lane & 31) == 0 && v < a.V) a.db[v] = (p.a + p.b) * G;
+      }
+  }
+};
+
+template <class T, int ET>
+__global__ __launch_bounds__(T::THREADS) void k_dz_few(FewArgs a) {
+  __shared__ __align__(16) char lds[DmaTile<T>::LDS];
+  __shared__ int s_y[64];
+  __shared__ float s_l2[64], s_m[64], s_e[64], s_G;
+  TileSched S;
+  int ntiles;
+  if (!S.init((a.V + T::BM - 1) / T::BM, 1, 1, ntiles)) return;
+  if (threadIdx.x < 64) {
+    const int t = threadIdx.x;
+    const FewRow r(a.target, a.lse, a.dloss, a.V, a.T, t);
+    s_y[t] = r.y;
+    s_l2[t] = r.l2;
+    s_m[t] = r.m;
+    s_e[t] = r.e;
+    s_G = r.G;
+  }
+  __syncthreads();
+  const FewSrc<T, ET> src{a, S, s_y, s_l2, s_m, s_e, s_G};
+  dma_gemm_stream<T>(lds, ntiles, a.d / BK, src);
+}
+
+struct FewTokens {
+  const bf16_t* h;
+  const float* s_e;  // 2^-e of live rows, -1 of the others
+  int T, d, V;
+  float scale;
+  __device__ __forceinline__ bf16_t w(int t, int c) const {
+    const float e = s_e[t];
+    return e >= 0.f ? f2bf(bf2f(h[(size_t)t * d + c]) * e) : bf16_t(0);
+  }
+  __device__ __forceinline__ unsigned long long mask(int tile) const {
+    const int n = V - tile * kRowTile;
+    return n >= 64 ? ~0ull : (1ull << n) - 1;
+  }
+};
+
+template <int ET, int CW>
+__global__ __launch_bounds__(256) void k_few_grad(FewArgs a, bf16_t* dw, float* part_dh) {
+  __shared__ __align__(16) char lds[RowsGrad<ET, CW, few_parts<ET>()>::LDS];
+  __shared__ float s_e[64], s_G;
+  if (threadIdx.x < 64) {
+    const FewRow r(a.target, a.lse, a.dloss, a.V, a.T, threadIdx.x);
+    s_e[threadIdx.x] = r.y >= 0 ? r.e : -1.f;
+    s_G = r.G;
+  }
+  __syncthreads();
+  rows_grad<ET, CW, few_parts<ET>()>(lds, FewTokens{a.h, s_e, a.T, a.d, a.V, s_G}, a.w, a.D, a.V,
+                                     a.T, a.d, dw, part_dh, nullptr);
+}
+
+// dh_t = g / m times the sum of the S slices; 4 elements a thread
+__global__ __launch_bounds__(256) void k_few_finish(FewArgs a, const float* part, int S, bf16_t* dh) {
+  __shared__ float s_gm[64];
+  if (threadIdx.x < 64) {
+    const FewRow r(a.target, a.lse, a.dloss, a.V, a.T, threadIdx.x);
+    s_gm[threadIdx.x] = r.gm;
+  }
+  __syncthreads();
+  const int n = a.T * a.d, i = 4 * (blockIdx.x * 256 + threadIdx.x);
+  if (i >= n) return;
+  f32x4_t s = *reinterpret_cast<const f32x4_t*>(part + i);
+#pragma unroll 4
+  for (int k = 1; k < S; ++k) s += *reinterpret_cast<const f32x4_t*>(part + (size_t)k * n + i);
+  const float g = s_gm[i / a.d];
+  uint2 w;
+  w.x = pack_bf16x2(s[0] * g, s[1] * g);
+  w.y = pack_bf16x2(s[2] * g, s[3] * g);
+  *reinterpret_cast<uint2*>(dh + i) = w;
+}
+
 // ------------------------------------------------------------------ plan --
 // bytes of D that a piece may take
 constexpr size_t kPieceBytes = (size_t)256 << 20;
@@ -620,6 +829,8 @@ hipError_t loss_f32(const HeadLossArgs& a, hipStream_t st) {
                      (operand<T, true>(a.w, a.d, a.V, a.d)), (operand<T, true>(a.h, a.d, a.T, a.d)),
                      a.b, n_vt, part);
   hipLaunchKernelGGL((k_loss_join<T, false>), dim3(cdiv(a.T, 4)), dim3(256), 0, st, part, n_vt, a.V, a.d, a.T,
+                     a.d % 4 == 0 && ((reinterpret_cast<uintptr_t>(a.w) |
+                                       reinterpret_cast<uintptr_t>(a.h)) & 15) == 0,
                      static_cast<const T*>(a.w), a.b, static_cast<const T*>(a.h), a.target, a.loss,
                      a.lse);
   return hipGetLastError();
@@ -678,6 +889,24 @@ hipError_t backward_f32(const HeadLossArgs& a, hipStream_t st) {
   return hipGetLastError();
 }
 
+// bf16, up to kSkinnyTokens rows
+constexpr int kFewCols = 4;  // columns / 64 of a block of both products
+struct FewPlan {
+  int et, R;  // token tiles of 16, slices of dh
+  size_t o_dh, total;
+};
+
+FewPlan few_plan(int V, int d, int T) {
+  FewPlan p;
+  p.et = T <= 16 ? 1 : T <= 32 ? 2 : 4;
+  const int n_c = cdiv(d, 64 * kFewCols), n_t = cdiv(V, kRowTile);
+  p.R = std::max(1, std::min(n_t, cdiv(2 * kCu, n_c)));
+  const size_t rows = cdiv(V, 128) * (size_t)128;
+  p.o_dh = align256(rows * 32 * p.et * (p.et == 1 ? 2 : 1));
+  p.total = p.o_dh + align256((size_t)p.R * std::max(T, 1) * d * 4);
+  return p;
+}
+
 struct BackPlanBf16 {
   int Vp, s_dh;  // columns of a piece (a multiple of the tile), splits of dh
   size_t o_rows, o_hw, o_d, o_dh, o_db, total;
@@ -729,12 +958,35 @@ hipError_t loss_bf16(const HeadLossArgs& a, hipStream_t st) {
       launch_head_loss_partials(a.w, a.b, a.h, a.T, a.V, a.d, n_vt, part, a.n_cu, st);
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((k_loss_join<bf16_t, true>), dim3(cdiv(a.T, 4)), dim3(256), 0, st, part, n_vt,
-                     a.V, a.d, a.T, static_cast<const bf16_t*>(a.w), a.b,
+                     a.V, a.d, a.T, true, static_cast<const bf16_t*>(a.w), a.b,
                      static_cast<const bf16_t*>(a.h), a.target, a.loss, a.lse);
   return hipGetLastError();
 }
 
+template <int ET>
+hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st) {
+  constexpr int CW = kFewCols;
+  using Tl = Tile<128, ET == 4 ? 64 : 32, 1, 4, 1>;
+  const FewArgs f{static_cast<const bf16_t*>(a.w), static_cast<const bf16_t*>(a.h), a.b, a.target,
+                  a.lse, a.dloss, a.V, a.d, a.T, reinterpret_cast<bf16_t*>(a.ws), a.db};
+  float* part = a.dh ? reinterpret_cast<float*>(a.ws + p.o_dh) : nullptr;
+  hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS), 0,
+                     st, f);
+  if (a.dw || a.dh)
+    hipLaunchKernelGGL((k_few_grad<ET, CW>), dim3(cdiv(a.d, 64 * CW), p.R), dim3(256), 0, st, f,
+                       static_cast<bf16_t*>(a.dw), part);
+  if (a.dh)
+    hipLaunchKernelGGL(k_few_finish, dim3(cdiv(a.T * a.d, 1024)), dim3(256), 0, st, f, part, p.R,
+                       static_cast<bf16_t*>(a.dh));
+  return hipGetLastError();
+}
+
 hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
+  if (a.T > 0 && a.T <= kSkinnyTokens) {
+    const FewPlan p = few_plan(a.V, a.d, a.T);
+    return p.et == 1 ? backward_few<1>(a, p, st)
+                     : p.et == 2 ? backward_few<2>(a, p, st) : backward_few<4>(a, p, st);
+  }
   const BackPlanBf16 p = back_plan_bf16(a.V, a.d, a.T);
   const size_t rows = a.T > 0 ? a.T : 1;
   float* f = reinterpret_cast<float*>(a.ws + p.o_rows);
@@ -794,7 +1046,8 @@ size_t head_loss_ws(bool bf16, int V, int, int T) {
                   sizeof(float2));
 }
 size_t head_loss_backward_ws(bool bf16, int V, int d, int T) {
-  return bf16 ? back_plan_bf16(V, d, T).total : back_plan(V, d, T).total;
+  if (!bf16) return back_plan(V, d, T).total;
+  return T > 0 && T <= kSkinnyTokens ? few_plan(V, d, T).total : back_plan_bf16(V, d, T).total;
 }
 
 hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t st) {
