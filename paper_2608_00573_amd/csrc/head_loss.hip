@@ -416,11 +416,21 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
         a.D + ((size_t)vt * a.T + t0) * 256, (short)0, t_valid * 512, 0x00020000);
     const uint32_t col = (uint32_t)(L.wm * 128 + pack_col(L.lane));
+    // (all of them first: behind a store the compiler would wait for each)
+    int ty[8];
+    float tl2[8], tm[8], te[BIAS ? 8 : 1];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int tl = L.wn * 128 + 16 * j + c, t = min(t0 + tl, a.T - 1);
-      const int y = a.rows.y[t];
-      const float l2 = a.rows.l2[t], m = a.rows.m[t], g = BIAS ? m * a.rows.e[t] : 0.f;
+      const int t = min(t0 + L.wn * 128 + 16 * j + c, a.T - 1);
+      ty[j] = a.rows.y[t];
+      tl2[j] = a.rows.l2[t];
+      tm[j] = a.rows.m[t];
+      if constexpr (BIAS) te[j] = a.rows.e[t];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int tl = L.wn * 128 + 16 * j + c, y = ty[j];
+      const float l2 = tl2[j], m = tm[j], g = BIAS ? m * te[BIAS ? j : 0] : 0.f;
       const bool live = y >= 0 && tl < t_valid;
       const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
       const int l = live ? lim : 0;
@@ -928,13 +938,31 @@ int big_splits(int m, int n, int nk) {
   return best;
 }
 
+// vocabulary tiles of a piece, of `all` and at most `most`: as many pieces as
+// `most` makes, rounded up (while that stays below it) to what fills whole rounds
+// of the grid, with n_tt tiles each for D and n_dt for dw
+int even_rounds(int all, int most, int n_tt, int n_dt) {
+  int per = cdiv(all, cdiv(all, most));
+  if (per == all) return per;
+  for (int n : {n_dt, n_tt}) {
+    int g = kCu;  // kCu / gcd(kCu, n)
+    while (g > 1 && n % 2 == 0) {
+      g /= 2;
+      n /= 2;
+    }
+    const int up = cdiv(per, g) * g;
+    if (up <= most) per = up;
+  }
+  return per;
+}
+
 BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   BackPlanBf16 p;
   const size_t rows = T > 0 ? T : 1;
   const size_t fit = kPieceBytes / (2 * rows) / big::BM * big::BM;
   const int most = (int)std::min<size_t>(std::max<size_t>(fit, big::BM), (size_t)1 << 22);
-  const int n_pieces = cdiv(V, most);
-  p.Vp = cdiv(cdiv(V, n_pieces), big::BM) * big::BM;
+  p.Vp = even_rounds(cdiv(V, big::BM), most / big::BM, cdiv((int)rows, big::BN), cdiv(d, big::BM)) *
+         big::BM;
   p.s_dh = big_splits((int)rows, d, p.Vp / BK);
   size_t o = 0;
   const auto take = [&](size_t bytes) {
