@@ -369,7 +369,8 @@ struct DzArgs {
   float* db_part;     // [token tiles][Vp] or NULL
 };
 
-// D of a piece: A = w (vocabulary rows), B = h.  BIAS: with a bias, db or both
+// D of a piece: A = w (vocabulary rows), B = h.  BIAS: with a bias, db or both.
+// A tile's epilogue runs while the next tile's first loads are in flight.
 template <bool BIAS>
 __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
   __shared__ __align__(16) char lds[big::LDS];
@@ -381,28 +382,41 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
   L.rows(la, L.wm);
   L.rows(lb, L.wn);
   const int nk = a.d / BK;
-  AccBig acc;
-  for (int jt = 0; jt < ntiles; ++jt) {
-    int vt, tt, sp;
+  const auto start = [&](BigRows& q, int jt, int& vt, int& tt) {
+    int sp;
     S.decode(jt, vt, tt, sp);
     const int c0 = vt * big::BM, t0 = tt * big::BN;
     const int v_valid = min(big::BM, a.nv - c0), t_valid = min(big::BN, a.T - t0);
-    {
-      BigRows q;
-      q.ra = buf_rsrc(a.w + (size_t)c0 * a.d);
-      q.rb0 = q.rb1 = buf_rsrc(a.h + (size_t)t0 * a.d);
-      q.none = buf_rsrc_empty(a.w);
+    q.ra = buf_rsrc(a.w + (size_t)c0 * a.d);
+    q.rb0 = q.rb1 = buf_rsrc(a.h + (size_t)t0 * a.d);
+    q.none = buf_rsrc_empty(a.w);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const int r = L.r0 + big::RPP * u;
-        q.off[u] = ((uint32_t)min(r, v_valid - 1) * a.d + L.cc) * 2;
-        q.off[8 + u] = ((uint32_t)min(r, t_valid - 1) * a.d + L.cc) * 2;
-      }
-      big_zero(acc);
-      big_tile<false, true>(lds, q, nk, acc, la, lb);
+    for (int u = 0; u < 8; ++u) {
+      const int r = L.r0 + big::RPP * u;
+      q.off[u] = ((uint32_t)min(r, v_valid - 1) * a.d + L.cc) * 2;
+      q.off[8 + u] = ((uint32_t)min(r, t_valid - 1) * a.d + L.cc) * 2;
     }
+    big_start<false>(lds, q, nk);
+  };
+  AccBig acc;
+  BigRows q;
+  int vt, tt;
+  start(q, 0, vt, tt);
+  for (int jt = 0; jt < ntiles; ++jt) {
+    big_zero(acc);
+    if (jt == 0)
+      big_wait<0>();
+    else
+      big_wait<32>();  // (every wavefront issues the epilogue's 32 stores)
+    big_run<false, true>(lds, q, nk, acc, la, lb);
+    const int c0 = vt * big::BM, t0 = tt * big::BN, tile = tt;
+    const int v_valid = min(big::BM, a.nv - c0), t_valid = min(big::BN, a.T - t0);
     const int c = L.lane & 15, rl = L.wm * 128 + 4 * (L.lane >> 4);  // the lane's first row
-    const int lim = v_valid - rl;  // its row o (16 i + r) is valid for o < lim
+    // rows of D past the last one lie behind the buffer's end and are dropped
+    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
+        a.D + ((size_t)vt * a.T + t0) * 256, (short)0, t_valid * 512, 0x00020000);
+    // what the epilogue reads, before the next tile's loads (it would wait for
+    // those too) and before its stores
     float b[BIAS ? 8 : 1][4], sum[BIAS ? 8 : 1][4];
     if constexpr (BIAS)
 #pragma unroll
@@ -412,11 +426,6 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
           b[i][r] = a.bias ? a.bias[c0 + min(rl + 16 * i + r, v_valid - 1)] * kLog2e : 0.f;
           sum[i][r] = 0.f;
         }
-    // rows of D past the last one lie behind the buffer's end and are dropped
-    const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
-        a.D + ((size_t)vt * a.T + t0) * 256, (short)0, t_valid * 512, 0x00020000);
-    const uint32_t col = (uint32_t)(L.wm * 128 + pack_col(L.lane));
-    // (all of them first: behind a store the compiler would wait for each)
     int ty[8];
     float tl2[8], tm[8], te[BIAS ? 8 : 1];
 #pragma unroll
@@ -427,14 +436,19 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
       tm[j] = a.rows.m[t];
       if constexpr (BIAS) te[j] = a.rows.e[t];
     }
+    sched_fence();
+    if (jt + 1 < ntiles) start(q, jt + 1, vt, tt);
+    const uint32_t col = (uint32_t)(L.wm * 128 + pack_col(L.lane));
+    const int lim = v_valid - rl;  // the lane's row o (16 i + r) is valid for o < lim
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int tl = L.wn * 128 + 16 * j + c, y = ty[j];
       const float l2 = tl2[j], m = tm[j], g = BIAS ? m * te[BIAS ? j : 0] : 0.f;
       const bool live = y >= 0 && tl < t_valid;
       const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
-      const int l = live ? lim : 0;
       const uint32_t off = ((uint32_t)tl * 256 + col) * 2;
+      // few tiles hold a target of these rows, one a piece is cut short
+      const bool plain = v_valid == big::BM && __ballot((unsigned)yr < 128u) == 0;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         float x[2][4];
@@ -442,11 +456,23 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const int o = 16 * (i + k) + r;
             const float s = BIAS ? b[i + k][r] - l2 : -l2;
-            float p = __builtin_amdgcn_exp2f(fmaf(acc[i + k][j][r], kLog2e, s));
-            p = o == yr ? p - 1.f : p;
-            p = o < l ? p : 0.f;
+            x[k][r] = __builtin_amdgcn_exp2f(fmaf(acc[i + k][j][r], kLog2e, s));
+          }
+        if (!plain)
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int o = 16 * (i + k) + r;
+              x[k][r] = o == yr ? x[k][r] - 1.f : x[k][r];
+              x[k][r] = o < lim ? x[k][r] : 0.f;
+            }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float p = live ? x[k][r] : 0.f;
             x[k][r] = p * m;
             if constexpr (BIAS) sum[i + k][r] = fmaf(g, p, sum[i + k][r]);
           }
@@ -455,7 +481,9 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
     }
     if constexpr (BIAS) {
       if (!a.db_part) continue;
-      float* s_db = reinterpret_cast<float*>(lds);  // [2][256]
+      // [2][256], in the B stage that the next tile's loads do not reach before its
+      // first barrier
+      float* s_db = reinterpret_cast<float*>(lds + big::B0 + 2 * big::BB);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -464,8 +492,7 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
           if (c == 0) s_db[L.wn * 256 + rl + 16 * i + r] = v;
         }
       lds_barrier();
-      a.db_part[(size_t)tt * a.Vp + c0 + threadIdx.x] = s_db[threadIdx.x] + s_db[256 + threadIdx.x];
-      lds_barrier();
+      a.db_part[(size_t)tile * a.Vp + c0 + threadIdx.x] = s_db[threadIdx.x] + s_db[256 + threadIdx.x];
     }
   }
 }
@@ -496,76 +523,91 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
   else
     L.rows(lb, L.wn);
   const int nk = cdiv_d(a.K, BK);
-  AccBig acc;
-  for (int jt = 0; jt < ntiles; ++jt) {
+  struct At {
+    int m0, n0, sp, nk;
+  };
+  const auto start = [&](BigRowsT<DW>& q, int jt, At& t) {
     int nt, mt, sp;
     S.decode(jt, nt, mt, sp);
-    const int m0 = mt * big::BM, n0 = nt * big::BN;
-    const int m_valid = min(big::BM, a.M - m0), n_valid = min(big::BN, a.N - n0);
+    const int m0 = mt * big::BM, n0 = nt * big::BN, n_valid = min(big::BN, a.N - n0);
     const int ka = (int)((long)sp * nk / a.splits), kb = (int)((long)(sp + 1) * nk / a.splits);
-    {
-      BigRowsT<DW> q;
-      q.none = buf_rsrc_empty(a.A);
-      if constexpr (DW) {
-        q.la = big_panel(a.A, a.K, ka * BK, m0);
-        q.lb = big_panel(a.B, a.K, ka * BK, n0);
-      } else {
-        q.la = big_long(a.A, a.M, a.K, ka * BK, m0);
-        q.rb0 = buf_rsrc(a.B + (size_t)n0 * 256);
-        q.panel = (uint32_t)a.N * 512;
-        q.k0 = ka;
-      }
-#pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        q.off[u] = L.fetch(u, DW ? 256 : a.M);
-        q.off[8 + u] = DW ? L.fetch(u, 256)
-                          : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * 256 + L.cc) * 2;
-      }
-      if (!DW && a.add) {
-        // the sums so far in place of zeros
-        const int c = L.lane & 15, m = L.wm * 128 + 4 * (L.lane >> 4);
-        const float* was = static_cast<const float*>(a.out) + ((size_t)sp * a.N + n0) * a.M + m0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float* p = was + (size_t)min(L.wn * 128 + 16 * j + c, n_valid - 1) * a.M;
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            acc[i][j] = *reinterpret_cast<const f32x4_t*>(p + (m + 16 * i < m_valid ? m + 16 * i : 0));
-        }
-      } else {
-        big_zero(acc);
-      }
-      big_tile<false, true>(lds, q, kb - ka, acc, la, lb);
+    t = At{m0, n0, sp, kb - ka};
+    q.none = buf_rsrc_empty(a.A);
+    if constexpr (DW) {
+      q.la = big_panel(a.A, a.K, ka * BK, m0);
+      q.lb = big_panel(a.B, a.K, ka * BK, n0);
+    } else {
+      q.la = big_long(a.A, a.M, a.K, ka * BK, m0);
+      q.rb0 = buf_rsrc(a.B + (size_t)n0 * 256);
+      q.panel = (uint32_t)a.N * 512;
+      q.k0 = ka;
     }
-    const int c = L.lane & 15;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      q.off[u] = L.fetch(u, DW ? 256 : a.M);
+      q.off[8 + u] = DW ? L.fetch(u, 256)
+                        : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * 256 + L.cc) * 2;
+    }
+    big_start<false>(lds, q, t.nk);
+  };
+  constexpr int ES = DW ? 2 : 4, STORES = DW ? 32 : 64;
+  const float g = DW ? *a.scale : 0.f;
+  const int c = L.lane & 15;
+  AccBig acc;
+  BigRowsT<DW> q;
+  At at;
+  start(q, 0, at);
+  for (int jt = 0; jt < ntiles; ++jt) {
+    const int m0 = at.m0, n0 = at.n0, sp = at.sp;
+    const int m_valid = min(big::BM, a.M - m0), n_valid = min(big::BN, a.N - n0);
+    if (!DW && a.add) {
+      // the sums so far in place of zeros
+      const int m = L.wm * 128 + 4 * (L.lane >> 4);
+      const float* was = static_cast<const float*>(a.out) + ((size_t)sp * a.N + n0) * a.M + m0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float* p = was + (size_t)min(L.wn * 128 + 16 * j + c, n_valid - 1) * a.M;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          acc[i][j] = *reinterpret_cast<const f32x4_t*>(p + (m + 16 * i < m_valid ? m + 16 * i : 0));
+      }
+    } else {
+      big_zero(acc);
+    }
+    if (jt == 0)
+      big_wait<0>();
+    else
+      big_wait<STORES>();  // (every wavefront issues all of the epilogue's stores)
+    big_run<false, true>(lds, q, at.nk, acc, la, lb);
+    sched_fence();
+    if (jt + 1 < ntiles) start(q, jt + 1, at);
     int M = a.M;
     asm volatile("" : "+s"(M));  // per-tile value: keeps the offsets below inside the tile loop
-    constexpr int ES = DW ? 2 : 4;
     const size_t o = ((size_t)(DW ? 0 : sp) * a.N + n0) * M + m0;
-    // rows past the last one lie behind the buffer's end
+    // rows past the last one lie behind the buffer's end; so do columns past it by
+    // their offset (M is a multiple of 64: blocks of 32 are valid or not as a whole)
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
         static_cast<char*>(a.out) + o * ES, (short)0, (int)((uint32_t)n_valid * M * ES), 0x00020000);
-    const float g = DW ? *a.scale : 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t row = (uint32_t)(L.wn * 128 + 16 * j + c) * M;
       const uint32_t off = (row + L.wm * 128 + (DW ? pack_col(L.lane) : 4 * (L.lane >> 4))) * ES;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
-        if (L.wm * 128 + 16 * i >= m_valid) continue;  // (M is a multiple of 64)
+        const uint32_t at_i = L.wm * 128 + 16 * i < m_valid ? off : 0xffff0000u;
         if constexpr (DW) {
           float x[2][4];
 #pragma unroll
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[k][r] = acc[i + k][j][r] * g;
-          __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, off, 32 * i, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, at_i, 32 * i, 0);
         } else {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             f32x4_t x = acc[i + k][j];
             asm volatile("" : "+v"(x));  // through VGPRs (see big_store_partial_rows)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), ro, off,
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), ro, at_i,
                                                    64 * (i + k), 0);
           }
         }

@@ -760,42 +760,46 @@ __device__ __forceinline__ void big_half(const BigLds& L, int g, int wave, const
   big_slot<0, true, DUAL, R>(fa, fb1, fb0, acc, na + a_lane[0], nb + b_lane[0], dma_a2, dma_b);
 }
 
-// C tile += A rows x B rows over nk slices from the rows' K origin; returns
-// with every load landed and every wave past its last LDS access
+// A tile's first loads: slice 0, B of slice 1 and the first half of its A.  LDS is
+// free from the end of a tile on (the epilogue may use the last B stage).
+template <bool DUAL, class R>
+__device__ __forceinline__ void big_start(char* lds, const R& q, int nk) {
+  const BigLds L{lds_addr(lds)};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const typename BigSrcOf<R>::type s0(q, 0, nk), s1(q, 1, nk);
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma_a(L.a(0), wave, q, s0, u);
+    sched_fence();
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma<DUAL>(L.b(0), wave, q, s0, u);
+    sched_fence();
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma<DUAL>(L.b(1), wave, q, s1, u);
+    sched_fence();
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    big_dma_a(L.a(1), wave, q, s1, u);
+    sched_fence();
+  }
+}
+
+// C tile += A rows x B rows over nk slices from the rows' K origin, after
+// big_start and its wait; returns with every load landed and every wave past its
+// last LDS access
 // (SETTLE: the last row's wait states come inside the loop, after its last slice,
 // for kernels in which the compiler copies accumulators on the way out of it).
 template <bool DUAL, bool SETTLE = false, class R>
-__device__ __forceinline__ void big_tile(char* lds, const R& q, int nk, AccBig& acc,
-                                         const uint32_t (&a_lane)[2],
-                                         const uint32_t (&b_lane)[2]) {
+__device__ __forceinline__ void big_run(char* lds, const R& q, int nk, AccBig& acc,
+                                        const uint32_t (&a_lane)[2],
+                                        const uint32_t (&b_lane)[2]) {
   const BigLds L{lds_addr(lds)};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  {
-    const typename BigSrcOf<R>::type s0(q, 0, nk), s1(q, 1, nk);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      big_dma_a(L.a(0), wave, q, s0, u);
-      sched_fence();
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      big_dma<DUAL>(L.b(0), wave, q, s0, u);
-      sched_fence();
-    }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      big_dma<DUAL>(L.b(1), wave, q, s1, u);
-      sched_fence();
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      big_dma_a(L.a(1), wave, q, s1, u);
-      sched_fence();
-    }
-  }
-  // A and B of slice 0 have landed (12 newer operations: B of slice 1 and
-  // the first half of its A)
-  asm volatile("s_waitcnt vmcnt(12)\n\ts_barrier" ::: "memory");
   // the first k-step's fragments, in the order the last k-step of a slice
   // reads them (the first k-step's waits count on it)
   FragA fa;
@@ -847,6 +851,24 @@ __device__ __forceinline__ void big_tile(char* lds, const R& q, int nk, AccBig& 
                  "+a"(acc[7][4]), "+a"(acc[7][5]), "+a"(acc[7][6]), "+a"(acc[7][7])
                :
                : "memory");
+}
+
+// The wait between big_start and big_run: A and B of slice 0 have landed (12 newer
+// loads, B of slice 1 and the first half of its A, and NEWER vector-memory
+// operations issued since)
+template <int NEWER>
+__device__ __forceinline__ void big_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NEWER + 12 < 63 ? NEWER + 12 : 63)
+               : "memory");
+}
+
+template <bool DUAL, class R>
+__device__ __forceinline__ void big_tile(char* lds, const R& q, int nk, AccBig& acc,
+                                         const uint32_t (&a_lane)[2],
+                                         const uint32_t (&b_lane)[2]) {
+  big_start<DUAL>(lds, q, nk);
+  big_wait<0>();
+  big_run<DUAL>(lds, q, nk, acc, a_lane, b_lane);
 }
 
 // Two accumulators' values of one row (columns 16 i .. and 16 (i + 1) ..; a lane
