@@ -492,7 +492,7 @@ int trimmoe_train_exit_head(int32_t dtype, int32_t d_model, int32_t n_rows, cons
  * TRIMMOE_LOSS_MAX_D.  Sums run in a fixed order: repeated calls give identical
  * results.  A NaN (or infinite) logit makes its row's results NaN.
  */
-#define TRIMMOE_LOSS_MAX_ROWS (1 << 22)
+#define TRIMMOE_LOSS_MAX_ROWS (1 << 21)
 #define TRIMMOE_LOSS_MAX_VOCAB (1 << 28)
 #define TRIMMOE_LOSS_MAX_D (1 << 20)
 

@@ -25,9 +25,9 @@ namespace trimmoe {
 namespace {
 
 // ------------------------------------------------------- forward, fp32 --
-// A = w (vocabulary rows), B = h: a lane holds 32 vocabulary rows of a token
-// column, so the pair of a column is a reduction over registers, one lane
-// exchange and the two wavefronts of the column.  A NaN logit makes the sum NaN.
+// A = w (vocabulary rows), B = h: a lane holds 4 kTM vocabulary rows of a token
+// column, so the pair of a column is a reduction over registers, two lane
+// exchanges and the two wavefronts of the column.  A NaN logit makes the sum NaN.
 template <typename T>
 __global__ __launch_bounds__(f32p::THREADS) void k_loss_f32(Operand<T, true> W, Operand<T, true> H,
                                                             const float* bias, int n_vt,
@@ -41,12 +41,12 @@ __global__ __launch_bounds__(f32p::THREADS) void k_loss_f32(Operand<T, true> W, 
   f32_tile(W, H, v0, t0, 0, W.K, lds, acc);
   const float ninf = -__builtin_inff();
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < kTN; ++j) {
     float m = ninf;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kTM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 4; ++r) {
         const int v = v0 + f32_row(i, r);
         float z = acc[i][j][r];
         if (bias) z += bias[min(v, W.rows - 1)];
@@ -54,23 +54,23 @@ __global__ __launch_bounds__(f32p::THREADS) void k_loss_f32(Operand<T, true> W, 
         acc[i][j][r] = z;
         m = fmaxf(m, z);
       }
+    m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     const float ms = m == ninf ? 0.f : m;
-    float sum = 0.f;
+    // (in a tree: a chain would round each small term at the size of the largest)
+    float e[4 * kTM];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      // (in pairs: a chain would round each small term at the size of the largest)
-      float e[16];
+    for (int i = 0; i < kTM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) e[r] = expf(acc[i][j][r] - ms);
+      for (int r = 0; r < 4; ++r) e[4 * i + r] = expf(acc[i][j][r] - ms);
 #pragma unroll
-      for (int n = 8; n > 0; n >>= 1)
+    for (int n = 2 * kTM; n > 0; n >>= 1)
 #pragma unroll
-        for (int r = 0; r < n; ++r) e[r] += e[r + n];
-      sum += e[0];
-    }
+      for (int r = 0; r < n; ++r) e[r] += e[r + n];
+    float sum = e[0];
+    sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if ((threadIdx.x & 63) < 32) s_p[threadIdx.x >> 7][f32_col(j)] = make_float2(m, sum);
+    if ((threadIdx.x & 63) < 16) s_p[threadIdx.x >> 7][f32_col(j)] = make_float2(m, sum);
   }
   __syncthreads();
   const int c = threadIdx.x;
@@ -155,28 +155,40 @@ __global__ __launch_bounds__(f32p::THREADS) void k_dz_f32(Operand<T, true> H, Op
   F32Acc acc;
   f32_tile(H, W, t0, c0, 0, H.K, lds, acc);
   float* s_sum = lds;  // [2][BN]; the tile ended on a barrier
+  // the lane's rows first: behind a store the compiler would wait for each
+  int ty[kTM][4];
+  float tl[kTM][4], tg[kTM][4];
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int i = 0; i < kTM; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int t = min(t0 + f32_row(i, r), H.rows - 1);
+      ty[i][r] = target[t];
+      tl[i][r] = lse[t];
+      tg[i][r] = dloss[t];
+    }
+#pragma unroll
+  for (int j = 0; j < kTN; ++j) {
     const int c = c0 + f32_col(j);
     const float bj = bias && c < W.rows ? bias[c] : 0.f;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kTM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int t = t0 + f32_row(i, r);
+      for (int r = 0; r < 4; ++r) {
+        const int t = t0 + f32_row(i, r), y = ty[i][r];
+        const float L = tl[i][r];
         float x = 0.f;
         if (t < H.rows) {
-          const int y = target[t];
-          const float L = lse[t];
           if (c < W.rows && y >= 0 && y < V && L != -__builtin_inff())
-            x = dloss[t] * (expf(acc[i][j][r] + bj - L) - (v0 + c == y ? 1.f : 0.f));
+            x = tg[i][r] * (expf(acc[i][j][r] + bj - L) - (v0 + c == y ? 1.f : 0.f));
           D[(size_t)t * ldd + c] = x;
         }
         sum += x;
       }
+    sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if ((threadIdx.x & 63) < 32) s_sum[(threadIdx.x >> 7) * BN + f32_col(j)] = sum;
+    if ((threadIdx.x & 63) < 16) s_sum[(threadIdx.x >> 7) * BN + f32_col(j)] = sum;
   }
   __syncthreads();
   if (db_part && threadIdx.x < BN)

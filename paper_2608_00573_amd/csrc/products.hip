@@ -17,13 +17,13 @@ __global__ __launch_bounds__(f32p::THREADS) void k_prod_f32(Operand<TA, AK> A, O
   f32_tile(A, B, mt * BM, nt * BN, k0, k1, lds, acc);
   TO* o = out + (size_t)blockIdx.z * A.rows * B.rows;
 #pragma unroll
-  for (int j = 0; j < 2; ++j) {
+  for (int j = 0; j < kTN; ++j) {
     const int c = nt * BN + f32_col(j);
     if (c >= B.rows) continue;
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kTM; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
+      for (int r = 0; r < 4; ++r) {
         const int m = mt * BM + f32_row(i, r);
         if (m >= A.rows) continue;
         TO* q = o + (size_t)m * B.rows + c;

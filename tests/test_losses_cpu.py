@@ -118,7 +118,7 @@ def _bal_b(dtype=1, E=8, k=2, d=64, Q=8, w=A, h=A, t=A, p=A, c=A, g=A, dh=A, dw=
 
 BAD_DIMS = [(dict(dtype=2), DTYPE), (dict(dtype=-1), DTYPE), (dict(d=96), SHAPE),
             (dict(d=0), SHAPE), (dict(dtype=0, d=0), SHAPE), (dict(d=(1 << 20) + 64), SHAPE),
-            (dict(Q=-1), SHAPE), (dict(Q=(1 << 22) + 1), SHAPE)]
+            (dict(Q=-1), SHAPE), (dict(Q=(1 << 21) + 1), SHAPE)]
 BAD_BUFFERS = [(dict(w=0), NULL), (dict(ws=0), NULL), (dict(h=0), NULL), (dict(w=A + 8), SHAPE),
                (dict(h=A + 2), SHAPE), (dict(dtype=0, h=A + 2), SHAPE), (dict(ws=A + 128), WORKSPACE),
                (dict(n=64), WORKSPACE)]
@@ -175,7 +175,7 @@ def test_workspace_sizes(name, dims, dtype):
     assert f(dtype, *dims, 8, None) == NULL
     assert f(2, *dims, 8, C.byref(n)) == DTYPE
     assert f(dtype, *dims, -1, C.byref(n)) == SHAPE
-    for rows in (0, 1, 37, 64, 65, 1000, 8192, 100000, 1 << 22):
+    for rows in (0, 1, 37, 64, 65, 1000, 8192, 100000, 1 << 21):
         assert f(dtype, *dims, rows, C.byref(n)) == 0 and n.value % 256 == 0
     # far less than the logits of a large batch
     if "cross_entropy" in name and dims[0] > 1000:
