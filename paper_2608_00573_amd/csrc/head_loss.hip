@@ -15,6 +15,7 @@
 
 #include <algorithm>
 
+#include "few_rows.h"
 #include "gemm.h"
 #include "loss.h"
 #include "products.h"
@@ -81,8 +82,6 @@ __global__ __launch_bounds__(f32p::THREADS) void k_loss_f32(Operand<T, true> W, 
         make_float2(M, p0.y * expf(p0.x - Ms) + p1.y * expf(p1.x - Ms));
   }
 }
-
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // One wavefront a row: joins the pairs and takes the target's logit from one
 // more dot product (a gathered row of w; the pairs do not keep it).
@@ -243,15 +242,6 @@ struct RowPart {
   float* G;    // [1]
 };
 
-// m, 2^-e and g / m of a weight g
-__device__ __forceinline__ void row_weight(float g, float G, float& m, float& e, float& gm) {
-  int x = 0;
-  const float f = g == 0.f ? 0.5f : frexpf(g / G, &x);  // (NaN stays NaN)
-  m = f == 0.f ? 1.f : 2.f * f;
-  e = g == 0.f || f == 0.f ? 0.f : ldexpf(1.f, x - 1);
-  gm = g / m;
-}
-
 __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const float* lse,
                                                    const float* dloss, int V, int T, RowPart p) {
   __shared__ float s_m[16];
@@ -359,15 +349,6 @@ __device__ __forceinline__ void big_zero(AccBig& acc) {
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{};
-}
-
-__device__ __forceinline__ float row16_sum(float v) {
-  // over the 16 lanes of a row (rotations by 8, 4, 2, 1)
-  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x128, 0xf, 0xf, false));
-  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x124, 0xf, 0xf, false));
-  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x122, 0xf, 0xf, false));
-  v += __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x121, 0xf, 0xf, false));
-  return v;
 }
 
 struct DzArgs {
@@ -668,41 +649,6 @@ __global__ __launch_bounds__(256) void k_db_finish(const float* part, int n_tt, 
 // products in one pass over w (rows_grad.h; its rows are the vocabulary's, its
 // experts the tokens).  D lies [vocabulary row][token], in two bf16 parts where
 // the products' k-step leaves room for them (up to 16 rows).
-template <int ET>
-constexpr int few_parts() {
-  return ET == 1 ? 2 : 1;
-}
-
-// the rows' parts (see RowPart), by the lanes of a wavefront; G by all of them
-struct FewRow {
-  int y;
-  float l2, m, e, gm, G;
-  __device__ __forceinline__ FewRow(const int32_t* target, const float* lse, const float* dloss,
-                                    int V, int T, int t) {
-    const bool in = t < T;
-    const float L = in ? lse[t] : 0.f;
-    y = in ? target[t] : -1;
-    const bool live = y >= 0 && y < V && L != -__builtin_inff();
-    if (!live) y = -1;
-    l2 = live ? L * kLog2e : 0.f;
-    const float g = live ? dloss[t] : 0.f;
-    G = fabsf(g);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) G = fmaxf(G, __shfl_xor(G, o));
-    row_weight(g, G, m, e, gm);
-  }
-};
-
-struct FewArgs {
-  const bf16_t *w, *h;
-  const float* b;
-  const int32_t* target;
-  const float *lse, *dloss;
-  int V, d, T;
-  bf16_t* D;
-  float* db;
-};
-
 // D: the first core's tiles of 128 vocabulary rows x 16 ET tokens (32 at least)
 template <class T, int ET>
 struct FewSrc {
@@ -1052,8 +998,13 @@ hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st)
   const FewArgs f{static_cast<const bf16_t*>(a.w), static_cast<const bf16_t*>(a.h), a.b, a.target,
                   a.lse, a.dloss, a.V, a.d, a.T, reinterpret_cast<bf16_t*>(a.ws), a.db};
   float* part = a.dh ? reinterpret_cast<float*>(a.ws + p.o_dh) : nullptr;
-  hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS), 0,
-                     st, f);
+  if (exit_streams(true, true, a.T, a.V, a.d) && (ET == 1 || !a.db)) {
+    const hipError_t e = launch_dz_skinny(f, a.n_cu, st);
+    if (e != hipSuccess) return e;
+  } else {
+    hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS),
+                       0, st, f);
+  }
   if (a.dw || a.dh)
     hipLaunchKernelGGL((k_few_grad<ET, CW>), dim3(cdiv(a.d, 64 * CW), p.R), dim3(256), 0, st, f,
                        static_cast<bf16_t*>(a.dw), part);

@@ -38,6 +38,7 @@
 // shared expert's weights stay in the last-level cache for a second pass).
 #include <math.h>
 
+#include "few_rows.h"
 #include "gemm.h"
 
 namespace trimmoe {
@@ -588,6 +589,70 @@ __global__ __launch_bounds__(skinny::THREADS) void k_loss_skinny(ExitArgs a, int
     skinny_exit_rows<false, Stream<1, 4, wide_kind(KIND)>, true>(a, lds, n_x, v0, v1);
 }
 
+// D of the head loss's gradient (head_loss.hip) for a few rows of h: the logits'
+// stream with D as its epilogue, [vocabulary row][part][16 MT] in parts of bf16.
+// Vocabulary rows from V up to a multiple of 64 are written as zeros.
+template <class T>
+__device__ __forceinline__ void skinny_dz_rows(const FewArgs& a, char* lds, int v0, int v1,
+                                               const FewRow& row) {
+  constexpr int MT = T::MT, UC = T::G * skinny::COLS, PARTS = few_parts<MT>(), W = 16 * MT * PARTS;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int fr = lane & 15, q = lane >> 4;
+  XSrc<MT> xs;
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    xs.p[m] = a.h + (size_t)min(16 * m + fr, a.T - 1) * a.d + 8 * q;
+    xs.step[m] = skinny::KSTEP;
+  }
+  auto wbase = [&](int u, int) { return a.w + (size_t)min(v0 + u * UC, a.V - 1) * a.d; };
+  auto wrows = [&](int u) { return min(v1, a.V) - v0 - u * UC; };
+  // the lane's token: tile wave % MT
+  const int t = 16 * (wave % MT) + fr;
+  const int y = __shfl(row.y, t);
+  const float l2 = __shfl(row.l2, t), m = __shfl(row.m, t), e = m * __shfl(row.e, t);
+  int par = 0;
+  auto epi = [&](int u, const f32x4_t(&acc)[1][T::G][MT]) {
+#pragma unroll
+    for (int g = 0; g < T::G; g += T::GR) {
+      f32x4_t z[1];
+      if (!skinny_sum<T>(lds, par, acc, g, z)) continue;
+      const int r0 = v0 + u * UC + (g + wave / MT) * skinny::COLS + 4 * q;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int v = r0 + r;
+        if (v >= v1) continue;  // (v1 and v0 are multiples of 16: a whole row of lanes)
+        float s = z[0][r];
+        if (a.b) s += a.b[min(v, a.V - 1)];
+        float p = __builtin_amdgcn_exp2f(fmaf(s, kLog2e, -l2));
+        p = v == y ? p - 1.f : p;
+        p = y >= 0 && v < a.V ? p : 0.f;
+        const float x = p * m;
+        const bf16_t hi = f2bf(x);
+        bf16_t* o = a.D + (size_t)v * W + t;
+        o[0] = hi;
+        if constexpr (PARTS == 2) o[16 * MT] = f2bf(x - bf2f(hi));
+        if constexpr (MT == 1)
+          if (a.db) {
+            const float d = row16_sum(e * p);
+            if (fr == 0 && v < a.V) a.db[v] = d * row.G;
+          }
+      }
+    }
+  };
+  const int units = (v1 - v0 + UC - 1) / UC;
+  skinny_stream<T>(lds, xs, units, a.d / skinny::KSTEP, wbase, wrows, epi);
+}
+
+template <int MT, int KIND>
+__global__ __launch_bounds__(skinny::THREADS) void k_dz_skinny(FewArgs a) {
+  __shared__ __align__(16) char lds[skinny::LDS];
+  const FewRow row(a.target, a.lse, a.dloss, a.V, a.T, threadIdx.x & 63);
+  const long n_u = (a.V + 63) / 64 * 4;
+  const int v0 = (int)(n_u * blockIdx.x / gridDim.x) * skinny::COLS;
+  const int v1 = (int)(n_u * (blockIdx.x + 1) / gridDim.x) * skinny::COLS;
+  if (v0 < v1) skinny_dz_rows<Stream<1, MT, KIND>>(a, lds, v0, v1, row);
+}
+
 // -------------------------------------------------------------- launchers --
 // set shape for a K of ks k-steps: sets must fit K
 static int stream_kind(int ks) { return ks < 8 ? kShort : kLong; }
@@ -634,6 +699,20 @@ hipError_t launch_loss_skinny(const ExitArgs& a, int n_rows, hipStream_t st) {
     hipLaunchKernelGGL(k_loss_skinny<kShort>, grid, block, 0, st, a, n_rows);
   else
     hipLaunchKernelGGL(k_loss_skinny<kLong>, grid, block, 0, st, a, n_rows);
+  return hipGetLastError();
+}
+
+hipError_t launch_dz_skinny(const FewArgs& a, int n_cu, hipStream_t st) {
+  const dim3 grid(n_cu), block(skinny::THREADS);
+  const bool low = stream_kind(a.d / skinny::KSTEP) == kShort;
+  if (a.T <= 16 && low)
+    hipLaunchKernelGGL((k_dz_skinny<1, kShort>), grid, block, 0, st, a);
+  else if (a.T <= 16)
+    hipLaunchKernelGGL((k_dz_skinny<1, kLong>), grid, block, 0, st, a);
+  else if (low)  // (exit_streams: never 17 to 32 rows)
+    hipLaunchKernelGGL((k_dz_skinny<4, kShort>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((k_dz_skinny<4, kMid>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 

@@ -140,6 +140,11 @@ HEADS = [
     (BF16, 1003, 128, 1, True),     # one row
     (BF16, 1003, 192, 16, False),
     (BF16, 4001, 2112, 33, True),
+    (BF16, 1003, 2048, 15, True),   # streams of w: few rows, ragged vocabulary
+    (BF16, 130, 2112, 16, False),
+    (BF16, 24700, 2048, 40, False), # ... up to 64 rows of a large vocabulary
+    (BF16, 24577, 2048, 64, True),  # ... whose bias gradient takes the tiles
+    (BF16, 24600, 2112, 20, True),
     (BF16, 1003, 64, 64, True),     # the last decode-sized batch
     (BF16, 1003, 64, 65, True),     # the first one beyond
     (BF16, 5000, 128, 300, True),
