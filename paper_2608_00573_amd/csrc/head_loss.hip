@@ -326,23 +326,43 @@ struct BigLane {
     for (int ks = 0; ks < 2; ++ks)
       o[ks] = (32 * ks + k) * 512 + half * 256 + (tr_swz(k) << 5) + 8 * (i & 3);
   }
-  // fetch offset u of a transposed operand with leading dimension ld
-  __device__ __forceinline__ uint32_t fetch(int u, int ld) const {
-    const int k = 2 * wave + 8 * u + (lane >> 5), p = lane & 31;
-    return (uint32_t)((k * ld + 16 * ((p >> 1) ^ tr_swz(k)) + 8 * (p & 1)) * 2);
+  // A TR operand of `rows` rows of ld elements along K, from row k0 (k1: the end of
+  // the tile's run) and column c0
+  __device__ __forceinline__ BigOperand<true> along(const bf16_t* p, int ld, int rows, int k0, int k1,
+                                                    int c0) const {
+    BigOperand<true> o;
+    o.p = reinterpret_cast<const char*>(p + ((size_t)k0 * ld + c0));
+    o.left = min(rows, k1) - k0;
+    o.row = (uint32_t)ld * 2;
+    o.cut = (uint32_t)c0 * 2;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int k = 2 * wave + 8 * u + (lane >> 5), c = lane & 31;
+      o.off[u] = (uint32_t)((k * ld + 16 * ((c >> 1) ^ tr_swz(k)) + 8 * (c & 1)) * 2);
+    }
+    return o;
+  }
+  // ... that lies in panels of 256 columns
+  __device__ __forceinline__ BigOperand<true> along_panel(const bf16_t* p, int rows, int k0, int k1,
+                                                          int c0) const {
+    return along(p + (size_t)c0 * rows, 256, rows, k0, k1, 0);
+  }
+  // a K-contiguous operand of ld elements a row, `valid` rows from p on, nk slices
+  // from slice k0 on; panel: bytes from one panel of 256 to the next, or 0
+  __device__ __forceinline__ BigOperand<false> across(const bf16_t* p, int ld, int valid, int k0,
+                                                      int nk, uint32_t panel) const {
+    BigOperand<false> o;
+    o.p = reinterpret_cast<const char*>(p);
+    o.left = nk;
+    o.panel = panel ? panel - 512 : 0;
+    o.ko = panel ? (uint32_t)(k0 >> 2) * panel + (uint32_t)(k0 & 3) * big::RB
+                 : (uint32_t)k0 * big::RB;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      o.off[u] = ((uint32_t)min(r0 + big::RPP * u, valid - 1) * ld + cc) * 2;
+    return o;
   }
 };
-
-// an operand of `rows` rows along K from row k0 and column c0, or panel c0 / 256
-// of one in panels
-__device__ __forceinline__ BigLong big_long(const bf16_t* p, int ld, int rows, int k0, int c0) {
-  const long long o = ((long long)k0 * ld + c0) * 2;
-  return BigLong{reinterpret_cast<const char*>(p) + o, (long long)rows * ld * 2 - o,
-                 (long long)ld * 128};
-}
-__device__ __forceinline__ BigLong big_panel(const bf16_t* p, int rows, int k0, int c0) {
-  return big_long(p + (size_t)c0 * rows, 256, rows, k0, 0);
-}
 
 __device__ __forceinline__ void big_zero(AccBig& acc) {
 #pragma unroll
@@ -375,24 +395,16 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
   L.rows(la, L.wm);
   L.rows(lb, L.wn);
   const int nk = a.d / BK;
-  const auto start = [&](BigRows& q, int jt, int& vt, int& tt) {
+  const auto start = [&](BigFeed<false, false>& q, int jt, int& vt, int& tt) {
     int sp;
     S.decode(jt, vt, tt, sp);
     const int c0 = vt * big::BM, t0 = tt * big::BN;
-    const int v_valid = min(big::BM, a.nv - c0), t_valid = min(big::BN, a.T - t0);
-    q.ra = buf_rsrc(a.w + (size_t)c0 * a.d);
-    q.rb0 = q.rb1 = buf_rsrc(a.h + (size_t)t0 * a.d);
-    q.none = buf_rsrc_empty(a.w);
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int r = L.r0 + big::RPP * u;
-      q.off[u] = ((uint32_t)min(r, v_valid - 1) * a.d + L.cc) * 2;
-      q.off[8 + u] = ((uint32_t)min(r, t_valid - 1) * a.d + L.cc) * 2;
-    }
-    big_start<false>(lds, q, nk);
+    q.a = L.across(a.w + (size_t)c0 * a.d, a.d, min(big::BM, a.nv - c0), 0, nk, 0);
+    q.b = L.across(a.h + (size_t)t0 * a.d, a.d, min(big::BN, a.T - t0), 0, nk, 0);
+    big_start(lds, q);
   };
   AccBig acc;
-  BigRows q;
+  BigFeed<false, false> q;
   int vt, tt;
   start(q, 0, vt, tt);
   for (int jt = 0; jt < ntiles; ++jt) {
@@ -401,7 +413,7 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
       big_wait<0>();
     else
       big_wait<32>();  // (every wavefront issues the epilogue's 32 stores)
-    big_run<false, true>(lds, q, nk, acc, la, lb);
+    big_run(lds, q, nk, acc, la, lb);
     const int c0 = vt * big::BM, t0 = tt * big::BN, tile = tt;
     const int v_valid = min(big::BM, a.nv - c0), t_valid = min(big::BN, a.T - t0);
     const int c = L.lane & 15, rl = L.wm * 128 + 4 * (L.lane >> 4);  // the lane's first row
@@ -519,35 +531,27 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
   struct At {
     int m0, n0, sp, nk;
   };
-  const auto start = [&](BigRowsT<DW>& q, int jt, At& t) {
+  const auto start = [&](BigFeed<true, DW>& q, int jt, At& t) {
     int nt, mt, sp;
     S.decode(jt, nt, mt, sp);
-    const int m0 = mt * big::BM, n0 = nt * big::BN, n_valid = min(big::BN, a.N - n0);
+    const int m0 = mt * big::BM, n0 = nt * big::BN;
     const int ka = (int)((long)sp * nk / a.splits), kb = (int)((long)(sp + 1) * nk / a.splits);
     t = At{m0, n0, sp, kb - ka};
-    q.none = buf_rsrc_empty(a.A);
     if constexpr (DW) {
-      q.la = big_panel(a.A, a.K, ka * BK, m0);
-      q.lb = big_panel(a.B, a.K, ka * BK, n0);
+      q.a = L.along_panel(a.A, a.K, ka * BK, kb * BK, m0);
+      q.b = L.along_panel(a.B, a.K, ka * BK, kb * BK, n0);
     } else {
-      q.la = big_long(a.A, a.M, a.K, ka * BK, m0);
-      q.rb0 = buf_rsrc(a.B + (size_t)n0 * 256);
-      q.panel = (uint32_t)a.N * 512;
-      q.k0 = ka;
+      q.a = L.along(a.A, a.M, a.K, ka * BK, kb * BK, m0);
+      q.b = L.across(a.B + (size_t)n0 * 256, 256, min(big::BN, a.N - n0), ka, kb - ka,
+                     (uint32_t)a.N * 512);
     }
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      q.off[u] = L.fetch(u, DW ? 256 : a.M);
-      q.off[8 + u] = DW ? L.fetch(u, 256)
-                        : ((uint32_t)min(L.r0 + big::RPP * u, n_valid - 1) * 256 + L.cc) * 2;
-    }
-    big_start<false>(lds, q, t.nk);
+    big_start(lds, q);
   };
   constexpr int ES = DW ? 2 : 4, STORES = DW ? 32 : 64;
   const float g = DW ? *a.scale : 0.f;
   const int c = L.lane & 15;
   AccBig acc;
-  BigRowsT<DW> q;
+  BigFeed<true, DW> q;
   At at;
   start(q, 0, at);
   for (int jt = 0; jt < ntiles; ++jt) {
@@ -571,7 +575,7 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
       big_wait<0>();
     else
       big_wait<STORES>();  // (every wavefront issues all of the epilogue's stores)
-    big_run<false, true>(lds, q, at.nk, acc, la, lb);
+    big_run(lds, q, at.nk, acc, la, lb);
     sched_fence();
     if (jt + 1 < ntiles) start(q, jt + 1, at);
     int M = a.M;
@@ -922,15 +926,17 @@ struct BackPlanBf16 {
   size_t o_rows, o_hw, o_d, o_dh, o_db, total;
 };
 
-// K splits of an m x n product of nk slices on the large-group core: the fewest
-// slices on the busiest CU, a doubling of the partials for no less than an eighth
+// K splits of the m x n product dh of nk slices on the large-group core: the fewest
+// slices on the busiest CU, a tile's start and end counted as 8 of them, plus the
+// sum's read of the partials at 5.5 TB/s (a slice takes about 1.5 us)
 int big_splits(int m, int n, int nk) {
   const long tiles = (long)cdiv(m, big::BM) * cdiv(n, big::BN);
+  const double read = (double)m * n * 4 / 8.25e6;
   int best = 1;
-  long cost = (tiles + kCu - 1) / kCu * nk;
-  for (int s = 2; s <= 32 && nk / s >= 16; s *= 2) {
-    const long c = (tiles * s + kCu - 1) / kCu * cdiv(nk, s);
-    if (8 * c <= 7 * cost) {
+  double cost = 0;
+  for (int s = 1; s <= 32 && (s == 1 || nk / s >= 8); ++s) {
+    const double c = (double)((tiles * s + kCu - 1) / kCu) * (cdiv(nk, s) + 8) + s * read;
+    if (s == 1 || c < cost) {
       best = s;
       cost = c;
     }

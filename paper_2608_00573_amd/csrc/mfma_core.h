@@ -616,55 +616,85 @@ struct BigSrc {
   }
 };
 
-// An operand that lies row by row along K is fetched 64 rows a slice: the
-// buffer starts at the slice's first row (so its offsets stay within one slice)
-// and ends with the operand, whose missing rows land as zeros.  Thread offsets:
-// row 2 w + 8 u + l / 32, 16-byte chunk l % 32 of the swizzled LDS row.
-struct BigLong {
-  const char* p;      // row 0 of the tile's K range, column 0 of the tile
-  long long bytes;    // from there to the operand's end
-  long long slice;    // 64 rows
-  __device__ __forceinline__ __amdgpu_buffer_rsrc_t at(int kt, int nk) const {
-    const long long o = kt * slice, left = bytes - o;
-    const bool live = kt < nk && left > 0;
-    const int n = live ? (int)(unsigned)(left < 0xffffffffll ? left : 0xffffffffll) : 0;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p) + (live ? o : 0), (short)0, n,
-                                             0x00020000);
+// The operands of a tile as the head loss's products use the core: each
+// K-contiguous, its K in one run or in panels of 256 (4 slices), or row by row
+// along K (TR: fetched 64 rows a slice, read transposed; the buffer starts at the
+// slice's first row, so its offsets stay within one slice, and ends with the
+// operand, whose missing rows land as zeros).  The sources of the slice two ahead
+// are made ready between the MFMAs of the slice before it, in a few scalar steps
+// (a wavefront alone on its SIMD leaves the matrix pipe idle for every other
+// instruction that it issues in a row).
+template <bool TR>
+struct BigOperand {
+  const char* p;    // TR: the slice's first row; else the operand's first row at K = 0
+  uint32_t off[8];  // of the thread's fetches
+  int left;         // TR: rows from the slice on; else slices
+  uint32_t row;     // TR: bytes of a row
+  uint32_t cut;     // TR: bytes of a row before the tile's columns
+  uint32_t ko;      // not TR: K offset of the slice
+  uint32_t panel;   // not TR: bytes from the end of a panel's row to the next panel's
+  uint32_t bytes;   // the buffer's
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc() const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, (int)bytes, 0x00020000);
+  }
+  __device__ __forceinline__ void limit() {
+    if constexpr (TR) {
+      const int n = min(left, 64);
+      bytes = n > 0 ? (uint32_t)n * row - cut : 0;
+    } else {
+      // (the compiler selects all ones or zero in a vector register, which would turn
+      // every fetch into a loop over lanes)
+      bytes = __builtin_amdgcn_readfirstlane(left > 0 ? 0xffffffffu : 0);
+    }
+  }
+  // to the next slice, in two steps
+  __device__ __forceinline__ void step() {
+    if constexpr (TR) {
+      p += (size_t)row * 64;
+      left -= 64;
+    } else {
+      left -= 1;
+      ko += big::RB;
+      ko += ko & 511 ? 0 : panel;
+    }
   }
 };
-// A such an operand, B one too (BTR) or K-contiguous in panels of 256 columns
-// (K), `panel` bytes each, from slice k0
-template <bool BTR_>
-struct BigRowsT {
-  static constexpr bool ATR = true, BTR = BTR_;
-  __amdgpu_buffer_rsrc_t rb0, none;  // B, unless BTR
-  BigLong la, lb;
-  uint32_t panel;
-  int k0;
-  uint32_t off[16];
-};
-template <bool BTR>
-struct BigSrcT {
-  __amdgpu_buffer_rsrc_t ra, rb0;
-  uint32_t ko;
-  __device__ __forceinline__ BigSrcT(const BigRowsT<BTR>& q, int kt, int nk) {
-    const bool live = kt < nk;
-    ra = q.la.at(kt, nk);
-    if constexpr (BTR)
-      rb0 = q.lb.at(kt, nk);
-    else
-      rb0 = live ? q.rb0 : q.none;
-    const int k = q.k0 + kt;
-    ko = live && !BTR ? (uint32_t)(k >> 2) * q.panel + (uint32_t)(k & 3) * big::RB : 0;
+template <bool ATR_, bool BTR_>
+struct BigFeed {
+  static constexpr bool ATR = ATR_, BTR = BTR_;
+  BigOperand<ATR> a;  // two slices ahead of the one computed; a1: one ahead
+  BigOperand<BTR> b;
+  __amdgpu_buffer_rsrc_t a1, a2, b2;
+  uint32_t k1, k2, kb;
+  __device__ __forceinline__ void take_a() {
+    a2 = a.rsrc();
+    k2 = ATR ? 0 : a.ko;
   }
-};
-template <class R>
-struct BigSrcOf {
-  using type = BigSrcT<R::BTR>;
-};
-template <>
-struct BigSrcOf<BigRows> {
-  using type = BigSrc;
+  __device__ __forceinline__ void take_b() {
+    b2 = b.rsrc();
+    kb = BTR ? 0 : b.ko;
+  }
+  // what slot T of a slice's first k-step does for the next ones
+  template <int T>
+  __device__ __forceinline__ void slot() {
+    if constexpr (T == 8) {
+      a1 = a2;
+      k1 = k2;
+    } else if constexpr (T == 9) {
+      a.step();
+    } else if constexpr (T == 10) {
+      a.limit();
+    } else if constexpr (T == 11) {
+      take_a();
+    } else if constexpr (T == 12) {
+      b.step();
+    } else if constexpr (T == 13) {
+      b.limit();
+    } else if constexpr (T == 14) {
+      take_b();
+    }
+    if constexpr (T >= 8 && T <= 14) sched_fence();
+  }
 };
 
 // Row group u (0..7) of the wave straight into an LDS stage: lane l lands at
@@ -684,8 +714,13 @@ __device__ __forceinline__ void big_dma(uint32_t bst, int wave, const R& q, cons
 }
 template <class R, class Src>
 __device__ __forceinline__ void big_dma_a(uint32_t ast, int wave, const R& q, const Src& b, int u) {
-  big_dma_group(ast, wave, b.ra, q.off[u], R::ATR ? 0 : b.ko, u);
+  big_dma_group(ast, wave, b.ra, q.off[u], b.ko, u);
 }
+
+struct BigNoFeed {
+  template <int T>
+  __device__ __forceinline__ void slot() {}
+};
 
 // MFMA slot T of a k-step (LAST: the second of the slice) from fragments fa,
 // fb, with the next k-step's reads into fa (rotating) and fn: the wait, the
@@ -697,9 +732,10 @@ __device__ __forceinline__ void big_dma_a(uint32_t ast, int wave, const R& q, co
 // in the first, 4..7 in the last).  The barrier waits for the next slice's
 // A DMAs (the last issued at MFMA 28 of the first k-step, followed by 4 B
 // DMAs) and its B DMAs (issued a slice earlier).
-template <int T, bool LAST, bool DUAL, class R, class DmaA, class DmaB>
+template <int T, bool LAST, bool DUAL, class R, class DmaA, class DmaB, class Feed>
 __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig& acc,
-                                         uint32_t pa, uint32_t pb, DmaA& dma_a, DmaB& dma_b) {
+                                         uint32_t pa, uint32_t pb, DmaA& dma_a, DmaB& dma_b,
+                                         Feed& feed) {
   constexpr int i = T / 8, j = T % 8;
   constexpr int w = big_waits(R::ATR, R::BTR).w[LAST ? 1 : 0][T];
   if constexpr (w >= 0) {
@@ -721,6 +757,7 @@ __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig
   big_read<DUAL, R::ATR, R::BTR, LAST ? kRead1[T] : kRead0[T]>(fa, fn, pa, pb);
   // the first k-step's a_0 for the next k-step, after its last use
   if constexpr (!LAST && T == 7) big_read<DUAL, R::ATR, R::BTR, 0>(fa, fn, pa, pb);
+  if constexpr (!LAST) feed.template slot<T>();
   if constexpr (!LAST && (T == 16 || T == 20 || T == 24 || T == 28)) {
     dma_a(4 + (T - 16) / 4);
     sched_fence();
@@ -733,7 +770,7 @@ __device__ __forceinline__ void big_slot(FragA& fa, FragB& fb, FragB& fn, AccBig
     dma_b((LAST ? 4 : 0) + (T == 18 ? 0 : T == 26 ? 1 : T == 50 ? 2 : 3));
     sched_fence();
   }
-  if constexpr (T < 63) big_slot<T + 1, LAST, DUAL, R>(fa, fb, fn, acc, pa, pb, dma_a, dma_b);
+  if constexpr (T < 63) big_slot<T + 1, LAST, DUAL, R>(fa, fb, fn, acc, pa, pb, dma_a, dma_b, feed);
 }
 
 // LDS of the large-group core: A stages at s0 and s0 + AB (slice parity), B
@@ -752,12 +789,40 @@ __device__ __forceinline__ void big_half(const BigLds& L, int g, int wave, const
                                          const uint32_t (&b_lane)[2], FragA& fa, FragB& fb0,
                                          FragB& fb1) {
   const uint32_t ca = L.a(g), cb = L.b(g), na = L.a(g + 1), nb = L.b(g + 1), db = L.b(g + 2);
-  const typename BigSrcOf<R>::type sa(q, g + 1, nk), sb(q, g + 2, nk);
+  const BigSrc sa(q, g + 1, nk), sb(q, g + 2, nk);
   auto dma_a = [&](int u) { big_dma_a(na, wave, q, sa, u); };
   auto dma_a2 = [&](int u) { big_dma_a(ca, wave, q, sb, u); };
   auto dma_b = [&](int u) { big_dma<DUAL>(db, wave, q, sb, u); };
-  big_slot<0, false, DUAL, R>(fa, fb0, fb1, acc, ca + a_lane[1], cb + b_lane[1], dma_a, dma_b);
-  big_slot<0, true, DUAL, R>(fa, fb1, fb0, acc, na + a_lane[0], nb + b_lane[0], dma_a2, dma_b);
+  BigNoFeed none;
+  big_slot<0, false, DUAL, R>(fa, fb0, fb1, acc, ca + a_lane[1], cb + b_lane[1], dma_a, dma_b, none);
+  big_slot<0, true, DUAL, R>(fa, fb1, fb0, acc, na + a_lane[0], nb + b_lane[0], dma_a2, dma_b, none);
+}
+
+// The same for a feed: stages of the slices (c: this one, n: the next, d: B of the
+// one after) instead of their number
+struct BigStages {
+  uint32_t ca, na, cb, nb, db;
+  __device__ __forceinline__ explicit BigStages(const BigLds& L)
+      : ca(L.a(0)), na(L.a(1)), cb(L.b(0)), nb(L.b(1)), db(L.b(2)) {}
+  __device__ __forceinline__ void next() {
+    uint32_t t = ca;
+    ca = na;
+    na = t;
+    t = cb;
+    cb = nb;
+    nb = db;
+    db = t;
+  }
+};
+template <class F>
+__device__ __forceinline__ void big_slice(const BigStages& L, int wave, F& q, AccBig& acc,
+                                          const uint32_t (&a_lane)[2], const uint32_t (&b_lane)[2],
+                                          FragA& fa, FragB& fb0, FragB& fb1) {
+  auto dma_a = [&](int u) { big_dma_group(L.na, wave, q.a1, q.a.off[u], q.k1, u); };
+  auto dma_a2 = [&](int u) { big_dma_group(L.ca, wave, q.a2, q.a.off[u], q.k2, u); };
+  auto dma_b = [&](int u) { big_dma_group(L.db, wave, q.b2, q.b.off[u], q.kb, u); };
+  big_slot<0, false, false, F>(fa, fb0, fb1, acc, L.ca + a_lane[1], L.cb + b_lane[1], dma_a, dma_b, q);
+  big_slot<0, true, false, F>(fa, fb1, fb0, acc, L.na + a_lane[0], L.nb + b_lane[0], dma_a2, dma_b, q);
 }
 
 // A tile's first loads: slice 0, B of slice 1 and the first half of its A.  LDS is
@@ -766,7 +831,7 @@ template <bool DUAL, class R>
 __device__ __forceinline__ void big_start(char* lds, const R& q, int nk) {
   const BigLds L{lds_addr(lds)};
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const typename BigSrcOf<R>::type s0(q, 0, nk), s1(q, 1, nk);
+  const BigSrc s0(q, 0, nk), s1(q, 1, nk);
 #pragma unroll
   for (int u = 0; u < 8; ++u) {
     big_dma_a(L.a(0), wave, q, s0, u);
@@ -789,22 +854,10 @@ __device__ __forceinline__ void big_start(char* lds, const R& q, int nk) {
   }
 }
 
-// C tile += A rows x B rows over nk slices from the rows' K origin, after
-// big_start and its wait; returns with every load landed and every wave past its
-// last LDS access
-// (SETTLE: the last row's wait states come inside the loop, after its last slice,
-// for kernels in which the compiler copies accumulators on the way out of it).
-template <bool DUAL, bool SETTLE = false, class R>
-__device__ __forceinline__ void big_run(char* lds, const R& q, int nk, AccBig& acc,
-                                        const uint32_t (&a_lane)[2],
-                                        const uint32_t (&b_lane)[2]) {
-  const BigLds L{lds_addr(lds)};
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // the first k-step's fragments, in the order the last k-step of a slice
-  // reads them (the first k-step's waits count on it)
-  FragA fa;
-  FragB fb0, fb1;
-  const uint32_t pa = L.a(0) + a_lane[0], pb = L.b(0) + b_lane[0];
+// the first k-step's fragments, in the order the last k-step of a slice
+// reads them (the first k-step's waits count on it)
+template <bool DUAL, class R>
+__device__ __forceinline__ void big_first_reads(FragA& fa, FragB& fb0, uint32_t pa, uint32_t pb) {
   big_read<DUAL, R::ATR, R::BTR, 0>(fa, fb0, pa, pb);
   big_read<DUAL, R::ATR, R::BTR, 1>(fa, fb0, pa, pb);
   big_read<DUAL, R::ATR, R::BTR, 2>(fa, fb0, pa, pb);
@@ -821,13 +874,10 @@ __device__ __forceinline__ void big_run(char* lds, const R& q, int nk, AccBig& a
   big_read<DUAL, R::ATR, R::BTR, 10>(fa, fb0, pa, pb);
   big_read<DUAL, R::ATR, R::BTR, 12>(fa, fb0, pa, pb);
   big_read<DUAL, R::ATR, R::BTR, 14>(fa, fb0, pa, pb);
-  for (int g = 0; g < nk; ++g) {
-    big_half<DUAL, R>(L, g, wave, q, nk, acc, a_lane, b_lane, fa, fb0, fb1);
-    if (SETTLE && g + 1 == nk)
-      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 3"
-                   : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]),
-                     "+a"(acc[7][4]), "+a"(acc[7][5]), "+a"(acc[7][6]), "+a"(acc[7][7]));
-  }
+}
+
+// what follows the last slice
+__device__ __forceinline__ void big_close(FragA& fa, FragB& fb0, AccBig& acc) {
   // The last k-step read the first fragments of the slice past the end
   // (never used).  Those reads land whenever the LDS returns them, which the
   // compiler cannot see: the wait for them takes their registers as inputs,
@@ -851,6 +901,81 @@ __device__ __forceinline__ void big_run(char* lds, const R& q, int nk, AccBig& a
                  "+a"(acc[7][4]), "+a"(acc[7][5]), "+a"(acc[7][6]), "+a"(acc[7][7])
                :
                : "memory");
+}
+
+// C tile += A rows x B rows over nk slices from the rows' K origin, after
+// big_start and its wait; returns with every load landed and every wave past its
+// last LDS access
+template <bool DUAL, class R>
+__device__ __forceinline__ void big_run(char* lds, const R& q, int nk, AccBig& acc,
+                                        const uint32_t (&a_lane)[2],
+                                        const uint32_t (&b_lane)[2]) {
+  const BigLds L{lds_addr(lds)};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  FragA fa;
+  FragB fb0, fb1;
+  big_first_reads<DUAL, R>(fa, fb0, L.a(0) + a_lane[0], L.b(0) + b_lane[0]);
+  for (int g = 0; g < nk; ++g)
+    big_half<DUAL, R>(L, g, wave, q, nk, acc, a_lane, b_lane, fa, fb0, fb1);
+  big_close(fa, fb0, acc);
+}
+
+// the same on a feed, whose operands end after nk slices
+template <bool ATR, bool BTR>
+__device__ __forceinline__ void big_start(char* lds, BigFeed<ATR, BTR>& q) {
+  const BigLds L{lds_addr(lds)};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const auto take = [&] {
+    q.a.limit();
+    q.b.limit();
+    q.take_a();
+    q.take_b();
+  };
+  take();
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma_group(L.a(0), wave, q.a2, q.a.off[u], q.k2, u);
+    sched_fence();
+  }
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma_group(L.b(0), wave, q.b2, q.b.off[u], q.kb, u);
+    sched_fence();
+  }
+  q.a.step();
+  q.b.step();
+  take();
+#pragma unroll
+  for (int u = 0; u < 8; ++u) {
+    big_dma_group(L.b(1), wave, q.b2, q.b.off[u], q.kb, u);
+    sched_fence();
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    big_dma_group(L.a(1), wave, q.a2, q.a.off[u], q.k2, u);
+    sched_fence();
+  }
+}
+// (the last row's wait states come inside the loop, after its last slice: the
+// compiler copies accumulators on the way out of it)
+template <bool ATR, bool BTR>
+__device__ __forceinline__ void big_run(char* lds, BigFeed<ATR, BTR>& q, int nk, AccBig& acc,
+                                        const uint32_t (&a_lane)[2],
+                                        const uint32_t (&b_lane)[2]) {
+  BigStages L{BigLds{lds_addr(lds)}};
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  FragA fa;
+  FragB fb0, fb1;
+  big_first_reads<false, BigFeed<ATR, BTR>>(fa, fb0, L.ca + a_lane[0], L.cb + b_lane[0]);
+  for (int g = 0; g < nk; ++g) {
+    big_slice(L, wave, q, acc, a_lane, b_lane, fa, fb0, fb1);
+    L.next();
+    if (g + 1 == nk)
+      asm volatile("s_nop 7\n\ts_nop 7\n\ts_nop 3"
+                   : "+a"(acc[7][0]), "+a"(acc[7][1]), "+a"(acc[7][2]), "+a"(acc[7][3]),
+                     "+a"(acc[7][4]), "+a"(acc[7][5]), "+a"(acc[7][6]), "+a"(acc[7][7]));
+  }
+  big_close(fa, fb0, acc);
 }
 
 // The wait between big_start and big_run: A and B of slice 0 have landed (12 newer

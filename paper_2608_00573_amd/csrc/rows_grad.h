@@ -103,11 +103,9 @@ __device__ __forceinline__ void rows_grad(char* lds, const P& p, const bf16_t* x
         xz[u] = *reinterpret_cast<const u32x4_t*>(z + (size_t)tile * kRowTile * (G::ZB / 2) + 8 * i);
     }
   };
-  // from the last tile back: what the caller read last is still in the last-level
-  // cache
-  int tile = n_t - 1 - (int)blockIdx.y;
-  if (tile >= 0) load(tile);
-  for (; tile >= 0; tile -= gridDim.y) {
+  int tile = blockIdx.y;
+  if (tile < n_t) load(tile);
+  for (; tile < n_t; tile += gridDim.y) {
     __syncthreads();  // the last tile is read
 #pragma unroll
     for (int u = 0; u < G::HL; ++u) {
@@ -122,7 +120,7 @@ __device__ __forceinline__ void rows_grad(char* lds, const P& p, const bf16_t* x
         *reinterpret_cast<u32x4_t*>(s_z + r * G::ZR + 16 * ch) = xz[u];
     }
     __syncthreads();
-    if (tile >= (int)gridDim.y) load(tile - gridDim.y);
+    if (tile + (int)gridDim.y < n_t) load(tile + gridDim.y);
     // z^T x: two k-steps of 32 rows
     if (part || whole) {
 #pragma unroll
