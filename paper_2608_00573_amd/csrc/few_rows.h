@@ -21,6 +21,13 @@ __device__ __forceinline__ float row16_sum(float v) {
   return row_add<0x121>(row_add<0x122>(row_add<0x124>(row_add<0x128>(v))));
 }
 
+// exp(z - lse) of a lane's logit.  The difference is taken first: it is small where the
+// probability is not, and its rounding with it (z log2 e - lse log2 e would carry the
+// rounding of lse log2 e, some 2^-20, into every term of a row).
+__device__ __forceinline__ float softmax_of(float z, float lse) {
+  return __builtin_amdgcn_exp2f((z - lse) * kLog2e);
+}
+
 // m, 2^-e and g / m of a weight g
 __device__ __forceinline__ void row_weight(float g, float G, float& m, float& e, float& gm) {
   int x = 0;
@@ -31,19 +38,19 @@ __device__ __forceinline__ void row_weight(float g, float G, float& m, float& e,
 }
 
 // A row's part in the backward, by the lanes of a wavefront (t: the lane's row):
-// its target, or -1 where it takes no part; lse log2 e; m, 2^-e and g / m of its
+// its target, or -1 where it takes no part; lse; m, 2^-e and g / m of its
 // weight, and the largest |g| of all rows
 struct FewRow {
   int y;
-  float l2, m, e, gm, G;
-  __device__ __forceinline__ FewRow(const int32_t* target, const float* lse, const float* dloss,
+  float lse, m, e, gm, G;
+  __device__ __forceinline__ FewRow(const int32_t* target, const float* lses, const float* dloss,
                                     int V, int T, int t) {
     const bool in = t < T;
-    const float L = in ? lse[t] : 0.f;
+    const float L = in ? lses[t] : 0.f;
     y = in ? target[t] : -1;
     const bool live = y >= 0 && y < V && L != -__builtin_inff();
     if (!live) y = -1;
-    l2 = live ? L * kLog2e : 0.f;
+    lse = live ? L : 0.f;
     const float g = live ? dloss[t] : 0.f;
     G = fabsf(g);
 #pragma unroll

@@ -26,60 +26,65 @@ namespace trimmoe {
 namespace {
 
 // ------------------------------------------------------- forward, fp32 --
-// A = w (vocabulary rows), B = h: a lane holds 4 kTM vocabulary rows of a token
-// column, so the pair of a column is a reduction over registers, two lane
-// exchanges and the two wavefronts of the column.  A NaN logit makes the sum NaN.
-template <typename T>
-__global__ __launch_bounds__(f32p::THREADS) void k_loss_f32(Operand<T, true> W, Operand<T, true> H,
-                                                            const float* bias, int n_vt,
-                                                            float2* part) {
-  using namespace f32p;
-  __shared__ __align__(16) float lds[4 * KS * LS];
-  __shared__ float2 s_p[2][BN];
+// A = w (vocabulary rows), B = h: a lane holds 16 vocabulary rows of a token, so the
+// pair of a token is a reduction over registers, two lane exchanges and the
+// wavefronts along the vocabulary.  A NaN logit makes the sum NaN.
+template <int KIND>
+__global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_loss_f32(
+    Operand<true> W, Operand<true> H, const float* bias, int n_vt, float2* part) {
+  using T = f32p::Tile<KIND>;
+  __shared__ __align__(16) float lds[T::FLOATS];
+  __shared__ float2 s_p[T::WA][T::B];
   const int vt = blockIdx.x, tt = blockIdx.y;
-  const int v0 = vt * BM, t0 = tt * BN;
-  F32Acc acc;
-  f32_tile(W, H, v0, t0, 0, W.K, lds, acc);
+  const int v0 = vt * T::A, t0 = tt * T::B;
+  F32Tile<KIND> t(v0, W.rows, t0, H.rows);
+  f32_product<KIND>(W, H, v0, t0, 0, W.K, lds, t);
   const float ninf = -__builtin_inff();
 #pragma unroll
-  for (int j = 0; j < kTN; ++j) {
+  for (int j = 0; j < T::NB; ++j) {
+    if (j >= t.nb) continue;
     float m = ninf;
 #pragma unroll
-    for (int i = 0; i < kTM; ++i)
+    for (int i = 0; i < T::NA; ++i)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const int v = v0 + f32_row(i, r);
-        float z = acc[i][j][r];
+        const int v = t.row_a(i, r);
+        float z = t.acc[i][j][r];
         if (bias) z += bias[min(v, W.rows - 1)];
-        z = v < W.rows ? z : ninf;
-        acc[i][j][r] = z;
+        z = i < t.na && v < W.rows ? z : ninf;
+        t.acc[i][j][r] = z;
         m = fmaxf(m, z);
       }
     m = fmaxf(m, __shfl_xor(m, 16));
     m = fmaxf(m, __shfl_xor(m, 32));
     const float ms = m == ninf ? 0.f : m;
     // (in a tree: a chain would round each small term at the size of the largest)
-    float e[4 * kTM];
+    float e[4 * T::NA];
 #pragma unroll
-    for (int i = 0; i < kTM; ++i)
+    for (int i = 0; i < T::NA; ++i)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) e[4 * i + r] = expf(acc[i][j][r] - ms);
+      for (int r = 0; r < 4; ++r) e[4 * i + r] = expf(t.acc[i][j][r] - ms);
 #pragma unroll
-    for (int n = 2 * kTM; n > 0; n >>= 1)
+    for (int n = 2 * T::NA; n > 0; n >>= 1)
 #pragma unroll
       for (int r = 0; r < n; ++r) e[r] += e[r + n];
     float sum = e[0];
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if ((threadIdx.x & 63) < 16) s_p[threadIdx.x >> 7][f32_col(j)] = make_float2(m, sum);
+    if ((threadIdx.x & 63) < 16)
+      s_p[(threadIdx.x >> 6) % T::WA][t.row_b(j) - t0] = make_float2(m, sum);
   }
   __syncthreads();
   const int c = threadIdx.x;
-  if (c < BN && t0 + c < H.rows) {
-    const float2 p0 = s_p[0][c], p1 = s_p[1][c];
-    const float M = fmaxf(p0.x, p1.x), Ms = M == ninf ? 0.f : M;
-    part[(size_t)(t0 + c) * n_vt + vt] =
-        make_float2(M, p0.y * expf(p0.x - Ms) + p1.y * expf(p1.x - Ms));
+  if (c < T::B && t0 + c < H.rows) {
+    float M = s_p[0][c].x;
+#pragma unroll
+    for (int i = 1; i < T::WA; ++i) M = fmaxf(M, s_p[i][c].x);
+    const float Ms = M == ninf ? 0.f : M;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < T::WA; ++i) sum += s_p[i][c].y * expf(s_p[i][c].x - Ms);
+    part[(size_t)(t0 + c) * n_vt + vt] = make_float2(M, sum);
   }
 }
 
@@ -139,70 +144,74 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt,
 }
 
 // ------------------------------------------------------ backward, fp32 --
-// D of the tokens x a piece's columns (v0 ..), and per token tile the column
-// sums of D (db); columns past the piece up to its leading dimension are zero
-template <typename T>
-__global__ __launch_bounds__(f32p::THREADS) void k_dz_f32(Operand<T, true> H, Operand<T, true> W,
-                                                          const float* bias, const int32_t* target,
-                                                          const float* lse, const float* dloss, int V,
-                                                          int v0, float* D, size_t ldd,
-                                                          float* db_part) {
-  using namespace f32p;
-  __shared__ __align__(16) float lds[4 * KS * LS];
-  const int vt = blockIdx.x, tt = blockIdx.y;
-  const int c0 = vt * BN, t0 = tt * BM;
-  F32Acc acc;
-  f32_tile(H, W, t0, c0, 0, H.K, lds, acc);
-  float* s_sum = lds;  // [2][BN]; the tile ended on a barrier
+// D of the tokens x a piece's columns (v0 ..; a row's elements behind the piece hold
+// anything), and per token tile the column sums of D (db).  A = w: a lane holds NA x 4
+// consecutive columns of a token.
+template <int KIND>
+__global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_dz_f32(
+    Operand<true> W, Operand<true> H, const float* bias, const int32_t* target, const float* lse,
+    const float* dloss, int V, int v0, float* D, size_t ldd, float* db_part) {
+  using T = f32p::Tile<KIND>;
+  __shared__ __align__(16) float lds[T::FLOATS];
+  const int c0 = blockIdx.x * T::A, tt = blockIdx.y, t0 = tt * T::B;
+  F32Tile<KIND> tile(c0, W.rows, t0, H.rows);
+  f32_product<KIND>(W, H, c0, t0, 0, H.K, lds, tile);
+  float* s_sum = lds;  // [T::WB][T::A]; the tile ended on a barrier
   // the lane's rows first: behind a store the compiler would wait for each
-  int ty[kTM][4];
-  float tl[kTM][4], tg[kTM][4];
+  int ty[T::NB];
+  float tl[T::NB], tg[T::NB];
 #pragma unroll
-  for (int i = 0; i < kTM; ++i)
+  for (int j = 0; j < T::NB; ++j) {
+    const int t = min(tile.row_b(j), H.rows - 1), y = target[t];
+    tl[j] = lse[t];
+    const bool live = y >= 0 && y < V && tl[j] != -__builtin_inff();
+    ty[j] = live && tile.row_b(j) < H.rows ? y - v0 : INT32_MIN;
+    tg[j] = dloss[t];
+  }
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int t = min(t0 + f32_row(i, r), H.rows - 1);
-      ty[i][r] = target[t];
-      tl[i][r] = lse[t];
-      tg[i][r] = dloss[t];
+  for (int i = 0; i < T::NA; ++i) {
+    if (i >= tile.na) continue;
+    const int c = tile.row_a(i, 0);
+    f32x4_t bi = {}, sum = {};
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (bias) bi[r] = bias[min(c + r, W.rows - 1)];
+#pragma unroll
+    for (int j = 0; j < T::NB; ++j) {
+      if (j >= tile.nb) continue;
+      const int t = tile.row_b(j);
+      f32x4_t x;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        x[r] = ty[j] != INT32_MIN && c + r < W.rows
+                   ? tg[j] * (expf(tile.acc[i][j][r] + bi[r] - tl[j]) - (c + r == ty[j] ? 1.f : 0.f))
+                   : 0.f;
+      if (t < H.rows) *reinterpret_cast<f32x4_t*>(D + (size_t)t * ldd + c) = x;
+      sum += x;
     }
 #pragma unroll
-  for (int j = 0; j < kTN; ++j) {
-    const int c = c0 + f32_col(j);
-    const float bj = bias && c < W.rows ? bias[c] : 0.f;
-    float sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < kTM; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int t = t0 + f32_row(i, r), y = ty[i][r];
-        const float L = tl[i][r];
-        float x = 0.f;
-        if (t < H.rows) {
-          if (c < W.rows && y >= 0 && y < V && L != -__builtin_inff())
-            x = tg[i][r] * (expf(acc[i][j][r] + bj - L) - (v0 + c == y ? 1.f : 0.f));
-          D[(size_t)t * ldd + c] = x;
-        }
-        sum += x;
-      }
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if ((threadIdx.x & 63) < 16) s_sum[(threadIdx.x >> 7) * BN + f32_col(j)] = sum;
+    for (int r = 0; r < 4; ++r) {
+      const float s = row16_sum(sum[r]);
+      if ((threadIdx.x & 15) == 0) s_sum[(threadIdx.x >> 6) / T::WA * T::A + c + r - c0] = s;
+    }
   }
   __syncthreads();
-  if (db_part && threadIdx.x < BN)
-    db_part[(size_t)tt * ldd + c0 + threadIdx.x] = s_sum[threadIdx.x] + s_sum[BN + threadIdx.x];
+  if (db_part && threadIdx.x < T::A && c0 + (int)threadIdx.x < W.rows) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < T::WB; ++i) s += s_sum[i * T::A + threadIdx.x];
+    db_part[(size_t)tt * ldd + c0 + threadIdx.x] = s;
+  }
 }
 
 // rows that take part, zeros for the others: an ignored row's h may hold
 // anything, and 0 * NaN is NaN
-template <typename T>
-__global__ __launch_bounds__(256) void k_live_rows(const T* h, const int32_t* target,
-                                                   const float* lse, int V, int d, T* out) {
+__global__ __launch_bounds__(256) void k_live_rows(const float* h, const int32_t* target,
+                                                   const float* lse, int V, int d, float* out) {
   const size_t t = blockIdx.x;
   const int y = target[t];
   const bool live = y >= 0 && y < V && lse[t] != -__builtin_inff();
-  for (int k = threadIdx.x; k < d; k += 256) out[t * d + k] = live ? h[t * d + k] : T(0);
+  for (int k = threadIdx.x; k < d; k += 256) out[t * d + k] = live ? h[t * d + k] : 0.f;
 }
 
 __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, size_t ld, int n,
@@ -235,7 +244,7 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 // a row's part in the backward
 struct RowPart {
   int32_t* y;  // its target, or -1 where it takes no part
-  float* l2;   // lse log2 e
+  float* lse;  // its lse
   float* m;    // m, 2^-e (0 for a weight of 0) and g / m (0 where it takes no part)
   float* e;
   float* gm;
@@ -253,7 +262,7 @@ __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const 
     const float g = live ? dloss[t] : 0.f;
     p.y[t] = live ? y : -1;
     p.gm[t] = g;
-    p.l2[t] = live ? L * kLog2e : 0.f;
+    p.lse[t] = live ? L : 0.f;
     G = fmaxf(G, fabsf(g));
   }
 #pragma unroll
@@ -428,16 +437,16 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          b[i][r] = a.bias ? a.bias[c0 + min(rl + 16 * i + r, v_valid - 1)] * kLog2e : 0.f;
+          b[i][r] = a.bias ? a.bias[c0 + min(rl + 16 * i + r, v_valid - 1)] : 0.f;
           sum[i][r] = 0.f;
         }
     int ty[8];
-    float tl2[8], tm[8], te[BIAS ? 8 : 1];
+    float tL[8], tm[8], te[BIAS ? 8 : 1];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int t = min(t0 + L.wn * 128 + 16 * j + c, a.T - 1);
       ty[j] = a.rows.y[t];
-      tl2[j] = a.rows.l2[t];
+      tL[j] = a.rows.lse[t];
       tm[j] = a.rows.m[t];
       if constexpr (BIAS) te[j] = a.rows.e[t];
     }
@@ -448,7 +457,7 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const int tl = L.wn * 128 + 16 * j + c, y = ty[j];
-      const float l2 = tl2[j], m = tm[j], g = BIAS ? m * te[BIAS ? j : 0] : 0.f;
+      const float lse = tL[j], m = tm[j], g = BIAS ? m * te[BIAS ? j : 0] : 0.f;
       const bool live = y >= 0 && tl < t_valid;
       const int yr = y - a.v0 - c0 - rl;  // the target's row, relative to the lane's first
       const uint32_t off = ((uint32_t)tl * 256 + col) * 2;
@@ -461,8 +470,8 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
         for (int k = 0; k < 2; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const float s = BIAS ? b[i + k][r] - l2 : -l2;
-            x[k][r] = __builtin_amdgcn_exp2f(fmaf(acc[i + k][j][r], kLog2e, s));
+            const float z = acc[i + k][j][r];
+            x[k][r] = softmax_of(BIAS ? z + b[i + k][r] : z, lse);
           }
         if (!plain)
 #pragma unroll
@@ -665,7 +674,7 @@ struct FewSrc {
   const FewArgs& a;
   const TileSched& S;
   const int* s_y;
-  const float *s_l2, *s_m, *s_e;
+  const float *s_lse, *s_m, *s_e;
   float G;
 
   __device__ __forceinline__ Desc desc(int j) const {
@@ -694,7 +703,7 @@ struct FewSrc {
     for (int j = 0; j < T::TN; ++j) {
       const int t = acc_col<T>(0, j, lane);
       const int y = s_y[t];
-      const float l2 = s_l2[t], m = s_m[t], e = m * s_e[t];
+      const float lse = s_lse[t], m = s_m[t], e = m * s_e[t];
 #pragma unroll
       for (int i = 0; i < T::TM; ++i)
 #pragma unroll
@@ -702,7 +711,7 @@ struct FewSrc {
           const int v = v0 + acc_row<T>(wm, i, r, lane);
           float z = acc[i][j][r];
           if (a.b) z += a.b[min(v, a.V - 1)];
-          float p = __builtin_amdgcn_exp2f(fmaf(z, kLog2e, -l2));
+          float p = softmax_of(z, lse);
           p = v == y ? p - 1.f : p;
           p = y >= 0 && v < a.V ? p : 0.f;
           sum[i][r] = fmaf(e, p, sum[i][r]);
@@ -732,7 +741,7 @@ template <class T, int ET>
 __global__ __launch_bounds__(T::THREADS) void k_dz_few(FewArgs a) {
   __shared__ __align__(16) char lds[DmaTile<T>::LDS];
   __shared__ int s_y[64];
-  __shared__ float s_l2[64], s_m[64], s_e[64], s_G;
+  __shared__ float s_lse[64], s_m[64], s_e[64], s_G;
   TileSched S;
   int ntiles;
   if (!S.init((a.V + T::BM - 1) / T::BM, 1, 1, ntiles)) return;
@@ -740,13 +749,13 @@ __global__ __launch_bounds__(T::THREADS) void k_dz_few(FewArgs a) {
     const int t = threadIdx.x;
     const FewRow r(a.target, a.lse, a.dloss, a.V, a.T, t);
     s_y[t] = r.y;
-    s_l2[t] = r.l2;
+    s_lse[t] = r.lse;
     s_m[t] = r.m;
     s_e[t] = r.e;
     s_G = r.G;
   }
   __syncthreads();
-  const FewSrc<T, ET> src{a, S, s_y, s_l2, s_m, s_e, s_G};
+  const FewSrc<T, ET> src{a, S, s_y, s_lse, s_m, s_e, s_G};
   dma_gemm_stream<T>(lds, ntiles, a.d / BK, src);
 }
 
@@ -804,6 +813,7 @@ __global__ __launch_bounds__(256) void k_few_finish(FewArgs a, const float* part
 constexpr size_t kPieceBytes = (size_t)256 << 20;
 constexpr int kCu = 256;
 struct BackPlan {
+  int kind;        // of D's tiles (A = the vocabulary)
   int Vc;          // columns of a piece (a multiple of the tile)
   int s_dh, s_dw;  // K splits of the two products
   bool direct_dh;  // one piece, one split: dh needs no partials
@@ -813,12 +823,14 @@ struct BackPlan {
 BackPlan back_plan(int V, int d, int T) {
   BackPlan p;
   const size_t rows = T > 0 ? T : 1;
-  const size_t fit = kPieceBytes / (4 * rows) / f32p::BN * f32p::BN;
-  const int most = (int)std::min<size_t>(std::max<size_t>(fit, f32p::BN), (size_t)1 << 30);
+  p.kind = f32p::tile_kind(V, T);
+  const int BA = f32p::tile_a(p.kind), BB = f32p::tile_b(p.kind);
+  const size_t fit = kPieceBytes / (4 * rows) / BA * BA;
+  const int most = (int)std::min<size_t>(std::max<size_t>(fit, BA), (size_t)1 << 30);
   const int n_pieces = cdiv(V, most);
-  p.Vc = cdiv(cdiv(V, n_pieces), f32p::BN) * f32p::BN;
-  p.s_dh = product_splits(T, d, p.Vc);
-  p.s_dw = product_splits(p.Vc, d, T);
+  p.Vc = cdiv(cdiv(V, n_pieces), BA) * BA;
+  p.s_dh = product_splits(f32p::product_kind(false, true, d, T), d, T, p.Vc);
+  p.s_dw = product_splits(f32p::product_kind(false, false, d, p.Vc), d, p.Vc, T);
   p.direct_dh = n_pieces == 1 && p.s_dh == 1;
   size_t o = 0;
   const auto take = [&](size_t bytes) {
@@ -829,77 +841,73 @@ BackPlan back_plan(int V, int d, int T) {
   p.o_dh = take(p.direct_dh ? 0 : (size_t)p.s_dh * rows * d * 4);
   p.o_dw = take(p.s_dw == 1 ? 0 : (size_t)p.s_dw * p.Vc * d * 4);
   p.o_d = take(rows * p.Vc * 4);
-  p.o_db = take((size_t)cdiv(rows, f32p::BM) * p.Vc * 4);
+  p.o_db = take((size_t)cdiv((int)rows, BB) * p.Vc * 4);
   p.o_h = take(rows * d * 4);
   p.total = o;
   return p;
 }
 
-template <typename T>
 hipError_t loss_f32(const HeadLossArgs& a, hipStream_t st) {
   float2* part = reinterpret_cast<float2*>(a.ws);
-  const int n_vt = cdiv(a.V, f32p::BM);
-  hipLaunchKernelGGL(k_loss_f32<T>, dim3(n_vt, cdiv(a.T, f32p::BN)), dim3(f32p::THREADS), 0, st,
-                     (operand<T, true>(a.w, a.d, a.V, a.d)), (operand<T, true>(a.h, a.d, a.T, a.d)),
-                     a.b, n_vt, part);
-  hipLaunchKernelGGL((k_loss_join<T, false>), dim3(cdiv(a.T, 4)), dim3(256), 0, st, part, n_vt, a.V, a.d, a.T,
+  const float *w = static_cast<const float*>(a.w), *h = static_cast<const float*>(a.h);
+  const size_t d = a.d;
+  const int kind = f32p::tile_kind(a.V, a.T), n_vt = cdiv(a.V, f32p::tile_a(kind));
+  f32p::with_kind(kind, [&](auto c) {
+    hipLaunchKernelGGL(k_loss_f32<c>, dim3(n_vt, cdiv(a.T, f32p::Tile<c>::B)), dim3(f32p::THREADS), 0,
+                       st, (Operand<true>{w, d, a.V, a.d}), (Operand<true>{h, d, a.T, a.d}), a.b, n_vt,
+                       part);
+  });
+  hipLaunchKernelGGL((k_loss_join<float, false>), dim3(cdiv(a.T, 4)), dim3(256), 0, st, part, n_vt,
+                     a.V, a.d, a.T,
                      a.d % 4 == 0 && ((reinterpret_cast<uintptr_t>(a.w) |
                                        reinterpret_cast<uintptr_t>(a.h)) & 15) == 0,
-                     static_cast<const T*>(a.w), a.b, static_cast<const T*>(a.h), a.target, a.loss,
-                     a.lse);
+                     w, a.b, h, a.target, a.loss, a.lse);
   return hipGetLastError();
 }
 
-template <typename T>
 hipError_t backward_f32(const HeadLossArgs& a, hipStream_t st) {
-  using namespace f32p;
   const BackPlan p = back_plan(a.V, a.d, a.T);
-  float* dh = reinterpret_cast<float*>(a.ws + p.o_dh);
-  float* dw = reinterpret_cast<float*>(a.ws + p.o_dw);
+  float* part_dh = reinterpret_cast<float*>(a.ws + p.o_dh);
+  float* part_dw = reinterpret_cast<float*>(a.ws + p.o_dw);
   float* D = reinterpret_cast<float*>(a.ws + p.o_d);
   float* db = reinterpret_cast<float*>(a.ws + p.o_db);
-  const int n_tt = cdiv(a.T, BM);
-  const T* w = static_cast<const T*>(a.w);
-  T* hl = reinterpret_cast<T*>(a.ws + p.o_h);
-  if (a.dw && a.T > 0)
-    hipLaunchKernelGGL(k_live_rows<T>, dim3(a.T), dim3(256), 0, st, static_cast<const T*>(a.h),
-                       a.target, a.lse, a.V, a.d, hl);
+  float* hl = reinterpret_cast<float*>(a.ws + p.o_h);
+  const float *w = static_cast<const float*>(a.w), *h = static_cast<const float*>(a.h);
+  float *dh = static_cast<float*>(a.dh), *dw = static_cast<float*>(a.dw);
+  const size_t d = a.d;
+  const int BA = f32p::tile_a(p.kind), n_tt = cdiv(a.T, f32p::tile_b(p.kind));
+  if (dw && a.T > 0)
+    hipLaunchKernelGGL(k_live_rows, dim3(a.T), dim3(256), 0, st, h, a.target, a.lse, a.V, a.d, hl);
   for (int v0 = 0; v0 < a.V; v0 += p.Vc) {
     const int nv = std::min(p.Vc, a.V - v0);
-    const size_t ldd = (size_t)cdiv(nv, BN) * BN;
-    const T* wp = w + (size_t)v0 * a.d;
+    const size_t ldd = (size_t)cdiv(nv, BA) * BA;
+    const float* wp = w + v0 * d;
     if (a.T > 0)
-      hipLaunchKernelGGL(k_dz_f32<T>, dim3((unsigned)(ldd / BN), n_tt), dim3(THREADS), 0, st,
-                       (operand<T, true>(a.h, a.d, a.T, a.d)), (operand<T, true>(wp, a.d, nv, a.d)),
-                       a.b ? a.b + v0 : nullptr, a.target, a.lse, a.dloss, a.V, v0, D, ldd,
-                       a.db ? db : nullptr);
+      f32p::with_kind(p.kind, [&](auto c) {
+        hipLaunchKernelGGL(k_dz_f32<c>, dim3((unsigned)(ldd / BA), n_tt), dim3(f32p::THREADS), 0, st,
+                           (Operand<true>{wp, d, nv, a.d}), (Operand<true>{h, d, a.T, a.d}),
+                           a.b ? a.b + v0 : nullptr, a.target, a.lse, a.dloss, a.V, v0, D, ldd,
+                           a.db ? db : nullptr);
+      });
     if (a.db)
       hipLaunchKernelGGL(k_db_sum, dim3(cdiv(nv, 256)), dim3(256), 0, st, db, n_tt, ldd, nv,
                          a.db + v0);
-    if (a.dw) {
-      const auto A = operand<float, false>(D, ldd, nv, a.T);
-      const auto B = operand<T, false>(hl, a.d, a.d, a.T);
-      T* out = static_cast<T*>(a.dw) + (size_t)v0 * a.d;
-      hipError_t e = hipSuccess;
-      if (p.s_dw == 1) {
-        e = launch_product(A, B, 1, false, out, st);
-      } else {
-        e = launch_product(A, B, p.s_dw, false, dw, st);
-        if (e == hipSuccess) e = launch_sum_parts(dw, p.s_dw, (size_t)nv * a.d, out, st);
-      }
+    if (dw) {
+      const Operand<false> A{hl, d, a.d, a.T}, B{D, ldd, nv, a.T};
+      float* out = dw + v0 * d;
+      hipError_t e = launch_product(A, B, p.s_dw, false, p.s_dw == 1 ? out : part_dw, st);
+      if (e == hipSuccess && p.s_dw > 1) e = launch_sum_parts(part_dw, p.s_dw, nv * d, out, st);
       if (e != hipSuccess) return e;
     }
-    if (a.dh) {
-      const auto A = operand<float, true>(D, ldd, a.T, nv);
-      const auto B = operand<T, false>(wp, a.d, a.d, nv);
-      const hipError_t e = p.direct_dh
-                               ? launch_product(A, B, 1, false, static_cast<T*>(a.dh), st)
-                               : launch_product(A, B, p.s_dh, v0 > 0, dh, st);
+    if (dh) {
+      const Operand<false> A{wp, d, a.d, nv};
+      const Operand<true> B{D, ldd, a.T, nv};
+      const hipError_t e =
+          launch_product(A, B, p.s_dh, !p.direct_dh && v0 > 0, p.direct_dh ? dh : part_dh, st);
       if (e != hipSuccess) return e;
     }
   }
-  if (a.dh && !p.direct_dh)
-    return launch_sum_parts(dh, p.s_dh, (size_t)a.T * a.d, static_cast<T*>(a.dh), st);
+  if (dh && !p.direct_dh) return launch_sum_parts(part_dh, p.s_dh, a.T * d, dh, st);
   return hipGetLastError();
 }
 
@@ -1081,7 +1089,7 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
 
 size_t head_loss_ws(bool bf16, int V, int, int T) {
   const int rows = T > 0 ? T : 1;
-  return align256((size_t)rows * cdiv(V, bf16 ? exit_tile_rows(true, rows) : f32p::BM) *
+  return align256((size_t)rows * cdiv(V, bf16 ? exit_tile_rows(true, rows) : f32p::tile_a(f32p::tile_kind(V, T))) *
                   sizeof(float2));
 }
 size_t head_loss_backward_ws(bool bf16, int V, int d, int T) {
@@ -1090,11 +1098,11 @@ size_t head_loss_backward_ws(bool bf16, int V, int d, int T) {
 }
 
 hipError_t launch_head_loss(const HeadLossArgs& a, hipStream_t st) {
-  return a.bf16 ? loss_bf16(a, st) : loss_f32<float>(a, st);
+  return a.bf16 ? loss_bf16(a, st) : loss_f32(a, st);
 }
 
 hipError_t launch_head_loss_backward(const HeadLossArgs& a, hipStream_t st) {
-  return a.bf16 ? backward_bf16(a, st) : backward_f32<float>(a, st);
+  return a.bf16 ? backward_bf16(a, st) : backward_f32(a, st);
 }
 
 }  // namespace trimmoe

@@ -609,7 +609,7 @@ __device__ __forceinline__ void skinny_dz_rows(const FewArgs& a, char* lds, int 
   // the lane's token: tile wave % MT
   const int t = 16 * (wave % MT) + fr;
   const int y = __shfl(row.y, t);
-  const float l2 = __shfl(row.l2, t), m = __shfl(row.m, t), e = m * __shfl(row.e, t);
+  const float lse = __shfl(row.lse, t), m = __shfl(row.m, t), e = m * __shfl(row.e, t);
   int par = 0;
   auto epi = [&](int u, const f32x4_t(&acc)[1][T::G][MT]) {
 #pragma unroll
@@ -623,7 +623,7 @@ __device__ __forceinline__ void skinny_dz_rows(const FewArgs& a, char* lds, int 
         if (v >= v1) continue;  // (v1 and v0 are multiples of 16: a whole row of lanes)
         float s = z[0][r];
         if (a.b) s += a.b[min(v, a.V - 1)];
-        float p = __builtin_amdgcn_exp2f(fmaf(s, kLog2e, -l2));
+        float p = softmax_of(s, lse);
         p = v == y ? p - 1.f : p;
         p = y >= 0 && v < a.V ? p : 0.f;
         const float x = p * m;
