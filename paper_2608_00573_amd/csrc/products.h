@@ -19,9 +19,10 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 //     image (two buffers, the next slices' loads in flight under the MFMAs), so a
 //     fragment read is 32 consecutive floats and the order of the operand in memory
 //     only changes how a slice is written.
-//   kFew 128 x 64, kFewer 256 x 32 (few rows of B, a small batch of tokens): the
-//     wavefronts lie along A and share none of it, so both operands go straight to
-//     the registers (f32_stream): no LDS, no barrier, several slices in flight.
+//   kFew 128 x 64, kFewer 256 x 32 (few rows of B, a small batch of tokens), kSmall
+//     128 x 32: the wavefronts lie along A and share none of it, so both operands go
+//     straight to the registers (f32_stream): no LDS, no barrier, several slices in
+//     flight.
 namespace f32p {
 constexpr int KS = 16, THREADS = 256;
 // An LDS row (one k) of `rows` floats takes LS, and every fourth one starts 16 floats
@@ -30,12 +31,17 @@ constexpr int KS = 16, THREADS = 256;
 __host__ __device__ constexpr int ls(int rows) { return rows + 48; }
 __device__ __forceinline__ constexpr int row(int k, int LS) { return k * LS + 16 * ((k >> 2) & 3); }
 
-enum Kind { kNarrow, kSquare, kFew, kFewer };
+enum Kind { kNarrow, kSquare, kFew, kFewer, kSmall };
+__host__ __device__ constexpr int tile_a(int kind) {
+  return kind == kNarrow ? 64 : kind == kFewer ? 256 : 128;
+}
+__host__ __device__ constexpr int tile_b(int kind) {
+  return kind == kNarrow ? 256 : kind == kSquare ? 128 : kind == kFew ? 64 : 32;
+}
 template <int KIND>
 struct Tile {
   static constexpr bool STREAM = KIND >= kFew;
-  static constexpr int A = KIND == kNarrow ? 64 : KIND == kFewer ? 256 : 128;  // rows
-  static constexpr int B = 16384 / (KIND >= kFew ? 2 : 1) / A;
+  static constexpr int A = tile_a(KIND), B = tile_b(KIND);  // rows
   static constexpr int WA = KIND == kNarrow ? 1 : KIND == kSquare ? 2 : 4;  // wavefronts
   static constexpr int WB = 4 / WA;
   static constexpr int NA = A / WA / 16, NB = B / WB / 16;  // a wavefront's 16-row groups
@@ -43,17 +49,26 @@ struct Tile {
   static constexpr int OCC = STREAM ? 3 : 2;  // wavefronts a SIMD
 };
 
+inline long tiles(int kind, int a, int b) {
+  return (long)cdiv(a, tile_a(kind)) * cdiv(b, tile_b(kind));
+}
+
 // the kind for a product of a x b rows
-inline int tile_kind(int a, int b) {
+inline int shape_kind(int a, int b) {
   return a <= 64 ? kNarrow : b <= 32 ? kFewer : b <= 64 ? kFew : kSquare;
+}
+// ... that is not split along K: smaller tiles where they would leave half of the CUs
+// without one (300 tokens, d 1316, vocabulary 530: 43 instead of 107 us)
+inline int tile_kind(int a, int b) {
+  const int k = shape_kind(a, b);
+  if (k == kNarrow || tiles(k, a, b) > 128) return k;
+  return k != kSquare || tiles(k, a, b) <= 64 ? kSmall : kFew;
 }
 // ... of launch_product: the streams take A row-contiguous and B K-contiguous
 inline int product_kind(bool a_k, bool b_k, int a, int b) {
-  const int k = tile_kind(a, b);
+  const int k = shape_kind(a, b);
   return k >= kFew && (a_k || !b_k) ? kSquare : k;
 }
-inline int tile_a(int kind) { return kind == kNarrow ? 64 : kind == kFewer ? 256 : 128; }
-inline int tile_b(int kind) { return 16384 / (kind >= kFew ? 2 : 1) / tile_a(kind); }
 
 // f(integral constant of the kind)
 template <typename F>
@@ -64,6 +79,8 @@ inline void with_kind(int kind, F f) {
     f(std::integral_constant<int, kSquare>());
   else if (kind == kFew)
     f(std::integral_constant<int, kFew>());
+  else if (kind == kSmall)
+    f(std::integral_constant<int, kSmall>());
   else
     f(std::integral_constant<int, kFewer>());
 }
@@ -81,29 +98,34 @@ struct Operand {
 };
 
 // This thread's part of an operand's slices: N groups of four elements, rows from
-// r0.  Groups inside the bounds take one load, the others test every element (past
-// the bounds: zeros).
+// r0, in 16-byte loads.  Rows past the end hold anything: the last row's elements
+// (KC), or a group moved back to end with the operand and turned when it is stored.
+// Elements past the end of K are zeros.
 template <int N, bool KC>
 struct Fetch {
   const float* p[N];
-  int lim[N];  // KC: > 0 for a valid row; else elements from r on that are valid
-  int k;       // KC: first k of the thread's groups, else its row's k
+  int sh[N];  // row-contiguous: rows the group was moved back by
+  int k;      // KC: first k of the thread's groups, else its row's k
+  int rows;
+  bool turn, wide;
   size_t step;
-  bool whole;
   __device__ __forceinline__ Fetch(const Operand<KC>& o, int r0, int k0) {
     step = KC ? (size_t)f32p::KS : (size_t)f32p::KS * o.ld;
-    whole = r0 + 64 * N <= o.rows;
+    rows = o.rows;
+    turn = !KC && r0 + 64 * N > o.rows;
+    wide = KC || o.rows >= 4;
     k = k0 + (KC ? 4 * (threadIdx.x & 3) : threadIdx.x >> 4);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int r = r0 + 64 * i + (KC ? threadIdx.x >> 2 : 4 * (threadIdx.x & 15));
-      lim[i] = o.rows - r;
-      p[i] = o.p + (KC ? (size_t)min(r, o.rows - 1) * o.ld + k : (size_t)k * o.ld + r);
+      const int at = KC ? min(r, o.rows - 1) : min(r, max(o.rows - 4, 0));
+      sh[i] = r - at;
+      p[i] = o.p + (KC ? (size_t)at * o.ld + k : (size_t)k * o.ld + at);
     }
   }
   // the slice that begins at k0, and on to the next one
   __device__ __forceinline__ void next(int k0, int k_end, float (&x)[N][4]) {
-    if (whole && k0 + f32p::KS <= k_end) {
+    if (wide && k0 + f32p::KS <= k_end) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const f32x4_any v = *reinterpret_cast<const f32x4_any*>(p[i]);
@@ -111,42 +133,40 @@ struct Fetch {
         for (int u = 0; u < 4; ++u) x[i][u] = v[u];
       }
     } else {
+      // elements of a group that may be read
+      const int n = KC ? k_end - k : k < k_end ? (wide ? 4 : rows) : 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int n = KC ? (lim[i] > 0 ? k_end - k : 0) : (k < k_end ? lim[i] : 0);
-        if (n >= 4) {
-          const f32x4_any v = *reinterpret_cast<const f32x4_any*>(p[i]);
+      for (int i = 0; i < N; ++i)
 #pragma unroll
-          for (int u = 0; u < 4; ++u) x[i][u] = v[u];
-        } else {
-#pragma unroll
-          for (int u = 0; u < 4; ++u) x[i][u] = u < n ? p[i][u] : 0.f;
-        }
-      }
+        for (int u = 0; u < 4; ++u) x[i][u] = u < n ? p[i][u] : 0.f;
     }
     k += f32p::KS;
 #pragma unroll
     for (int i = 0; i < N; ++i) p[i] += step;
   }
-};
-
-template <bool KC, int N>
-__device__ __forceinline__ void store_slice(float* s, const float (&x)[N][4]) {
-  using namespace f32p;
-  constexpr int LS = ls(64 * N);
+  __device__ __forceinline__ void store(float* s, const float (&x)[N][4]) const {
+    using namespace f32p;
+    constexpr int LS = ls(64 * N);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if constexpr (KC) {
-      const int r = (threadIdx.x >> 2) + 64 * i, k = 4 * (threadIdx.x & 3);
+    for (int i = 0; i < N; ++i) {
+      if constexpr (KC) {
+        const int r = (threadIdx.x >> 2) + 64 * i, k = 4 * (threadIdx.x & 3);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) s[row(k, LS) + u * LS + r] = x[i][u];
-    } else {
-      const int k = threadIdx.x >> 4, r = 4 * (threadIdx.x & 15) + 64 * i;
-      *reinterpret_cast<float4*>(s + row(k, LS) + r) =
-          make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        for (int u = 0; u < 4; ++u) s[row(k, LS) + u * LS + r] = x[i][u];
+      } else {
+        const int k = threadIdx.x >> 4, r = 4 * (threadIdx.x & 15) + 64 * i;
+        float4 v = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        if (turn) {
+          const int m = sh[i];
+          v.x = m == 0 ? v.x : m == 1 ? v.y : m == 2 ? v.z : v.w;
+          v.y = m == 0 ? v.y : m == 1 ? v.z : v.w;
+          v.z = m == 0 ? v.z : v.w;
+        }
+        *reinterpret_cast<float4*>(s + row(k, LS) + r) = v;
+      }
     }
   }
-}
+};
 
 // A wavefront's part of a tile's product, 16 x 16 accumulators [A][B].  A tile cut
 // short is shared out evenly: its 16-row groups of an operand go to the wavefronts in
@@ -199,8 +219,8 @@ __device__ __forceinline__ void f32_tile(const Operand<AK>& A, const Operand<BKC
   Fetch<T::A / 64, AK> la(A, r0, k0);
   Fetch<T::B / 64, BKC> lb(B, n0, k0);
   const auto put = [&](const Regs& x, int buf) {
-    store_slice<AK>(lds + buf * T::BUF, x.a);
-    store_slice<BKC>(lds + buf * T::BUF + KS * LA, x.b);
+    la.store(lds + buf * T::BUF, x.a);
+    lb.store(lds + buf * T::BUF + KS * LA, x.b);
   };
   const auto fetch = [&](Regs& x, int k) {
     la.next(k, k_end, x.a);
@@ -228,7 +248,7 @@ __device__ __forceinline__ void f32_tile(const Operand<AK>& A, const Operand<BKC
   Frags f0, f1;
 #pragma unroll
   for (int n = 0; n < 2 * KS; ++n) read(f0, 0, n);
-  const auto slice = [&](auto whole, Frags& f, Frags& next, Regs& x, int k, int buf) {
+  const auto slice = [&](auto whole_a, auto whole_b, Frags& f, Frags& next, Regs& x, int k, int buf) {
 #pragma unroll
     for (int g = 0; g < KS; ++g) {  // a row of MFMAs: k-step g / 4, group g % 4 of B
       if (g == KS / 2) {
@@ -239,10 +259,10 @@ __device__ __forceinline__ void f32_tile(const Operand<AK>& A, const Operand<BKC
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if (whole || g % 4 < nb)
+      if (whole_b || g % 4 < nb)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (whole || i < na)
+          if (whole_a || i < na)
             t.acc[i][g % 4] = __builtin_amdgcn_mfma_f32_16x16x4f32(f.a[g / 4][i], f.b[g / 4][g % 4],
                                                                    t.acc[i][g % 4], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
@@ -253,16 +273,18 @@ __device__ __forceinline__ void f32_tile(const Operand<AK>& A, const Operand<BKC
       }
     }
   };
-  const auto run = [&](auto whole) {
+  const auto run = [&](auto whole_a, auto whole_b) {
     for (int k = k0; k < k_end; k += 2 * KS) {
-      slice(whole, f0, f1, x0, k, 0);
-      if (k + KS < k_end) slice(whole, f1, f0, x1, k + KS, 1);
+      slice(whole_a, whole_b, f0, f1, x0, k, 0);
+      if (k + KS < k_end) slice(whole_a, whole_b, f1, f0, x1, k + KS, 1);
     }
   };
   if (na >= 4 && nb >= 4)
-    run(std::true_type());
+    run(std::true_type(), std::true_type());
+  else if (na >= 4)
+    run(std::true_type(), std::false_type());
   else
-    run(std::false_type());
+    run(std::false_type(), std::false_type());
   __syncthreads();
 }
 
@@ -381,6 +403,8 @@ __device__ __forceinline__ void f32_stream(const Operand<AK>& A, const Operand<t
       f32_stream_of<1, 4>(A, B, k0, k_end, t);
     else
       f32_stream_of<2, 4>(A, B, k0, k_end, t);
+  } else if constexpr (KIND == f32p::kSmall) {
+    f32_stream_of<2, 6>(A, B, k0, k_end, t);
   } else {
     if (t.nb == 3)
       f32_stream_of<3, 4>(A, B, k0, k_end, t);
@@ -401,16 +425,16 @@ __device__ __forceinline__ void f32_product(const Operand<AK>& A, const Operand<
 }
 
 // K splits of an a x b product over K on a 256-CU device: the fewest slices on the
-// busiest CU, a block's start and end counted as 16 of them, and a tenth more for a
-// block that has no other one beside it
+// busiest CU, a block's start and end counted as 16 of them, a tenth more for a
+// block that has no other one beside it, and the partials' sum as 4
 inline int product_splits(int kind, int a, int b, int K) {
-  const long tiles = (long)cdiv(a, f32p::tile_a(kind)) * cdiv(b, f32p::tile_b(kind));
+  const long tiles = f32p::tiles(kind, a, b);
   const int nk = cdiv(K, f32p::KS);
   int best = 1;
   long cost = 0;
-  for (int s = 1; s <= 64 && (s == 1 || nk / s >= 16); ++s) {
+  for (int s = 1; s <= 64 && (s == 1 || nk / s >= 6); ++s) {
     const long rounds = (tiles * s + 255) / 256;
-    const long c = rounds * (cdiv(nk, s) + 16) * (rounds == 1 ? 11 : 10);
+    const long c = rounds * (cdiv(nk, s) + 16) * (rounds == 1 ? 11 : 10) + (s > 1 ? 40 : 0);
     if (s == 1 || c < cost) {
       best = s;
       cost = c;

@@ -73,7 +73,7 @@ hipError_t launch_product(const Operand<AK>& A, const Operand<BKC>& B, int split
   const int k_per = cdiv(cdiv(A.K, splits), KS) * KS;
   with_kind(product_kind(AK, BKC, A.rows, B.rows), [&](auto kind) {
     using T = Tile<kind>;
-    if constexpr (!T::STREAM || (!AK && BKC)) {
+    if constexpr (kind != kSmall && (!T::STREAM || (!AK && BKC))) {
       const dim3 grid((unsigned)cdiv(A.rows, T::A) * cdiv(B.rows, T::B), 1, splits);
       hipLaunchKernelGGL((k_prod_f32<kind, AK, BKC>), grid, dim3(THREADS), 0, st, A, B, k_per, out,
                          add ? 1 : 0);

@@ -134,6 +134,17 @@ HEADS = [
     (F32, 1003, 41, 129, True),     # rows that are not whole vectors
     (F32, 300, 97, 1000, False),
     (F32, 5000, 264, 17, True),
+    (F32, 70, 3, 129, True),        # rows shorter than a load
+    (F32, 70, 2, 20, False),
+    (F32, 40, 100, 300, True),      # no more than 64 of either side
+    (F32, 1003, 40, 700, False),
+    (F32, 530, 1316, 300, True),    # few tiles, a long d
+    (F32, 33100, 66, 5, False),     # streams of w: up to 16, 32, 48 and 64 rows
+    (F32, 33100, 71, 20, True),
+    (F32, 17000, 65, 33, True),
+    (F32, 17000, 130, 50, False),
+    (F32, 8300, 67, 200, True),     # tiles cut short in every direction
+    (F32, 30000, 70, 100, True),
     (BF16, 512, 64, 37, True),
     (BF16, 1, 64, 5, True),
     (BF16, 2, 64, 1, False),
