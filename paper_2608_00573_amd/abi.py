@@ -430,6 +430,8 @@ def _on_stream(t: torch.Tensor, stream):
     if not t.is_cuda:
         raise ValueError("the training losses run on GPU tensors")
     if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"a stream of {stream.device} for tensors on {t.device}")
         return torch.cuda.stream(stream)
     if t.device.index == torch.cuda.current_device():
         return _NO_CONTEXT

@@ -81,3 +81,53 @@ def train_sigmoid_heads(hs, labels, epochs: int, lr: float):
         out.append((w, c, loss[:epochs]))
     torch.cuda.synchronize()
     return out
+
+
+def train_softmax_heads(hs, target, w_head: torch.Tensor, epochs: int, lr: float):
+    """One vocabulary head per representation in hs, from the output head w_head
+    and a zero bias, by full-batch gradient descent on the cross entropy towards
+    target int32 [Q] (the output head's answers at full depth, say; a target
+    outside [0, V) is ignored).  Weights are kept in fp32 and used in the rows'
+    dtype; returns [(w [V, d], b fp32 [V], mean losses fp32 [epochs])]."""
+    live = ((target >= 0) & (target < w_head.shape[0])).float()
+    mean = live / live.sum().clamp_min(1.0)
+    out = []
+    for h in hs:
+        w32 = w_head.float().clone()
+        b = torch.zeros(w_head.shape[0], dtype=torch.float32, device=h.device)
+        losses = torch.zeros(epochs, dtype=torch.float32, device=h.device)
+        for e in range(epochs):
+            w = w32.to(h.dtype)
+            loss, lse = abi.trimmoe_head_cross_entropy(w, h, target, b)
+            losses[e] = (loss * mean).sum()
+            _, dw, db = abi.trimmoe_head_cross_entropy_backward(w, h, target, lse, mean, b,
+                                                                want_dh=False)
+            w32.add_(dw, alpha=-lr)
+            b.add_(db, alpha=-lr)
+        out.append((w32.to(h.dtype), b, losses))
+    torch.cuda.synchronize()
+    return out
+
+
+def balance_routers(routers, hs, targets, epochs: int, lr: float):
+    """Gradient descent on the balance loss of each router (w [E, d], bias fp32
+    [E]) over the rows it routed, hs[l] [Q, d] with the recorded experts
+    targets[l] int16 [Q, k]: probabilities move away from the experts that took
+    more than their share.  Weights are kept in fp32 and used in the rows'
+    dtype; returns [(w, b fp32 [E], losses fp32 [epochs], counts int32 [E + 1])]."""
+    out = []
+    for (w0, b0), h, t in zip(routers, hs, targets):
+        w32, b = w0.float().clone(), b0.clone()
+        one = torch.ones(1, dtype=torch.float32, device=h.device)
+        losses = torch.zeros(epochs, dtype=torch.float32, device=h.device)
+        counts = torch.zeros(w0.shape[0] + 1, dtype=torch.int32, device=h.device)
+        for e in range(epochs):
+            w = w32.to(h.dtype)
+            loss, counts, _, prob = abi.trimmoe_balance_loss(w, h, t, b)
+            losses[e] = loss[0]
+            _, dw, db = abi.trimmoe_balance_loss_backward(w, h, t, prob, counts, one, want_dh=False)
+            w32.add_(dw, alpha=-lr)
+            b.add_(db, alpha=-lr)
+        out.append((w32.to(h.dtype), b, losses, counts))
+    torch.cuda.synchronize()
+    return out

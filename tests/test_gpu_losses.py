@@ -13,7 +13,7 @@ import pytest
 import torch
 
 from oracle import losses as X
-from paper_2608_00573_amd import abi
+from paper_2608_00573_amd import abi, offline
 from synthgen import make_inputs, workload
 from synthgen.rng import normal_f32
 
@@ -632,3 +632,61 @@ def test_training_objective_over_a_traced_stack():
     loss, lse = c.forward()
     c.check_forward(loss, lse)
     c.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_softmax_heads_take_the_gradients_steps(dtype):
+    # a descent of two steps is the two steps written out; a head without steps
+    # and rows without a target stay as they are
+    c = Head(81, dtype, 700, 128, 90).dev()
+    other = Head(82, dtype, 700, 128, 90).dev()
+    lr, V = 0.5, 700
+    got = offline.train_softmax_heads([c.Hd, other.Hd], c.yd, c.Wd, 2, lr)
+    assert len(got) == 2
+    # (divided by a tensor: division by a number multiplies by its rounded reciprocal)
+    live = ((c.yd >= 0) & (c.yd < V)).float()
+    mean = live / live.sum()
+    for (w, b, losses), h in zip(got, (c.Hd, other.Hd)):
+        w32, b32 = c.Wd.float().clone(), torch.zeros(V, device=DEV)
+        for e in range(2):
+            loss, lse = abi.trimmoe_head_cross_entropy(w32.to(dtype), h, c.yd, b32)
+            assert losses[e] == (loss * mean).sum()
+            _, dw, db = abi.trimmoe_head_cross_entropy_backward(w32.to(dtype), h, c.yd, lse, mean,
+                                                                b32)
+            w32.add_(dw, alpha=-lr)
+            b32.add_(db, alpha=-lr)
+        # (the same calls on the same values)
+        assert torch.equal(w, w32.to(dtype)) and torch.equal(b, b32)
+    w, b, losses = offline.train_softmax_heads([c.Hd], c.yd, c.Wd, 0, lr)[0]
+    assert torch.equal(w, c.Wd) and not b.any() and losses.numel() == 0
+    none = torch.full_like(c.yd, -1)
+    w, b, losses = offline.train_softmax_heads([c.Hd], none, c.Wd, 1, lr)[0]
+    assert torch.equal(w, c.Wd) and not b.any() and not losses.any()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_balanced_routers_take_the_gradients_steps(dtype):
+    r = Router(83, dtype, 8, 2, 128, 150).dev()
+    lr = 0.25
+    (w, b, losses, counts), = offline.balance_routers([(r.Wd, r.bd)], [r.Hd], [r.td], 1, lr)
+    loss, own, _, prob = abi.trimmoe_balance_loss(r.Wd, r.Hd, r.td, r.bd)
+    one = torch.ones(1, device=DEV)
+    _, dw, db = abi.trimmoe_balance_loss_backward(r.Wd, r.Hd, r.td, prob, own, one)
+    assert losses[0] == loss[0] and torch.equal(counts, own)
+    want = (r.Wd.double() - lr * dw.double()).cpu().numpy()
+    half = torch.finfo(dtype).eps / 2
+    _within(w, want, (half + 2 * U) * np.abs(want) + 2 * U * lr * np.abs(dw.double().cpu().numpy()),
+            "w")
+    want = (r.bd.double() - lr * db.double()).cpu().numpy()
+    _within(b, want, 2 * U * (np.abs(want) + lr * np.abs(db.double().cpu().numpy())), "b")
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Other:
+        device = torch.device("cuda", 1)
+
+    c, r = Head(84, F32, 40, 32, 5).dev(), Router(85, F32, 4, 2, 32, 5).dev()
+    with pytest.raises(ValueError, match="stream of cuda:1"):
+        c.forward(stream=Other())
+    with pytest.raises(ValueError, match="stream of cuda:1"):
+        r.forward(stream=Other())
