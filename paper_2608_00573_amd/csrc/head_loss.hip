@@ -286,23 +286,25 @@ __global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const 
 // hw = 2^-e h_t in panels, zeros in the rows that take no part; 8 elements a thread
 __global__ __launch_bounds__(256) void k_scale_rows(const bf16_t* h, RowPart p, int T, int d,
                                                     bf16_t* hw) {
-  const size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x);
-  if (i >= (size_t)T * d) return;
-  const int t = (int)(i / d);
-  union {
-    uint4 v;
-    bf16_t e[8];
-    uint32_t w[4];
-  } x;
-  x.v = make_uint4(0, 0, 0, 0);
-  if (p.y[t] >= 0) {
-    x.v = *reinterpret_cast<const uint4*>(h + i);
-    const float s = p.e[t];
+  const size_t n = (size_t)T * d, step = (size_t)8 * 256 * gridDim.x;
+  for (size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x); i < n; i += step) {
+    const int t = (int)(i / d);
+    union {
+      uint4 v;
+      bf16_t e[8];
+      uint32_t w[4];
+    } x;
+    x.v = make_uint4(0, 0, 0, 0);
+    if (p.y[t] >= 0) {
+      x.v = *reinterpret_cast<const uint4*>(h + i);
+      const float s = p.e[t];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * s, bf2f(x.e[2 * u + 1]) * s);
+      for (int u = 0; u < 4; ++u)
+        x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * s, bf2f(x.e[2 * u + 1]) * s);
+    }
+    const int c = (int)(i - (size_t)t * d);
+    *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t) * 256 + (c & 255)) = x.v;
   }
-  const int c = (int)(i - (size_t)t * d);
-  *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t) * 256 + (c & 255)) = x.v;
 }
 
 }  // namespace
@@ -628,21 +630,22 @@ namespace {
 // is a multiple of 64)
 __global__ __launch_bounds__(256) void k_dh_finish(const float* part, int S, const float* gm, int T,
                                                    int d, bf16_t* dh) {
-  const size_t n = (size_t)T * d, i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x);
-  if (i >= n) return;
-  float4 s = *reinterpret_cast<const float4*>(part + i);
-  for (int k = 1; k < S; ++k) {
-    const float4 x = *reinterpret_cast<const float4*>(part + (size_t)k * n + i);
-    s.x += x.x;
-    s.y += x.y;
-    s.z += x.z;
-    s.w += x.w;
+  const size_t n = (size_t)T * d, step = (size_t)4 * 256 * gridDim.x;
+  for (size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x); i < n; i += step) {
+    float4 s = *reinterpret_cast<const float4*>(part + i);
+    for (int k = 1; k < S; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(part + (size_t)k * n + i);
+      s.x += x.x;
+      s.y += x.y;
+      s.z += x.z;
+      s.w += x.w;
+    }
+    const float g = gm[i / d];
+    uint2 w;
+    w.x = pack_bf16x2(s.x * g, s.y * g);
+    w.y = pack_bf16x2(s.z * g, s.w * g);
+    *reinterpret_cast<uint2*>(dh + i) = w;
   }
-  const float g = gm[i / d];
-  uint2 w;
-  w.x = pack_bf16x2(s.x * g, s.y * g);
-  w.y = pack_bf16x2(s.z * g, s.w * g);
-  *reinterpret_cast<uint2*>(dh + i) = w;
 }
 
 // db of a piece from the token tiles' sums
@@ -1047,7 +1050,10 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   const bf16_t* h = static_cast<const bf16_t*>(a.h);
   const int n_tt = cdiv(a.T, big::BN), n_dt = cdiv(a.d, big::BM);
   const auto grid = [&](long tiles) { return dim3((unsigned)std::min<long>(tiles, a.n_cu)); };
-  const auto threads = [](size_t n) { return dim3((unsigned)((n + 255) / 256)); };
+  // (a grid holds fewer than 2^32 threads: kernels over T d elements stride over it)
+  const auto threads = [](size_t n) {
+    return dim3((unsigned)std::min<size_t>((n + 255) / 256, (size_t)1 << 23));
+  };
   const dim3 block(256);
   static_assert(big::THREADS == 256, "one block shape");
   hipLaunchKernelGGL(k_row_prep, dim3(1), dim3(1024), 0, st, a.target, a.lse, a.dloss, a.V, a.T,

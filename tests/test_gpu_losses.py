@@ -191,6 +191,137 @@ def test_head_gradients_over_several_pieces(dtype, V, d, Q):
     c.check_backward(c.backward(lse))
 
 
+@pytest.mark.parametrize("V,Q", [(1200000, 60), (2300000, 30)])
+def test_fp32_gradients_of_few_rows_over_several_pieces(V, Q):
+    # streams of w (up to 64 and up to 32 rows) whose D is more than a piece holds.  All
+    # weights are positive, so dh is as large as the sum of its terms' magnitudes (but
+    # for the target's), and a piece that were missing or counted twice shows
+    log(f"[losses] head pieces of few rows V={V}")
+    d = 72
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    w = torch.rand(V, d, generator=g, device=DEV)
+    h = torch.randn(Q, d, generator=g, device=DEV) * 0.3
+    y = torch.randint(0, V, (Q,), generator=g, device=DEV, dtype=torch.int32)
+    y[3] = -1
+    gr = torch.rand(Q, generator=g, device=DEV) + 0.5
+    _, lse = abi.trimmoe_head_cross_entropy(w, h, y)
+    dh, dw, _ = abi.trimmoe_head_cross_entropy_backward(w, h, y, lse, gr)
+    wd, hd = w.double(), h.double()
+    z = hd @ wd.t()
+    gd = torch.where(y >= 0, gr.double(), torch.zeros((), dtype=torch.double, device=DEV))[:, None]
+    want_lse = torch.logsumexp(z, 1)
+    D = (z - want_lse[:, None]).exp() * gd
+    del z
+    # logits and lse: sums of d and (in tiles, then 64 lanes) of V terms of magnitude < 20
+    ex = U * 20 * (d + 9) + U * (V / 64 + 308 + 4 * 40)
+    assert ((lse.double() - want_lse).abs() <= ex).all()
+    rows = torch.arange(Q, device=DEV)[y >= 0]
+    D[rows, y[rows].long()] -= gd[rows, 0]
+    aD = D.abs()
+    bound = (2 * ex + (V / 16 + 200) * U) * (aD @ wd.abs()) * 1.01
+    # (V / 16: a chain of MFMAs adds 4 terms a step, in runs of at least 4 to a wavefront)
+    want = D @ wd
+    assert ((dh.double() - want).abs() <= bound).all()
+    assert (bound <= 0.05 * want.abs() + 0.05 * gd * wd.max()).all()
+    want = D.t() @ hd
+    assert ((dw.double() - want).abs() <= (2 * ex + (Q + 80) * U) * (aD.t() @ hd.abs()) * 1.01 +
+            4 * U * want.abs() + TINY).all()
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(BF16, 280001, 8192, 20), (BF16, 280001, 8192, 70),
+                                         (F32, 280001, 4100, 20), (F32, 280001, 4100, 130)])
+def test_head_weights_past_32_bit_offsets(dtype, V, d, Q):
+    # more than 2^32 bytes of weights: every kernel's way through them, checked in fp64
+    # in chunks of the vocabulary
+    log(f"[losses] head weights of 4.6 GB {dtype} Q={Q}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(Q)
+    w = torch.empty(V, d, dtype=dtype, device=DEV)
+    chunks = [slice(v, min(v + 40000, V)) for v in range(0, V, 40000)]
+    for c in chunks:
+        w[c] = torch.randn(c.stop - c.start, d, generator=g, device=DEV).mul_(d ** -0.5).to(dtype)
+    h = torch.randn(Q, d, generator=g, device=DEV).to(dtype)
+    y = torch.randint(0, V, (Q,), generator=g, device=DEV, dtype=torch.int32)
+    y[0], y[1], y[2] = V - 1, 0, -1
+    gr = torch.rand(Q, generator=g, device=DEV) + 0.5
+    b = torch.randn(V, generator=g, device=DEV)
+    loss, lse = abi.trimmoe_head_cross_entropy(w, h, y, b)
+    dh, dw, db = abi.trimmoe_head_cross_entropy_backward(w, h, y, lse, gr, b)
+    hd = h.double()
+    live = y >= 0
+    gd = torch.where(live, gr.double(), torch.zeros((), dtype=torch.double, device=DEV))[:, None]
+    z = torch.cat([hd @ w[c].double().t() + b[c].double() for c in chunks], 1)
+    want_lse = torch.logsumexp(z, 1)
+    mag = max(float((hd.abs() @ w[c].double().abs().t() + b[c].double().abs()).max())
+              for c in chunks)
+    ez = U * (d + 9) * mag
+    ex = ez + U * (V / 64 + 308 + 8 * 30)
+    assert ((lse.double() - want_lse).abs() <= ex).all()
+    t = torch.arange(Q, device=DEV)[live]
+    want = torch.zeros_like(want_lse)
+    want[t] = want_lse[t] - z[t, y[t].long()]
+    assert ((loss.double() - want).abs() <= ex + ez + 4 * U * want.abs()).all()
+    D = (z - want_lse[:, None]).exp() * gd
+    D[t, y[t].long()] -= gd[t, 0]
+    aD, half = D.abs(), torch.finfo(dtype).eps / 2
+    e = 2 * ex + (half if dtype == BF16 else 0) * 1.01 + 8 * U  # of D, relative
+    assert ((db.double() - D.sum(0)).abs() <= (2 * ex + (Q + 88) * U) * aD.sum(0) * 1.01 +
+            2 * U * gd.sum() + TINY).all()
+    want, wmag = torch.zeros_like(hd), torch.zeros_like(hd)
+    for c in chunks:
+        wc = w[c].double()
+        want += D[:, c] @ wc
+        wmag += aD[:, c] @ wc.abs()
+        x = D[:, c].t() @ hd
+        bound = (e + (Q + 80) * U) * (aD[:, c].t() @ hd.abs()) * 1.01
+        bound += half * (x.abs() + bound) + 2 * U * gd.max() * hd.abs().sum(0) + TINY
+        assert ((dw[c].double() - x).abs() <= bound).all()
+    bound = (e + (V / 16 + 200) * U) * wmag * 1.01
+    assert ((dh.double() - want).abs() <= bound + half * (want.abs() + bound) + TINY).all()
+
+
+@pytest.mark.parametrize("dtype,V,d,Q", [(BF16, 300, 4096, 600001), (F32, 300, 4097, 300001)])
+def test_head_rows_past_32_bit_offsets(dtype, V, d, Q):
+    log(f"[losses] head over 4.9 GB of rows {dtype}")
+    g = torch.Generator(device=DEV)
+    g.manual_seed(V)
+    w = (torch.randn(V, d, generator=g, device=DEV) * d ** -0.5).to(dtype)
+    h = torch.empty(Q, d, dtype=dtype, device=DEV)
+    chunks = [slice(t, min(t + 50000, Q)) for t in range(0, Q, 50000)]
+    for c in chunks:
+        h[c] = torch.randn(c.stop - c.start, d, generator=g, device=DEV).to(dtype)
+    y = torch.randint(-1, V, (Q,), generator=g, device=DEV, dtype=torch.int32)
+    gr = torch.rand(Q, generator=g, device=DEV) + 0.5
+    loss, lse = abi.trimmoe_head_cross_entropy(w, h, y)
+    dh, dw, _ = abi.trimmoe_head_cross_entropy_backward(w, h, y, lse, gr)
+    wd, live = w.double(), y >= 0
+    half = torch.finfo(dtype).eps / 2
+    want_dw, mag_dw = (torch.zeros(V, d, dtype=torch.double, device=DEV) for _ in range(2))
+    for c in chunks:
+        hd = h[c].double()
+        z = hd @ wd.t()
+        ez = U * (d + 9) * float((hd.abs() @ wd.abs().t()).max())
+        ex = ez + U * (V / 64 + 308 + 8 * 20)
+        L = torch.logsumexp(z, 1)
+        assert ((lse[c].double() - L).abs() <= ex).all()
+        col = y[c].clamp_min(0).long()[:, None]
+        want = torch.where(live[c], L - z.gather(1, col)[:, 0], torch.zeros_like(L))
+        assert ((loss[c].double() - want).abs() <= ex + ez + 4 * U * want.abs()).all()
+        gd = torch.where(live[c], gr[c].double(), torch.zeros_like(L))[:, None]
+        D = (z - L[:, None]).exp()
+        D = gd * D.scatter_add(1, col, torch.full_like(D[:, :1], -1.0))
+        e = 2 * ex + (half * 1.01 if dtype == BF16 else 0) + 8 * U
+        want = D @ wd
+        bound = (e + (V + 80) * U) * (D.abs() @ wd.abs()) * 1.01 + 2 * U * gd * wd.abs().sum(0)
+        assert ((dh[c].double() - want).abs() <= bound + half * (want.abs() + bound) + TINY).all()
+        want_dw += D.t() @ hd
+        # (rows are summed in MFMA steps of at least 4, K splits apart)
+        mag_dw += (e + (Q / 4 + 200) * U) * (D.abs().t() @ hd.abs())
+    bound = mag_dw * 1.01 + TINY
+    assert ((dw.double() - want_dw).abs() <= bound + half * (want_dw.abs() + bound)).all()
+
+
 @pytest.mark.parametrize("dtype,V,d,Q", [(F32, 300, 96, 40), (BF16, 300, 128, 40),
                                          (BF16, 700, 128, 200)])
 def test_head_gradient_is_the_difference_quotient(dtype, V, d, Q):
@@ -489,6 +620,59 @@ def test_balance_with_inactive_rows_of_anything(dtype, E, d, Q, bad):
     c.Hd[int(keep[0])] = bad
     loss, counts, prob_sum, prob = c.forward()
     assert torch.isnan(loss).all()
+
+
+@pytest.mark.parametrize("dtype,Q", [(BF16, 1100003), (F32, 600001)])
+def test_balance_rows_past_32_bit_offsets(dtype, Q):
+    # more than 2^32 bytes of rows and of their gradient, in fp64 on the GPU
+    log(f"[losses] balance over 4.5 GB of rows {dtype}")
+    E, k, d = 8, 2, 2048
+    g = torch.Generator(device=DEV)
+    g.manual_seed(Q)
+    w = (torch.randn(E, d, generator=g, device=DEV) * d ** -0.5).to(dtype)
+    b = torch.randn(E, generator=g, device=DEV)
+    h = torch.empty(Q, d, dtype=dtype, device=DEV)
+    chunks = [slice(t, min(t + 200000, Q)) for t in range(0, Q, 200000)]
+    for c in chunks:
+        h[c] = torch.randn(c.stop - c.start, d, generator=g, device=DEV).to(dtype)
+    t = torch.randint(-1, E, (Q, k), generator=g, device=DEV).to(torch.int16)
+    loss, counts, psum, prob = abi.trimmoe_balance_loss(w, h, t, b)
+    one = torch.ones(1, device=DEV)
+    dh, dw, db = abi.trimmoe_balance_loss_backward(w, h, t, prob, counts, one)
+    live = (t >= 0).any(1)
+    slots = (t[:, :, None] == torch.arange(E, device=DEV)).sum((0, 1))
+    assert torch.equal(counts.long(), torch.cat([slots, live.sum()[None]]))
+    wd = w.double()
+    mag = max(float((h[c].double().abs() @ wd.abs().t() + b.double().abs()).max()) for c in chunks)
+    rp = 2 * U * (d + 9) * mag + U * (2 * (8 + 4 * 20) + E + 4)
+    S, n = int(slots.sum()), int(live.sum())
+    cm = slots.double() - slots.double().mean()
+    kk = E / (S * n)
+    sums, want_dw, mag_dw = (torch.zeros(E, x, dtype=torch.double, device=DEV) for x in (1, d, d))
+    half, rz = torch.finfo(dtype).eps / 2, 2.0 ** -16 if dtype == BF16 else 0.0
+    want_db, err_db = (torch.zeros(E, dtype=torch.double, device=DEV) for _ in range(2))
+    for c in chunks:
+        hd, lv = h[c].double(), live[c].double()[:, None]
+        p = torch.softmax(hd @ wd.t() + b.double(), 1)
+        assert ((prob[c].double() - p).abs() <= rp * p * 1.01 + TINY).all()
+        sums[:, 0] += (p * lv).sum(0)
+        dz = kk * p * (cm - (p @ cm)[:, None]) * lv
+        ac = (p * cm.abs()).sum(1, keepdim=True)
+        ez = kk * p * lv * (rp * ((cm - (p @ cm)[:, None]).abs() + ac) + (E + 8) * U * ac +
+                            2 * U * slots.max() + 8 * U * cm.abs()) * 1.01 + rz * dz.abs()
+        want = dz @ wd
+        bound = (ez + (E + 80) * U * dz.abs()) @ wd.abs() * 1.01
+        assert ((dh[c].double() - want).abs() <= bound + half * (want.abs() + bound) + TINY).all()
+        want_dw += dz.t() @ hd
+        mag_dw += (ez + (Q + 80) * U * dz.abs()).t() @ hd.abs()
+        want_db += dz.sum(0)
+        err_db += (ez + (Q + 80) * U * dz.abs()).sum(0)
+    want = sums[:, 0]
+    assert ((psum.double() - want).abs() <= (rp + (Q + 8) * U) * want * 1.01).all()
+    want_loss = kk * float(slots.double() @ want)
+    assert abs(float(loss) - want_loss) <= (rp + (Q + 16) * U) * want_loss * 1.01
+    assert ((dw.double() - want_dw).abs() <= mag_dw * 1.01 + half * (want_dw.abs() + mag_dw)).all()
+    assert ((db.double() - want_db).abs() <= err_db * 1.01 + TINY).all()
 
 
 def test_balance_with_experts_left_out():
