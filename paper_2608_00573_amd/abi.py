@@ -189,7 +189,8 @@ def _ptr(t):
 
 def _stream_handle(stream):
     if stream is None:
-        stream = torch.cuda.current_stream()
+        # (current_stream() makes a Stream object for it: 2.9 us of a small call's 20)
+        return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
     return C.c_void_p(stream.cuda_stream)
 
 

@@ -574,8 +574,6 @@ void with_tiles(int E, F f) {
     default: f(std::integral_constant<int, 16>()); break;
   }
 }
-// rows / 16 a forward block takes at once: w passes the block once for them
-constexpr int kRowTiles = 2;
 // wavefronts of a forward block: its K parts fit LDS
 constexpr int wavefronts(int et) { return et == 16 ? 4 : 8; }
 // columns / 64 of a gradient block: accumulators of dw and fragments of w in registers
@@ -590,13 +588,20 @@ bool rows_aligned(int d, const void* p, const void* q) {
 }
 
 struct Plan {
-  int et, nb;  // expert tiles, forward blocks
+  int et, rt, nb;  // expert tiles, rows / 16 a forward block takes at once, its blocks
   size_t f_c, f_total;
   int n_t, R;  // tiles of 64 rows, slices of dw
   size_t b_mask, b_db, b_dw, b_total;
   Plan(bool bf16, int E, int d, int T) : et(expert_tiles(E)) {
     const int rows = std::max(T, 1);
-    nb = std::min(kRowBlocks, cdiv(rows, 16 * kRowTiles));
+    // Little work takes one block, whose passes cost less than the loss's own launch (30
+    // rows, d 4096, 8 experts: 15 us, 18 in two blocks; 64 rows, d 1024, 200 experts: 48,
+    // 28 in two).  Blocks of 16 rows while that gives no CU a second one (1000 rows, d
+    // 1000, 200 experts, fp32: 52 us, 103 with 32 rows; 8191 rows, d 2048, 60 experts,
+    // bf16: 30 and 22, as w is read by twice the blocks).
+    const bool one = rows <= 64 && et * d * cdiv(rows, 32) <= 4096;
+    rt = !one && cdiv(rows, 16) <= 256 ? 1 : 2;
+    nb = one ? 1 : std::min(kRowBlocks, cdiv(rows, 16 * rt));
     f_c = align256((size_t)nb * E * 4);
     f_total = f_c + align256((size_t)nb * (E + 1) * 4);
     n_t = cdiv(rows, kTile);
@@ -623,10 +628,16 @@ hipError_t forward(const BalanceArgs& a, hipStream_t st) {
   if (nb > 0)
     with_tiles(a.E, [&](auto c) {
       constexpr int ET = c;
-      hipLaunchKernelGGL((k_balance_forward<TT, ET, kRowTiles, wavefronts(ET)>), dim3(nb),
-                         dim3(64 * wavefronts(ET)), 0, st,
-                         static_cast<const TT*>(a.w), a.b, static_cast<const TT*>(a.h), a.target, a.T,
-                         a.E, EP, a.k, a.d, rows_aligned(a.d, a.w, a.h), a.prob, part_p, part_c, out);
+      const auto run = [&](auto rt) {
+        hipLaunchKernelGGL((k_balance_forward<TT, ET, rt, wavefronts(ET)>), dim3(nb),
+                           dim3(64 * wavefronts(ET)), 0, st, static_cast<const TT*>(a.w), a.b,
+                           static_cast<const TT*>(a.h), a.target, a.T, a.E, EP, a.k, a.d,
+                           rows_aligned(a.d, a.w, a.h), a.prob, part_p, part_c, out);
+      };
+      if (p.rt == 1)
+        run(std::integral_constant<int, 1>());
+      else
+        run(std::integral_constant<int, 2>());
     });
   if (nb != 1)
     hipLaunchKernelGGL(k_balance_loss, dim3(1), dim3(1024), 0, st, part_p, part_c, nb, a.E, EP, out);
