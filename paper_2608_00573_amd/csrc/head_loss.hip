@@ -251,58 +251,64 @@ struct RowPart {
   float* G;    // [1]
 };
 
-__global__ __launch_bounds__(1024) void k_row_prep(const int32_t* target, const float* lse,
-                                                   const float* dloss, int V, int T, RowPart p) {
-  __shared__ float s_m[16];
+// The rows' parts, and hw = 2^-e h_t in panels, zeros in the rows that take no part (hw
+// may be NULL); 8 elements a thread.  Every block takes the largest weight of all
+// rows by itself: a launch of one block for it cost 8 us at 4096 rows.
+__global__ __launch_bounds__(256) void k_row_parts(const int32_t* target, const float* lse,
+                                                   const float* dloss, int V, int T, int d,
+                                                   const bf16_t* h, RowPart p, bf16_t* hw) {
+  __shared__ float s_m[4];
+  const auto row = [&](int t, int& y, float& L, float& g) {
+    y = target[t];
+    L = lse[t];
+    g = dloss[t];
+    if (y < 0 || y >= V || L == -__builtin_inff()) {
+      y = -1;
+      L = g = 0.f;
+    }
+  };
   float G = 0.f;
-  for (int t = threadIdx.x; t < T; t += 1024) {
-    const int y = target[t];
-    const float L = lse[t];
-    const bool live = y >= 0 && y < V && L != -__builtin_inff();
-    const float g = live ? dloss[t] : 0.f;
-    p.y[t] = live ? y : -1;
-    p.gm[t] = g;
-    p.lse[t] = live ? L : 0.f;
+#pragma unroll 4
+  for (int t = threadIdx.x; t < T; t += 256) {
+    int y;
+    float L, g;
+    row(t, y, L, g);
     G = fmaxf(G, fabsf(g));
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) G = fmaxf(G, __shfl_xor(G, o));
   if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = G;
   __syncthreads();
-  G = s_m[0];
-#pragma unroll
-  for (int i = 1; i < 16; ++i) G = fmaxf(G, s_m[i]);
-  if (threadIdx.x == 0) *p.G = G;
-  // (each thread reads back its own rows)
-  for (int t = threadIdx.x; t < T; t += 1024) {
-    float m, e, gm;
-    row_weight(p.gm[t], G, m, e, gm);
-    p.m[t] = m;
-    p.e[t] = e;
-    p.gm[t] = gm;
-  }
-}
-
-// hw = 2^-e h_t in panels, zeros in the rows that take no part; 8 elements a thread
-__global__ __launch_bounds__(256) void k_scale_rows(const bf16_t* h, RowPart p, int T, int d,
-                                                    bf16_t* hw) {
-  const size_t n = (size_t)T * d, step = (size_t)8 * 256 * gridDim.x;
-  for (size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x); i < n; i += step) {
-    const int t = (int)(i / d);
+  G = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)256 * gridDim.x;
+  if (at == 0) *p.G = G;
+  const size_t n = hw ? (size_t)T * d / 8 : T;
+  for (size_t i = at; i < n; i += step) {
+    const int t = hw ? (int)(8 * i / d) : (int)i, c = hw ? (int)(8 * i - (size_t)t * d) : 0;
+    int y;
+    float L, g, m, e, gm;
+    row(t, y, L, g);
+    row_weight(g, G, m, e, gm);
+    if (c == 0) {
+      p.y[t] = y;
+      p.lse[t] = L;
+      p.m[t] = m;
+      p.e[t] = e;
+      p.gm[t] = gm;
+    }
+    if (!hw) continue;
     union {
       uint4 v;
       bf16_t e[8];
       uint32_t w[4];
     } x;
     x.v = make_uint4(0, 0, 0, 0);
-    if (p.y[t] >= 0) {
-      x.v = *reinterpret_cast<const uint4*>(h + i);
-      const float s = p.e[t];
+    if (y >= 0) {
+      x.v = *reinterpret_cast<const uint4*>(h + 8 * i);
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * s, bf2f(x.e[2 * u + 1]) * s);
+        x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * e, bf2f(x.e[2 * u + 1]) * e);
     }
-    const int c = (int)(i - (size_t)t * d);
     *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t) * 256 + (c & 255)) = x.v;
   }
 }
@@ -626,36 +632,43 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
 
 namespace {
 
-// dh = g_t / m_t times the sum of the S slices, rounded once; 4 elements a thread (d
-// is a multiple of 64)
-__global__ __launch_bounds__(256) void k_dh_finish(const float* part, int S, const float* gm, int T,
-                                                   int d, bf16_t* dh) {
-  const size_t n = (size_t)T * d, step = (size_t)4 * 256 * gridDim.x;
+// Blocks up to dh_blocks: dh = g_t / m_t times the sum of the S slices, rounded once; 4
+// elements a thread (d is a multiple of 64).  The others: db of a piece from the
+// token tiles' sums.
+struct Finish {
+  const float* dh_part;
+  int S, T, d;
+  bf16_t* dh;
+  int dh_blocks;
+  const float* db_part;
+  int n_tt, ld, n;
+  float* db;
+};
+__global__ __launch_bounds__(256) void k_finish(Finish f, RowPart p) {
+  if ((int)blockIdx.x >= f.dh_blocks) {
+    const int c = (blockIdx.x - f.dh_blocks) * 256 + threadIdx.x;
+    if (c >= f.n) return;
+    float s = 0.f;
+    for (int i = 0; i < f.n_tt; ++i) s += f.db_part[(size_t)i * f.ld + c];
+    f.db[c] = s * *p.G;
+    return;
+  }
+  const size_t n = (size_t)f.T * f.d, step = (size_t)4 * 256 * f.dh_blocks;
   for (size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x); i < n; i += step) {
-    float4 s = *reinterpret_cast<const float4*>(part + i);
-    for (int k = 1; k < S; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(part + (size_t)k * n + i);
+    float4 s = *reinterpret_cast<const float4*>(f.dh_part + i);
+    for (int k = 1; k < f.S; ++k) {
+      const float4 x = *reinterpret_cast<const float4*>(f.dh_part + (size_t)k * n + i);
       s.x += x.x;
       s.y += x.y;
       s.z += x.z;
       s.w += x.w;
     }
-    const float g = gm[i / d];
+    const float g = p.gm[i / f.d];
     uint2 w;
     w.x = pack_bf16x2(s.x * g, s.y * g);
     w.y = pack_bf16x2(s.z * g, s.w * g);
-    *reinterpret_cast<uint2*>(dh + i) = w;
+    *reinterpret_cast<uint2*>(f.dh + i) = w;
   }
-}
-
-// db of a piece from the token tiles' sums
-__global__ __launch_bounds__(256) void k_db_finish(const float* part, int n_tt, int ld, int n,
-                                                   const float* G, float* db) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= n) return;
-  float s = 0.f;
-  for (int i = 0; i < n_tt; ++i) s += part[(size_t)i * ld + c];
-  db[c] = s * *G;
 }
 
 // ------------------------------------ backward, bf16, a few tokens --
@@ -1050,17 +1063,13 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   const bf16_t* h = static_cast<const bf16_t*>(a.h);
   const int n_tt = cdiv(a.T, big::BN), n_dt = cdiv(a.d, big::BM);
   const auto grid = [&](long tiles) { return dim3((unsigned)std::min<long>(tiles, a.n_cu)); };
-  // (a grid holds fewer than 2^32 threads: kernels over T d elements stride over it)
-  const auto threads = [](size_t n) {
-    return dim3((unsigned)std::min<size_t>((n + 255) / 256, (size_t)1 << 23));
-  };
   const dim3 block(256);
   static_assert(big::THREADS == 256, "one block shape");
-  hipLaunchKernelGGL(k_row_prep, dim3(1), dim3(1024), 0, st, a.target, a.lse, a.dloss, a.V, a.T,
-                     part);
-  if (a.dw && a.T > 0)
-    hipLaunchKernelGGL(k_scale_rows, threads((size_t)a.T * a.d / 8), block, 0, st, h, part, a.T, a.d,
-                       hw);
+  // (grids hold fewer than 2^32 threads: what runs over T d elements strides)
+  const auto blocks = [](size_t n, size_t most) { return (unsigned)std::min((n + 255) / 256, most); };
+  hipLaunchKernelGGL(k_row_parts, dim3(blocks(a.dw ? rows * a.d / 8 : rows, 512)), block, 0, st,
+                     a.target, a.lse, a.dloss, a.V, a.T, a.d, h, part, a.dw ? hw : nullptr);
+  const bool one = p.Vp >= a.V;  // piece: its db is finished with dh
   for (int v0 = 0; v0 < a.V; v0 += p.Vp) {
     const int nv = std::min(p.Vp, a.V - v0), Vp = cdiv(nv, big::BM) * big::BM;
     const bf16_t* wp = w + (size_t)v0 * a.d;
@@ -1073,8 +1082,11 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       else
         hipLaunchKernelGGL(k_dz_big<false>, g, block, 0, st, z);
     }
-    if (a.db)
-      hipLaunchKernelGGL(k_db_finish, threads(nv), block, 0, st, db, n_tt, Vp, nv, part.G, a.db + v0);
+    Finish f{dh, p.s_dh, a.T, a.d, static_cast<bf16_t*>(a.dh), 0, db, n_tt, Vp, nv,
+             a.db ? a.db + v0 : nullptr};
+    const unsigned db_blocks = a.db ? blocks(nv, ~(size_t)0) : 0;
+    if (db_blocks && !(one && a.dh))
+      hipLaunchKernelGGL(k_finish, dim3(db_blocks), block, 0, st, f, part);
     if (a.dw) {
       const BigProdArgs q{hw, D, a.d, nv, a.T, part.G,
                           static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d, 1, 0};
@@ -1084,10 +1096,11 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       const BigProdArgs q{wp, D, a.d, a.T, nv, nullptr, dh, p.s_dh, v0 > 0};
       hipLaunchKernelGGL(k_prod_big<false>, grid((long)n_tt * n_dt * p.s_dh), block, 0, st, q);
     }
+    if (a.dh && v0 + p.Vp >= a.V) {
+      f.dh_blocks = (int)blocks((size_t)a.T * a.d / 4, (size_t)1 << 22);
+      hipLaunchKernelGGL(k_finish, dim3(f.dh_blocks + (one ? db_blocks : 0)), block, 0, st, f, part);
+    }
   }
-  if (a.dh)
-    hipLaunchKernelGGL(k_dh_finish, threads((size_t)a.T * a.d / 4), block, 0, st, dh, p.s_dh, part.gm,
-                       a.T, a.d, static_cast<bf16_t*>(a.dh));
   return hipGetLastError();
 }
 
