@@ -523,15 +523,15 @@ struct BigProdArgs {
   const bf16_t* A;  // [K, M], DW: in panels
   const bf16_t* B;  // D in panels: [K, N] (DW) or [N, K]
   int M, N, K;
-  const float* scale;  // DW
-  void* out;           // DW: bf16 [N, M] times *scale; else fp32 slices [splits][N, M]
+  const float* scale;  // not PART
+  void* out;           // PART: fp32 slices [splits][N, M]; else bf16 [N, M] times *scale
   int splits;
   int add;             // not DW: added to what the slices hold
 };
 
 // out = B' A with the sums over K: dw (DW: A = scaled h, B = D, both transposed)
-// or partials of dh (A = w transposed, B = D)
-template <bool DW>
+// or dh (A = w transposed, B = D); PART: partials
+template <bool DW, bool PART>
 __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
   __shared__ __align__(16) char lds[big::LDS];
   const BigLane L;
@@ -564,8 +564,9 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
     }
     big_start(lds, q);
   };
-  constexpr int ES = DW ? 2 : 4, STORES = DW ? 32 : 64;
-  const float g = DW ? *a.scale : 0.f;
+  static_assert(DW || PART, "dh is scaled by row");
+  constexpr int ES = PART ? 4 : 2, STORES = PART ? 64 : 32;
+  const float g = PART ? 0.f : *a.scale;
   const int c = L.lane & 15;
   AccBig acc;
   BigFeed<true, DW> q;
@@ -597,7 +598,7 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
     if (jt + 1 < ntiles) start(q, jt + 1, at);
     int M = a.M;
     asm volatile("" : "+s"(M));  // per-tile value: keeps the offsets below inside the tile loop
-    const size_t o = ((size_t)(DW ? 0 : sp) * a.N + n0) * M + m0;
+    const size_t o = ((size_t)(PART ? sp : 0) * a.N + n0) * M + m0;
     // rows past the last one lie behind the buffer's end; so do columns past it by
     // their offset (M is a multiple of 64: blocks of 32 are valid or not as a whole)
     const __amdgpu_buffer_rsrc_t ro = __builtin_amdgcn_make_buffer_rsrc(
@@ -605,11 +606,11 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       const uint32_t row = (uint32_t)(L.wn * 128 + 16 * j + c) * M;
-      const uint32_t off = (row + L.wm * 128 + (DW ? pack_col(L.lane) : 4 * (L.lane >> 4))) * ES;
+      const uint32_t off = (row + L.wm * 128 + (PART ? 4 * (L.lane >> 4) : pack_col(L.lane))) * ES;
 #pragma unroll
       for (int i = 0; i < 8; i += 2) {
         const uint32_t at_i = L.wm * 128 + 16 * i < m_valid ? off : 0xffff0000u;
-        if constexpr (DW) {
+        if constexpr (!PART) {
           float x[2][4];
 #pragma unroll
           for (int k = 0; k < 2; ++k)
@@ -632,42 +633,53 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
 
 namespace {
 
-// Blocks up to dh_blocks: dh = g_t / m_t times the sum of the S slices, rounded once; 4
-// elements a thread (d is a multiple of 64).  The others: db of a piece from the
-// token tiles' sums.
-struct Finish {
-  const float* dh_part;
-  int S, T, d;
-  bf16_t* dh;
-  int dh_blocks;
-  const float* db_part;
-  int n_tt, ld, n;
-  float* db;
+// out [n / d, d] = scale times the sum of the S slices of n partials, rounded once; 4
+// elements a thread (d is a multiple of 64).  scale: of a row, or one for all
+struct SliceSum {
+  const float* part;
+  int S, d;
+  size_t n;
+  const float* scale;
+  bool by_row;
+  bf16_t* out;
+  int blocks;
 };
-__global__ __launch_bounds__(256) void k_finish(Finish f, RowPart p) {
-  if ((int)blockIdx.x >= f.dh_blocks) {
-    const int c = (blockIdx.x - f.dh_blocks) * 256 + threadIdx.x;
+// the column sums of a piece from its token tiles', times *scale
+struct ColSum {
+  const float* part;
+  int n_tt, ld, n;
+  const float* scale;
+  float* out;
+};
+// blocks: those of x, of y, then the columns'
+__global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f) {
+  const int b = blockIdx.x - x.blocks - y.blocks;
+  if (b >= 0) {
+    const int c = b * 256 + threadIdx.x;
     if (c >= f.n) return;
     float s = 0.f;
-    for (int i = 0; i < f.n_tt; ++i) s += f.db_part[(size_t)i * f.ld + c];
-    f.db[c] = s * *p.G;
+    for (int i = 0; i < f.n_tt; ++i) s += f.part[(size_t)i * f.ld + c];
+    f.out[c] = s * *f.scale;
     return;
   }
-  const size_t n = (size_t)f.T * f.d, step = (size_t)4 * 256 * f.dh_blocks;
-  for (size_t i = 4 * ((size_t)blockIdx.x * 256 + threadIdx.x); i < n; i += step) {
-    float4 s = *reinterpret_cast<const float4*>(f.dh_part + i);
-    for (int k = 1; k < f.S; ++k) {
-      const float4 x = *reinterpret_cast<const float4*>(f.dh_part + (size_t)k * n + i);
-      s.x += x.x;
-      s.y += x.y;
-      s.z += x.z;
-      s.w += x.w;
+  const bool first = (int)blockIdx.x < x.blocks;
+  const SliceSum& o = first ? x : y;
+  const size_t step = (size_t)4 * 256 * o.blocks;
+  for (size_t i = 4 * ((size_t)(blockIdx.x - (first ? 0 : x.blocks)) * 256 + threadIdx.x); i < o.n;
+       i += step) {
+    float4 s = *reinterpret_cast<const float4*>(o.part + i);
+    for (int k = 1; k < o.S; ++k) {
+      const float4 v = *reinterpret_cast<const float4*>(o.part + (size_t)k * o.n + i);
+      s.x += v.x;
+      s.y += v.y;
+      s.z += v.z;
+      s.w += v.w;
     }
-    const float g = p.gm[i / f.d];
+    const float g = o.scale[o.by_row ? i / o.d : 0];
     uint2 w;
     w.x = pack_bf16x2(s.x * g, s.y * g);
     w.y = pack_bf16x2(s.z * g, s.w * g);
-    *reinterpret_cast<uint2*>(f.dh + i) = w;
+    *reinterpret_cast<uint2*>(o.out + i) = w;
   }
 }
 
@@ -946,20 +958,23 @@ FewPlan few_plan(int V, int d, int T) {
 }
 
 struct BackPlanBf16 {
-  int Vp, s_dh;  // columns of a piece (a multiple of the tile), splits of dh
-  size_t o_rows, o_hw, o_d, o_dh, o_db, total;
+  int Vp;          // columns of a piece (a multiple of the tile)
+  int s_dh, s_dw;  // K splits of the two products
+  size_t o_rows, o_hw, o_d, o_dh, o_dw, o_db, total;
 };
 
-// K splits of the m x n product dh of nk slices on the large-group core: the fewest
-// slices on the busiest CU, a tile's start and end counted as 8 of them, plus the
-// sum's read of the partials at 5.5 TB/s (a slice takes about 1.5 us)
-int big_splits(int m, int n, int nk) {
+// K splits of an m x n product of nk slices on the large-group core: the fewest slices
+// on the busiest CU, a tile's start and end counted as 8 of them, plus the partials'
+// way through memory at 5.5 TB/s (a slice takes about 1.5 us).  whole: one run
+// needs no partials (dw); else (dh) it writes them as every other does.
+int big_splits(int m, int n, int nk, bool whole) {
   const long tiles = (long)cdiv(m, big::BM) * cdiv(n, big::BN);
-  const double read = (double)m * n * 4 / 8.25e6;
+  const double part = (double)m * n * 4 / 8.25e6;
   int best = 1;
   double cost = 0;
-  for (int s = 1; s <= 32 && (s == 1 || nk / s >= 8); ++s) {
-    const double c = (double)((tiles * s + kCu - 1) / kCu) * (cdiv(nk, s) + 8) + s * read;
+  for (int s = 1; s <= 32 && (s == 1 || nk / s >= 4); ++s) {
+    const double c = (double)((tiles * s + kCu - 1) / kCu) * (cdiv(nk, s) + 8) +
+                     (whole ? (s > 1 ? 2 * s * part : 0) : s * part);
     if (s == 1 || c < cost) {
       best = s;
       cost = c;
@@ -993,7 +1008,8 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   const int most = (int)std::min<size_t>(std::max<size_t>(fit, big::BM), (size_t)1 << 22);
   p.Vp = even_rounds(cdiv(V, big::BM), most / big::BM, cdiv((int)rows, big::BN), cdiv(d, big::BM)) *
          big::BM;
-  p.s_dh = big_splits((int)rows, d, p.Vp / BK);
+  p.s_dh = big_splits((int)rows, d, p.Vp / BK, false);
+  p.s_dw = big_splits(p.Vp, d, cdiv((int)rows, BK), true);
   size_t o = 0;
   const auto take = [&](size_t bytes) {
     const size_t at = o;
@@ -1004,6 +1020,7 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   p.o_hw = take(rows * cdiv(d, 256) * 512);
   p.o_d = take(rows * p.Vp * 2);
   p.o_dh = take((size_t)p.s_dh * rows * d * 4);
+  p.o_dw = take(p.s_dw == 1 ? 0 : (size_t)p.s_dw * p.Vp * d * 4);
   p.o_db = take((size_t)cdiv((int)rows, big::BN) * p.Vp * 4);
   p.total = o;
   return p;
@@ -1058,6 +1075,7 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   bf16_t* hw = reinterpret_cast<bf16_t*>(a.ws + p.o_hw);
   bf16_t* D = reinterpret_cast<bf16_t*>(a.ws + p.o_d);
   float* dh = reinterpret_cast<float*>(a.ws + p.o_dh);
+  float* dw = reinterpret_cast<float*>(a.ws + p.o_dw);
   float* db = reinterpret_cast<float*>(a.ws + p.o_db);
   const bf16_t* w = static_cast<const bf16_t*>(a.w);
   const bf16_t* h = static_cast<const bf16_t*>(a.h);
@@ -1069,7 +1087,7 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   const auto blocks = [](size_t n, size_t most) { return (unsigned)std::min((n + 255) / 256, most); };
   hipLaunchKernelGGL(k_row_parts, dim3(blocks(a.dw ? rows * a.d / 8 : rows, 512)), block, 0, st,
                      a.target, a.lse, a.dloss, a.V, a.T, a.d, h, part, a.dw ? hw : nullptr);
-  const bool one = p.Vp >= a.V;  // piece: its db is finished with dh
+  SliceSum sum_dh{}, sum_dw{};
   for (int v0 = 0; v0 < a.V; v0 += p.Vp) {
     const int nv = std::min(p.Vp, a.V - v0), Vp = cdiv(nv, big::BM) * big::BM;
     const bf16_t* wp = w + (size_t)v0 * a.d;
@@ -1082,24 +1100,34 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       else
         hipLaunchKernelGGL(k_dz_big<false>, g, block, 0, st, z);
     }
-    Finish f{dh, p.s_dh, a.T, a.d, static_cast<bf16_t*>(a.dh), 0, db, n_tt, Vp, nv,
-             a.db ? a.db + v0 : nullptr};
-    const unsigned db_blocks = a.db ? blocks(nv, ~(size_t)0) : 0;
-    if (db_blocks && !(one && a.dh))
-      hipLaunchKernelGGL(k_finish, dim3(db_blocks), block, 0, st, f, part);
     if (a.dw) {
-      const BigProdArgs q{hw, D, a.d, nv, a.T, part.G,
-                          static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d, 1, 0};
-      hipLaunchKernelGGL(k_prod_big<true>, grid((long)cdiv(nv, big::BN) * n_dt), block, 0, st, q);
+      bf16_t* out = static_cast<bf16_t*>(a.dw) + (size_t)v0 * a.d;
+      const dim3 g = grid((long)cdiv(nv, big::BN) * n_dt * p.s_dw);
+      BigProdArgs q{hw, D, a.d, nv, a.T, part.G, out, 1, 0};
+      if (p.s_dw == 1) {
+        hipLaunchKernelGGL((k_prod_big<true, false>), g, block, 0, st, q);
+      } else {
+        q.out = dw;
+        q.splits = p.s_dw;
+        hipLaunchKernelGGL((k_prod_big<true, true>), g, block, 0, st, q);
+        sum_dw = SliceSum{dw, p.s_dw, a.d, (size_t)nv * a.d, part.G, false, out, 0};
+        sum_dw.blocks = (int)blocks(sum_dw.n / 4, (size_t)1 << 22);
+      }
     }
     if (a.dh) {
       const BigProdArgs q{wp, D, a.d, a.T, nv, nullptr, dh, p.s_dh, v0 > 0};
-      hipLaunchKernelGGL(k_prod_big<false>, grid((long)n_tt * n_dt * p.s_dh), block, 0, st, q);
+      hipLaunchKernelGGL((k_prod_big<false, true>), grid((long)n_tt * n_dt * p.s_dh), block, 0, st,
+                         q);
+      if (v0 + p.Vp >= a.V) {
+        sum_dh = SliceSum{dh, p.s_dh, a.d, (size_t)a.T * a.d, part.gm, true,
+                          static_cast<bf16_t*>(a.dh), 0};
+        sum_dh.blocks = (int)blocks(sum_dh.n / 4, (size_t)1 << 22);
+      }
     }
-    if (a.dh && v0 + p.Vp >= a.V) {
-      f.dh_blocks = (int)blocks((size_t)a.T * a.d / 4, (size_t)1 << 22);
-      hipLaunchKernelGGL(k_finish, dim3(f.dh_blocks + (one ? db_blocks : 0)), block, 0, st, f, part);
-    }
+    // one launch a piece for what is left of it
+    const ColSum cols{db, n_tt, Vp, a.db ? nv : 0, part.G, a.db ? a.db + v0 : nullptr};
+    const unsigned n = sum_dh.blocks + sum_dw.blocks + cdiv(cols.n, 256);
+    if (n > 0) hipLaunchKernelGGL(k_finish, dim3(n), block, 0, st, sum_dh, sum_dw, cols);
   }
   return hipGetLastError();
 }

@@ -163,6 +163,8 @@ HEADS = [
     (BF16, 255, 2048, 1030, False),
     (BF16, 2049, 64, 2050, True),
     (BF16, 32000, 256, 256, False),
+    (BF16, 700, 64, 3000, True),    # few tiles of dw, its sums split over the rows
+    (BF16, 1025, 320, 1500, False),
 ]
 
 
