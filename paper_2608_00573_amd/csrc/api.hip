@@ -810,7 +810,8 @@ int trimmoe_balance_loss(int32_t dtype, int32_t n_experts, int32_t top_k, int32_
   if (rc) return rc;
   const bool bf16 = dtype == TRIMMOE_BF16;
   if (!aligned_rows(bf16, w_router) || !aligned_rows(bf16, h)) return TRIMMOE_ERR_SHAPE;
-  if ((rc = check_ws(workspace, workspace_bytes, balance_ws(dtype == TRIMMOE_BF16, n_experts, d_model, n_rows)))) return rc;
+  if ((rc = check_ws(workspace, workspace_bytes, balance_ws(bf16, n_experts, d_model, n_rows))))
+    return rc;
   BalanceArgs a{};
   a.bf16 = bf16;
   a.E = n_experts;
@@ -849,9 +850,11 @@ int trimmoe_balance_loss_backward(int32_t dtype, int32_t n_experts, int32_t top_
   int rc = balance_dims(dtype, n_experts, top_k, d_model, n_rows);
   if (rc) return rc;
   const bool bf16 = dtype == TRIMMOE_BF16;
-  for (const void* p : {w_router, h, static_cast<const void*>(dh), static_cast<const void*>(dw_router)})
+  for (const void* p :
+       {w_router, h, static_cast<const void*>(dh), static_cast<const void*>(dw_router)})
     if (!aligned_rows(bf16, p)) return TRIMMOE_ERR_SHAPE;
-  if ((rc = check_ws(workspace, workspace_bytes, balance_backward_ws(dtype == TRIMMOE_BF16, n_experts, d_model, n_rows))))
+  if ((rc = check_ws(workspace, workspace_bytes,
+                     balance_backward_ws(bf16, n_experts, d_model, n_rows))))
     return rc;
   if (!dh && !dw_router && !db_router) return TRIMMOE_OK;
   BalanceArgs a{};

@@ -188,10 +188,9 @@ __global__ __launch_bounds__(1024) void k_balance_loss(const float* part_p, cons
 // h: a block keeps its wavefronts' loads of several k-steps in flight.  A single
 // block goes on to the loss itself.
 template <typename TT, int ET, int RT, int NW>
-__global__ __launch_bounds__(64 * NW) void k_balance_forward(const TT* w, const float* b, const TT* h,
-                                                         const int16_t* target, int T, int E, int EP2,
-                                                         int k, int d, bool vec, float* prob,
-                                                         float* part_p, int32_t* part_c, LossOut out) {
+__global__ __launch_bounds__(64 * NW) void k_balance_forward(
+    const TT* w, const float* b, const TT* h, const int16_t* target, int T, int E, int EP2, int k,
+    int d, bool vec, float* prob, float* part_p, int32_t* part_c, LossOut out) {
   using F = Frag<TT>;
   using V = typename F::V;
   constexpr int U = ET <= 2 ? 4 : ET <= 8 ? 2 : 1;  // k-steps in flight

@@ -252,64 +252,87 @@ struct RowPart {
 };
 
 // The rows' parts, and hw = 2^-e h_t in panels, zeros in the rows that take no part (hw
-// may be NULL); 8 elements a thread.  Every block takes the largest weight of all
-// rows by itself: a launch of one block for it cost 8 us at 4096 rows.
+// may be NULL).  A block takes a run of rows, and the largest weight of all rows by
+// itself (a launch of one block for it cost 8 us at 4096 rows), its first loads of h in
+// flight meanwhile.
+constexpr int kPartBlocks = 1024, kPartRows = TRIMMOE_LOSS_MAX_ROWS / kPartBlocks;
 __global__ __launch_bounds__(256) void k_row_parts(const int32_t* target, const float* lse,
                                                    const float* dloss, int V, int T, int d,
                                                    const bf16_t* h, RowPart p, bf16_t* hw) {
-  __shared__ float s_m[4];
-  const auto row = [&](int t, int& y, float& L, float& g) {
-    y = target[t];
-    L = lse[t];
-    g = dloss[t];
-    if (y < 0 || y >= V || L == -__builtin_inff()) {
-      y = -1;
-      L = g = 0.f;
-    }
+  __shared__ float s_m[4], s_e[kPartRows];  // s_e: -1 for a row that takes no part
+  const int t0 = (int)((long)T * blockIdx.x / gridDim.x);
+  const int n = (int)((long)T * (blockIdx.x + 1) / gridDim.x) - t0;
+  // rows of d / 8 pieces of 16 bytes
+  const int pieces = d / 8, all = hw ? n * pieces : 0;
+  struct Pieces {
+    union {
+      uint4 v;
+      bf16_t e[8];
+      uint32_t w[4];
+    } x[4];
   };
+  const auto load = [&](Pieces& q, int i0) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i0 + 256 * k < all)
+        q.x[k].v = *reinterpret_cast<const uint4*>(h + (size_t)t0 * d + (size_t)8 * (i0 + 256 * k));
+  };
+  Pieces q;
+  load(q, threadIdx.x);
   float G = 0.f;
-#pragma unroll 4
-  for (int t = threadIdx.x; t < T; t += 256) {
-    int y;
-    float L, g;
-    row(t, y, L, g);
-    G = fmaxf(G, fabsf(g));
+  for (int t = threadIdx.x; t < T; t += 8 * 256) {
+    // (eight rows' loads in flight; behind the last row: it again)
+    int y[8];
+    float L[8], g[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int tk = min(t + 256 * k, T - 1);
+      y[k] = target[tk];
+      L[k] = lse[tk];
+      g[k] = dloss[tk];
+    }
+    sched_fence();
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      G = fmaxf(G, y[k] >= 0 && y[k] < V && L[k] != -__builtin_inff() ? fabsf(g[k]) : 0.f);
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) G = fmaxf(G, __shfl_xor(G, o));
   if ((threadIdx.x & 63) == 0) s_m[threadIdx.x >> 6] = G;
   __syncthreads();
   G = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-  const size_t at = (size_t)blockIdx.x * 256 + threadIdx.x, step = (size_t)256 * gridDim.x;
-  if (at == 0) *p.G = G;
-  const size_t n = hw ? (size_t)T * d / 8 : T;
-  for (size_t i = at; i < n; i += step) {
-    const int t = hw ? (int)(8 * i / d) : (int)i, c = hw ? (int)(8 * i - (size_t)t * d) : 0;
-    int y;
-    float L, g, m, e, gm;
-    row(t, y, L, g);
-    row_weight(g, G, m, e, gm);
-    if (c == 0) {
-      p.y[t] = y;
-      p.lse[t] = L;
-      p.m[t] = m;
-      p.e[t] = e;
-      p.gm[t] = gm;
-    }
-    if (!hw) continue;
-    union {
-      uint4 v;
-      bf16_t e[8];
-      uint32_t w[4];
-    } x;
-    x.v = make_uint4(0, 0, 0, 0);
-    if (y >= 0) {
-      x.v = *reinterpret_cast<const uint4*>(h + 8 * i);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.G = G;
+  for (int r = threadIdx.x; r < n; r += 256) {
+    const int t = t0 + r;
+    const int y = target[t];
+    const float L = lse[t];
+    const bool live = y >= 0 && y < V && L != -__builtin_inff();
+    float m, e, gm;
+    row_weight(live ? dloss[t] : 0.f, G, m, e, gm);
+    p.y[t] = live ? y : -1;
+    p.lse[t] = live ? L : 0.f;
+    p.m[t] = m;
+    p.e[t] = e;
+    p.gm[t] = gm;
+    s_e[r] = live ? e : -1.f;
+  }
+  __syncthreads();
+  for (int i0 = threadIdx.x; i0 < all; i0 += 4 * 256) {
+    Pieces next;
+    load(next, i0 + 4 * 256);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int i = i0 + 256 * k;
+      if (i >= all) break;
+      const int r = i / pieces, c = 8 * (i - r * pieces);
+      const float e = s_e[r];
 #pragma unroll
       for (int u = 0; u < 4; ++u)
-        x.w[u] = pack_bf16x2(bf2f(x.e[2 * u]) * e, bf2f(x.e[2 * u + 1]) * e);
+        q.x[k].w[u] = e < 0.f ? 0u
+                              : pack_bf16x2(bf2f(q.x[k].e[2 * u]) * e, bf2f(q.x[k].e[2 * u + 1]) * e);
+      *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t0 + r) * 256 + (c & 255)) = q.x[k].v;
     }
-    *reinterpret_cast<uint4*>(hw + ((size_t)(c >> 8) * T + t) * 256 + (c & 255)) = x.v;
+    q = next;
   }
 }
 
@@ -1085,7 +1108,7 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
   static_assert(big::THREADS == 256, "one block shape");
   // (grids hold fewer than 2^32 threads: what runs over T d elements strides)
   const auto blocks = [](size_t n, size_t most) { return (unsigned)std::min((n + 255) / 256, most); };
-  hipLaunchKernelGGL(k_row_parts, dim3(blocks(a.dw ? rows * a.d / 8 : rows, 512)), block, 0, st,
+  hipLaunchKernelGGL(k_row_parts, dim3((unsigned)std::min<size_t>(rows, kPartBlocks)), block, 0, st,
                      a.target, a.lse, a.dloss, a.V, a.T, a.d, h, part, a.dw ? hw : nullptr);
   SliceSum sum_dh{}, sum_dw{};
   for (int v0 = 0; v0 < a.V; v0 += p.Vp) {
@@ -1136,8 +1159,8 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
 
 size_t head_loss_ws(bool bf16, int V, int, int T) {
   const int rows = T > 0 ? T : 1;
-  return align256((size_t)rows * cdiv(V, bf16 ? exit_tile_rows(true, rows) : f32p::tile_a(f32p::tile_kind(V, T))) *
-                  sizeof(float2));
+  const int tile = bf16 ? exit_tile_rows(true, rows) : f32p::tile_a(f32p::tile_kind(V, T));
+  return align256((size_t)rows * cdiv(V, tile) * sizeof(float2));
 }
 size_t head_loss_backward_ws(bool bf16, int V, int d, int T) {
   if (!bf16) return back_plan(V, d, T).total;
