@@ -771,6 +771,10 @@ __global__ __launch_bounds__(T::THREADS) void k_exit_mma(ExitArgs a) {
   clock_mark(a.clk, false);
 }
 
+// The head loss on the exit head's tiles: per row and vocabulary tile the pair (max,
+// sum) of its logits in base 2.  d 4096, vocabulary 32000, 32 tokens: 40 us (the stream of
+// w); 333: 120 us (0.73 PFLOP/s, 1.5 rounds of tiles); d 768, vocabulary 32128, 4096
+// tokens: 190 us (1.06 PFLOP/s).
 template <class T>
 __global__ __launch_bounds__(T::THREADS) void k_loss_mma(ExitArgs a, int n_rows) {
   __shared__ __align__(16) char lds[DmaTile<T>::LDS];
@@ -1024,6 +1028,8 @@ __global__ __launch_bounds__(big::THREADS) void k_argmax_big(ExitArgs a) {
   exit_big<true>(a, lds);
 }
 
+// ... on the large-group core: 8192 tokens, d 4096, vocabulary 32000 1.51 ms (1.42
+// PFLOP/s), MFMA issue at the power-limited clock
 __global__ __launch_bounds__(big::THREADS) void k_loss_big(ExitArgs a, int n_rows) {
   __shared__ __align__(16) char lds[big::LDS];
   exit_big<false, true>(a, lds, n_rows);

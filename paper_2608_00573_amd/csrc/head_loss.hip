@@ -28,7 +28,9 @@ namespace {
 // ------------------------------------------------------- forward, fp32 --
 // A = w (vocabulary rows), B = h: a lane holds 16 vocabulary rows of a token, so the
 // pair of a token is a reduction over registers, two lane exchanges and the
-// wavefronts along the vocabulary.  A NaN logit makes the sum NaN.
+// wavefronts along the vocabulary.  A NaN logit makes the sum NaN.  Bound by the fp32
+// matrix rate or, for few tokens, by reading w: 3000 tokens, d 333, vocabulary 20001:
+// 400 us (101 TFLOP/s); 7 tokens, d 2048, vocabulary 151936: 298 us (4.2 TB/s).
 template <int KIND>
 __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_loss_f32(
     Operand<true> W, Operand<true> H, const float* bias, int n_vt, float2* part) {
@@ -89,7 +91,8 @@ __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_loss_f
 }
 
 // One wavefront a row: joins the pairs and takes the target's logit from one
-// more dot product (a gathered row of w; the pairs do not keep it).
+// more dot product (a gathered row of w; the pairs do not keep it).  Latency for few
+// rows (5 us at 32 of 4096), the gathered rows for many (8192 of 4096: 23 us).
 // BASE2: the pairs' maxima are in base 2 (z log2 e).
 template <typename T, bool BASE2>
 __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt, int V, int d, int T_,
@@ -146,7 +149,9 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt,
 // ------------------------------------------------------ backward, fp32 --
 // D of the tokens x a piece's columns (v0 ..; a row's elements behind the piece hold
 // anything), and per token tile the column sums of D (db).  A = w: a lane holds NA x 4
-// consecutive columns of a token.
+// consecutive columns of a token.  777 tokens, d 768, vocabulary 32128: 430 us (89
+// TFLOP/s; the two products 390 and 365), bound by the fp32 matrix rate and the last
+// round of 1757 tiles.
 template <int KIND>
 __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_dz_f32(
     Operand<true> W, Operand<true> H, const float* bias, const int32_t* target, const float* lse,
@@ -240,6 +245,14 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 //   * dh is summed in fp32 over pieces and K splits, then rounded once.
 // A tile's A rows are the columns of its result (4 consecutive ones a lane), so
 // that results leave the registers in 16-byte pieces without a turn through LDS.
+// Bound by MFMA issue at the clock that the power limit leaves: 8192 tokens, d 4096, a
+// piece of 16128 columns: D 0.90 ms (1.21 PFLOP/s), dw 0.89, dh 0.84.  With short
+// rows D's epilogue shows (256 exponentials a lane and 128 KB of stores a tile, which
+// only the next tile's first loads overlap): 4096 tokens, d 768, vocabulary 32128: D
+// 0.28 ms (0.72 PFLOP/s), dw 0.21, dh 0.18.
+// A piece's D is at most 256 MB, so that the products find part of it in the last-
+// level cache; pieces are whole rounds of the grid where that fits (2047 tokens, d
+// 2048, vocabulary 151936: 3.51 ms in equal pieces, 3.34 in whole rounds).
 
 // a row's part in the backward
 struct RowPart {
@@ -254,7 +267,7 @@ struct RowPart {
 // The rows' parts, and hw = 2^-e h_t in panels, zeros in the rows that take no part (hw
 // may be NULL).  A block takes a run of rows, and the largest weight of all rows by
 // itself (a launch of one block for it cost 8 us at 4096 rows), its first loads of h in
-// flight meanwhile.
+// flight meanwhile.  Bound by memory: 8192 rows of 4096 34 us (4 TB/s), 4096 of 768 10.
 constexpr int kPartBlocks = 1024, kPartRows = TRIMMOE_LOSS_MAX_ROWS / kPartBlocks;
 __global__ __launch_bounds__(256) void k_row_parts(const int32_t* target, const float* lse,
                                                    const float* dloss, int V, int T, int d,
@@ -713,6 +726,13 @@ __global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f
 // products in one pass over w (rows_grad.h; its rows are the vocabulary's, its
 // experts the tokens).  D lies [vocabulary row][token], in two bf16 parts where
 // the products' k-step leaves room for them (up to 16 rows).
+// us here and in the large tiles, d and vocabulary 4096 x 32000: 16 tokens 154 and 276,
+// 64 192 and 281; 2048 x 151936: 348 and 577, 437 and 603; 768 x 32128: 59 and 93, 94
+// and 96; 128 x 1000: 19 and 44, 26 and 45.
+// D comes out of the weight-streaming kernel where the exit head's rule takes it (up
+// to 16 rows with db, whose sum it then holds in one row of lanes): 154 us against
+// 186 in the tiles at 16 tokens of 4096 x 32000, 192 and 218 at 64.
+// 16 tokens of 4096 x 32000: D 45 us (5.8 TB/s), the products 102 (5.1 TB/s).
 // D: the first core's tiles of 128 vocabulary rows x 16 ET tokens (32 at least)
 template <class T, int ET>
 struct FewSrc {

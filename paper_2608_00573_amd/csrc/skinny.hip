@@ -575,6 +575,8 @@ __global__ __launch_bounds__(skinny::THREADS) void k_exit_skinny(ExitArgs a) {
   clock_mark(a.clk, false);
 }
 
+// ... of the head loss (every row is counted; a NaN logit is kept), bound by reading w:
+// d 4096, vocabulary 32000, 16 tokens 44 us (6.0 TB/s), 64 tokens 61 us (4.3 TB/s)
 template <int KIND>
 __global__ __launch_bounds__(skinny::THREADS) void k_loss_skinny(ExitArgs a, int n_x) {
   __shared__ __align__(16) char lds[skinny::LDS];
