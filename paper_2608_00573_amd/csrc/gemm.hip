@@ -1028,7 +1028,7 @@ __global__ __launch_bounds__(big::THREADS) void k_argmax_big(ExitArgs a) {
   exit_big<true>(a, lds);
 }
 
-// ... on the large-group core: 8192 tokens, d 4096, vocabulary 32000 1.51 ms (1.42
+// ... on the large-group core: 8192 tokens, d 4096, vocabulary 32000 1.52 ms (1.41
 // PFLOP/s), MFMA issue at the power-limited clock
 __global__ __launch_bounds__(big::THREADS) void k_loss_big(ExitArgs a, int n_rows) {
   __shared__ __align__(16) char lds[big::LDS];
