@@ -555,6 +555,101 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
   }
 }
 
+// D where 256 x 256 tiles would leave half of the CUs without one: the first core's
+// tiles of 128 x 128, the same outputs (db_part: a run of rows per column of
+// wavefronts).  A lane holds runs of 4 columns of a token, and the two halves of a
+// wavefront the neighbouring ones.
+using MidTile = Tile<128, 128, 1, 4, 2>;
+struct MidSrc {
+  using T = MidTile;
+  struct Desc {
+    int mt, nt;
+    static __device__ __forceinline__ Desc pick(bool c, const Desc& x, const Desc& y) {
+      return Desc{c ? x.mt : y.mt, c ? x.nt : y.nt};
+    }
+  };
+  const DzArgs& a;
+  const TileSched& S;
+
+  __device__ __forceinline__ Desc desc(int j) const {
+    int mt, nt, sp;
+    S.decode(j, mt, nt, sp);
+    return Desc{mt, nt};
+  }
+  __device__ __forceinline__ void rows(const Desc& d, int (&src)[T::A_PT]) const {
+    const int c0 = d.mt * T::BM, valid = min(T::BM, a.nv - c0);
+#pragma unroll
+    for (int i = 0; i < T::A_PT; ++i) src[i] = c0 + min(dma_row(i, T::ROWS_PER_PASS), valid - 1);
+  }
+  __device__ __forceinline__ void ptrs(DPtrs<T>& q, const Desc& d,
+                                       const int (&src)[T::A_PT]) const {
+    const int t0 = d.nt * T::BN;
+    make_dptrs<T>(q, a.w, src, a.h, nullptr, t0, min(T::BN, a.T - t0), a.d, 0);
+  }
+  __device__ __forceinline__ void epilogue(const Desc& d, Acc<T>& acc) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int wm = wave / T::GN, wn = wave % T::GN;
+    const int c0 = d.mt * T::BM, t0 = d.nt * T::BN;
+    int ty[T::TN];
+    float tL[T::TN], tm[T::TN], te[T::TN];
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = min(t0 + acc_col<T>(wn, j, lane), a.T - 1);
+      ty[j] = a.rows.y[t];
+      tL[j] = a.rows.lse[t];
+      tm[j] = a.rows.m[t];
+      te[j] = a.rows.e[t];
+    }
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+      float b[16], sum[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        b[r] = a.bias ? a.bias[min(c0 + acc_row<T>(wm, i, r, lane), a.nv - 1)] : 0.f;
+        sum[r] = 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < T::TN; ++j) {
+        const int t = t0 + acc_col<T>(wn, j, lane), y = ty[j] - a.v0;
+        const bool live = ty[j] >= 0 && t < a.T;
+        const float m = tm[j], g = m * te[j];
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += 4) {
+          const int c = c0 + acc_row<T>(wm, i, r0, lane);
+          float x[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float p = softmax_of(acc[i][j][r0 + r] + b[r0 + r], tL[j]);
+            p = c + r == y ? p - 1.f : p;
+            p = live && c + r < a.nv ? p : 0.f;
+            sum[r0 + r] = fmaf(g, p, sum[r0 + r]);
+            x[r] = p * m;
+          }
+          uint2 v;
+          v.x = pack_bf16x2(x[0], x[1]);
+          v.y = pack_bf16x2(x[2], x[3]);
+          if (t < a.T)
+            *reinterpret_cast<uint2*>(a.D + ((size_t)(c >> 8) * a.T + t) * 256 + (c & 255)) = v;
+        }
+      }
+      if (!a.db_part) continue;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const LanePair p = lanes_xor16(row16_sum(sum[r]));
+        if ((lane & 31) == 0)
+          a.db_part[(size_t)(d.nt * T::GN + wn) * a.Vp + c0 + acc_row<T>(wm, i, r, lane)] = p.a + p.b;
+      }
+    }
+  }
+};
+__global__ __launch_bounds__(MidTile::THREADS) void k_dz_mid(DzArgs a) {
+  __shared__ __align__(16) char lds[DmaTile<MidTile>::LDS];
+  TileSched S;
+  int ntiles;
+  if (!S.init(cdiv_d(a.nv, MidTile::BM), cdiv_d(a.T, MidTile::BN), 1, ntiles)) return;
+  dma_gemm_stream<MidTile>(lds, ntiles, a.d / BK, MidSrc{a, S});
+}
+
 struct BigProdArgs {
   const bf16_t* A;  // [K, M], DW: in panels
   const bf16_t* B;  // D in panels: [K, N] (DW) or [N, K]
@@ -694,6 +789,7 @@ __global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f
     const int c = b * 256 + threadIdx.x;
     if (c >= f.n) return;
     float s = 0.f;
+#pragma unroll 8
     for (int i = 0; i < f.n_tt; ++i) s += f.part[(size_t)i * f.ld + c];
     f.out[c] = s * *f.scale;
     return;
@@ -1002,6 +1098,7 @@ FewPlan few_plan(int V, int d, int T) {
 
 struct BackPlanBf16 {
   int Vp;          // columns of a piece (a multiple of the tile)
+  bool mid;        // D in tiles of 128 x 128
   int s_dh, s_dw;  // K splits of the two products
   size_t o_rows, o_hw, o_d, o_dh, o_dw, o_db, total;
 };
@@ -1044,6 +1141,11 @@ int even_rounds(int all, int most, int n_tt, int n_dt) {
   return per;
 }
 
+// D of up to so many 256 x 256 tiles goes in tiles of 128 x 128.  us of the whole
+// gradient, there and in the large tiles (tokens x vocabulary x d): 16 tiles, 300 x 2000
+// x 768: 59 and 78; 58, 397 x 7286 x 2560: 111 and 148; 126, 228 x 32128 x 768: 109 and
+// 118; 189, 600 x 16000 x 2048: 191 and 185; 252, 1000 x 16000 x 1024: 149 and 136.
+constexpr int kMidTiles = 128;
 BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   BackPlanBf16 p;
   const size_t rows = T > 0 ? T : 1;
@@ -1051,6 +1153,7 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   const int most = (int)std::min<size_t>(std::max<size_t>(fit, big::BM), (size_t)1 << 22);
   p.Vp = even_rounds(cdiv(V, big::BM), most / big::BM, cdiv((int)rows, big::BN), cdiv(d, big::BM)) *
          big::BM;
+  p.mid = (long)(p.Vp / big::BM) * cdiv((int)rows, big::BN) <= kMidTiles;
   p.s_dh = big_splits((int)rows, d, p.Vp / BK, false);
   p.s_dw = big_splits(p.Vp, d, cdiv((int)rows, BK), true);
   size_t o = 0;
@@ -1064,7 +1167,8 @@ BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   p.o_d = take(rows * p.Vp * 2);
   p.o_dh = take((size_t)p.s_dh * rows * d * 4);
   p.o_dw = take(p.s_dw == 1 ? 0 : (size_t)p.s_dw * p.Vp * d * 4);
-  p.o_db = take((size_t)cdiv((int)rows, big::BN) * p.Vp * 4);
+  p.o_db = take((size_t)(p.mid ? cdiv((int)rows, MidTile::BN) * MidTile::GN
+                               : cdiv((int)rows, big::BN)) * p.Vp * 4);
   p.total = o;
   return p;
 }
@@ -1138,7 +1242,11 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       const DzArgs z{wp, h, a.b ? a.b + v0 : nullptr, part, nv, v0, a.d, a.T, Vp, D,
                      a.db ? db : nullptr};
       const dim3 g = grid((long)(Vp / big::BM) * n_tt);
-      if (a.b || a.db)
+      if (p.mid)
+        hipLaunchKernelGGL(k_dz_mid,
+                           grid((long)cdiv(nv, MidTile::BM) * cdiv(a.T, MidTile::BN)),
+                           dim3(MidTile::THREADS), 0, st, z);
+      else if (a.b || a.db)
         hipLaunchKernelGGL(k_dz_big<true>, g, block, 0, st, z);
       else
         hipLaunchKernelGGL(k_dz_big<false>, g, block, 0, st, z);
@@ -1168,7 +1276,7 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       }
     }
     // one launch a piece for what is left of it
-    const ColSum cols{db, n_tt, Vp, a.db ? nv : 0, part.G, a.db ? a.db + v0 : nullptr};
+    const ColSum cols{db, p.mid ? cdiv(a.T, MidTile::BN) * MidTile::GN : n_tt, Vp, a.db ? nv : 0, part.G, a.db ? a.db + v0 : nullptr};
     const unsigned n = sum_dh.blocks + sum_dw.blocks + cdiv(cols.n, 256);
     if (n > 0) hipLaunchKernelGGL(k_finish, dim3(n), block, 0, st, sum_dh, sum_dw, cols);
   }

@@ -163,6 +163,9 @@ HEADS = [
     (BF16, 255, 2048, 1030, False),
     (BF16, 2049, 64, 2050, True),
     (BF16, 32000, 256, 256, False),
+    (BF16, 33100, 128, 300, True),  # large tiles of D, ragged in both directions
+    (BF16, 4999, 192, 1999, False),
+    (BF16, 5121, 64, 2049, True),
     (BF16, 700, 64, 3000, True),    # few tiles of dw, its sums split over the rows
     (BF16, 1025, 320, 1500, False),
 ]

@@ -1,5 +1,5 @@
 """Generated-code checks of the training losses' kernels (CPU: hipcc
-cross-compiles), with the checkers of the GEMM core's: their slice loops do not
+cross-compiles), as of the GEMM cores: their slice loops do not
 spill, the large-group kernels' accumulators are not touched before the MFMAs
 that write them (inline asm, whose latency the compiler does not see) have
 finished, LDS reads land before their registers are used, and no copy into LDS
@@ -13,7 +13,7 @@ from test_gemm_codegen import (_compile, _function, _hazards, _lds_races, _loops
                                _mfma_lds_hazards, _part_races, pytestmark)  # noqa: F401
 
 SOURCES = {
-    "head_loss.hip": ["k_dz_big", "k_prod_big", "k_dz_few", "k_few_grad", "k_loss_f32", "k_dz_f32"],
+    "head_loss.hip": ["k_dz_big", "k_prod_big", "k_dz_mid", "k_dz_few", "k_few_grad", "k_loss_f32", "k_dz_f32"],
     "products.hip": ["k_prod_f32"],
     "gemm.hip": ["k_loss_big", "k_loss_mma"],
     "skinny.hip": ["k_loss_skinny", "k_dz_skinny"],
