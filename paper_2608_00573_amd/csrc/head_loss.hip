@@ -822,9 +822,9 @@ __global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f
 // products in one pass over w (rows_grad.h; its rows are the vocabulary's, its
 // experts the tokens).  D lies [vocabulary row][token], in two bf16 parts where
 // the products' k-step leaves room for them (up to 16 rows).
-// us here and in the large tiles, d and vocabulary 4096 x 32000: 16 tokens 154 and 276,
-// 64 192 and 281; 2048 x 151936: 348 and 577, 437 and 603; 768 x 32128: 59 and 93, 94
-// and 96; 128 x 1000: 19 and 44, 26 and 45.
+// us here and in the kernels of more tokens, d and vocabulary 4096 x 32000: 16 tokens
+// 154 and 276; 2048 x 151936: 17 tokens 402 and 597, 64 464 and 617; 768 x 32128: 45 and
+// 77, 68 and 83; 128 x 1000: 20 and 36, 25 and 38.
 // D comes out of the weight-streaming kernel where the exit head's rule takes it (up
 // to 16 rows with db, whose sum it then holds in one row of lanes): 154 us against
 // 186 in the tiles at 16 tokens of 4096 x 32000, 192 and 218 at 64.
@@ -1087,16 +1087,21 @@ hipError_t backward_f32(const HeadLossArgs& a, hipStream_t st) {
 }
 
 // bf16, up to kSkinnyTokens rows
-constexpr int few_cols(int et) { return et == 4 ? 2 : 4; }  // columns / 64 of a block of both products
 struct FewPlan {
   int et, R;  // token tiles of 16, slices of dh
+  int cols;   // columns / 64 of a block of both products
   size_t o_dh, total;
 };
 
 FewPlan few_plan(int V, int d, int T) {
   FewPlan p;
   p.et = T <= 16 ? 1 : T <= 32 ? 2 : 4;
-  const int n_c = cdiv(d, 64 * few_cols(p.et)), n_t = cdiv(V, kRowTile);
+  const int n_t = cdiv(V, kRowTile);
+  // Blocks of 256 columns where each has 12 tiles of rows and more to make up for its
+  // start (17 tokens of 2048 x 151936: 399 us, 421 in 128 columns; 768 x 32128: 52 and
+  // 45); with 64 tokens they take 296 registers (768 x 32128: 96, 65 in 128 columns).
+  p.cols = p.et < 4 && (long)n_t * cdiv(d, 256) >= 12 * 2 * kCu ? 4 : 2;
+  const int n_c = cdiv(d, 64 * p.cols);
   p.R = std::max(1, std::min(n_t, cdiv(2 * kCu, n_c)));
   const size_t rows = cdiv(V, 128) * (size_t)128;
   p.o_dh = align256(rows * 32 * p.et * (p.et == 1 ? 2 : 1));
@@ -1195,7 +1200,6 @@ hipError_t loss_bf16(const HeadLossArgs& a, hipStream_t st) {
 
 template <int ET>
 hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st) {
-  constexpr int CW = few_cols(ET);
   using Tl = Tile<128, ET == 4 ? 64 : 32, 1, 4, 1>;
   const FewArgs f{static_cast<const bf16_t*>(a.w), static_cast<const bf16_t*>(a.h), a.b, a.target,
                   a.lse, a.dloss, a.V, a.d, a.T, reinterpret_cast<bf16_t*>(a.ws), a.db};
@@ -1207,9 +1211,14 @@ hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st)
     hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS),
                        0, st, f);
   }
-  if (a.dw || a.dh)
-    hipLaunchKernelGGL((k_few_grad<ET, CW>), dim3(cdiv(a.d, 64 * CW), p.R), dim3(256), 0, st, f,
-                       static_cast<bf16_t*>(a.dw), part);
+  if (a.dw || a.dh) {
+    if (const dim3 g(cdiv(a.d, 64 * p.cols), p.R); p.cols == 2)
+      hipLaunchKernelGGL((k_few_grad<ET, 2>), g, dim3(256), 0, st, f, static_cast<bf16_t*>(a.dw),
+                         part);
+    else if constexpr (ET < 4)
+      hipLaunchKernelGGL((k_few_grad<ET, 4>), g, dim3(256), 0, st, f, static_cast<bf16_t*>(a.dw),
+                         part);
+  }
   if (a.dh)
     hipLaunchKernelGGL(k_few_finish, dim3(cdiv(a.T * a.d, 128)), dim3(256), 0, st, f, part, p.R,
                        static_cast<bf16_t*>(a.dh));
