@@ -1004,8 +1004,8 @@ BackPlan back_plan(int V, int d, int T) {
   const int most = (int)std::min<size_t>(std::max<size_t>(fit, BA), (size_t)1 << 30);
   const int n_pieces = cdiv(V, most);
   p.Vc = cdiv(cdiv(V, n_pieces), BA) * BA;
-  p.s_dh = product_splits(f32p::product_kind(false, true, d, T), d, T, p.Vc);
-  p.s_dw = product_splits(f32p::product_kind(false, false, d, p.Vc), d, p.Vc, T);
+  p.s_dh = product_splits(f32p::product_kind(true, d, T), d, T, p.Vc);
+  p.s_dw = product_splits(f32p::product_kind(false, d, p.Vc), d, p.Vc, T);
   p.direct_dh = n_pieces == 1 && p.s_dh == 1;
   size_t o = 0;
   const auto take = [&](size_t bytes) {

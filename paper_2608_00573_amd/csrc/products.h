@@ -64,10 +64,10 @@ inline int tile_kind(int a, int b) {
   if (k == kNarrow || tiles(k, a, b) > 128) return k;
   return k != kSquare || tiles(k, a, b) <= 64 ? kSmall : kFew;
 }
-// ... of launch_product: the streams take A row-contiguous and B K-contiguous
-inline int product_kind(bool a_k, bool b_k, int a, int b) {
+// ... of launch_product: the streams take a K-contiguous B
+inline int product_kind(bool b_k, int a, int b) {
   const int k = shape_kind(a, b);
-  return k >= kFew && (a_k || !b_k) ? kSquare : k;
+  return k >= kFew && !b_k ? kSquare : k;
 }
 
 // f(integral constant of the kind)
@@ -445,8 +445,8 @@ inline int product_splits(int kind, int a, int b, int K) {
 
 // out [B.rows, A.rows] = B A^T in `splits` runs of K, one slice of partials per run,
 // added to what the slices hold (`add`)
-template <bool AK, bool BKC>
-hipError_t launch_product(const Operand<AK>& A, const Operand<BKC>& B, int splits, bool add,
+template <bool BKC>
+hipError_t launch_product(const Operand<false>& A, const Operand<BKC>& B, int splits, bool add,
                           float* out, hipStream_t st);
 
 // out = sum of the S slices of n partials

@@ -8,9 +8,9 @@ namespace trimmoe {
 
 // B A^T over split blockIdx.z of K into the split's slice of out, added to what is
 // there (`add`): a lane holds 4 consecutive elements of a row
-template <int KIND, bool AK, bool BKC>
+template <int KIND, bool BKC>
 __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_prod_f32(
-    Operand<AK> A, Operand<BKC> B, int k_per, float* out, int add) {
+    Operand<false> A, Operand<BKC> B, int k_per, float* out, int add) {
   using namespace f32p;
   using T = Tile<KIND>;
   __shared__ __align__(16) float lds[T::FLOATS];
@@ -27,7 +27,6 @@ __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_prod_f
     const int b = t.row_b(j);
     if (j >= t.nb || b >= B.rows) continue;
     if constexpr (T::STREAM) {
-      static_assert(!AK, "rows of A in the stream's order");
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         // elements `at` .. at + NA - 1; those before `a` are another lane's
@@ -66,16 +65,16 @@ __global__ __launch_bounds__(256) void k_sum_parts(const float* part, int S, siz
   }
 }
 
-template <bool AK, bool BKC>
-hipError_t launch_product(const Operand<AK>& A, const Operand<BKC>& B, int splits, bool add,
+template <bool BKC>
+hipError_t launch_product(const Operand<false>& A, const Operand<BKC>& B, int splits, bool add,
                           float* out, hipStream_t st) {
   using namespace f32p;
   const int k_per = cdiv(cdiv(A.K, splits), KS) * KS;
-  with_kind(product_kind(AK, BKC, A.rows, B.rows), [&](auto kind) {
+  with_kind(product_kind(BKC, A.rows, B.rows), [&](auto kind) {
     using T = Tile<kind>;
-    if constexpr (kind != kSmall && (!T::STREAM || (!AK && BKC))) {
+    if constexpr (kind != kSmall && (!T::STREAM || BKC)) {
       const dim3 grid((unsigned)cdiv(A.rows, T::A) * cdiv(B.rows, T::B), 1, splits);
-      hipLaunchKernelGGL((k_prod_f32<kind, AK, BKC>), grid, dim3(THREADS), 0, st, A, B, k_per, out,
+      hipLaunchKernelGGL((k_prod_f32<kind, BKC>), grid, dim3(THREADS), 0, st, A, B, k_per, out,
                          add ? 1 : 0);
     }
   });
@@ -89,9 +88,9 @@ hipError_t launch_sum_parts(const float* part, int S, size_t n, float* out, hipS
 }
 
 // the gradients of the rows (D w) and of the weights (D^T h)
-template hipError_t launch_product<false, true>(const Operand<false>&, const Operand<true>&, int, bool,
-                                                float*, hipStream_t);
-template hipError_t launch_product<false, false>(const Operand<false>&, const Operand<false>&, int,
-                                                 bool, float*, hipStream_t);
+template hipError_t launch_product<true>(const Operand<false>&, const Operand<true>&, int, bool,
+                                         float*, hipStream_t);
+template hipError_t launch_product<false>(const Operand<false>&, const Operand<false>&, int, bool,
+                                          float*, hipStream_t);
 
 }  // namespace trimmoe

@@ -870,6 +870,32 @@ def test_balanced_routers_take_the_gradients_steps(dtype):
     _within(b, want, 2 * U * (np.abs(want) + lr * np.abs(db.double().cpu().numpy())), "b")
 
 
+@pytest.mark.parametrize("dtype,V,d,Q", [(F32, 3000, 96, 150), (BF16, 3000, 128, 40),
+                                         (BF16, 3000, 128, 500)])
+def test_losses_on_two_streams_at_once(dtype, V, d, Q):
+    # calls in flight together share nothing: the results of each are those of it alone
+    heads = [Head(90 + i, dtype, V, d, Q).dev() for i in range(2)]
+    routers = [Router(95 + i, dtype, 8, 2, d, Q).dev() for i in range(2)]
+
+    def run(i, st):
+        loss, lse = heads[i].forward(st)
+        b = routers[i].forward(st)
+        return [loss, lse, *heads[i].backward(lse, stream=st), *b,
+                *routers[i].backward(b[3], b[1], stream=st)]
+
+    alone = [run(i, None) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    both = [[], []]
+    for _ in range(4):
+        for i in range(2):
+            both[i].append(run(i, streams[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for got in both[i]:
+            assert all(torch.equal(x, y) for x, y in zip(got, alone[i]))
+
+
 def test_a_stream_of_another_device_is_refused():
     class Other:
         device = torch.device("cuda", 1)
