@@ -75,8 +75,7 @@ constexpr int few_parts() {
   return ET == 1 ? 2 : 1;
 }
 
-// D of up to 16 rows of h, or of up to 64 without db, in one stream of w
-// (skinny.hip)
-hipError_t launch_dz_skinny(const FewArgs& a, int n_cu, hipStream_t st);
+// D in rows of 16 et tokens in one stream of w (skinny.hip): et 1 or, without db, 4
+hipError_t launch_dz_skinny(const FewArgs& a, int et, int n_cu, hipStream_t st);
 
 }  // namespace trimmoe

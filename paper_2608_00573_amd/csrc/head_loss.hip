@@ -1204,8 +1204,10 @@ hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st)
   const FewArgs f{static_cast<const bf16_t*>(a.w), static_cast<const bf16_t*>(a.h), a.b, a.target,
                   a.lse, a.dloss, a.V, a.d, a.T, reinterpret_cast<bf16_t*>(a.ws), a.db};
   float* part = a.dh ? reinterpret_cast<float*>(a.ws + p.o_dh) : nullptr;
-  if (exit_streams(true, true, a.T, a.V, a.d) && (ET == 1 || !a.db)) {
-    const hipError_t e = launch_dz_skinny(f, a.n_cu, st);
+  // (17 to 32 rows have no stream: the exit head's rule takes theirs for heads of up to 16
+  // vocabulary rows only, a few units)
+  if (ET != 2 && exit_streams(true, true, a.T, a.V, a.d) && (ET == 1 || !a.db)) {
+    const hipError_t e = launch_dz_skinny(f, ET, a.n_cu, st);
     if (e != hipSuccess) return e;
   } else {
     hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS),

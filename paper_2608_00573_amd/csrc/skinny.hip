@@ -704,17 +704,19 @@ hipError_t launch_loss_skinny(const ExitArgs& a, int n_rows, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_dz_skinny(const FewArgs& a, int n_cu, hipStream_t st) {
+hipError_t launch_dz_skinny(const FewArgs& a, int et, int n_cu, hipStream_t st) {
   const dim3 grid(n_cu), block(skinny::THREADS);
   const bool low = stream_kind(a.d / skinny::KSTEP) == kShort;
-  if (a.T <= 16 && low)
+  if (et == 1 && low)
     hipLaunchKernelGGL((k_dz_skinny<1, kShort>), grid, block, 0, st, a);
-  else if (a.T <= 16)
+  else if (et == 1)
     hipLaunchKernelGGL((k_dz_skinny<1, kLong>), grid, block, 0, st, a);
-  else if (low)  // (exit_streams: never 17 to 32 rows)
+  else if (et == 4 && low)
     hipLaunchKernelGGL((k_dz_skinny<4, kShort>), grid, block, 0, st, a);
-  else
+  else if (et == 4)
     hipLaunchKernelGGL((k_dz_skinny<4, kMid>), grid, block, 0, st, a);
+  else
+    return hipErrorInvalidValue;  // (no other width of D's rows)
   return hipGetLastError();
 }
 

@@ -186,6 +186,31 @@ def test_head_gradients_match_oracle(dtype, V, d, Q, bias):
     c.check_backward(c.backward(lse))
 
 
+# heads of no more than one group of 16 vocabulary rows, at every count of token tiles
+SMALL_HEADS = [(V, d, Q) for V, d in ((2, 64), (10, 64), (16, 2048), (17, 128), (16, 1088))
+               for Q in (1, 16, 17, 20, 32, 33, 48, 64, 65)]
+
+
+@pytest.mark.parametrize("V,d,Q", SMALL_HEADS)
+def test_bf16_gradients_of_small_heads(V, d, Q):
+    log(f"[losses] small head backward V={V} d={d} Q={Q}")
+    for bias in (False, True):
+        c = Head(42, BF16, V, d, Q, bias).dev()
+        loss, lse = c.forward()
+        c.check_forward(loss, lse)
+        c.check_backward(c.backward(lse))
+    # (a bias whose gradient is not asked for)
+    dims = (abi._dtype_code(c.Hd), V, d, Q)
+    ws = abi._loss_ws("trimmoe_head_cross_entropy_backward", dims, c.Hd.device)
+    dh, dw = torch.empty_like(c.Hd), torch.empty_like(c.Wd)
+    rc = abi.lib().trimmoe_head_cross_entropy_backward(
+        *dims, c.Wd.data_ptr(), c.bd.data_ptr(), c.Hd.data_ptr(), c.yd.data_ptr(), lse.data_ptr(),
+        c.gd.data_ptr(), dh.data_ptr(), dw.data_ptr(), None, ws.data_ptr(), ws.numel(),
+        abi._stream_handle(None))
+    assert rc == 0
+    c.check_backward((dh, dw, None))
+
+
 @pytest.mark.parametrize("dtype,V,d,Q", [(F32, 20001, 64, 4100), (BF16, 40001, 64, 4100)])
 def test_head_gradients_over_several_pieces(dtype, V, d, Q):
     # more of D than a piece holds: dh is summed over the pieces
