@@ -109,12 +109,25 @@ def train_softmax_heads(hs, target, w_head: torch.Tensor, epochs: int, lr: float
     return out
 
 
+def _routed_again(prob: torch.Tensor, target: torch.Tensor):
+    """The routed slots that target [Q, k] has, filled anew by probabilities prob
+    [Q, E]: a row's n slots get its n likeliest experts (ties: the lower one)."""
+    live = (target >= 0) & (target < prob.shape[1])
+    best = torch.sort(prob, dim=1, descending=True, stable=True).indices
+    rank = (live.cumsum(1) - 1).clamp_min(0)
+    return torch.where(live, best.gather(1, rank), -1).to(torch.int16)
+
+
 def balance_routers(routers, hs, targets, epochs: int, lr: float):
     """Gradient descent on the balance loss of each router (w [E, d], bias fp32
     [E]) over the rows it routed, hs[l] [Q, d] with the recorded experts
-    targets[l] int16 [Q, k]: probabilities move away from the experts that took
-    more than their share.  Weights are kept in fp32 and used in the rows'
-    dtype; returns [(w, b fp32 [E], losses fp32 [epochs], counts int32 [E + 1])]."""
+    targets[l] int16 [Q, k]: probabilities move away from the experts that take
+    more than their share.  The counts have no derivative but follow the router:
+    the first step takes the recorded experts, every later one routes the rows
+    again with the router that it starts from (the slots a row has, no others).
+    Weights are kept in fp32 and used in the rows' dtype; returns [(w, b fp32
+    [E], losses fp32 [epochs], counts int32 [E + 1])]: the loss that each step
+    starts from and the last step's counts."""
     out = []
     for (w0, b0), h, t in zip(routers, hs, targets):
         w32, b = w0.float().clone(), b0.clone()
@@ -124,6 +137,9 @@ def balance_routers(routers, hs, targets, epochs: int, lr: float):
         for e in range(epochs):
             w = w32.to(h.dtype)
             loss, counts, _, prob = abi.trimmoe_balance_loss(w, h, t, b)
+            if e > 0:  # (t: the last step's experts, prob: this step's router)
+                t = _routed_again(prob, t)
+                loss, counts, _, prob = abi.trimmoe_balance_loss(w, h, t, b)
             losses[e] = loss[0]
             _, dw, db = abi.trimmoe_balance_loss_backward(w, h, t, prob, counts, one, want_dh=False)
             w32.add_(dw, alpha=-lr)

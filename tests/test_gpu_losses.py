@@ -895,6 +895,35 @@ def test_balanced_routers_take_the_gradients_steps(dtype):
     _within(b, want, 2 * U * (np.abs(want) + lr * np.abs(db.double().cpu().numpy())), "b")
 
 
+@pytest.mark.parametrize("dtype,E,k", [(F32, 8, 2), (BF16, 60, 4)])
+def test_balanced_routers_route_again_at_every_step(dtype, E, k):
+    # four steps are the four steps written out, each with the experts of its own router;
+    # rows keep the number of their slots, and inactive ones have none
+    r = Router(86, dtype, E, k, 128, 150).dev()
+    lr, one = 4.0, torch.ones(1, device=DEV)
+    (w, b, losses, counts), = offline.balance_routers([(r.Wd, r.bd)], [r.Hd], [r.td], 4, lr)
+    live = (r.t >= 0) & (r.t < E)
+    w32, b32, t, moved = r.Wd.float().clone(), r.bd.clone(), r.td, 0
+    for e in range(4):
+        we = w32.to(dtype)
+        if e > 0:
+            p = abi.trimmoe_balance_loss(we, r.Hd, r.td, b32)[3].cpu().numpy()
+            best = np.argsort(-p, axis=1, kind="stable")
+            new = np.full_like(r.t, -1)
+            for q in range(len(new)):
+                new[q, live[q]] = best[q, :live[q].sum()]
+            moved += int((np.sort(new) != np.sort(t.cpu().numpy())).sum())
+            t = torch.from_numpy(new).to(DEV)
+        loss, own, _, prob = abi.trimmoe_balance_loss(we, r.Hd, t, b32)
+        assert losses[e] == loss[0]
+        _, dw, db = abi.trimmoe_balance_loss_backward(we, r.Hd, t, prob, own, one)
+        w32.add_(dw, alpha=-lr)
+        b32.add_(db, alpha=-lr)
+    assert torch.equal(counts, own) and moved > 0
+    # (the same calls on the same values)
+    assert torch.equal(w, w32.to(dtype)) and torch.equal(b, b32)
+
+
 @pytest.mark.parametrize("dtype,V,d,Q", [(F32, 3000, 96, 150), (BF16, 3000, 128, 40),
                                          (BF16, 3000, 128, 500)])
 def test_losses_on_two_streams_at_once(dtype, V, d, Q):

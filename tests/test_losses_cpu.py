@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from oracle import losses as X
-from paper_2608_00573_amd import abi
+from paper_2608_00573_amd import abi, offline
 
 NULL, SHAPE, DTYPE, WORKSPACE = -1, -2, -3, -6
 
@@ -198,3 +198,74 @@ def test_wrappers_refuse_host_and_mismatched_tensors():
         abi.trimmoe_head_cross_entropy(w.half(), h.half(), y)
     with pytest.raises(ValueError):
         abi.trimmoe_balance_loss(w, h, y)                          # target not [Q, k] int16
+
+
+# ---------------------------------------------------------- offline descent --
+@pytest.fixture
+def oracle_losses(monkeypatch):
+    """offline.balance_routers on the CPU, its losses and gradients by the oracle."""
+    def forward(w, h, t, b=None):
+        l, c, s, p = X.balance_loss(w.numpy(), h.numpy(), t.numpy(), None if b is None else b.numpy())
+        return (torch.tensor([l]).float(), torch.from_numpy(c).int(), torch.from_numpy(s).float(),
+                torch.from_numpy(p).float())
+
+    def backward(w, h, t, prob, counts, dloss, want_dh=True):
+        # (dz from prob alone: the bias is in it)
+        E, cn = w.shape[0], counts.numpy().astype(np.float64)
+        p, c = prob.double().numpy(), cn[:E]
+        live = ((t >= 0) & (t < E)).any(1).numpy()
+        dz = float(dloss) * E / (c.sum() * cn[E]) * p * (c - (p @ c)[:, None]) * live[:, None]
+        f = lambda x: torch.from_numpy(x).float()
+        return None, f(dz.T @ h.double().numpy()), f(dz.sum(0))
+
+    monkeypatch.setattr(abi, "trimmoe_balance_loss", forward)
+    monkeypatch.setattr(abi, "trimmoe_balance_loss_backward", backward)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+
+
+def _skewed_router(E=8, k=2, d=16, Q=512):
+    r = _rng(7)
+    w = torch.from_numpy(r.normal(size=(E, d)).astype(np.float32) * d ** -0.5)
+    b = torch.from_numpy((-0.5 * np.log(1 + np.arange(E))).astype(np.float32))
+    h = torch.from_numpy(r.normal(size=(Q, d)).astype(np.float32))
+    t = np.argsort(-X.logits(w.numpy(), h.numpy(), b.numpy()), axis=1, kind="stable")[:, :k]
+    t[r.random(Q) < 0.1] = -1                       # inactive rows
+    t[3], t[4] = [-1, t[3, 0]], [t[4, 0], E]        # rows of fewer slots
+    return w, b, h, torch.from_numpy(t.astype(np.int16))
+
+
+def _load(w, b, h, t):
+    """Slots per expert of the router (w, b) over the rows that t routes."""
+    E = w.shape[0]
+    order = np.argsort(-X.logits(w.numpy(), h.numpy(), b.numpy()), axis=1, kind="stable")
+    live = ((t >= 0) & (t < E)).numpy().sum(1)
+    return np.bincount(np.concatenate([o[:n] for o, n in zip(order, live)]), minlength=E)
+
+
+def test_balanced_routers_balance_the_load_they_make(oracle_losses):
+    # a step moves probability away from the experts that the router of that step loads
+    # most: over many steps the load itself becomes even and stays so
+    w, b, h, t = _skewed_router()
+    start = _load(w, b, h, t)
+    assert start.max() > 1.5 * start.mean()
+    for epochs in (20, 100):
+        (w1, b1, losses, counts), = offline.balance_routers([(w, b)], [h], [t], epochs, 0.5)
+        load = _load(w1, b1, h, t)
+        assert load.sum() == start.sum() and load.max() / load.mean() - 1 < (start.max() / start.mean() - 1) / 2, \
+            (epochs, load)
+
+
+def test_balanced_routers_report_the_loss_of_their_own_routing(oracle_losses):
+    w, b, h, t = _skewed_router()
+    live = ((t >= 0) & (t < 8)).any(1)
+    whole = [offline.balance_routers([(w, b)], [h], [t], n, 0.5)[0] for n in range(5)]
+    for n in range(1, 5):
+        # step n starts from the router that n - 1 steps end with
+        w0, b0 = whole[n - 1][:2]
+        load = _load(w0, b0, h, t)
+        losses, counts = whole[n][2], whole[n][3]
+        assert counts.tolist() == [*load.tolist(), int(live.sum())]
+        p = X.balance_loss(w0.numpy(), h.numpy(), t.numpy(), b0.numpy())[2]
+        want = 8 * float(load @ p) / (float(load.sum()) * int(live.sum()))
+        assert abs(float(losses[n - 1]) - want) <= 4 * 2.0 ** -24 * want  # rounded to fp32
+        assert torch.equal(whole[4][2][:n], losses)
