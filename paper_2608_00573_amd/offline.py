@@ -120,7 +120,7 @@ def _routed_again(prob: torch.Tensor, target: torch.Tensor):
 
 def balance_routers(routers, hs, targets, epochs: int, lr: float):
     """Gradient descent on the balance loss of each router (w [E, d], bias fp32
-    [E]) over the rows it routed, hs[l] [Q, d] with the recorded experts
+    [E] or None: from zero) over the rows it routed, hs[l] [Q, d] with the recorded experts
     targets[l] int16 [Q, k]: probabilities move away from the experts that take
     more than their share.  The counts have no derivative but follow the router:
     the first step takes the recorded experts, every later one routes the rows
@@ -130,7 +130,8 @@ def balance_routers(routers, hs, targets, epochs: int, lr: float):
     starts from and the last step's counts."""
     out = []
     for (w0, b0), h, t in zip(routers, hs, targets):
-        w32, b = w0.float().clone(), b0.clone()
+        w32 = w0.float().clone()
+        b = b0.clone() if b0 is not None else w32.new_zeros(w0.shape[0])
         one = torch.ones(1, dtype=torch.float32, device=h.device)
         losses = torch.zeros(epochs, dtype=torch.float32, device=h.device)
         counts = torch.zeros(w0.shape[0] + 1, dtype=torch.int32, device=h.device)

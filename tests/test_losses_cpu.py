@@ -269,3 +269,10 @@ def test_balanced_routers_report_the_loss_of_their_own_routing(oracle_losses):
         want = 8 * float(load @ p) / (float(load.sum()) * int(live.sum()))
         assert abs(float(losses[n - 1]) - want) <= 4 * 2.0 ** -24 * want  # rounded to fp32
         assert torch.equal(whole[4][2][:n], losses)
+
+
+def test_balanced_routers_without_a_bias_start_from_zero(oracle_losses):
+    w, b, h, t = _skewed_router()
+    got = offline.balance_routers([(w, None)], [h], [t], 3, 0.5)[0]
+    want = offline.balance_routers([(w, torch.zeros(8))], [h], [t], 3, 0.5)[0]
+    assert all(torch.equal(x, y) for x, y in zip(got, want)) and got[1].any()
