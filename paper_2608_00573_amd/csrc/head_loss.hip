@@ -219,13 +219,33 @@ __global__ __launch_bounds__(256) void k_live_rows(const float* h, const int32_t
   for (int k = threadIdx.x; k < d; k += 256) out[t * d + k] = live ? h[t * d + k] : 0.f;
 }
 
+// Column c's sum over the n rows of a [n][ld] array (the tiles' parts of db), by the 8
+// lanes of a column in a block of 32 of them: each takes every eighth row, in four sums
+// (one chain over the 8192 tiles of 2^21 rows would lose 11 bits and wait for each
+// load), then a tree.  The result is in the first 32 threads.
+constexpr int kColBlock = 32;
+__device__ __forceinline__ float col_sum(const float* part, int n, size_t ld, int c, bool in) {
+  __shared__ float s_c[8][kColBlock];
+  const int l = threadIdx.x & 31, r0 = threadIdx.x >> 5;
+  float s[4] = {};
+  if (in)
+    for (int i = r0; i < n; i += 32)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + 8 * k < n) s[k] += part[(size_t)(i + 8 * k) * ld + c];
+  s_c[r0][l] = (s[0] + s[1]) + (s[2] + s[3]);
+  __syncthreads();
+  float x[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) x[k] = s_c[k][l];
+  return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
 __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, size_t ld, int n,
                                                 float* db) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= n) return;
-  float s = 0.f;
-  for (int i = 0; i < n_tt; ++i) s += part[(size_t)i * ld + c];
-  db[c] = s;
+  const int c = blockIdx.x * kColBlock + (threadIdx.x & 31);
+  const float s = col_sum(part, n_tt, ld, c, c < n);
+  if (threadIdx.x < kColBlock && c < n) db[c] = s;
 }
 
 // ------------------------------------------------------ backward, bf16 --
@@ -786,12 +806,9 @@ struct ColSum {
 __global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f) {
   const int b = blockIdx.x - x.blocks - y.blocks;
   if (b >= 0) {
-    const int c = b * 256 + threadIdx.x;
-    if (c >= f.n) return;
-    float s = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < f.n_tt; ++i) s += f.part[(size_t)i * f.ld + c];
-    f.out[c] = s * *f.scale;
+    const int c = b * kColBlock + (threadIdx.x & 31);
+    const float s = col_sum(f.part, f.n_tt, f.ld, c, c < f.n);
+    if (threadIdx.x < kColBlock && c < f.n) f.out[c] = s * *f.scale;
     return;
   }
   const bool first = (int)blockIdx.x < x.blocks;
@@ -1065,7 +1082,7 @@ hipError_t backward_f32(const HeadLossArgs& a, hipStream_t st) {
                            a.db ? db : nullptr);
       });
     if (a.db)
-      hipLaunchKernelGGL(k_db_sum, dim3(cdiv(nv, 256)), dim3(256), 0, st, db, n_tt, ldd, nv,
+      hipLaunchKernelGGL(k_db_sum, dim3(cdiv(nv, kColBlock)), dim3(256), 0, st, db, n_tt, ldd, nv,
                          a.db + v0);
     if (dw) {
       const Operand<false> A{hl, d, a.d, a.T}, B{D, ldd, nv, a.T};
@@ -1295,8 +1312,10 @@ hipError_t backward_bf16(const HeadLossArgs& a, hipStream_t st) {
       }
     }
     // one launch a piece for what is left of it
-    const ColSum cols{db, p.mid ? cdiv(a.T, MidTile::BN) * MidTile::GN : n_tt, Vp, a.db ? nv : 0, part.G, a.db ? a.db + v0 : nullptr};
-    const unsigned n = sum_dh.blocks + sum_dw.blocks + cdiv(cols.n, 256);
+    const ColSum cols{db,     p.mid ? cdiv(a.T, MidTile::BN) * MidTile::GN : n_tt,
+                      Vp,     a.db ? nv : 0,
+                      part.G, a.db ? a.db + v0 : nullptr};
+    const unsigned n = sum_dh.blocks + sum_dw.blocks + cdiv(cols.n, kColBlock);
     if (n > 0) hipLaunchKernelGGL(k_finish, dim3(n), block, 0, st, sum_dh, sum_dw, cols);
   }
   return hipGetLastError();

@@ -352,6 +352,32 @@ def test_head_rows_past_32_bit_offsets(dtype, V, d, Q):
     assert ((dw.double() - want_dw).abs() <= bound + half * (want_dw.abs() + bound)).all()
 
 
+@pytest.mark.parametrize("dtype,V,d,tile", [(BF16, 200, 64, 256), (F32, 200, 8, 128)])
+def test_bias_gradient_over_many_rows(dtype, V, d, tile):
+    # as many rows as a call takes, all alike: every tile of rows leaves the same sum, so
+    # that a chain over the tiles would round the same way at every step.  Weights of zero
+    # leave the logits to the bias: the exponent's error is that of its argument (a
+    # difference and two products, up to R) and of the function
+    Q = 1 << 21
+    log(f"[losses] bias gradient over {Q} rows {dtype}")
+    r = np.random.default_rng(43)
+    b = r.normal(size=V).astype(np.float32)
+    bd = torch.from_numpy(b).to(DEV)
+    w, h = torch.zeros(V, d, dtype=dtype, device=DEV), torch.ones(Q, d, dtype=dtype, device=DEV)
+    y, g = torch.zeros(Q, dtype=torch.int32, device=DEV), torch.ones(Q, device=DEV)
+    lse = np.float32(np.log(np.exp(b.astype(np.float64)).sum()))
+    _, _, db = abi.trimmoe_head_cross_entropy_backward(
+        w, h, y, torch.full((Q,), float(lse), device=DEV), g, bd, want_dh=False, want_dw=False)
+    x = b.astype(np.float64) - float(lse)
+    p = np.exp(x)
+    D = p - (np.arange(V) == 0)
+    # of a tile: 8 terms a lane, 16 lanes, up to 4 parts; of the tiles: every 32nd of
+    # them in a row, then a tree of 32
+    chain = 8 + 4 + 4 + Q // tile / 32 + 5 + 4
+    bound = p * U * (16 + 4 * np.abs(x)) * 1.01 + chain * U * np.abs(D) + 2 * U
+    _within(db, Q * D, Q * bound, "db")
+
+
 @pytest.mark.parametrize("dtype,V,d,Q", [(F32, 300, 96, 40), (BF16, 300, 128, 40),
                                          (BF16, 700, 128, 200)])
 def test_head_gradient_is_the_difference_quotient(dtype, V, d, Q):
