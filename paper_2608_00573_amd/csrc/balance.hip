@@ -23,7 +23,8 @@ inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 constexpr int kTile = kRowTile;
 constexpr int kRowBlocks = 512;
 
-__device__ __forceinline__ float sum16(float x) {
+template <typename T>
+__device__ __forceinline__ T sum16(T x) {
 #pragma unroll
   for (int o = 8; o > 0; o >>= 1) x += __shfl_xor(x, o);
   return x;
@@ -306,24 +307,27 @@ __global__ __launch_bounds__(256) void k_balance_dz(const float* prob, const int
   const size_t t = (size_t)blockIdx.x * 16 + row;
   bool live = false;
   if (t < (size_t)T) row_slot(target, t, k, E, l, live);
-  float c[ET], p[ET], total = 0.f;
+  int32_t n_e[ET];
+  float c[ET], p[ET];
+  double total = 0.0;
 #pragma unroll
   for (int i = 0; i < ET; ++i) {
     const bool in = l + 16 * i < E;
-    c[i] = in ? (float)counts[l + 16 * i] : 0.f;
+    n_e[i] = in ? counts[l + 16 * i] : 0;
     p[i] = in && t < (size_t)T ? prob[t * E + l + 16 * i] : 0.f;
-    total += c[i];
+    total += n_e[i];
   }
   // counts against their mean: sum_j p_tj = 1, so the mean drops out of
-  // c_e - sum_j p_tj c_j and would only cost digits
+  // c_e - sum_j p_tj c_j and would only cost digits.  In 64 bits up to the difference,
+  // which is rounded to fp32: counts of several ranks together pass 2^24
   total = sum16(total);
   const int n = counts[E];
-  const float scale = n > 0 ? *dloss * (float)((double)E / ((double)total * n)) : 0.f;
-  const float mean = total / E;
+  const float scale = n > 0 ? *dloss * (float)((double)E / (total * n)) : 0.f;
+  const double mean = total / E;
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < ET; ++i) {
-    c[i] -= mean;
+    c[i] = (float)(n_e[i] - mean);
     s = fmaf(p[i], c[i], s);
   }
   s = sum16(s);

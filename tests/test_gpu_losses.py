@@ -766,6 +766,38 @@ def test_balance_of_two_ranks(dtype):
     assert np.allclose(joint[1], split[0][1] + split[1][1], rtol=0, atol=1e-12)
 
 
+@pytest.mark.parametrize("dtype,E,k", [(F32, 8, 2), (BF16, 60, 4), (F32, 200, 8)])
+def test_balance_of_many_ranks_with_a_nearly_even_load(dtype, E, k):
+    # counts summed over many ranks pass 2^24 and differ by a few slots: dz follows those
+    # differences, so each count has to keep all of its digits until the mean is off.  The
+    # bound is check_backward's, with a rounding of c - mean in place of one of c
+    r = Router(59, dtype, E, k, 128, 150).dev()
+    _, own, _, prob = r.forward()
+    c = (1 << 26) + np.arange(E) * 7 % 5 - 2
+    cn = np.append(c, c.sum() // k).astype(np.int64)
+    assert cn.max() < 1 << 31 and c.sum() > 1 << 24
+    dh, dw, db = r.backward(prob, torch.from_numpy(cn.astype(np.int32)).to(DEV))
+    _, ww, wb, dz = X.balance_grad(r.Wn, r.Hn, r.t, float(r.g), r.b, cn)
+    p = X.balance_loss(r.Wn, r.Hn, r.t, r.b)[3]
+    live = ((r.t >= 0) & (r.t < E)).any(axis=1)[:, None]
+    cm = c - c.mean()
+    kk = abs(float(r.g)) * E / (float(c.sum()) * cn[E])
+    ac = (p * np.abs(cm)).sum(axis=1, keepdims=True)
+    ez = kk * p * (r._prob_bound()[:, None] * (np.abs(cm - (p @ cm)[:, None]) + ac) +
+                   (E + 8) * U * ac + 10 * U * np.abs(cm)) * 1.01 * live
+    half = torch.finfo(dtype).eps / 2
+    rz = 2.0 ** -16 if dtype == BF16 else 0.0
+    az, Q, Hl = np.abs(dz), p.shape[0], np.where(live, r.Hn, 0.0)
+    assert (ez.sum(axis=0) < 0.01 * az.sum(axis=0)).all()
+    tiny = 1e-37  # (dz is some 1e-18: far from where fp32 and bf16 end)
+    _within(db, wb, (ez + (Q + 80) * U * (az + ez)).sum(axis=0) + tiny, "db")
+    e = (ez + (rz + (2 * Q + 80) * U) * (az + ez)).T @ np.abs(Hl)
+    _within(dw, ww, e + half * (np.abs(ww) + e) + tiny, "dw")
+    e = (ez + (rz + (2 * E + 16) * U) * (az + ez)) @ np.abs(r.Wn)
+    want = dz @ r.Wn
+    _within(dh, want, e + half * (np.abs(want) + e) + tiny, "dh")
+
+
 def test_balance_wanted_gradients():
     c = Router(58, BF16, 60, 4, 256, 300).dev()
     _, counts, _, prob = c.forward()
