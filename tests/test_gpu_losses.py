@@ -1017,3 +1017,21 @@ def test_a_stream_of_another_device_is_refused():
         c.forward(stream=Other())
     with pytest.raises(ValueError, match="stream of cuda:1"):
         r.forward(stream=Other())
+
+
+def test_stream_handles_without_the_short_way(monkeypatch):
+    # the current stream's handle comes from torch's documented call where the short one
+    # is missing; both name the same stream, in and out of a stream's context
+    c = Head(87, F32, 300, 96, 40).dev()
+    first = c.forward()
+    s = torch.cuda.Stream()
+    ways = []
+    for raw in (abi._raw_stream, None):
+        monkeypatch.setattr(abi, "_raw_stream", raw)
+        with torch.cuda.stream(s):
+            inside = abi._stream_handle(None).value
+        ways.append((abi._stream_handle(None).value, inside, abi._stream_handle(s).value))
+        assert inside == s.cuda_stream
+    assert ways[0] == ways[1]
+    got = c.forward()
+    assert all(torch.equal(x, y) for x, y in zip(first, got))
