@@ -522,8 +522,9 @@ int trimmoe_head_cross_entropy(int32_t dtype, int32_t vocab, int32_t d_model, in
  * lse as trimmoe_head_cross_entropy wrote it for the same inputs.  The logits
  * are computed again in pieces of the vocabulary; the workspace holds D of one
  * piece.  Gradients are written, not added to what is there; dh and dw_head may
- * not overlap any input.  bf16: D is rounded to bf16 before the two products
- * (by at most 2^-8 of each entry, as the results are), db_head sums it before.
+ * not overlap any input.  bf16: D enters the two products rounded to bf16 (by at
+ * most 2^-8 of each entry, as the results are); of up to 64 rows in two parts
+ * (2^-16).  db_head sums it before.
  */
 int trimmoe_head_cross_entropy_backward_workspace_size(int32_t dtype, int32_t vocab, int32_t d_model,
                                                        int32_t n_rows, size_t* bytes);

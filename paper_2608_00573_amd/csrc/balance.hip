@@ -379,14 +379,14 @@ __global__ __launch_bounds__(256) void k_balance_grad(const bf16_t* w, const bf1
                                                       const unsigned long long* mask, int T, int E,
                                                       int d, bf16_t* dh, float* part_dw, bf16_t* dw,
                                                       const float* part_db, float* db) {
-  __shared__ __align__(16) char lds[RowsGrad<ET, CW, 2>::LDS];
+  __shared__ __align__(16) char lds[RowsGrad<ET, CW>::LDS];
   if (db && blockIdx.x == 0 && (int)threadIdx.x < E) {  // of a single tile
     float s = 0.f;
 #pragma unroll
     for (int i = 0; i < kTile / 16; ++i) s += part_db[i * E + threadIdx.x];
     db[threadIdx.x] = s;
   }
-  rows_grad<ET, CW, 2>(lds, RouterRows{w, mask, E, d, 1.f}, h, dz, T, E, d, dh, part_dw, dw);
+  rows_grad<ET, CW>(lds, RouterRows{w, mask, E, d, 1.f}, h, dz, T, E, d, dh, part_dw, dw);
 }
 
 // The same in fp32, 16 x 16 x 4 MFMAs: a lane holds single elements, so both

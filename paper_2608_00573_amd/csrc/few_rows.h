@@ -69,13 +69,7 @@ struct FewArgs {
   float* db;
 };
 
-// parts of D per token tile count
-template <int ET>
-constexpr int few_parts() {
-  return ET == 1 ? 2 : 1;
-}
-
-// D in rows of 16 et tokens in one stream of w (skinny.hip): et 1 or, without db, 4
+// D (z of rows_grad.h) in rows of 16 et tokens in one stream of w (skinny.hip): et 1 or, without db, 4
 hipError_t launch_dz_skinny(const FewArgs& a, int et, int n_cu, hipStream_t st);
 
 }  // namespace trimmoe

@@ -254,12 +254,13 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 // dh and h for dw: nothing is turned in memory).
 //   * D and the scaled copy of h lie in panels of 256 columns, [panel][row][256]:
 //     a 64-row slice of a tile is then one run of 32 KB.
-//   * D enters the products in bf16, once rounded.  A row's weight g is G m 2^-e
-//     with G the largest |g| and |m| in [1, 2): D holds m (softmax - onehot), dh
-//     takes g / m on its fp32 sums, dw G on its own and 2^-e on the rows of h,
-//     where it is exact.  So weights that are all alike (m = 1) add no rounding
-//     to the -1 of an unlikely target, which carries most of an untrained row's
-//     gradient.
+//   * D enters the products in bf16, once rounded: dh and dw are some 2.0e-3 off
+//     (relative to their norm), where two parts would leave the 1.7e-3 of the results'
+//     own rounding for twice the MFMAs of both products.  A row's weight g is G m 2^-e
+//     with G the largest |g| and |m| in [1, 2): D holds m (softmax - onehot), dh takes
+//     g / m on its fp32 sums, dw G on its own and 2^-e on the rows of h, where it is
+//     exact.  So weights that are all alike (m = 1) add no rounding to the -1 of an
+//     unlikely target, which carries most of an untrained row's gradient.
 //   * The scaled copy of h has zeros in the rows that take no part: their h may
 //     hold anything, and 0 * NaN is NaN.
 //   * dh is summed in fp32 over pieces and K splits, then rounded once.
@@ -837,14 +838,17 @@ __global__ __launch_bounds__(256) void k_finish(SliceSum x, SliceSum y, ColSum f
 // twice (for z and for dh; past the last-level cache both come from HBM) and dw
 // written once, whatever the rows: three kernels, the second of them both
 // products in one pass over w (rows_grad.h; its rows are the vocabulary's, its
-// experts the tokens).  D lies [vocabulary row][token], in two bf16 parts where
-// the products' k-step leaves room for them (up to 16 rows).
+// experts the tokens).  D lies [vocabulary row][part][token] in two bf16 parts: what
+// counts here is w's way through memory, beside which the second part is small (one part:
+// 17 to 32 tokens 1 to 6% faster, 33 to 64 5 to 10%, dh and dw 2.0e-3 off instead of the
+// 1.7e-3 that their own rounding to bf16 leaves).
 // us here and in the kernels of more tokens, d and vocabulary 4096 x 32000: 16 tokens
-// 154 and 276; 2048 x 151936: 17 tokens 402 and 597, 64 464 and 617; 768 x 32128: 45 and
-// 77, 68 and 83; 128 x 1000: 20 and 36, 25 and 38.
+// 154 and 276; 2048 x 151936: 17 tokens 391 and 597, 64 478 and 617; 768 x 32128 with a
+// bias: 48 and 77, 75 and 83; 128 x 1000 with a bias: 20 and 36, 26 and 38.
 // D comes out of the weight-streaming kernel where the exit head's rule takes it (up
-// to 16 rows with db, whose sum it then holds in one row of lanes): 154 us against
-// 186 in the tiles at 16 tokens of 4096 x 32000, 192 and 218 at 64.
+// to 16 rows with db, whose sum it then holds in one row of lanes), stream and tiles in
+// us: 16 tokens of 4096 x 32000: 154 and 175 to 186, 2048 x 151936 342 and 384, 4096 x 4000
+// 33 and 47; 64 tokens 197 and 206 to 211, 478 and 468.
 // 16 tokens of 4096 x 32000: D 45 us (5.8 TB/s), the products 102 (5.1 TB/s).
 // D: the first core's tiles of 128 vocabulary rows x 16 ET tokens (32 at least)
 template <class T, int ET>
@@ -875,7 +879,7 @@ struct FewSrc {
     make_dptrs<T>(q, a.w, src, a.h, nullptr, 0, min(T::BN, a.T), a.d, 0);
   }
   __device__ __forceinline__ void epilogue(const Desc& d, Acc<T>& acc) const {
-    constexpr int PARTS = few_parts<ET>(), W = 16 * ET * PARTS;
+    constexpr int W = 32 * ET;
     const int lane = threadIdx.x & 63, wm = threadIdx.x >> 6;
     const int v0 = d.mt * T::BM;
     float sum[T::TM][16];
@@ -904,7 +908,7 @@ struct FewSrc {
           if (16 * ET >= T::BN || t < 16 * ET) {
             const bf16_t hi = f2bf(x);
             o[0] = hi;
-            if constexpr (PARTS == 2) o[16 * ET] = f2bf(x - bf2f(hi));
+            o[16 * ET] = f2bf(x - bf2f(hi));
           }
         }
     }
@@ -960,7 +964,7 @@ struct FewTokens {
 
 template <int ET, int CW>
 __global__ __launch_bounds__(256) void k_few_grad(FewArgs a, bf16_t* dw, float* part_dh) {
-  __shared__ __align__(16) char lds[RowsGrad<ET, CW, few_parts<ET>()>::LDS];
+  __shared__ __align__(16) char lds[RowsGrad<ET, CW>::LDS];
   __shared__ float s_e[64], s_G;
   if (threadIdx.x < 64) {
     const FewRow r(a.target, a.lse, a.dloss, a.V, a.T, threadIdx.x);
@@ -968,8 +972,8 @@ __global__ __launch_bounds__(256) void k_few_grad(FewArgs a, bf16_t* dw, float* 
     s_G = r.G;
   }
   __syncthreads();
-  rows_grad<ET, CW, few_parts<ET>()>(lds, FewTokens{a.h, s_e, a.T, a.d, a.V, s_G}, a.w, a.D, a.V,
-                                     a.T, a.d, dw, part_dh, nullptr);
+  rows_grad<ET, CW>(lds, FewTokens{a.h, s_e, a.T, a.d, a.V, s_G}, a.w, a.D, a.V, a.T, a.d, dw,
+                    part_dh, nullptr);
 }
 
 // dh_t = g / m times the sum of the S slices: 4 elements a thread, every eighth slice
@@ -1115,13 +1119,14 @@ FewPlan few_plan(int V, int d, int T) {
   p.et = T <= 16 ? 1 : T <= 32 ? 2 : 4;
   const int n_t = cdiv(V, kRowTile);
   // Blocks of 256 columns where each has 12 tiles of rows and more to make up for its
-  // start (17 tokens of 2048 x 151936: 399 us, 421 in 128 columns; 768 x 32128: 52 and
-  // 45); with 64 tokens they take 296 registers (768 x 32128: 96, 65 in 128 columns).
+  // start (us in 256 and 128 columns: 17 tokens of 2048 x 151936 391 and 418, of 4096 x
+  // 32000 186 and 189, of 768 x 32128 50 and 45, of 128 x 100000 44 and 41); with 64 tokens
+  // they take more than 256 registers (768 x 32128, one part of D: 96 and 65).
   p.cols = p.et < 4 && (long)n_t * cdiv(d, 256) >= 12 * 2 * kCu ? 4 : 2;
   const int n_c = cdiv(d, 64 * p.cols);
   p.R = std::max(1, std::min(n_t, cdiv(2 * kCu, n_c)));
   const size_t rows = cdiv(V, 128) * (size_t)128;
-  p.o_dh = align256(rows * 32 * p.et * (p.et == 1 ? 2 : 1));
+  p.o_dh = align256(rows * 64 * p.et);
   p.total = p.o_dh + align256((size_t)p.R * std::max(T, 1) * d * 4);
   return p;
 }

@@ -8,9 +8,9 @@
 // w's fragments stay in registers (a lane's 8 experts of a column), those of x (8
 // rows of a column) come transposed out of LDS, as do z's for z^T x.  The next
 // tile's loads are in flight under a tile's products.
-//   z in PARTS parts of bf16 (added up in the products), [row][part][16 ET].  ET =
-// 1 (two parts): both are one k-step of 32 (16 experts each, w's fragment twice);
-// else a k-step is 32 experts of a part.
+//   z in two parts of bf16 (what bf16 holds of it and of the rest: within 2^-16; added up
+// in the products), [row][part][16 ET].  ET = 1: both are one k-step of 32 (16 experts
+// each, w's fragment twice); else a k-step is 32 experts of a part.
 #pragma once
 
 #include "mfma_core.h"
@@ -18,16 +18,16 @@
 namespace trimmoe {
 
 constexpr int kRowTile = 64;
+constexpr int kZParts = 2;
 
-template <int ET, int CW, int PARTS>
+template <int ET, int CW>
 struct RowsGrad {
-  static_assert(ET > 1 || PARTS == 2, "a k-step of 32");
   static constexpr int BC = 64 * CW;                // columns of a block
   static constexpr int HR = 2 * BC;                 // LDS bytes of a row of x
-  static constexpr int ZB = 32 * PARTS * ET;        // bytes of a row of z
+  static constexpr int ZB = 32 * kZParts * ET;      // bytes of a row of z
   static constexpr int ZR = ZB + 32;                // ... in LDS: rows on distinct banks
   static constexpr int KS = ET == 1 ? 1 : ET / 2;   // fragments of w
-  static constexpr int ZS = ET * PARTS / 2;         // k-steps of out
+  static constexpr int ZS = ET * kZParts / 2;       // k-steps of out
   static constexpr int LDS = kRowTile * (HR + ZR);
   static constexpr int HL = kRowTile * HR / 16 / 256, ZL = kRowTile * ZB / 16;  // 16-byte loads
 };
@@ -47,11 +47,11 @@ __device__ __forceinline__ bf16x8_t read_tr(uint32_t a0, uint32_t a1) {
 // P: w(e, c) element of w (0 past E and in rows that take no part), mask(tile) the
 // tile's rows to read (the others are zeros), scale of out.  out [rows, d], part
 // [gridDim.y][E, d] fp32, whole [E, d] bf16 (instead of part): each may be NULL.
-template <int ET, int CW, int PARTS, class P>
+template <int ET, int CW, class P>
 __device__ __forceinline__ void rows_grad(char* lds, const P& p, const bf16_t* x, const bf16_t* z,
                                           int rows, int E, int d, bf16_t* out, float* part,
                                           bf16_t* whole) {
-  using G = RowsGrad<ET, CW, PARTS>;
+  using G = RowsGrad<ET, CW>;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, fr = lane & 15, q = lane >> 4;
   const int c0 = blockIdx.x * G::BC, cw = 16 * CW * wave;  // first columns: block, wavefront
   const int c_valid = min(G::BC, d - c0);
@@ -136,7 +136,7 @@ __device__ __forceinline__ void rows_grad(char* lds, const P& p, const bf16_t* x
 #pragma unroll
         for (int i = 0; i < ET; ++i)
 #pragma unroll
-          for (int n = 0; n < PARTS; ++n) {
+          for (int n = 0; n < kZParts; ++n) {
             const uint32_t a = az + k * G::ZR + (n * ET + i) * 32 + 8 * (fr & 3);
             const bf16x8_t fz = read_tr(a, a + 4 * G::ZR);
 #pragma unroll

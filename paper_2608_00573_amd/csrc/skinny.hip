@@ -592,12 +592,12 @@ __global__ __launch_bounds__(skinny::THREADS) void k_loss_skinny(ExitArgs a, int
 }
 
 // D of the head loss's gradient (head_loss.hip) for a few rows of h: the logits'
-// stream with D as its epilogue, [vocabulary row][part][16 MT] in parts of bf16.
+// stream with D as its epilogue, [vocabulary row][part][16 MT] in two parts of bf16.
 // Vocabulary rows from V up to a multiple of 64 are written as zeros.
 template <class T>
 __device__ __forceinline__ void skinny_dz_rows(const FewArgs& a, char* lds, int v0, int v1,
                                                const FewRow& row) {
-  constexpr int MT = T::MT, UC = T::G * skinny::COLS, PARTS = few_parts<MT>(), W = 16 * MT * PARTS;
+  constexpr int MT = T::MT, UC = T::G * skinny::COLS, W = 32 * MT;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int fr = lane & 15, q = lane >> 4;
   XSrc<MT> xs;
@@ -632,7 +632,7 @@ __device__ __forceinline__ void skinny_dz_rows(const FewArgs& a, char* lds, int 
         const bf16_t hi = f2bf(x);
         bf16_t* o = a.D + (size_t)v * W + t;
         o[0] = hi;
-        if constexpr (PARTS == 2) o[16 * MT] = f2bf(x - bf2f(hi));
+        o[16 * MT] = f2bf(x - bf2f(hi));
         if constexpr (MT == 1)
           if (a.db) {
             const float d = row16_sum(e * p);

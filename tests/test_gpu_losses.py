@@ -211,6 +211,30 @@ def test_bf16_gradients_of_small_heads(V, d, Q):
     c.check_backward((dh, dw, None))
 
 
+@pytest.mark.parametrize("V,d,Q,bias", [
+    (1003, 64, 1, True), (1003, 192, 16, False), (1003, 64, 17, True), (5000, 256, 32, False),
+    (10, 64, 20, False), (1003, 128, 33, True), (700, 64, 64, True), (4001, 2112, 40, False),
+    (24700, 2048, 64, False), (24577, 2048, 48, True)])
+def test_bf16_gradients_of_few_rows_keep_16_bits_of_dz(V, d, Q, bias):
+    # up to 64 rows D enters the products in two parts of bf16, off by half a step of what
+    # half a step leaves: where terms cancel, half a step of D itself would show beside
+    # half a step of the result.  Otherwise the bound is check_backward's
+    log(f"[losses] two parts of D V={V} d={d} Q={Q}")
+    c = Head(44, BF16, V, d, Q, bias, ignored=0.0).dev()
+    loss, lse = c.forward()
+    dh, dw, _ = c.backward(lse)
+    D, p, _ = X.head_loss_d(c.Wn, c.Hn, c.y, c.g, c.b)
+    _, wl = X.head_loss(c.Wn, c.Hn, c.y, c.b)
+    R = np.abs(X.logits(c.Wn, c.Hn, c.b)).max(axis=1)
+    ex = 2 * _lse_bound(c.Wn, c.Hn, c.b, wl) + U * (16 + 4 * R + 4 * np.abs(wl))
+    g, aD, half = np.abs(c.g.astype(np.float64))[:, None], np.abs(D), 2.0 ** -8
+    eD = g * p * ex[:, None] * 1.01 + 8 * U * aD + 2 * U * g + half ** 2 * (1 + half) * aD
+    for got, want, e, what in (
+            (dh, D @ c.Wn, (eD + (V + 80) * U * aD) @ np.abs(c.Wn) * 1.01, "dh"),
+            (dw, D.T @ c.Hn, (eD + (Q + 80) * U * aD).T @ np.abs(c.Hn) * 1.01, "dw")):
+        _within(got, want, e + half * (np.abs(want) + e) + TINY, what)
+
+
 @pytest.mark.parametrize("dtype,V,d,Q", [(F32, 20001, 64, 4100), (BF16, 40001, 64, 4100)])
 def test_head_gradients_over_several_pieces(dtype, V, d, Q):
     # more of D than a piece holds: dh is summed over the pieces
