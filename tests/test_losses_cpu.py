@@ -276,3 +276,35 @@ def test_balanced_routers_without_a_bias_start_from_zero(oracle_losses):
     got = offline.balance_routers([(w, None)], [h], [t], 3, 0.5)[0]
     want = offline.balance_routers([(w, torch.zeros(8))], [h], [t], 3, 0.5)[0]
     assert all(torch.equal(x, y) for x, y in zip(got, want)) and got[1].any()
+
+
+def test_softmax_heads_step_down_the_gradient(monkeypatch):
+    # a step of lr lowers the mean loss by lr |g|^2, up to the second order: the Hessian of a
+    # row's loss in (w, b) is at most (|h|^2 + 1) / 2, and lr^2 / 2 times it times |g|^2 is
+    # what a step may differ by
+    def forward(w, h, y, b=None):
+        loss, lse = X.head_loss(w.numpy(), h.numpy(), y.numpy(), b.numpy())
+        return torch.from_numpy(loss).float(), torch.from_numpy(lse).float()
+
+    def backward(w, h, y, lse, g, b=None, want_dh=True):
+        _, dw, db = X.head_loss_grad(w.numpy(), h.numpy(), y.numpy(), g.numpy(), b.numpy())
+        return None, torch.from_numpy(dw).float(), torch.from_numpy(db).float()
+
+    monkeypatch.setattr(abi, "trimmoe_head_cross_entropy", forward)
+    monkeypatch.setattr(abi, "trimmoe_head_cross_entropy_backward", backward)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda *a: None)
+    r = _rng(8)
+    V, d, Q, lr = 13, 6, 40, 0.1
+    w = torch.from_numpy(r.normal(size=(V, d)).astype(np.float32))
+    h = torch.from_numpy(r.normal(size=(Q, d)).astype(np.float32))
+    y = torch.from_numpy(r.integers(-1, V, size=Q).astype(np.int32))
+    live = (y >= 0).numpy()
+    (w1, b1, losses), = offline.train_softmax_heads([h], y, w, 1, lr)
+    start, end = (float(X.head_loss(a.numpy(), h.numpy(), y.numpy(), b.numpy())[0].sum()) /
+                  live.sum() for a, b in ((w, torch.zeros(V)), (w1, b1)))
+    g2 = (float((w1 - w).double().square().sum()) + float(b1.double().square().sum())) / lr ** 2
+    most = float((h.double().square().sum(1) + 1)[y >= 0].mean()) / 2
+    u = 2.0 ** -24
+    assert abs(float(losses[0]) - start) <= 100 * u * start   # a sum of 40 fp32 terms and weights
+    assert abs(end - start + lr * g2) <= lr ** 2 / 2 * most * g2 * 1.01
+    assert lr * most / 2 < 0.9 and g2 > 0.05                  # (so that the loss does fall)
