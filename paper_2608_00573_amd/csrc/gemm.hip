@@ -1028,8 +1028,8 @@ __global__ __launch_bounds__(big::THREADS) void k_argmax_big(ExitArgs a) {
   exit_big<true>(a, lds);
 }
 
-// ... on the large-group core: 8192 tokens, d 4096, vocabulary 32000 1.52 ms (1.41
-// PFLOP/s), MFMA issue at the power-limited clock
+// ... on the large-group core: 8192 tokens, d 4096, vocabulary 32000 1.48 to 1.63 ms by
+// box (1.45 to 1.32 PFLOP/s), MFMA issue at the power-limited clock
 __global__ __launch_bounds__(big::THREADS) void k_loss_big(ExitArgs a, int n_rows) {
   __shared__ __align__(16) char lds[big::LDS];
   exit_big<false, true>(a, lds, n_rows);

@@ -150,8 +150,8 @@ __global__ __launch_bounds__(256) void k_loss_join(const float2* part, int n_vt,
 // D of the tokens x a piece's columns (v0 ..; a row's elements behind the piece hold
 // anything), and per token tile the column sums of D (db).  A = w: a lane holds NA x 4
 // consecutive columns of a token.  777 tokens, d 768, vocabulary 32128: 430 us (89
-// TFLOP/s; the two products 390 and 365), bound by the fp32 matrix rate and the last
-// round of 1757 tiles.
+// TFLOP/s; the two products 385 and 360), bound by the fp32 matrix rate and the last
+// round: 1757 tiles, two to a CU, are 3.4 rounds of 512.
 template <int KIND>
 __global__ __launch_bounds__(f32p::THREADS, f32p::Tile<KIND>::OCC) void k_dz_f32(
     Operand<true> W, Operand<true> H, const float* bias, const int32_t* target, const float* lse,
@@ -267,10 +267,12 @@ __global__ __launch_bounds__(256) void k_db_sum(const float* part, int n_tt, siz
 // A tile's A rows are the columns of its result (4 consecutive ones a lane), so
 // that results leave the registers in 16-byte pieces without a turn through LDS.
 // Bound by MFMA issue at the clock that the power limit leaves: 8192 tokens, d 4096, a
-// piece of 16128 columns: D 0.90 ms (1.21 PFLOP/s), dw 0.89, dh 0.84.  With short
-// rows D's epilogue shows (256 exponentials a lane and 128 KB of stores a tile, which
-// only the next tile's first loads overlap): 4096 tokens, d 768, vocabulary 32128: D
-// 0.28 ms (0.72 PFLOP/s), dw 0.21, dh 0.18.
+// piece of 16128 columns: D 0.86 to 0.90 ms (1.26 to 1.21 PFLOP/s), dw 0.84 to 0.89, dh
+// 0.80 to 0.84.  The kernels take every register and spill 12 to 38 (dh: 82) around the
+// slice loop, none in it.  With short rows D's epilogue shows (256 exponentials a lane
+// and 128 KB of stores a tile, which only the next tile's first loads overlap): 4096
+// tokens, d 768, vocabulary 32128: D 0.28 to 0.30 ms (0.72 to 0.68 PFLOP/s), dw 0.21 to
+// 0.22, dh 0.18.
 // A piece's D is at most 256 MB, so that the products find part of it in the last-
 // level cache; pieces are whole rounds of the grid where that fits (2047 tokens, d
 // 2048, vocabulary 151936: 3.51 ms in equal pieces, 3.34 in whole rounds).
@@ -1007,6 +1009,8 @@ __global__ __launch_bounds__(256) void k_few_finish(FewArgs a, const float* part
 // ------------------------------------------------------------------ plan --
 // bytes of D that a piece may take
 constexpr size_t kPieceBytes = (size_t)256 << 20;
+// the plans (and with them the workspaces' sizes) are made for a whole MI355X, whatever
+// device is current; the launches go by the device's own count
 constexpr int kCu = 256;
 struct BackPlan {
   int kind;        // of D's tiles (A = the vocabulary)
@@ -1179,7 +1183,11 @@ int even_rounds(int all, int most, int n_tt, int n_dt) {
 // D of up to so many 256 x 256 tiles goes in tiles of 128 x 128.  us of the whole
 // gradient, there and in the large tiles (tokens x vocabulary x d): 16 tiles, 300 x 2000
 // x 768: 59 and 78; 58, 397 x 7286 x 2560: 111 and 148; 126, 228 x 32128 x 768: 109 and
-// 118; 189, 600 x 16000 x 2048: 191 and 185; 252, 1000 x 16000 x 1024: 149 and 136.
+// 118; 300 x 16000 (126): d 128 62 and 69, 768 80 and 90, 2048 132 and 148; 600 x 16000
+// (189): d 128 74 and 78, 512 89 and 92, 768 98 and 100, 2048 183 and 177; 1000 x 16000
+// (252): 83 and 83, 107 and 104, 121 and 115, 232 and 210; 2000 x 16000 (504): d 128 105 and
+// 107, 768 188 and 176.  So the length of the rows matters too (each tile's epilogue weighs
+// more where they are short), by no more than 5% on either side.
 constexpr int kMidTiles = 128;
 BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   BackPlanBf16 p;

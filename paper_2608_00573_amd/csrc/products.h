@@ -424,7 +424,8 @@ __device__ __forceinline__ void f32_product(const Operand<AK>& A, const Operand<
     f32_tile<KIND>(A, B, r0, n0, k0, k_end, lds, t);
 }
 
-// K splits of an a x b product over K on a 256-CU device: the fewest slices on the
+// K splits of an a x b product over K on a whole MI355X, 256 CUs (a plan for a workspace,
+// not the current device's count): the fewest slices on the
 // busiest CU, a block's start and end counted as 16 of them, a tenth more for a
 // block that has no other one beside it, and the partials' sum as 4
 inline int product_splits(int kind, int a, int b, int K) {

@@ -1059,3 +1059,98 @@ def test_stream_handles_without_the_short_way(monkeypatch):
     assert ways[0] == ways[1]
     got = c.forward()
     assert all(torch.equal(x, y) for x, y in zip(first, got))
+
+
+# every kernel path of a few bf16 rows: D in the weight stream or in tiles, each count of
+# token tiles
+FEW = [(1003, 64, 1), (700, 2048, 7), (700, 128, 16), (1003, 2048, 20), (700, 128, 33),
+       (24700, 2048, 50), (700, 64, 64)]
+
+
+@pytest.mark.parametrize("V,d,Q", FEW)
+def test_few_rows_with_extreme_logits_and_weights_far_apart(V, d, Q):
+    for bias in (True, False):
+        c = Head(45, BF16, V, d, Q, bias, ignored=0.0, sigma=64 / d)
+        c.g[:] = 1e-6
+        c.g[Q // 2] = 1.0
+        c.g[Q - 1] = -3e4
+        c.dev()
+        loss, lse = c.forward()
+        c.check_forward(loss, lse)
+        c.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("V,d,Q", FEW)
+def test_few_rows_wanted_gradients_and_nothing_to_learn(V, d, Q):
+    for bias in (True, False):
+        c = Head(46, BF16, V, d, Q, bias).dev()
+        _, lse = c.forward()
+        full = c.backward(lse)
+        for kw, none in ((dict(want_dh=False), 0), (dict(want_dw=False), 1)):
+            got = c.backward(lse, **kw)
+            assert got[none] is None
+            assert all(torch.equal(x, y) for i, (x, y) in enumerate(zip(got, full))
+                       if i != none and x is not None)
+        got = c.backward(lse, want_dh=False, want_dw=False)
+        assert got[2] is None if not bias else torch.equal(got[2], full[2])
+        c.yd.fill_(-1)
+        loss, lse = c.forward()
+        assert not loss.any()
+        assert not any(t.any() for t in c.backward(lse) if t is not None)
+
+
+@pytest.mark.parametrize("V,d,Q", FEW)
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_few_rows_that_hold_anything(V, d, Q, bad):
+    if Q < 3:
+        return
+    for bias in (True, False):
+        c, clean = (Head(47, BF16, V, d, Q, bias, ignored=0.0) for _ in range(2))
+        c.y[[0, Q - 1]] = clean.y[[0, Q - 1]] = -1
+        c.H[[0, Q - 1]] = bad
+        c.dev()
+        c.gd[0] = bad   # (nor does the weight of a row without a target count)
+        loss, lse = c.forward()
+        assert (loss[[0, Q - 1]] == 0).all() and torch.isfinite(loss).all()
+        clean.check_backward(c.backward(lse))
+
+
+@pytest.mark.parametrize("V,d,Q", FEW + [(1003, 128, 300)])
+def test_few_rows_captured_and_replayed(V, d, Q):
+    c = Head(48, BF16, V, d, Q, V % 2 == 1).dev()
+    run = lambda: (lambda f: (*f, *[t for t in c.backward(f[1]) if t is not None]))(c.forward())
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = run()
+    for k in range(3):
+        c.Hd.copy_(torch.randn(c.Hd.shape, device=DEV))
+        c.yd.copy_(torch.randint(-1, V, (Q,), device=DEV))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), k
+
+
+@pytest.mark.parametrize("dtype,E,k,d,Q", [(F32, 200, 8, 130, 64), (F32, 130, 2, 1000, 1000),
+                                           (F32, 60, 4, 64, 5000), (BF16, 200, 8, 1024, 4097),
+                                           (BF16, 130, 1, 64, 63), (F32, 256, 8, 3, 1)])
+def test_balance_of_many_experts_wanted_gradients(dtype, E, k, d, Q):
+    c = Router(71, dtype, E, k, d, Q).dev()
+    out = c.forward()
+    c.check_forward(*out)
+    full = c.backward(out[3], out[1])
+    c.check_backward(full)
+    for kw, none in ((dict(want_dh=False), (0,)), (dict(want_dw=False), (1,)),
+                     (dict(want_db=False), (2,)), (dict(want_dh=False, want_dw=False), (0, 1)),
+                     (dict(want_dh=False, want_db=False), (0, 2))):
+        got = c.backward(out[3], out[1], **kw)
+        for i in range(2):
+            assert got[i] is None if i in none else torch.equal(got[i], full[i])
+        # (db of a single tile is summed by another kernel, in another order, where no
+        # product runs: within the same bound, not the same bits)
+        assert (got[2] is None) == (2 in none)
+        if got[2] is not None:
+            c.check_backward((full[0], full[1], got[2]))
