@@ -1236,13 +1236,15 @@ hipError_t backward_few(const HeadLossArgs& a, const FewPlan& p, hipStream_t st)
   float* part = a.dh ? reinterpret_cast<float*>(a.ws + p.o_dh) : nullptr;
   // (17 to 32 rows have no stream: the exit head's rule takes theirs for heads of up to 16
   // vocabulary rows only, a few units)
-  if (ET != 2 && exit_streams(true, true, a.T, a.V, a.d) && (ET == 1 || !a.db)) {
-    const hipError_t e = launch_dz_skinny(f, ET, a.n_cu, st);
-    if (e != hipSuccess) return e;
-  } else {
+  bool stream = false;
+  if constexpr (ET != 2) {
+    stream = exit_streams(true, true, a.T, a.V, a.d) && (ET == 1 || !a.db);
+    if (stream)
+      if (const hipError_t e = launch_dz_skinny<ET>(f, a.n_cu, st); e != hipSuccess) return e;
+  }
+  if (!stream)
     hipLaunchKernelGGL((k_dz_few<Tl, ET>), dim3(std::min(cdiv(a.V, 128), a.n_cu)), dim3(Tl::THREADS),
                        0, st, f);
-  }
   if (a.dw || a.dh) {
     if (const dim3 g(cdiv(a.d, 64 * p.cols), p.R); p.cols == 2)
       hipLaunchKernelGGL((k_few_grad<ET, 2>), g, dim3(256), 0, st, f, static_cast<bf16_t*>(a.dw),

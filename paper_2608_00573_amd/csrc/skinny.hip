@@ -704,20 +704,16 @@ hipError_t launch_loss_skinny(const ExitArgs& a, int n_rows, hipStream_t st) {
   return hipGetLastError();
 }
 
-hipError_t launch_dz_skinny(const FewArgs& a, int et, int n_cu, hipStream_t st) {
+template <int ET>
+hipError_t launch_dz_skinny(const FewArgs& a, int n_cu, hipStream_t st) {
   const dim3 grid(n_cu), block(skinny::THREADS);
-  const bool low = stream_kind(a.d / skinny::KSTEP) == kShort;
-  if (et == 1 && low)
-    hipLaunchKernelGGL((k_dz_skinny<1, kShort>), grid, block, 0, st, a);
-  else if (et == 1)
-    hipLaunchKernelGGL((k_dz_skinny<1, kLong>), grid, block, 0, st, a);
-  else if (et == 4 && low)
-    hipLaunchKernelGGL((k_dz_skinny<4, kShort>), grid, block, 0, st, a);
-  else if (et == 4)
-    hipLaunchKernelGGL((k_dz_skinny<4, kMid>), grid, block, 0, st, a);
+  if (stream_kind(a.d / skinny::KSTEP) == kShort)
+    hipLaunchKernelGGL((k_dz_skinny<ET, kShort>), grid, block, 0, st, a);
   else
-    return hipErrorInvalidValue;  // (no other width of D's rows)
+    hipLaunchKernelGGL((k_dz_skinny<ET, ET == 1 ? kLong : kMid>), grid, block, 0, st, a);
   return hipGetLastError();
 }
+template hipError_t launch_dz_skinny<1>(const FewArgs&, int, hipStream_t);
+template hipError_t launch_dz_skinny<4>(const FewArgs&, int, hipStream_t);
 
 }  // namespace trimmoe
