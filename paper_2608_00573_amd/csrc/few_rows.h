@@ -69,7 +69,8 @@ struct FewArgs {
   float* db;
 };
 
-// D (z of rows_grad.h) in rows of 16 ET tokens in one stream of w (skinny.hip): ET 1 or, without db, 4
+// D (z of rows_grad.h) in rows of 16 ET tokens in one stream of w (skinny.hip): ET 1 or,
+// without db, 4
 template <int ET>
 hipError_t launch_dz_skinny(const FewArgs& a, int n_cu, hipStream_t st);
 

@@ -1186,8 +1186,8 @@ int even_rounds(int all, int most, int n_tt, int n_dt) {
 // 118; 300 x 16000 (126): d 128 62 and 69, 768 80 and 90, 2048 132 and 148; 600 x 16000
 // (189): d 128 74 and 78, 512 89 and 92, 768 98 and 100, 2048 183 and 177; 1000 x 16000
 // (252): 83 and 83, 107 and 104, 121 and 115, 232 and 210; 2000 x 16000 (504): d 128 105 and
-// 107, 768 188 and 176.  So the length of the rows matters too (each tile's epilogue weighs
-// more where they are short), by no more than 5% on either side.
+// 107, 768 188 and 176.  The length of the rows matters too (a tile's epilogue weighs more
+// where they are short); the rule without it gives up no more than 5% (189 tiles).
 constexpr int kMidTiles = 128;
 BackPlanBf16 back_plan_bf16(int V, int d, int T) {
   BackPlanBf16 p;

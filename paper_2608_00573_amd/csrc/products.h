@@ -425,9 +425,9 @@ __device__ __forceinline__ void f32_product(const Operand<AK>& A, const Operand<
 }
 
 // K splits of an a x b product over K on a whole MI355X, 256 CUs (a plan for a workspace,
-// not the current device's count): the fewest slices on the
-// busiest CU, a block's start and end counted as 16 of them, a tenth more for a
-// block that has no other one beside it, and the partials' sum as 4
+// not the current device's count): the fewest slices on the busiest CU, a block's start
+// and end counted as 16 of them, a tenth more for a block that has no other one beside
+// it, and the partials' sum as 4
 inline int product_splits(int kind, int a, int b, int K) {
   const long tiles = f32p::tiles(kind, a, b);
   const int nk = cdiv(K, f32p::KS);
