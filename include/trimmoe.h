@@ -572,6 +572,87 @@ int trimmoe_balance_loss_backward(int32_t dtype, int32_t n_experts, int32_t top_
                                   const float* dloss, void* dh, void* dw_router, float* db_router,
                                   void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Activations in 8 bits.  Each 32 consecutive values of a row (the last block
+ * may be shorter) share a step 2^(e - 6), where 2^e <= max |v| < 2^(e + 1)
+ * (e at least -127): scale byte e + 127, and code = the whole number nearest
+ * to v / step (ties to even) within -127 .. 127.  A value comes back as code *
+ * step: off by at most step / 2 (between 127.5 and 128 steps by less than one
+ * step, max |v| / 127), exactly if it was such a multiple before, and exact in
+ * bf16.  A block that holds a NaN or an infinity has scale byte 255 and comes
+ * back as NaN.  x [n_rows, n_cols] in `dtype`, codes int8 [n_rows, n_cols],
+ * scale uint8 [n_rows, (n_cols + 31) / 32]; arrays may be NULL when n_rows is
+ * 0, need the alignment of an element only (rows of whole 8 values in aligned
+ * arrays are read fastest), and may not overlap.  n_rows <= TRIMMOE_LOSS_MAX_ROWS,
+ * 1 <= n_cols <= TRIMMOE_LOSS_MAX_D.
+ */
+int trimmoe_checkpoint_pack(int32_t dtype, int32_t n_rows, int32_t n_cols, const void* x,
+                            int8_t* codes, uint8_t* scale, void* stream);
+int trimmoe_checkpoint_unpack(int32_t dtype, int32_t n_rows, int32_t n_cols, const int8_t* codes,
+                              const uint8_t* scale, void* x, void* stream);
+
+/*
+ * The expert feed-forward block on rows of its own, for training: rows x
+ * [n_rows, d] lie sorted by expert, those of expert e at offsets[e] ..
+ * offsets[e + 1] - 1 (int32 [E + 1] on the device, ascending, within 0 ..
+ * n_rows; NULL: all rows are expert 0's and E is 1).  With the weights of the
+ * row's expert, w_up and w_gate [E, F, d], w_down [E, d, F]:
+ *   u = w_up x,  g = w_gate x,
+ *   a = silu(g) u (TRIMMOE_ACT_SWIGLU) or relu(u) (TRIMMOE_ACT_RELU, w_gate NULL),
+ *   y = w_down a                                                   [n_rows, d].
+ * Rows of no expert (before offsets[0], from offsets[E] on) give zeros and are
+ * not read.  Borders outside 0 .. n_rows count as the nearer end; where they
+ * do not ascend, results of the rows concerned are unspecified.
+ *
+ * keep says what is kept of u and g for the gradient, [n_rows, F] each (gate:
+ * with a gate only): TRIMMOE_KEEP_NONE nothing; TRIMMOE_KEEP_FULL values in
+ * `dtype`; TRIMMOE_KEEP_PACKED codes with scale bytes [n_rows, (F + 31) / 32] as
+ * trimmoe_checkpoint_pack writes them (of the values before any rounding).
+ *
+ * dtype, alignment, limits, NULL arrays and workspaces as for the training
+ * losses (d_model and d_ff bf16: multiples of 64; codes of bf16 calls 16-byte
+ * aligned); E <= TRIMMOE_MAX_EXPERTS and E * d_model * d_ff <= 2^40.  bf16: a is
+ * rounded to bf16 before the product with w_down (by at most 2^-8 of it, as y
+ * is), u and g are not before a is taken.  Outputs may not overlap any input.
+ */
+#define TRIMMOE_KEEP_NONE 0
+#define TRIMMOE_KEEP_FULL 1
+#define TRIMMOE_KEEP_PACKED 2
+int trimmoe_expert_ffn_workspace_size(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model,
+                                      int32_t d_ff, int32_t n_rows, int32_t keep, size_t* bytes);
+int trimmoe_expert_ffn(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model, int32_t d_ff,
+                       int32_t n_rows, int32_t keep, const void* w_up, const void* w_gate,
+                       const void* w_down, const void* x, const int32_t* offsets, void* y, void* up,
+                       uint8_t* up_scale, void* gate, uint8_t* gate_scale, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of sum(dy * y) (dy [n_rows, d] in `dtype`) from u and g as the
+ * forward kept them (keep FULL or PACKED), taken as they are: da = dy w_down and,
+ * with s = 1 / (1 + exp(-g)),
+ *   du = da g s,  dg = da u s (1 + g (1 - s))   (relu: du = da where u > 0, else 0),
+ *   dx = du w_up + dg w_gate                                       [n_rows, d],
+ *   dw_up = du^T x,  dw_gate = dg^T x,  dw_down = dy^T a           per expert.
+ * dx and the weights' gradients have the rows' dtype; each may be NULL (not
+ * computed).  Rows of no expert have dx zero and take no part; an expert without
+ * rows has gradients of zero.  x_packed nonzero: x holds codes with scale bytes
+ * x_scale, whose values take x's place.  Gradients are written, not added to
+ * what is there.  bf16: a, du and dg enter the products rounded to bf16 (by at
+ * most 2^-8 of each).  Sums run in a fixed order: repeated calls give identical
+ * results.
+ */
+int trimmoe_expert_ffn_backward_workspace_size(int32_t dtype, int32_t act, int32_t n_experts,
+                                               int32_t d_model, int32_t d_ff, int32_t n_rows,
+                                               int32_t x_packed, size_t* bytes);
+int trimmoe_expert_ffn_backward(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model,
+                                int32_t d_ff, int32_t n_rows, int32_t keep, int32_t x_packed,
+                                const void* w_up, const void* w_gate, const void* w_down,
+                                const void* x, const uint8_t* x_scale, const void* dy,
+                                const int32_t* offsets, const void* up, const uint8_t* up_scale,
+                                const void* gate, const uint8_t* gate_scale, void* dx, void* dw_up,
+                                void* dw_gate, void* dw_down, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+from typing import NamedTuple
 
 import numpy as np
 
@@ -82,7 +83,10 @@ EXPORTS = ["trimmoe_abi_version", "trimmoe_status_str", "trimmoe_workspace_size"
            "trimmoe_head_cross_entropy_backward_workspace_size",
            "trimmoe_head_cross_entropy_backward",
            "trimmoe_balance_loss_workspace_size", "trimmoe_balance_loss",
-           "trimmoe_balance_loss_backward_workspace_size", "trimmoe_balance_loss_backward"]
+           "trimmoe_balance_loss_backward_workspace_size", "trimmoe_balance_loss_backward",
+           "trimmoe_checkpoint_pack", "trimmoe_checkpoint_unpack",
+           "trimmoe_expert_ffn_workspace_size", "trimmoe_expert_ffn",
+           "trimmoe_expert_ffn_backward_workspace_size", "trimmoe_expert_ffn_backward"]
 TIMED_CLASSES = ["route", "bucket", "up", "down", "shared", "combine", "exit", "gate"]
 
 _lib = None
@@ -165,6 +169,16 @@ def lib():
         L.trimmoe_balance_loss.argtypes = [i32] * 5 + [p] * 9 + [size, p]
         L.trimmoe_balance_loss_backward.restype = C.c_int
         L.trimmoe_balance_loss_backward.argtypes = [i32] * 5 + [p] * 10 + [size, p]
+        for name in ("trimmoe_checkpoint_pack", "trimmoe_checkpoint_unpack"):
+            getattr(L, name).restype = C.c_int
+            getattr(L, name).argtypes = [i32] * 3 + [p] * 4
+        for name in ("trimmoe_expert_ffn", "trimmoe_expert_ffn_backward"):
+            getattr(L, name + "_workspace_size").restype = C.c_int
+            getattr(L, name + "_workspace_size").argtypes = [i32] * 7 + [out]
+        L.trimmoe_expert_ffn.restype = C.c_int
+        L.trimmoe_expert_ffn.argtypes = [i32] * 7 + [p] * 11 + [size, p]
+        L.trimmoe_expert_ffn_backward.restype = C.c_int
+        L.trimmoe_expert_ffn_backward.argtypes = [i32] * 8 + [p] * 16 + [size, p]
         if L.trimmoe_abi_version() != ABI_VERSION:
             raise RuntimeError(f"{LIB_PATH} has ABI version {L.trimmoe_abi_version()}, the "
                                f"binding expects {ABI_VERSION}: rebuild it")
@@ -573,6 +587,167 @@ def trimmoe_balance_loss_backward(w_router: torch.Tensor, h: torch.Tensor, targe
                    _ptr(dloss), _ptr(dh), _ptr(dw), _ptr(db), _ptr(ws), ws.numel(),
                    _stream_handle(None)))
     return dh, dw, db
+
+
+# ------------------------------------------------ activations in 8 bits ----
+class Packed(NamedTuple):
+    """Rows in 8 bits: codes int8 [n, c] and scale bytes uint8 [n, ceil(c / 32)],
+    32 consecutive values of a row in steps of 2^(scale - 133)."""
+    codes: torch.Tensor
+    scale: torch.Tensor
+
+
+PACK_BLOCK = 32  # values of a row that share a scale byte
+
+
+def _packed_like(n: int, c: int, device) -> Packed:
+    return Packed(torch.empty(n, c, dtype=torch.int8, device=device),
+                  torch.empty(n, -(-c // PACK_BLOCK), dtype=torch.uint8, device=device))
+
+
+def _take_packed(name: str, x, n: int, c: int, device):
+    if not isinstance(x, (tuple, list)) or len(x) != 2:
+        raise ValueError(f"{name}: (codes, scale) as trimmoe_checkpoint_pack gives them is needed")
+    _take(name + " codes", x[0], (n, c), torch.int8, device)
+    _take(name + " scale", x[1], (n, -(-c // PACK_BLOCK)), torch.uint8, device)
+
+
+def trimmoe_checkpoint_pack(x: torch.Tensor, stream=None) -> Packed:
+    """x [n, c] (bf16 or fp32, on the GPU) in 8 bits a value and a byte a block of
+    32: off by at most 1 / 127 of the block's largest magnitude; a block that
+    holds a NaN or an infinity comes back as NaN."""
+    code = _dtype_code(x)
+    if x.dim() != 2 or x.shape[1] < 1 or not x.is_contiguous():
+        raise ValueError("a contiguous tensor [n, c] is needed")
+    n, c = x.shape
+    with _on_stream(x, stream):
+        out = _packed_like(n, c, x.device)
+        _check("trimmoe_checkpoint_pack",
+               lib().trimmoe_checkpoint_pack(code, n, c, _ptr(x), _ptr(out.codes),
+                                             _ptr(out.scale), _stream_handle(None)))
+    return out
+
+
+def trimmoe_checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor,
+                              dtype=torch.bfloat16, stream=None) -> torch.Tensor:
+    """The values that codes and scale (of trimmoe_checkpoint_pack) stand for, in
+    bf16 or fp32 (exact in both)."""
+    if codes.dim() != 2 or codes.shape[1] < 1:
+        raise ValueError("codes are [n, c]")
+    n, c = codes.shape
+    _take_packed("checkpoint", (codes, scale), n, c, codes.device)
+    with _on_stream(codes, stream):
+        x = torch.empty(n, c, dtype=dtype, device=codes.device)
+        _check("trimmoe_checkpoint_unpack",
+               lib().trimmoe_checkpoint_unpack(_dtype_code(x), n, c, _ptr(codes), _ptr(scale),
+                                               _ptr(x), _stream_handle(None)))
+    return x
+
+
+# ---------------------------------------------- expert feed-forward block --
+KEEP = {None: 0, "full": 1, "packed": 2}
+
+
+def _ffn_args(w_up, w_gate, w_down, rows, offsets):
+    """(dtype code, act, E, d, F, n) of the block's weights [E, F, d], [E, d, F]
+    (or [F, d], [d, F]: one expert) and rows [n, d] in the weights' dtype."""
+    code = _dtype_code(w_up)
+    one = w_up.dim() == 2
+    if w_up.dim() not in (2, 3) or rows.dim() != 2:
+        raise ValueError("the weights are [E, F, d] and [E, d, F] (or of one expert), the rows [n, d]")
+    E = 1 if one else w_up.shape[0]
+    F, d = w_up.shape[-2:]
+    dev = w_up.device
+    _take("w_up", w_up, (F, d) if one else (E, F, d), w_up.dtype, dev)
+    _take("w_down", w_down, (d, F) if one else (E, d, F), w_up.dtype, dev)
+    if w_gate is not None:
+        _take("w_gate", w_gate, tuple(w_up.shape), w_up.dtype, dev)
+    if offsets is not None:
+        _take("offsets", offsets, (E + 1,), torch.int32, dev)
+    elif E != 1:
+        raise ValueError("offsets: rows of several experts need their borders")
+    return code, ACT_RELU if w_gate is None else ACT_SWIGLU, E, d, F, rows.shape[0]
+
+
+def trimmoe_expert_ffn(w_up: torch.Tensor, w_gate, w_down: torch.Tensor, x: torch.Tensor,
+                       offsets=None, keep=None, stream=None):
+    """(y [n, d], kept) of the feed-forward block y = w_down (silu(w_gate x) *
+    (w_up x)), or w_down relu(w_up x) without w_gate, on rows x [n, d] sorted by
+    expert: expert e's are offsets[e] .. offsets[e + 1] - 1 (int32 [E + 1] on the
+    GPU; None: one expert's).  Weights [E, F, d], [E, F, d], [E, d, F], or [F, d],
+    [F, d], [d, F] of one expert.  Rows of no expert give zeros.  keep: what the
+    gradient needs of w_up x and w_gate x: "full" (in x's dtype), "packed" (8
+    bits) or None; kept is then (up, gate) as tensors or Packed, gate None
+    without w_gate, or None."""
+    if keep not in KEEP:
+        raise ValueError(f"keep is one of {list(KEEP)}")
+    dims = _ffn_args(w_up, w_gate, w_down, x, offsets)
+    code, act, E, d, F, n = dims
+    dev = w_up.device
+    _take("x", x, (n, d), w_up.dtype, dev)
+    with _on_stream(x, stream):
+        y = torch.empty_like(x)
+        kept = [None, None]
+        if keep is not None:
+            for i in range(1 if w_gate is None else 2):
+                kept[i] = (_packed_like(n, F, dev) if keep == "packed"
+                           else torch.empty(n, F, dtype=x.dtype, device=dev))
+        flat = [t for k in kept for t in _codes_and_scale(k)]
+        dims = dims + (KEEP[keep],)
+        ws = _loss_ws("trimmoe_expert_ffn", dims, dev)
+        _check("trimmoe_expert_ffn",
+               lib().trimmoe_expert_ffn(*dims, _ptr(w_up), _ptr(w_gate), _ptr(w_down), _ptr(x),
+                                        _ptr(offsets), _ptr(y), *map(_ptr, flat), _ptr(ws),
+                                        ws.numel(), _stream_handle(None)))
+    return y, None if keep is None else tuple(kept)
+
+
+def _codes_and_scale(k):
+    """(values or codes, scale or None) of a kept array."""
+    return tuple(k) if isinstance(k, (tuple, list)) else (k, None)
+
+
+def trimmoe_expert_ffn_backward(w_up: torch.Tensor, w_gate, w_down: torch.Tensor, x,
+                                dy: torch.Tensor, kept, offsets=None, want_dx=True, want_dw=True,
+                                stream=None):
+    """Gradients (dx [n, d], dw_up, dw_gate, dw_down, in the weights' shapes and
+    dtype) of sum(dy * y) with kept from trimmoe_expert_ffn (tensors or Packed, both
+    alike); x: the rows, or their Packed form.  None for one that is not wanted
+    (dw_gate: without w_gate)."""
+    code, act, E, d, F, n = _ffn_args(w_up, w_gate, w_down, dy, offsets)
+    dev = w_up.device
+    _take("dy", dy, (n, d), w_up.dtype, dev)
+    x_packed = not isinstance(x, torch.Tensor)
+    if x_packed:
+        _take_packed("x", x, n, d, dev)
+    else:
+        _take("x", x, (n, d), w_up.dtype, dev)
+    if not isinstance(kept, (tuple, list)) or len(kept) != 2 or (kept[1] is None) != (w_gate is None):
+        raise ValueError("kept: (up, gate) as trimmoe_expert_ffn gives them is needed")
+    packed = not isinstance(kept[0], torch.Tensor)
+    for name, k in zip(("up", "gate"), kept):
+        if k is None:
+            continue
+        if packed != (not isinstance(k, torch.Tensor)):
+            raise ValueError("up and gate are kept in one form")
+        if packed:
+            _take_packed(name, k, n, F, dev)
+        else:
+            _take(name, k, (n, F), w_up.dtype, dev)
+    up, up_scale = _codes_and_scale(kept[0])
+    gate, gate_scale = _codes_and_scale(kept[1])
+    x, x_scale = _codes_and_scale(x)
+    with _on_stream(dy, stream):
+        dx = torch.empty_like(dy) if want_dx else None
+        dw = [None if w is None or not want_dw else torch.empty_like(w)
+              for w in (w_up, w_gate, w_down)]
+        ws = _loss_ws("trimmoe_expert_ffn_backward", (code, act, E, d, F, n, int(x_packed)), dev)
+        _check("trimmoe_expert_ffn_backward",
+               lib().trimmoe_expert_ffn_backward(
+                   code, act, E, d, F, n, KEEP["packed" if packed else "full"], int(x_packed),
+                   *map(_ptr, (w_up, w_gate, w_down, x, x_scale, dy, offsets, up, up_scale, gate,
+                               gate_scale, dx, *dw, ws)), ws.numel(), _stream_handle(None)))
+    return (dx, *dw)
 
 
 # ------------------------------------------------ struct construction ------

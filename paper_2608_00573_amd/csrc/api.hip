@@ -16,6 +16,7 @@
 #include <mutex>
 
 #include "common.h"
+#include "expert_ffn.h"
 #include "loss.h"
 
 using namespace trimmoe;
@@ -876,6 +877,166 @@ int trimmoe_balance_loss_backward(int32_t dtype, int32_t n_experts, int32_t top_
   return launch_balance_backward(a, static_cast<hipStream_t>(stream)) == hipSuccess
              ? TRIMMOE_OK
              : TRIMMOE_ERR_HIP;
+}
+
+// ------------------------------------------------ activations in 8 bits --
+namespace {
+int checkpoint_args(int dtype, int n_rows, int n_cols, const void* x, const void* codes,
+                    const void* scale) {
+  if (n_rows != 0 && (!x || !codes || !scale)) return TRIMMOE_ERR_NULL;
+  if (dtype != TRIMMOE_F32 && dtype != TRIMMOE_BF16) return TRIMMOE_ERR_DTYPE;
+  if (n_rows < 0 || n_rows > TRIMMOE_LOSS_MAX_ROWS || n_cols < 1 || n_cols > TRIMMOE_LOSS_MAX_D ||
+      (reinterpret_cast<uintptr_t>(x) & (dtype == TRIMMOE_BF16 ? 1 : 3)))
+    return TRIMMOE_ERR_SHAPE;
+  return TRIMMOE_OK;
+}
+int launched(hipError_t e) { return e == hipSuccess ? TRIMMOE_OK : TRIMMOE_ERR_HIP; }
+}  // namespace
+
+int trimmoe_checkpoint_pack(int32_t dtype, int32_t n_rows, int32_t n_cols, const void* x,
+                            int8_t* codes, uint8_t* scale, void* stream) {
+  const int rc = checkpoint_args(dtype, n_rows, n_cols, x, codes, scale);
+  if (rc) return rc;
+  return launched(launch_checkpoint_pack(dtype == TRIMMOE_BF16, n_rows, n_cols, x, codes, scale,
+                                         static_cast<hipStream_t>(stream)));
+}
+
+int trimmoe_checkpoint_unpack(int32_t dtype, int32_t n_rows, int32_t n_cols, const int8_t* codes,
+                              const uint8_t* scale, void* x, void* stream) {
+  const int rc = checkpoint_args(dtype, n_rows, n_cols, x, codes, scale);
+  if (rc) return rc;
+  return launched(launch_checkpoint_unpack(dtype == TRIMMOE_BF16, n_rows, n_cols, codes, scale, x,
+                                           static_cast<hipStream_t>(stream)));
+}
+
+// ---------------------------------------------- expert feed-forward block --
+namespace {
+int ffn_dims(int dtype, int act, int E, int d, int F, int n_rows) {
+  if (act != TRIMMOE_ACT_RELU && act != TRIMMOE_ACT_SWIGLU) return TRIMMOE_ERR_DTYPE;
+  int rc = loss_dims(dtype, d, n_rows);
+  if (!rc) rc = loss_dims(dtype, F, n_rows);
+  if (rc) return rc;
+  return E < 1 || E > TRIMMOE_MAX_EXPERTS || (long long)d * F > (1ll << 40) / E ? TRIMMOE_ERR_SHAPE
+                                                                              : TRIMMOE_OK;
+}
+// what both directions ask of their arrays
+int ffn_arrays(const ExpertFfnArgs& a, int act, const int32_t* offsets) {
+  if (!a.w_up || !a.w_down || !a.ws || (a.gated && !a.w_gate)) return TRIMMOE_ERR_NULL;
+  if (!offsets && a.groups.E != 1) return TRIMMOE_ERR_NULL;
+  if (a.keep != TRIMMOE_KEEP_NONE && a.groups.n != 0) {
+    if (!a.up || (a.gated && !a.gate)) return TRIMMOE_ERR_NULL;
+    if (a.keep == TRIMMOE_KEEP_PACKED && (!a.up_scale || (a.gated && !a.gate_scale)))
+      return TRIMMOE_ERR_NULL;
+  }
+  if (act == TRIMMOE_ACT_RELU && a.w_gate) return TRIMMOE_ERR_SHAPE;
+  // (fp32 codes are bytes of any alignment)
+  const bool kept = a.keep == TRIMMOE_KEEP_FULL || (a.keep == TRIMMOE_KEEP_PACKED && a.bf16);
+  for (const void* p : {a.w_up, a.w_gate, a.w_down})
+    if (!aligned_rows(a.bf16, p)) return TRIMMOE_ERR_SHAPE;
+  if (kept && (!aligned_rows(a.bf16, a.up) || !aligned_rows(a.bf16, a.gate))) return TRIMMOE_ERR_SHAPE;
+  return reinterpret_cast<uintptr_t>(offsets) & 3 ? TRIMMOE_ERR_SHAPE : TRIMMOE_OK;
+}
+}  // namespace
+
+int trimmoe_expert_ffn_workspace_size(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model,
+                                      int32_t d_ff, int32_t n_rows, int32_t keep, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  if (keep < TRIMMOE_KEEP_NONE || keep > TRIMMOE_KEEP_PACKED) return TRIMMOE_ERR_DTYPE;
+  const int rc = ffn_dims(dtype, act, n_experts, d_model, d_ff, n_rows);
+  if (rc) return rc;
+  *bytes = expert_ffn_ws(dtype == TRIMMOE_BF16, act == TRIMMOE_ACT_SWIGLU, keep, n_experts, d_model,
+                         d_ff, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_expert_ffn(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model, int32_t d_ff,
+                       int32_t n_rows, int32_t keep, const void* w_up, const void* w_gate,
+                       const void* w_down, const void* x, const int32_t* offsets, void* y, void* up,
+                       uint8_t* up_scale, void* gate, uint8_t* gate_scale, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int rc = trimmoe_expert_ffn_workspace_size(dtype, act, n_experts, d_model, d_ff, n_rows, keep, &need);
+  if (rc) return rc;
+  ExpertFfnArgs a{};
+  a.bf16 = dtype == TRIMMOE_BF16;
+  a.gated = act == TRIMMOE_ACT_SWIGLU;
+  a.keep = keep;
+  a.d = d_model;
+  a.F = d_ff;
+  a.groups = Groups{offsets, n_experts, n_rows};
+  a.w_up = w_up;
+  a.w_gate = w_gate;
+  a.w_down = w_down;
+  a.x = x;
+  a.y = y;
+  a.up = up;
+  a.gate = gate;
+  a.up_scale = up_scale;
+  a.gate_scale = gate_scale;
+  a.ws = static_cast<char*>(workspace);
+  if ((rc = ffn_arrays(a, act, offsets))) return rc;
+  if (n_rows != 0 && (!x || !y)) return TRIMMOE_ERR_NULL;
+  if (!aligned_rows(a.bf16, x) || !aligned_rows(a.bf16, y)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes, need)) || (rc = device_cus(&a.n_cu))) return rc;
+  return launched(launch_expert_ffn(a, static_cast<hipStream_t>(stream)));
+}
+
+int trimmoe_expert_ffn_backward_workspace_size(int32_t dtype, int32_t act, int32_t n_experts,
+                                               int32_t d_model, int32_t d_ff, int32_t n_rows,
+                                               int32_t x_packed, size_t* bytes) {
+  if (!bytes) return TRIMMOE_ERR_NULL;
+  const int rc = ffn_dims(dtype, act, n_experts, d_model, d_ff, n_rows);
+  if (rc) return rc;
+  *bytes = expert_ffn_backward_ws(dtype == TRIMMOE_BF16, act == TRIMMOE_ACT_SWIGLU, x_packed != 0,
+                                  n_experts, d_model, d_ff, n_rows);
+  return TRIMMOE_OK;
+}
+
+int trimmoe_expert_ffn_backward(int32_t dtype, int32_t act, int32_t n_experts, int32_t d_model,
+                                int32_t d_ff, int32_t n_rows, int32_t keep, int32_t x_packed,
+                                const void* w_up, const void* w_gate, const void* w_down,
+                                const void* x, const uint8_t* x_scale, const void* dy,
+                                const int32_t* offsets, const void* up, const uint8_t* up_scale,
+                                const void* gate, const uint8_t* gate_scale, void* dx, void* dw_up,
+                                void* dw_gate, void* dw_down, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int rc = trimmoe_expert_ffn_backward_workspace_size(dtype, act, n_experts, d_model, d_ff, n_rows,
+                                                      x_packed, &need);
+  if (rc) return rc;
+  if (keep != TRIMMOE_KEEP_FULL && keep != TRIMMOE_KEEP_PACKED) return TRIMMOE_ERR_DTYPE;
+  ExpertFfnArgs a{};
+  a.bf16 = dtype == TRIMMOE_BF16;
+  a.gated = act == TRIMMOE_ACT_SWIGLU;
+  a.keep = keep;
+  a.d = d_model;
+  a.F = d_ff;
+  a.groups = Groups{offsets, n_experts, n_rows};
+  a.w_up = w_up;
+  a.w_gate = w_gate;
+  a.w_down = w_down;
+  a.x = x;
+  a.x_scale = x_packed ? x_scale : nullptr;
+  a.dy = dy;
+  a.up = const_cast<void*>(up);
+  a.gate = const_cast<void*>(gate);
+  a.up_scale = const_cast<uint8_t*>(up_scale);
+  a.gate_scale = const_cast<uint8_t*>(gate_scale);
+  a.dx = dx;
+  a.dw_up = dw_up;
+  a.dw_gate = dw_gate;
+  a.dw_down = dw_down;
+  a.ws = static_cast<char*>(workspace);
+  if ((rc = ffn_arrays(a, act, offsets))) return rc;
+  if (n_rows != 0 && (!x || !dy || (x_packed && !x_scale))) return TRIMMOE_ERR_NULL;
+  if (act == TRIMMOE_ACT_RELU && dw_gate) return TRIMMOE_ERR_SHAPE;
+  for (const void* p : {x_packed ? nullptr : x, dy, static_cast<const void*>(dx),
+                        static_cast<const void*>(dw_up), static_cast<const void*>(dw_gate),
+                        static_cast<const void*>(dw_down)})
+    if (!aligned_rows(a.bf16, p)) return TRIMMOE_ERR_SHAPE;
+  if ((rc = check_ws(workspace, workspace_bytes, need)) || (rc = device_cus(&a.n_cu))) return rc;
+  if (!dx && !dw_up && !dw_gate && !dw_down) return TRIMMOE_OK;
+  return launched(launch_expert_ffn_backward(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,546 @@
+// The expert feed-forward block on rows sorted by expert, and its gradient.
+//   u = x Wu^T, g = x Wg^T, a = silu(g) u (gated) or relu(u), y = a Wd^T
+//   da = dy Wd;  s = sigmoid(g):  du = da g s,  dg = da u s (1 + g (1 - s));
+//   relu: du = da [u > 0]
+//   dx = du Wu + dg Wg,  dWu = du^T x,  dWg = dg^T x,  dWd = dy^T a
+// Forward: one kernel makes both projections and the activation (and keeps u and g, in
+// bf16 or in 8 bits), one the product with Wd.  Backward: da with the activation's
+// derivative in its epilogue (a, du, dg to the workspace, in bf16: they are operands of
+// the products), then dx, then all weight gradients in one kernel.
+// A tile's A side is the contiguous side of its result, so that a lane holds 4
+// consecutive elements of a row and results leave the registers in 16-byte pieces.
+#include "expert_ffn.h"
+
+#include <algorithm>
+
+#include "mid_core.h"
+
+namespace trimmoe {
+
+namespace {
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// a tile of rows: its group (E and above: rows of no group, which have no product)
+struct RowTile {
+  int e, r0, valid;
+  __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, int mt, int tile) {
+    e = t.group(mt);
+    const int2 r = g.rows(e);
+    r0 = uniform(r.x + (mt - t.first[e]) * tile);
+    valid = uniform(min(tile, r.y - r0));
+  }
+};
+
+// sigmoid with the hardware exp2 and reciprocal (about 1 ulp each)
+__device__ __forceinline__ float sigmoid_hw(float g) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-g * 1.4426950408889634f));
+}
+
+// 8 codes of a row, 8 bytes a lane, and the block's scale byte, from two accumulators'
+// values (32 columns over 4 lanes)
+__device__ __forceinline__ void store_codes(const float (&x)[2][4], bool in, int lane, int8_t* codes,
+                                            uint8_t* scale) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) top = max(top, abs_bits(x[k][r]));
+  LanePair p = lanes_xor16(__uint_as_float(top));
+  top = max(__float_as_uint(p.a), __float_as_uint(p.b));
+  p = lanes_xor32(__uint_as_float(top));
+  top = max(__float_as_uint(p.a), __float_as_uint(p.b));
+  const uint32_t s = pack_scale(top);
+  uint32_t w[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    w[k] = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) w[k] |= (uint32_t)(pack_code(x[k][r], s) & 0xff) << (8 * r);
+    w[k] = s == 255 ? 0u : w[k];
+  }
+  const auto q = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+  const uint32_t q0 = q[0], q1 = q[1];
+  if (in) {
+    *reinterpret_cast<uint2*>(codes + pack_col(lane)) = make_uint2(q0, q1);
+    if (lane < 16) *scale = (uint8_t)s;
+  }
+}
+
+// ---------------------------------------------------------------- forward --
+struct UpArgs {
+  Groups groups;
+  const bf16_t *w_up, *w_gate, *x;
+  int d, F, keep;
+  bf16_t* a;  // [n, F]
+  void *up, *gate;
+  uint8_t *up_scale, *gate_scale;
+};
+
+template <bool GATED, int BN, int ST, int KEEP>
+__global__ __launch_bounds__(256, 2) void k_expert_up(UpArgs a) {
+  using T = MidTile<128, BN, ST, false, false, GATED>;
+  using C = MidCore<T>;
+  __shared__ __align__(16) char lds[T::LDS];
+  __shared__ int s_first[kGroupSlots + 1];
+  const C core(lds);
+  GroupTiles tiles;
+  tiles.init(s_first, a.groups, a.groups.E + 2, BN);
+  TileSched S;
+  int ntiles;
+  if (!S.init(tiles.total(), (a.F + T::ROWS_A - 1) / T::ROWS_A, 1, ntiles)) return;
+  constexpr int TMO = GATED ? T::TM / 2 : T::TM;  // 16-column groups of a wavefront
+  for (int jt = 0; jt < ntiles; ++jt) {
+    int mt, nt, sp;
+    S.decode(jt, mt, nt, sp);
+    const RowTile row(tiles, a.groups, mt, BN);
+    const int f0 = nt * T::ROWS_A, f_valid = min(T::ROWS_A, a.F - f0);
+    typename C::Acc acc;
+    C::zero(acc);
+    const bool live = row.e < a.groups.E;
+    if (live) {
+      const size_t w0 = ((size_t)row.e * a.F + f0) * a.d;
+      MidOperand<T::PA> A;
+      MidOperand<T::PB> B;
+      mid_rows(A, a.w_up + w0, a.d, f_valid, a.d, GATED);
+      if constexpr (GATED) A.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
+      mid_rows(B, a.x + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
+      core.run(A, B, a.d / BK, acc);
+    }
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+#pragma unroll
+      for (int i = 0; i < TMO; i += 2) {
+        const int c = f0 + core.wm * 16 * TMO + 16 * i;  // 32 columns, all of them or none in F
+        const bool in = t < row.valid && c < a.F;
+        const size_t o = (size_t)(row.r0 + t) * a.F + c;
+        float u[2][4], g[2][4], v[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            u[k][r] = acc[i + k][j][r];
+            if constexpr (GATED) {
+              g[k][r] = acc[i + k + TMO][j][r];
+              v[k][r] = g[k][r] * sigmoid_hw(g[k][r]) * u[k][r];
+            } else {
+              v[k][r] = u[k][r] < 0.f ? 0.f : u[k][r];  // (NaN stays)
+            }
+          }
+        const int pc = pack_col(core.lane);
+        const u32x4_t pv = pack_rows(v[0], v[1]);
+        if (in) *reinterpret_cast<u32x4_t*>(a.a + o + pc) = pv;
+        if constexpr (KEEP == TRIMMOE_KEEP_FULL) {
+          const u32x4_t pu = pack_rows(u[0], u[1]);
+          if (in) *reinterpret_cast<u32x4_t*>(static_cast<bf16_t*>(a.up) + o + pc) = pu;
+          if constexpr (GATED) {
+            const u32x4_t pg = pack_rows(g[0], g[1]);
+            if (in) *reinterpret_cast<u32x4_t*>(static_cast<bf16_t*>(a.gate) + o + pc) = pg;
+          }
+        }
+        if constexpr (KEEP == TRIMMOE_KEEP_PACKED) {
+          store_codes(u, in, core.lane, static_cast<int8_t*>(a.up) + o, a.up_scale + o / kPackBlock);
+          if constexpr (GATED)
+            store_codes(g, in, core.lane, static_cast<int8_t*>(a.gate) + o,
+                        a.gate_scale + o / kPackBlock);
+        }
+      }
+    }
+  }
+}
+
+// out [n, M] = rows times weights: y = a Wd^T (Wd K-contiguous) or, ATR, dx = du Wu (+
+// dg Wg) (weights along K; the second product continues the first one's K).  Rows of no
+// group get zeros.
+struct RowsArgs {
+  Groups groups;
+  const bf16_t *w, *w2;  // expert 0; w2: NULL or the second product's
+  const bf16_t *b, *b2;  // [n, K]
+  int M, K;
+  bf16_t* out;
+};
+
+template <bool ATR, int BN, int ST>
+__global__ __launch_bounds__(256, 2) void k_expert_rows(RowsArgs a) {
+  using T = MidTile<128, BN, ST, ATR, false>;
+  using C = MidCore<T>;
+  __shared__ __align__(16) char lds[T::LDS];
+  __shared__ int s_first[kGroupSlots + 1];
+  const C core(lds);
+  GroupTiles tiles;
+  tiles.init(s_first, a.groups, a.groups.E + 2, BN);
+  TileSched S;
+  int ntiles;
+  if (!S.init(tiles.total(), (a.M + T::BM - 1) / T::BM, 1, ntiles)) return;
+  for (int jt = 0; jt < ntiles; ++jt) {
+    int mt, nt, sp;
+    S.decode(jt, mt, nt, sp);
+    const RowTile row(tiles, a.groups, mt, BN);
+    const int m0 = nt * T::BM;
+    typename C::Acc acc;
+    C::zero(acc);
+    if (row.e < a.groups.E) {
+      const size_t e0 = (size_t)row.e * a.M * a.K, b0 = (size_t)row.r0 * a.K;
+      MidOperand<T::PA> A;
+      MidOperand<T::PB> B;
+      if constexpr (ATR) {
+        mid_along<T::BM>(A, a.w + e0, a.M, m0, a.K);
+        if (a.w2) {
+          A.q = reinterpret_cast<const char*>(a.w2 + e0 + m0);
+          A.kq = a.K;
+        }
+      } else {
+        mid_rows(A, a.w + e0 + (size_t)m0 * a.K, a.K, min(T::BM, a.M - m0), a.K);
+      }
+      mid_rows(B, a.b + b0, a.K, row.valid, a.K);
+      if (ATR && a.w2) {
+        B.q = reinterpret_cast<const char*>(a.b2 + b0);
+        B.kq = a.K;
+      }
+      core.run(A, B, a.K / BK * (ATR && a.w2 ? 2 : 1), acc);
+    }
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+#pragma unroll
+      for (int i = 0; i < T::TM; i += 2) {
+        const int c = m0 + core.wm * T::WM + 16 * i;
+        float v[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[k][r] = acc[i + k][j][r];
+        const u32x4_t p = pack_rows(v[0], v[1]);
+        if (t < row.valid && c < a.M)
+          *reinterpret_cast<u32x4_t*>(a.out + (size_t)(row.r0 + t) * a.M + c + pack_col(core.lane)) = p;
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------- backward --
+struct DactArgs {
+  Groups groups;
+  const bf16_t *w_down, *dy;
+  int d, F;
+  const void *up, *gate;
+  const uint8_t *up_scale, *gate_scale;
+  bf16_t *a, *du, *dg;  // [n, F]
+};
+
+// 4 consecutive kept values, from element o on
+template <bool PACKED>
+__device__ __forceinline__ void kept4(float (&v)[4], const void* p, const uint8_t* scale, size_t o) {
+  if constexpr (PACKED) {
+    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(p) + o);
+    const uint32_t s = scale[o / kPackBlock];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = pack_value((int8_t)(w >> (8 * r)), s);
+  } else {
+    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(p) + o);
+    v[0] = bf2f((bf16_t)w.x);
+    v[1] = bf2f((bf16_t)(w.x >> 16));
+    v[2] = bf2f((bf16_t)w.y);
+    v[3] = bf2f((bf16_t)(w.y >> 16));
+  }
+}
+
+template <bool GATED, bool PACKED, int BN, int ST>
+__global__ __launch_bounds__(256, 2) void k_expert_dact(DactArgs a) {
+  using T = MidTile<128, BN, ST, true, false>;
+  using C = MidCore<T>;
+  __shared__ __align__(16) char lds[T::LDS];
+  __shared__ int s_first[kGroupSlots + 1];
+  const C core(lds);
+  GroupTiles tiles;
+  tiles.init(s_first, a.groups, a.groups.E, BN);
+  TileSched S;
+  int ntiles;
+  if (!S.init(tiles.total(), (a.F + T::BM - 1) / T::BM, 1, ntiles)) return;
+  for (int jt = 0; jt < ntiles; ++jt) {
+    int mt, nt, sp;
+    S.decode(jt, mt, nt, sp);
+    const RowTile row(tiles, a.groups, mt, BN);
+    const int f0 = nt * T::BM;
+    typename C::Acc acc;
+    C::zero(acc);
+    MidOperand<T::PA> A;
+    MidOperand<T::PB> B;
+    mid_along<T::BM>(A, a.w_down + (size_t)row.e * a.d * a.F, a.F, f0, a.d);
+    mid_rows(B, a.dy + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
+    core.run(A, B, a.d / BK, acc);
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+#pragma unroll
+      for (int i = 0; i < T::TM; i += 2) {
+        const int c = f0 + core.wm * T::WM + 16 * i;
+        const bool in = t < row.valid && c < a.F;
+        const size_t o = (size_t)(row.r0 + t) * a.F + c;
+        float va[2][4], vu[2][4], vg[2][4];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float u[4] = {}, g[4] = {};
+          if (in) {
+            const size_t ok = o + 16 * k + 4 * (core.lane >> 4);
+            kept4<PACKED>(u, a.up, a.up_scale, ok);
+            if constexpr (GATED) kept4<PACKED>(g, a.gate, a.gate_scale, ok);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float da = acc[i + k][j][r];
+            if constexpr (GATED) {
+              const float s = sigmoid_hw(g[r]), gs = g[r] * s;
+              va[k][r] = gs * u[r];
+              vu[k][r] = da * gs;
+              vg[k][r] = da * u[r] * (s * (1.f + g[r] * (1.f - s)));
+            } else {
+              va[k][r] = u[r] < 0.f ? 0.f : u[r];
+              vu[k][r] = u[r] > 0.f ? da : 0.f;
+            }
+          }
+        }
+        const int pc = pack_col(core.lane);
+        const u32x4_t pa = pack_rows(va[0], va[1]), pu = pack_rows(vu[0], vu[1]);
+        if (in) {
+          *reinterpret_cast<u32x4_t*>(a.a + o + pc) = pa;
+          *reinterpret_cast<u32x4_t*>(a.du + o + pc) = pu;
+        }
+        if constexpr (GATED) {
+          const u32x4_t pg = pack_rows(vg[0], vg[1]);
+          if (in) *reinterpret_cast<u32x4_t*>(a.dg + o + pc) = pg;
+        }
+      }
+    }
+  }
+}
+
+// Weight gradients: of group e and product p, out [N, M] = B^T A over the group's rows
+// (dWd: A = a, B = dy; dWu, dWg: A = x, B = du, dg).  A group without rows gets zeros.
+struct WeightArgs {
+  Groups groups;
+  int n_prod;
+  const bf16_t *A[3], *B[3];
+  int M[3], N[3];
+  bf16_t* out[3];
+};
+
+template <int BM, int BN, int ST>
+__global__ __launch_bounds__(256, 2) void k_expert_weights(WeightArgs a) {
+  using T = MidTile<BM, BN, ST, true, true>;
+  using C = MidCore<T>;
+  __shared__ __align__(16) char lds[T::LDS];
+  const C core(lds);
+  TileSched S;
+  int ntiles;
+  int first[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int p = 0; p < 3; ++p)
+    first[p + 1] = first[p] + (p < a.n_prod ? ((a.M[p] + BM - 1) / BM) * ((a.N[p] + BN - 1) / BN) : 0);
+  if (!S.init_total(a.groups.E * first[3], 1, 1, ntiles)) return;
+  for (int jt = 0; jt < ntiles; ++jt) {
+    const int L = S.tb + S.i0 + jt * S.bx, e = L / first[3], at = L - e * first[3];
+    const int p = at >= first[2] ? 2 : at >= first[1] ? 1 : 0;
+    const int M = p == 0 ? a.M[0] : p == 1 ? a.M[1] : a.M[2];
+    const int N = p == 0 ? a.N[0] : p == 1 ? a.N[1] : a.N[2];
+    const bf16_t* pA = p == 0 ? a.A[0] : p == 1 ? a.A[1] : a.A[2];
+    const bf16_t* pB = p == 0 ? a.B[0] : p == 1 ? a.B[1] : a.B[2];
+    bf16_t* out = p == 0 ? a.out[0] : p == 1 ? a.out[1] : a.out[2];
+    TileSched P;
+    P.n_mt = (N + BN - 1) / BN;
+    P.n_nt = (M + BM - 1) / BM;
+    int mt, nt, sp;
+    P.decode_abs(at - (p == 0 ? 0 : p == 1 ? first[1] : first[2]), mt, nt, sp);
+    const int m0 = nt * BM, n0 = mt * BN;
+    const int2 r = a.groups.rows(e);
+    const int r0 = uniform(r.x), k = uniform(r.y) - r0;
+    typename C::Acc acc;
+    C::zero(acc);
+    if (k > 0) {
+      MidOperand<T::PA> A;
+      MidOperand<T::PB> B;
+      mid_along<BM>(A, pA + (size_t)r0 * M, M, m0, k);
+      mid_along<BN>(B, pB + (size_t)r0 * N, N, n0, k);
+      core.run(A, B, (k + BK - 1) / BK, acc);
+    }
+    bf16_t* o = out + (size_t)e * M * N;
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) {
+      const int t = n0 + core.wn * T::WN + 16 * j + (core.lane & 15);
+#pragma unroll
+      for (int i = 0; i < T::TM; i += 2) {
+        const int c = m0 + core.wm * T::WM + 16 * i;
+        float v[2][4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+          for (int s = 0; s < 4; ++s) v[q][s] = acc[i + q][j][s];
+        const u32x4_t w = pack_rows(v[0], v[1]);
+        if (t < N && c < M)
+          *reinterpret_cast<u32x4_t*>(o + (size_t)t * M + c + pack_col(core.lane)) = w;
+      }
+    }
+  }
+}
+
+// --------------------------------------------------------------- launching --
+// blocks of a launch over at most `tiles` tiles
+unsigned grid_of(long tiles) { return (unsigned)std::min<long>(std::max<long>(tiles, 1), 65536); }
+
+// rows a tile: no more than the groups have on average
+bool few_rows(const Groups& g) { return (long)g.n <= 32l * g.E; }
+
+// f(integral constant of the rows a tile, ... of its stages)
+template <typename F>
+hipError_t with_rows(const Groups& g, F f) {
+  if (few_rows(g))
+    f(std::integral_constant<int, 32>(), std::integral_constant<int, 3>());
+  else
+    f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>());
+  return hipGetLastError();
+}
+
+template <bool GATED, int KEEP>
+hipError_t launch_up(const UpArgs& a, hipStream_t st) {
+  return with_rows(a.groups, [&](auto bn, auto stages) {
+    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.F, GATED ? 64 : 128);
+    hipLaunchKernelGGL((k_expert_up<GATED, bn, stages, KEEP>), dim3(grid_of(n)), dim3(256), 0, st, a);
+  });
+}
+
+template <bool ATR>
+hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
+  return with_rows(a.groups, [&](auto bn, auto stages) {
+    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.M, 128);
+    hipLaunchKernelGGL((k_expert_rows<ATR, bn, stages>), dim3(grid_of(n)), dim3(256), 0, st, a);
+  });
+}
+
+template <bool GATED, bool PACKED>
+hipError_t launch_dact(const DactArgs& a, hipStream_t st) {
+  return with_rows(a.groups, [&](auto bn, auto stages) {
+    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.F, 128);
+    hipLaunchKernelGGL((k_expert_dact<GATED, PACKED, bn, stages>), dim3(grid_of(n)), dim3(256), 0, st, a);
+  });
+}
+
+const bf16_t* as_bf16(const void* p) { return static_cast<const bf16_t*>(p); }
+
+}  // namespace
+
+size_t expert_ffn_ws(bool bf16, bool gated, int keep, int E, int d, int F, int n) {
+  const size_t act = ffn_array(n, F, bf16 ? 2 : 4);
+  // (fp32 pre-activations are packed by a launch of their own)
+  return act + (!bf16 && keep == TRIMMOE_KEEP_PACKED ? (gated ? 2 : 1) * act : 0);
+}
+
+size_t expert_ffn_backward_ws(bool bf16, bool gated, bool x_packed, int E, int d, int F, int n) {
+  const int elem = bf16 ? 2 : 4;
+  return (gated ? 3 : 2) * ffn_array(n, F, elem) + (x_packed ? ffn_array(n, d, elem) : 0);
+}
+
+hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
+  if (a.groups.n == 0) return hipSuccess;
+  if (!a.bf16) return launch_expert_ffn_f32(a, st);
+  UpArgs u{};
+  u.groups = a.groups;
+  u.w_up = as_bf16(a.w_up);
+  u.w_gate = as_bf16(a.w_gate);
+  u.x = as_bf16(a.x);
+  u.d = a.d;
+  u.F = a.F;
+  u.keep = a.keep;
+  u.a = reinterpret_cast<bf16_t*>(a.ws);
+  u.up = a.up;
+  u.gate = a.gate;
+  u.up_scale = a.up_scale;
+  u.gate_scale = a.gate_scale;
+  hipError_t e;
+  if (a.gated)
+    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<true, TRIMMOE_KEEP_FULL>(u, st)
+        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<true, TRIMMOE_KEEP_PACKED>(u, st)
+                                        : launch_up<true, TRIMMOE_KEEP_NONE>(u, st);
+  else
+    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<false, TRIMMOE_KEEP_FULL>(u, st)
+        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<false, TRIMMOE_KEEP_PACKED>(u, st)
+                                        : launch_up<false, TRIMMOE_KEEP_NONE>(u, st);
+  if (e != hipSuccess) return e;
+  RowsArgs r{};
+  r.groups = a.groups;
+  r.w = as_bf16(a.w_down);
+  r.b = u.a;
+  r.M = a.d;
+  r.K = a.F;
+  r.out = static_cast<bf16_t*>(a.y);
+  return launch_rows<false>(r, st);
+}
+
+hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
+  if (!a.bf16) return launch_expert_ffn_backward_f32(a, st);
+  const int n = a.groups.n;
+  const size_t act = ffn_array(n, a.F, 2);
+  DactArgs t{};
+  t.groups = a.groups;
+  t.w_down = as_bf16(a.w_down);
+  t.dy = as_bf16(a.dy);
+  t.d = a.d;
+  t.F = a.F;
+  t.up = a.up;
+  t.gate = a.gate;
+  t.up_scale = a.up_scale;
+  t.gate_scale = a.gate_scale;
+  t.a = reinterpret_cast<bf16_t*>(a.ws);
+  t.du = reinterpret_cast<bf16_t*>(a.ws + act);
+  t.dg = a.gated ? reinterpret_cast<bf16_t*>(a.ws + 2 * act) : nullptr;
+  hipError_t e = hipSuccess;
+  const bf16_t* x = as_bf16(a.x);
+  if (n > 0) {
+    if (a.gated)
+      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<true, true>(t, st) : launch_dact<true, false>(t, st);
+    else
+      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<false, true>(t, st)
+                                        : launch_dact<false, false>(t, st);
+    if (e != hipSuccess) return e;
+    if (a.x_scale && (a.dw_up || a.dw_gate)) {
+      bf16_t* to = reinterpret_cast<bf16_t*>(a.ws + (a.gated ? 3 : 2) * act);
+      e = launch_checkpoint_unpack(true, n, a.d, static_cast<const int8_t*>(a.x), a.x_scale, to, st);
+      if (e != hipSuccess) return e;
+      x = to;
+    }
+    if (a.dx) {
+      RowsArgs r{};
+      r.groups = a.groups;
+      r.w = as_bf16(a.w_up);
+      r.w2 = a.gated ? as_bf16(a.w_gate) : nullptr;
+      r.b = t.du;
+      r.b2 = t.dg;
+      r.M = a.d;
+      r.K = a.F;
+      r.out = static_cast<bf16_t*>(a.dx);
+      if ((e = launch_rows<true>(r, st)) != hipSuccess) return e;
+    }
+  }
+  WeightArgs w{};
+  w.groups = a.groups;
+  long tiles = 0;
+  const auto add = [&](const bf16_t* A, const bf16_t* B, int M, int N, void* out) {
+    if (!out) return;
+    const int p = w.n_prod++;
+    w.A[p] = A;
+    w.B[p] = B;
+    w.M[p] = M;
+    w.N[p] = N;
+    w.out[p] = static_cast<bf16_t*>(out);
+    tiles += (long)cdiv(M, 128) * cdiv(N, 128);
+  };
+  add(t.a, t.dy, a.F, a.d, a.dw_down);
+  add(x, t.du, a.d, a.F, a.dw_up);
+  if (a.gated) add(x, t.dg, a.d, a.F, a.dw_gate);
+  if (w.n_prod == 0) return hipSuccess;
+  hipLaunchKernelGGL((k_expert_weights<128, 128, 2>), dim3(grid_of(tiles * a.groups.E)), dim3(256), 0, st,
+                     w);
+  return hipGetLastError();
+}
+
+}  // namespace trimmoe

@@ -1,0 +1,227 @@
+// A bf16 matrix core for products whose operands lie in either order: C = A B^T on BM x
+// BN tiles by four wavefronts, two or more blocks a CU.  Not part of the public ABI.
+//
+// An operand is K-contiguous ([rows][K]: 64-element K slices land as 128-byte rows) or
+// runs along K (TR, [K][rows]: a slice is 64 rows of BM or BN columns), and is read out
+// of LDS as it lies or transposed (ds_read_b64_tr_b16).  Slices go straight to LDS by
+// DMA into a ring of ST stages, ST - 1 of them in flight; one barrier a slice.  The
+// MFMAs are 16 x 16 x 32.  An operand may go on in a second array where the first one's
+// K ends.  Fragment reads are inline asm with explicit waits, as in the other cores: the
+// compiler would wait for every DMA before each of them.
+#pragma once
+
+#include "mfma_core.h"
+
+namespace trimmoe {
+
+// K slices of an operand as a tile takes them.  Everything but off is wave-uniform.
+template <int NP>  // DMAs a thread and slice
+struct MidOperand {
+  const char* p;     // not TR: row 0 at the slice; TR: the slice's first row, column 0 of the tile
+  const char* p1;    // the second operand of a pair (see MidTile::PAIR)
+  const char* q;     // where the second array begins (kq of it), or anything (kq 0)
+  uint32_t inc;      // bytes from slice to slice
+  uint32_t row, cut; // TR: bytes of a row, and of a row before the tile's columns
+  int k, kq;         // K left from the slice on, in this array and in the next
+  uint32_t off[NP];
+  template <bool TR>
+  __device__ __forceinline__ uint32_t bytes() const {
+    if constexpr (TR)
+      return k > 0 ? (uint32_t)min(k, BK) * row - cut : 0u;
+    else
+      // (a select of constants would be made in a vector register)
+      return __builtin_amdgcn_readfirstlane(k > 0 ? 0xffffffffu : 0u);
+  }
+  __device__ __forceinline__ void step() {
+    p += inc;
+    p1 += inc;
+    k -= BK;
+    if (k <= 0) {
+      p = q;
+      k = kq;
+      kq = 0;
+    }
+  }
+};
+
+// PAIR: A holds two K-contiguous operands in turns of 32 rows, so that a wavefront's
+// fragments 0 .. TM / 2 - 1 are rows of the first and the rest the same rows of the second.
+template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false>
+struct MidTile {
+  static constexpr int BM = BM_, BN = BN_, ST = ST_;
+  static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
+  static constexpr int THREADS = 256, GM = 2, GN = 2;
+  static constexpr int WM = BM / GM, WN = BN / GN, TM = WM / 16, TN = WN / 16;
+  static constexpr int PA = BM / 32, PB = BN / 32;  // DMAs a thread
+  static constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, LDS = ST * STAGE;
+  static constexpr int ROWS_A = PAIR ? BM / 2 : BM;  // rows of C's A side
+  static_assert(!PAIR || (WM == 64 && !ATR), "pairs go by 32 rows");
+  static_assert(ST >= 2 && (PA + PB) * (ST - 2) < 64, "waits");
+};
+
+// 32-byte piece of a transposed operand's row k where its piece 0 sits (exclusive or):
+// the eight rows that 32 lanes read together then touch distinct banks
+template <int COLS>
+__device__ __forceinline__ int mid_swz(int k) {
+  if constexpr (COLS >= 128) return (k & 3) | ((k >> 3 & 1) << 2);
+  if constexpr (COLS == 64) return (k >> 1 & 1) | ((k >> 3 & 1) << 1);
+  return k >> 3 & 1;
+}
+
+// this thread's DMA offsets: of a K-contiguous operand's rows (ld elements each, rows
+// past `valid` repeat the last one) ...
+template <int NP>
+__device__ __forceinline__ void mid_rows(MidOperand<NP>& o, const bf16_t* p, int ld, int valid, int k,
+                                         bool pair = false) {
+  const int r0 = threadIdx.x >> 3;
+  o.p = reinterpret_cast<const char*>(p);
+  o.inc = 2 * BK;
+  o.row = o.cut = 0;
+  o.k = k;
+  o.kq = 0;
+  o.q = o.p1 = o.p;
+#pragma unroll
+  for (int u = 0; u < NP; ++u) {
+    const int r = pair ? r0 + 32 * (u >> 1) : r0 + 32 * u;
+    o.off[u] = ((uint32_t)min(r, valid - 1) * (uint32_t)ld + 8 * ((threadIdx.x & 7) ^ swz16(r0))) * 2;
+  }
+}
+// ... and of one along K, k rows of it from row 0 at p, from column c0 on
+template <int COLS, int NP>
+__device__ __forceinline__ void mid_along(MidOperand<NP>& o, const bf16_t* p, int ld, int c0, int k) {
+  o.p = reinterpret_cast<const char*>(p + c0);
+  o.row = 2 * (uint32_t)ld;
+  o.cut = 2 * (uint32_t)c0;
+  o.inc = o.row * BK;
+  o.k = k;
+  o.kq = 0;
+  o.q = o.p1 = o.p;
+#pragma unroll
+  for (int u = 0; u < NP; ++u) {
+    const int i = u * 256 + (int)threadIdx.x, kr = i / (COLS / 8), c = i % (COLS / 8);
+    o.off[u] = ((uint32_t)kr * (uint32_t)ld + 16 * ((c >> 1) ^ mid_swz<COLS>(kr)) + 8 * (c & 1)) * 2;
+  }
+}
+
+template <class T>
+struct MidCore {
+  using Acc = f32x4_t[T::TM][T::TN];
+  struct Frags {
+    bf16x8_t a[T::TM], b[T::TN];
+  };
+  static constexpr int NDMA = T::PA + T::PB;
+  static constexpr int OPS = T::TM * (T::ATR ? 2 : 1) + T::TN * (T::BTR ? 2 : 1);  // LDS reads a k-step
+  int lane, wave, wm, wn;
+  uint32_t s0, la[2], lb[2];
+
+  __device__ __forceinline__ explicit MidCore(char* lds) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    wm = wave >> 1;
+    wn = wave & 1;
+    s0 = lds_addr(lds);
+    place<T::ATR, T::BM>(la, wm * T::WM);
+    place<T::BTR, T::BN>(lb, wn * T::WN);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) lb[ks] += T::A_BYTES;
+  }
+  // LDS offsets of the lane's part of fragment 0
+  template <bool TR, int COLS>
+  __device__ __forceinline__ void place(uint32_t (&o)[2], int first) const {
+    const int fr = lane & 15, hk = lane >> 4;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      if constexpr (TR) {
+        const int k = 32 * ks + 8 * hk + (fr >> 2);
+        o[ks] = k * COLS * 2 + (((first >> 4) ^ mid_swz<COLS>(k)) << 5) + 8 * (fr & 3);
+      } else {
+        o[ks] = (first + fr) * 128 + (((4 * ks + hk) ^ swz16(fr)) << 4);
+      }
+    }
+  }
+  template <bool TR, int COLS>
+  static __device__ __forceinline__ bf16x8_t read1(uint32_t at, int n) {
+    if constexpr (TR) {
+      typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+      u32x2_t lo, hi;
+      const uint32_t a = at ^ (uint32_t)(n << 5);
+      asm volatile("ds_read_b64_tr_b16 %0, %1" : "=v"(lo) : "v"(a));
+      asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(a), "n"(4 * COLS * 2));
+      return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
+    } else {
+      return lds_read(at + n * 16 * 128);
+    }
+  }
+  __device__ __forceinline__ void read(Frags& f, uint32_t stage, int ks) const {
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) f.a[i] = read1<T::ATR, T::BM>(stage + la[ks], i);
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) f.b[j] = read1<T::BTR, T::BN>(stage + lb[ks], j);
+  }
+  template <int N>
+  static __device__ __forceinline__ void wait(Frags& f) {
+    asm volatile("s_waitcnt lgkmcnt(%0)" ::"n"(N < 15 ? N : 15));
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) asm volatile("" : "+v"(f.a[i]));
+#pragma unroll
+    for (int j = 0; j < T::TN; ++j) asm volatile("" : "+v"(f.b[j]));
+  }
+  static __device__ __forceinline__ void mma(const Frags& f, Acc& acc) {
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < T::TN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+  }
+  template <bool TR, bool PAIR, int NP>
+  __device__ __forceinline__ void issue1(uint32_t dst, const MidOperand<NP>& o) const {
+    const uint32_t n = o.template bytes<TR>();
+    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p), (short)0, (int)n, 0x00020000);
+    const auto r1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(PAIR ? o.p1 : o.p), (short)0,
+                                                      (int)n, 0x00020000);
+#pragma unroll
+    for (int u = 0; u < NP; ++u)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(
+          PAIR && (u & 1) ? r1 : rs, (lds_byte*)(uintptr_t)(dst + (uint32_t)(u * 4096 + wave * 1024)), 16,
+          o.off[u], 0, 0, 0);
+  }
+  template <class A, class B>
+  __device__ __forceinline__ void issue(int stage, A& a, B& b) const {
+    const uint32_t s = s0 + stage * T::STAGE;
+    issue1<T::ATR, T::PAIR>(s, a);
+    issue1<T::BTR, false>(s + T::A_BYTES, b);
+    a.step();
+    b.step();
+  }
+  static __device__ __forceinline__ void zero(Acc& acc) {
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4_t{};
+  }
+  // acc += the tile's product over nk slices; afterwards LDS is free.  Loads past the
+  // last slice bring zeros into stages that nobody reads.
+  __device__ __forceinline__ void run(MidOperand<T::PA>& a, MidOperand<T::PB>& b, int nk, Acc& acc) const {
+    if (nk <= 0) return;
+#pragma unroll
+    for (int s = 0; s < T::ST - 1; ++s) issue(s, a, b);
+    int st = 0, in = T::ST - 1;
+    for (int g = 0; g < nk; ++g) {
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NDMA * (T::ST - 2)) : "memory");
+      issue(in, a, b);
+      in = in + 1 == T::ST ? 0 : in + 1;
+      const uint32_t s = s0 + st * T::STAGE;
+      st = st + 1 == T::ST ? 0 : st + 1;
+      Frags f0, f1;
+      read(f0, s, 0);
+      read(f1, s, 1);
+      wait<OPS>(f0);
+      mma(f0, acc);
+      wait<0>(f1);
+      mma(f1, acc);
+    }
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+};
+
+}  // namespace trimmoe

@@ -1,0 +1,486 @@
+"""GPU parity of the expert feed-forward block, its gradient and 8-bit
+checkpoints through the C ABI, against the fp64 oracle on the same stored values.
+
+Every tolerance is an error bound of the stated arithmetic, element by element:
+u = 2^-24 is half a step of fp32, and a sum of K products in any order is off by
+at most (K + 8) u times the sum of their magnitudes.  bf16 adds half a step, 2^-8
+of the value, for each output and for a, du and dg where they enter a product.
+A sigmoid by exp2 and a reciprocal of 1 ulp each is off by (4 + 2 |g|) u of
+itself (the exponent's argument rounds by |g| log2 e u, twice).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ffn as X
+from paper_2608_00573_amd import abi
+from synthgen.rng import normal_f32
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+TINY = 1e-30
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _half(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def _mat(seed, tid, shape, sigma, dtype):
+    t = normal_f32(seed, tid, shape, sigma, "cpu").to(dtype)
+    return t, t.double().numpy()
+
+
+def _np(t):
+    return t.double().cpu().numpy()
+
+
+def _within(got, want, bound, what):
+    got = _np(got)
+    assert got.shape == want.shape, what
+    with np.errstate(invalid="ignore"):
+        bad = ~(np.abs(got - want) <= bound) & ~(got == want)
+    assert not bad.any(), (what, int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4],
+                           want[bad][:4], np.broadcast_to(bound, bad.shape)[bad][:4])
+
+
+def _borders(sizes, head=0):
+    return (head + np.concatenate([[0], np.cumsum(sizes)])).astype(np.int32)
+
+
+class Block:
+    """One call's inputs: sizes of the experts' rows, rows of none before and behind."""
+
+    def __init__(self, seed, dtype, gated, d, F, sizes, head=0, tail=0, sigma_x=1.0):
+        self.dtype, self.gated, self.d, self.F = dtype, gated, d, F
+        self.off = _borders(sizes, head)
+        E, n = len(sizes), int(self.off[-1]) + tail
+        self.E, self.n = E, n
+        self.wu = _mat(seed, 1, (E, F, d), d ** -0.5, dtype)
+        self.wg = _mat(seed, 2, (E, F, d), d ** -0.5, dtype) if gated else (None, None)
+        self.wd = _mat(seed, 3, (E, d, F), F ** -0.5, dtype)
+        self.x = _mat(seed, 4, (n, d), sigma_x, dtype)
+        self.dy = _mat(seed, 5, (n, d), 0.1, dtype)
+        self.w = tuple(None if m[0] is None else m[0].to(DEV) for m in (self.wu, self.wg, self.wd))
+        self.xd, self.dyd = self.x[0].to(DEV), self.dy[0].to(DEV)
+        self.offd = torch.from_numpy(self.off).to(DEV)
+
+    def forward(self, keep, **kw):
+        return abi.trimmoe_expert_ffn(*self.w, self.xd, self.offd, keep=keep, **kw)
+
+    def backward(self, kept, x=None, **kw):
+        return abi.trimmoe_expert_ffn_backward(*self.w, self.xd if x is None else x, self.dyd, kept,
+                                               self.offd, **kw)
+
+    def rows(self, w, x):
+        return X.pre(w, x, self.off)
+
+    def check_forward(self, y, kept, keep, what=""):
+        h = _half(self.dtype)
+        wy, u, g = X.forward(self.wu[1], self.wg[1], self.wd[1], self.x[1], self.off)
+        k8 = (self.d + 8) * U
+        eu = k8 * self.rows(np.abs(self.wu[1]), np.abs(self.x[1]))
+        a = X.act(u, g)
+        ea = eu
+        if self.gated:
+            eg = k8 * self.rows(np.abs(self.wg[1]), np.abs(self.x[1]))
+            # |silu'| <= 1.1
+            ea = (np.abs(X.act(g, None) * 0 + X._sigmoid(g) * g) * eu + 1.1 * np.abs(u) * eg + 1.1 * eu * eg
+                  + (8 + 2 * np.abs(g)) * U * np.abs(a) * 1.01)
+        ra = ea + (h * (np.abs(a) + ea) if self.dtype == BF16 else 0.0)
+        ey = (self.rows(np.abs(self.wd[1]), ra) * 1.01
+              + (self.F + 8) * U * self.rows(np.abs(self.wd[1]), np.abs(a)) * 1.01)
+        _within(y, wy, ey + (h * (np.abs(wy) + ey) if self.dtype == BF16 else 0.0) + TINY, what + "y")
+        if keep is None:
+            assert kept is None
+            return
+        assert (kept[1] is None) == (not self.gated)
+        for name, k, v, e in (("up", kept[0], u, eu),) + ((("gate", kept[1], g, eg),) if self.gated else ()):
+            if keep == "full":
+                _within(k, v, e + (h * (np.abs(v) + e) if self.dtype == BF16 else 0.0), what + name)
+            else:
+                top = np.abs(np.pad(v, ((0, 0), (0, -self.F % 32)))).reshape(self.n, -1, 32).max(2)
+                et = np.pad(e, ((0, 0), (0, -self.F % 32))).reshape(self.n, -1, 32).max(2)
+                wide = np.repeat((top + et) / 127, 32, 1)[:, :self.F]
+                back = X.unpack(k.codes.cpu().numpy(), k.scale.cpu().numpy())
+                _within(torch.from_numpy(back), v, e + wide + TINY, what + name)
+
+    def check_backward(self, got, kept, what="", x=None):
+        """kept, x: the values that the call took, in fp64."""
+        u, g = kept
+        x = self.x[1] if x is None else x
+        h = _half(self.dtype)
+        r = h if self.dtype == BF16 else 0.0
+        dy = self.dy[1]
+        want = X.backward(self.wu[1], self.wg[1], self.wd[1], x, dy, u, g, self.off)
+        da, eda = np.zeros_like(u), np.zeros_like(u)
+        for e, (i, j) in enumerate(X.groups(self.off, self.n)):
+            da[i:j] = dy[i:j] @ self.wd[1][e]
+            eda[i:j] = (self.d + 8) * U * (np.abs(dy[i:j]) @ np.abs(self.wd[1][e]))
+        du, dg = X.dact(da, u, g)
+        a = X.act(u, g)
+        if self.gated:
+            s, ag = X._sigmoid(g), np.abs(g)
+            es = (4 + 2 * ag) * U
+            edu = np.abs(g * s) * eda + (es + 4 * U) * np.abs(du)
+            f = u * s * (1 + g * (1 - s))
+            edg = (np.abs(f) * eda + np.abs(da * u) * s * ((es + 6 * U) * (1 + ag)
+                                                            + ag * (es + U))) * 1.01
+            ea = (es + 3 * U) * np.abs(a)
+        else:
+            edu, ea = np.where(u > 0, eda, 0.0), 0.0 * a
+        rnd = lambda v, e: (e + r * (np.abs(v) + e)) * 1.01  # noqa: E731
+        bdu, ba = rnd(du, edu), rnd(a, ea)
+        bdg = rnd(dg, edg) if self.gated else None
+        out = lambda w, e: e + (h * (np.abs(w) + e) if self.dtype == BF16 else 0.0) + TINY  # noqa: E731
+        dx, dwu, dwg, dwd = got
+        ex = np.zeros_like(x)
+        ew = [np.zeros_like(w) if w is not None else None for w in (self.wu[1], self.wg[1], self.wd[1])]
+        sums = (2 * self.F + 16) * U
+        for e, (i, j) in enumerate(X.groups(self.off, self.n)):
+            wu = np.abs(self.wu[1][e])
+            rows = (j - i + 16) * U
+            ax, ady = np.abs(x[i:j]), np.abs(dy[i:j])
+            ex[i:j] = (bdu[i:j] + sums * np.abs(du[i:j])) @ wu
+            ew[0][e] = (bdu[i:j] + rows * np.abs(du[i:j])).T @ ax
+            ew[2][e] = ady.T @ (ba[i:j] + rows * np.abs(a[i:j]))
+            if self.gated:
+                ex[i:j] += (bdg[i:j] + sums * np.abs(dg[i:j])) @ np.abs(self.wg[1][e])
+                ew[1][e] = (bdg[i:j] + rows * np.abs(dg[i:j])).T @ ax
+        for name, t, w, e in zip(("dx", "dw_up", "dw_gate", "dw_down"), (dx, dwu, dwg, dwd), want, [ex] + ew):
+            if t is None:
+                continue
+            _within(t, w, out(w, e * 1.01), what + name)
+
+
+def _kept_np(kept):
+    """What a call takes of kept, in fp64."""
+    def one(k):
+        if k is None:
+            return None
+        if isinstance(k, torch.Tensor):
+            return _np(k)
+        return X.unpack(k.codes.cpu().numpy(), k.scale.cpu().numpy())
+    return tuple(map(one, kept))
+
+
+# dtype, gated, d, F, rows of each expert, rows of none before and behind
+BLOCKS = [
+    (BF16, True, 64, 64, [1], 0, 0),               # the smallest
+    (BF16, False, 64, 64, [1], 0, 0),
+    (BF16, False, 64, 256, [5, 0, 9, 1, 0, 17, 3, 2], 0, 0),     # the tiny model
+    (BF16, True, 128, 192, [33, 0, 31, 64, 65], 0, 0),  # tiles cut short, columns and rows
+    (BF16, True, 64, 320, [0, 0, 40], 3, 5),       # rows of no expert at both ends
+    (BF16, True, 192, 128, [129, 200], 0, 1),      # more than a tile of 128 rows
+    (BF16, False, 320, 448, [300], 2, 0),
+    (BF16, True, 512, 704, [257, 128, 0, 390], 0, 7),
+    (BF16, True, 64, 64, [0, 0], 0, 4),            # no rows at all
+    (F32, True, 64, 256, [5, 0, 9, 1, 0, 17, 3, 2], 0, 0),
+    (F32, False, 64, 256, [8] * 8, 0, 0),
+    (F32, True, 1, 1, [1], 0, 0),                  # the smallest
+    (F32, True, 41, 97, [130, 0, 3], 2, 3),        # odd sizes
+    (F32, False, 3, 33, [129, 1], 0, 0),
+    (F32, True, 130, 300, [260], 0, 0),
+    (F32, True, 5, 7, [0], 0, 2),
+]
+IDS = ["%s-%s-%dx%d-%s" % ("bf16" if b[0] == BF16 else "f32", "gated" if b[1] else "relu", b[2], b[3],
+                          ".".join(map(str, b[4]))) for b in BLOCKS]
+
+
+@pytest.mark.parametrize("keep", [None, "full", "packed"])
+@pytest.mark.parametrize("case", BLOCKS, ids=IDS)
+def test_forward(case, keep):
+    b = Block(11, *case)
+    y, kept = b.forward(keep)
+    b.check_forward(y, kept, keep)
+
+
+@pytest.mark.parametrize("keep", ["full", "packed"])
+@pytest.mark.parametrize("case", BLOCKS, ids=IDS)
+def test_backward_of_what_the_forward_kept(case, keep):
+    b = Block(12, *case)
+    _, kept = b.forward(keep)
+    b.check_backward(b.backward(kept), _kept_np(kept))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_in_8_bits(dtype):
+    b = Block(13, dtype, True, 128, 192, [70, 0, 35], 2, 3)
+    _, kept = b.forward("packed")
+    x8 = abi.trimmoe_checkpoint_pack(b.xd)
+    x = X.unpack(x8.codes.cpu().numpy(), x8.scale.cpu().numpy())
+    b.check_backward(b.backward(kept, x=x8), _kept_np(kept), x=x)
+
+
+def test_one_expert_without_borders():
+    b = Block(14, BF16, True, 128, 192, [150])
+    w = tuple(m[0] for m in b.w)
+    y, kept = abi.trimmoe_expert_ffn(*w, b.xd, keep="full")
+    y2, kept2 = b.forward("full")
+    assert torch.equal(y, y2) and torch.equal(kept[1], kept2[1])
+    got = abi.trimmoe_expert_ffn_backward(*w, b.xd, b.dyd, kept)
+    assert got[1].shape == w[0].shape
+    for one, many in zip(got, b.backward(kept)):
+        assert torch.equal(one, many.view_as(one))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_of_no_expert_may_hold_anything(dtype):
+    b = Block(15, dtype, True, 64, 128, [20, 0, 41], 3, 70)
+    y, kept = b.forward("packed")
+    want = b.backward(kept)
+    out = torch.ones(b.n, dtype=torch.bool)
+    out[3:64] = False
+    b.xd[out], b.dyd[out] = float("nan"), float("inf")
+    y2, kept2 = b.forward("packed")
+    assert torch.equal(y, y2) and not y2[out].any()
+    for k, k2 in zip(kept, kept2):
+        assert torch.equal(k.codes, k2.codes) and torch.equal(k.scale, k2.scale)
+        k2.scale[out] = 255  # (NaN)
+    for t, t2 in zip(want, b.backward(kept2)):
+        assert torch.equal(t, t2)
+    assert not want[0][out].any() and not want[1][1].any() and not want[3][1].any()
+
+
+def test_a_row_that_is_not_finite_stays_within_its_expert():
+    b = Block(16, BF16, True, 64, 128, [20, 30])
+    y, _ = b.forward(None)
+    b.xd[5, 7] = float("inf")
+    y2, kept = b.forward("full")
+    keep = torch.ones(50, dtype=torch.bool)
+    keep[5] = False
+    assert torch.equal(y[keep], y2[keep]) and not torch.isfinite(y2[5]).all()
+    got = b.backward(kept)
+    assert torch.isfinite(got[1][1]).all() and torch.isfinite(got[0][keep]).all()
+    assert not torch.isfinite(got[1][0]).all()
+
+
+def test_borders_outside_the_rows_count_as_the_nearer_end():
+    b = Block(17, BF16, True, 64, 128, [20, 30, 10])
+    y, kept = b.forward("full")
+    b.offd[0], b.offd[3] = -2 ** 31, 2 ** 31 - 1
+    y2, kept2 = b.forward("full")
+    assert torch.equal(y, y2) and torch.equal(kept[0], kept2[0])
+    for t, t2 in zip(b.backward(kept), b.backward(kept2)):
+        assert torch.equal(t, t2)
+
+
+def test_large_pre_activations():
+    """sigmoid at both ends of its range: gates up to some hundreds."""
+    b = Block(18, BF16, True, 64, 128, [40, 7], sigma_x=100.0)
+    y, kept = b.forward("full")
+    b.check_forward(y, kept, "full")
+    b.check_backward(b.backward(kept), _kept_np(kept))
+
+
+def test_wanted_gradients_only():
+    b = Block(19, BF16, True, 64, 128, [40, 7])
+    _, kept = b.forward("full")
+    all_ = b.backward(kept)
+    dx, *none = b.backward(kept, want_dw=False)
+    assert torch.equal(dx, all_[0]) and none == [None] * 3
+    none, *dw = b.backward(kept, want_dx=False)
+    assert none is None and all(torch.equal(p, q) for p, q in zip(dw, all_[1:]))
+    assert b.backward(kept, want_dx=False, want_dw=False) == (None,) * 4
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_no_rows(dtype):
+    b = Block(20, dtype, True, 64, 128, [0, 0])
+    y, kept = b.forward("packed")
+    assert y.shape == (0, 64)
+    got = b.backward(kept)
+    assert got[0].shape == (0, 64) and all(not t.any() for t in got[1:])
+
+
+def _same(some, others):
+    assert len(some) == len(others)
+    for p, q in zip(some, others):
+        assert (p is None and q is None) or torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype,case", [(BF16, (True, 128, 192, [33, 0, 31, 64, 65])),
+                                       (BF16, (True, 512, 704, [257, 128, 390])),
+                                       (F32, (False, 41, 97, [130, 3]))])
+def test_repeated_calls_are_identical(dtype, case):
+    b = Block(21, dtype, *case)
+    y, kept = b.forward("packed")
+    first = b.backward(kept)
+    for _ in range(4):
+        y2, kept2 = b.forward("packed")
+        assert torch.equal(y, y2) and torch.equal(kept[0].codes, kept2[0].codes)
+        _same(first, b.backward(kept2))
+
+
+def test_captured_step_replays():
+    """A step captured into a graph, replayed on new inputs with eager steps and
+    synchronizations between."""
+    b = Block(22, BF16, True, 128, 192, [33, 0, 31, 64], 0, 5)
+    c = Block(23, BF16, True, 128, 192, [33, 0, 31, 64], 0, 5)
+
+    def step():
+        y, kept = b.forward("packed")
+        return (y, *b.backward(kept))
+
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = step()
+    x0 = b.xd.clone()
+    for i in range(4):
+        b.xd.copy_(x0 if i % 2 else c.xd)
+        b.dyd.copy_(c.dyd)
+        g.replay()
+        torch.cuda.synchronize()
+        for p, q in zip(out, step()):
+            assert torch.equal(p, q), i
+
+
+def test_two_streams_at_once():
+    blocks = [Block(24 + i, BF16, True, 256, 320, [100, 0, 90]) for i in range(2)]
+    want = []
+    for b in blocks:
+        y, kept = b.forward("packed")
+        want.append((y, *b.backward(kept)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in blocks]
+    for _ in range(5):
+        got = []
+        for b, s in zip(blocks, streams):
+            y, kept = b.forward("packed", stream=s)
+            got.append((y, *b.backward(kept, stream=s)))
+        torch.cuda.synchronize()
+        for w, g in zip(want, got):
+            assert all(torch.equal(p, q) for p, q in zip(w, g))
+
+
+def _ref(b, e, rows, x, dy):
+    """fp64 on the GPU for some rows of expert e: (y, dx)."""
+    wu, wg, wd = (w[e].double() for w in b)
+    x, dy = x[rows].double(), dy[rows].double()
+    u, g = x @ wu.T, x @ wg.T
+    s = torch.sigmoid(g)
+    da = dy @ wd
+    return (s * g * u) @ wd.T, (da * g * s) @ wu + (da * u * s * (1 + g * (1 - s))) @ wg
+
+
+def _near(got, want):
+    """bf16 results of bf16 operands rounded once more: relative to the norm, three
+    roundings of 2^-8 at most each."""
+    assert (got.double() - want).norm() <= 3 * 2.0 ** -8 * want.norm()
+
+
+def test_activations_past_32_bit_offsets():
+    d, F, n = 64, 16384, 150000  # n F = 2.4e9 values
+    g = torch.Generator(device=DEV).manual_seed(5)
+    r = lambda *s, k=1.0: torch.randn(*s, generator=g, device=DEV, dtype=BF16).mul_(k)  # noqa: E731
+    w = r(1, F, d, k=d ** -0.5), r(1, F, d, k=d ** -0.5), r(1, d, F, k=F ** -0.5)
+    x, dy = r(n, d), r(n, d)
+    off = torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    for keep in ("full", "packed"):
+        y, kept = abi.trimmoe_expert_ffn(*w, x, off, keep=keep)
+        dx, *_ = abi.trimmoe_expert_ffn_backward(*w, x, dy, kept, off, want_dw=False)
+        for rows in (slice(0, 70), slice(131000, 131200), slice(n - 70, n)):
+            wy, wx = _ref(w, 0, rows, x, dy)
+            _near(y[rows], wy)
+            # (u and g are off by 2^-8 of themselves, or of 2^-7 of their block's largest,
+            # some 4 times their size: less than 2^-3 of the gradient's norm)
+            assert (dx[rows].double() - wx).norm() <= 2.0 ** -3 * wx.norm()
+        del kept, dx
+
+
+def test_weights_past_32_bit_offsets():
+    E, d, F = 40, 4096, 14336  # 2.3e9 values a weight
+    g = torch.Generator(device=DEV).manual_seed(6)
+    w = [torch.empty(E, *s, device=DEV, dtype=BF16).normal_(0, s[1] ** -0.5, generator=g)
+         for s in ((F, d), (F, d), (d, F))]
+    sizes = [0] * E
+    sizes[0], sizes[-2], sizes[-1] = 3, 40, 130
+    off = torch.from_numpy(_borders(sizes)).to(DEV)
+    n = sum(sizes)
+    x = torch.randn(n, d, generator=g, device=DEV).to(BF16)
+    dy = torch.randn(n, d, generator=g, device=DEV).to(BF16)
+    y, kept = abi.trimmoe_expert_ffn(*w, x, off, keep="full")
+    dx, dwu, dwg, dwd = abi.trimmoe_expert_ffn_backward(*w, x, dy, kept, off)
+    for e, a, b in ((0, 0, 3), (E - 2, 3, 43), (E - 1, 43, 173)):
+        wy, wx = _ref(w, e, slice(a, b), x, dy)
+        _near(y[a:b], wy)
+        u, gt = kept[0][a:b].double(), kept[1][a:b].double()
+        s = torch.sigmoid(gt)
+        da = dy[a:b].double() @ w[2][e].double()
+        _near(dwd[e], dy[a:b].double().T @ (s * gt * u))
+        _near(dwu[e], (da * gt * s).T @ x[a:b].double())
+        _near(dwg[e], (da * u * s * (1 + gt * (1 - s))).T @ x[a:b].double())
+    assert not dwu[1:-2].any() and not dwd[1:-2].any()
+
+
+# ------------------------------------------------- activations in 8 bits --
+def _packs(x):
+    """Codes, scale and values of a call equal the oracle's."""
+    got = abi.trimmoe_checkpoint_pack(x)
+    codes, scale = X.pack(_np(x))
+    q, s = got.codes.cpu().numpy(), got.scale.cpu().numpy()
+    assert np.array_equal(s, scale)
+    assert np.array_equal(q[np.repeat(s != 255, 32, 1)[:, :q.shape[1]]],
+                          codes[np.repeat(s != 255, 32, 1)[:, :q.shape[1]]])
+    for dtype in (BF16, F32):
+        back = abi.trimmoe_checkpoint_unpack(*got, dtype=dtype)
+        np.testing.assert_array_equal(_np(back), X.unpack(q, s))  # (NaN equal to NaN)
+    return got
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("n,c", [(1, 1), (1, 32), (3, 31), (5, 33), (7, 40), (64, 64), (130, 1000),
+                                 (33, 1001), (4099, 264)])
+def test_checkpoint(dtype, n, c):
+    x = normal_f32(n, c, (n, c), 1.0, "cpu") * torch.exp(3 * normal_f32(n, c + 1, (n, 1), 1.0, "cpu"))
+    _packs(x.to(dtype).to(DEV))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_checkpoint_of_special_values(dtype):
+    t = torch.zeros(9, 64, dtype=dtype)
+    t[1, 3], t[2, 40], t[3, 0] = float("nan"), float("inf"), -float("inf")
+    t[4, :4] = torch.tensor([torch.finfo(dtype).max, -torch.finfo(dtype).max, 1.0, -1e30]).to(dtype)
+    t[5, :4] = torch.tensor([2.0 ** -126, 2.0 ** -130, -(2.0 ** -133), 2.0 ** -127]).to(dtype)
+    t[6, 32] = 2.0 ** -133
+    t[7, :5] = torch.tensor([127.5, -127.5, 0.5, 1.5, 127.0]).to(dtype)  # ties, codes that stop at 127
+    t[8, :3] = torch.tensor([-0.0, 1.0, 2.0]).to(dtype)
+    _packs(t.to(DEV))
+
+
+def test_checkpoint_of_rows_at_any_address():
+    for dtype in (BF16, F32):
+        flat = torch.randn(10 * 40 + 3, device=DEV).to(dtype)
+        for at in (1, 2, 3):
+            _packs(flat[at:at + 400].view(10, 40))
+
+
+def test_checkpoint_comes_back_as_it_was():
+    x = torch.randn(100, 96, device=DEV)
+    first = abi.trimmoe_checkpoint_pack(x)
+    again = abi.trimmoe_checkpoint_pack(abi.trimmoe_checkpoint_unpack(*first))
+    assert torch.equal(abi.trimmoe_checkpoint_unpack(*first), abi.trimmoe_checkpoint_unpack(*again))
+
+
+def test_checkpoint_of_no_rows():
+    p = abi.trimmoe_checkpoint_pack(torch.empty(0, 40, device=DEV))
+    assert p.codes.shape == (0, 40) and p.scale.shape == (0, 2)
+    assert abi.trimmoe_checkpoint_unpack(*p).shape == (0, 40)
+
+
+@pytest.mark.parametrize("c", [16384, 16383])
+def test_checkpoint_past_32_bit_offsets(c):
+    n = 140000
+    x = torch.randn(n, c, device=DEV, dtype=BF16)
+    p = abi.trimmoe_checkpoint_pack(x)
+    back = abi.trimmoe_checkpoint_unpack(*p)
+    for rows in (slice(0, 50), slice(131050, 131150), slice(n - 50, n)):
+        codes, scale = X.pack(_np(x[rows]))
+        assert np.array_equal(p.codes[rows].cpu().numpy(), codes)
+        assert np.array_equal(p.scale[rows].cpu().numpy(), scale)
+        assert np.array_equal(_np(back[rows]), X.unpack(codes, scale))
