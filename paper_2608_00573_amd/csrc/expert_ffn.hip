@@ -13,7 +13,7 @@
 
 #include <algorithm>
 
-#include "mid_core.h"
+#include "big_feed.h"
 
 namespace trimmoe {
 
@@ -25,9 +25,10 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 struct RowTile {
   int e, r0, valid;
   __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, int mt, int tile) {
-    e = t.group(mt);
+    int within;
+    e = t.group(mt, within);
     const int2 r = g.rows(e);
-    r0 = uniform(r.x + (mt - t.first[e]) * tile);
+    r0 = uniform(r.x + within * tile);
     valid = uniform(min(tile, r.y - r0));
   }
 };
@@ -77,44 +78,48 @@ struct UpArgs {
   uint8_t *up_scale, *gate_scale;
 };
 
-template <bool GATED, int BN, int ST, int KEEP>
-__global__ __launch_bounds__(256, 2) void k_expert_up(UpArgs a) {
-  using T = MidTile<128, BN, ST, false, false, GATED>;
-  using C = MidCore<T>;
+// A tile's first loads go out before the tile before it leaves its registers.
+template <class C, bool GATED, int KEEP>
+__global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
+  using T = typename C::T;
   __shared__ __align__(16) char lds[T::LDS];
-  __shared__ int s_first[kGroupSlots + 1];
-  const C core(lds);
-  GroupTiles tiles;
-  tiles.init(s_first, a.groups, a.groups.E + 2, BN);
+  const GroupTiles tiles(a.groups, a.groups.E + 2, T::BN);
   TileSched S;
   int ntiles;
-  if (!S.init(tiles.total(), (a.F + T::ROWS_A - 1) / T::ROWS_A, 1, ntiles)) return;
-  constexpr int TMO = GATED ? T::TM / 2 : T::TM;  // 16-column groups of a wavefront
-  for (int jt = 0; jt < ntiles; ++jt) {
+  if (!S.init(tiles.n, (a.F + T::ROWS_A - 1) / T::ROWS_A, 1, ntiles)) return;
+  C core(lds);
+  struct At {
+    int r0, valid, f0, nk;
+  };
+  const auto begin = [&](int jt) {
     int mt, nt, sp;
     S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, BN);
-    const int f0 = nt * T::ROWS_A, f_valid = min(T::ROWS_A, a.F - f0);
+    const RowTile row(tiles, a.groups, mt, T::BN);
+    const int f0 = nt * T::ROWS_A, k = row.e < a.groups.E ? a.d : 0;
+    const size_t w0 = ((size_t)(k ? row.e : 0) * a.F + f0) * a.d;
+    TileOperand<T::PA> A;
+    TileOperand<T::PB> B;
+    tile_rows(A, a.w_up + w0, a.d, min(T::ROWS_A, a.F - f0), k, T::SPAN);
+    if constexpr (GATED) A.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
+    tile_rows(B, a.x + (size_t)row.r0 * a.d, a.d, row.valid, k);
+    core.begin(A, B);
+    return At{row.r0, row.valid, f0, k / BK};
+  };
+  constexpr int TMO = GATED ? T::TM / 2 : T::TM;  // 16-column groups of a wavefront
+  At at = begin(0);
+  for (int jt = 0; jt < ntiles; ++jt) {
     typename C::Acc acc;
-    C::zero(acc);
-    const bool live = row.e < a.groups.E;
-    if (live) {
-      const size_t w0 = ((size_t)row.e * a.F + f0) * a.d;
-      MidOperand<T::PA> A;
-      MidOperand<T::PB> B;
-      mid_rows(A, a.w_up + w0, a.d, f_valid, a.d, GATED);
-      if constexpr (GATED) A.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
-      mid_rows(B, a.x + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
-      core.run(A, B, a.d / BK, acc);
-    }
+    core.run(at.nk, acc);
+    const At was = at;
+    if (jt + 1 < ntiles) at = begin(jt + 1);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
       const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
 #pragma unroll
       for (int i = 0; i < TMO; i += 2) {
-        const int c = f0 + core.wm * 16 * TMO + 16 * i;  // 32 columns, all of them or none in F
-        const bool in = t < row.valid && c < a.F;
-        const size_t o = (size_t)(row.r0 + t) * a.F + c;
+        const int c = was.f0 + core.wm * 16 * TMO + 16 * i;  // 32 columns, all of them or none in F
+        const bool in = t < was.valid && c < a.F;
+        const size_t o = (size_t)(was.r0 + t) * a.F + c;
         float u[2][4], g[2][4], v[2][4];
 #pragma unroll
         for (int k = 0; k < 2; ++k)
@@ -161,61 +166,70 @@ struct RowsArgs {
   bf16_t* out;
 };
 
-template <bool ATR, int BN, int ST>
-__global__ __launch_bounds__(256, 2) void k_expert_rows(RowsArgs a) {
-  using T = MidTile<128, BN, ST, ATR, false>;
-  using C = MidCore<T>;
+// a tile's results: bf16, 16 bytes a lane
+template <class C>
+__device__ __forceinline__ void store_tile(const C& core, const typename C::Acc& acc, bf16_t* out, size_t row0,
+                                           int valid, int m0, int M) {
+  using T = typename C::T;
+#pragma unroll
+  for (int j = 0; j < T::TN; ++j) {
+    const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+#pragma unroll
+    for (int i = 0; i < T::TM; i += 2) {
+      const int c = m0 + core.wm * T::WM + 16 * i;
+      float v[2][4];
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) v[k][r] = acc[i + k][j][r];
+      const u32x4_t p = pack_rows(v[0], v[1]);
+      if (t < valid && c < M)
+        *reinterpret_cast<u32x4_t*>(out + (row0 + t) * M + c + pack_col(core.lane)) = p;
+    }
+  }
+}
+
+template <class C>
+__global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
+  using T = typename C::T;
   __shared__ __align__(16) char lds[T::LDS];
-  __shared__ int s_first[kGroupSlots + 1];
-  const C core(lds);
-  GroupTiles tiles;
-  tiles.init(s_first, a.groups, a.groups.E + 2, BN);
+  const GroupTiles tiles(a.groups, a.groups.E + 2, T::BN);
   TileSched S;
   int ntiles;
-  if (!S.init(tiles.total(), (a.M + T::BM - 1) / T::BM, 1, ntiles)) return;
-  for (int jt = 0; jt < ntiles; ++jt) {
+  if (!S.init(tiles.n, (a.M + T::BM - 1) / T::BM, 1, ntiles)) return;
+  C core(lds);
+  struct At {
+    int r0, valid, m0, nk;
+  };
+  const auto begin = [&](int jt) {
     int mt, nt, sp;
     S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, BN);
-    const int m0 = nt * T::BM;
+    const RowTile row(tiles, a.groups, mt, T::BN);
+    const int m0 = nt * T::BM, K = row.e < a.groups.E ? a.K : 0;
+    const size_t e0 = K ? (size_t)row.e * a.M * a.K : 0, b0 = (size_t)row.r0 * a.K;
+    TileOperand<T::PA> A;
+    TileOperand<T::PB> B;
+    if constexpr (T::ATR)
+      tile_along<T::BM>(A, a.w + e0, a.M, m0, K);
+    else
+      tile_rows(A, a.w + e0 + (size_t)m0 * a.K, a.K, min(T::BM, a.M - m0), K);
+    tile_rows(B, a.b + b0, a.K, row.valid, K);
+    const bool two = T::ATR && a.w2 && K;
+    if (two) {
+      A.q = reinterpret_cast<const char*>(a.w2 + e0 + m0);
+      B.q = reinterpret_cast<const char*>(a.b2 + b0);
+      A.kq = B.kq = K;
+    }
+    core.begin(A, B);
+    return At{row.r0, row.valid, m0, K / BK * (two ? 2 : 1)};
+  };
+  At at = begin(0);
+  for (int jt = 0; jt < ntiles; ++jt) {
     typename C::Acc acc;
-    C::zero(acc);
-    if (row.e < a.groups.E) {
-      const size_t e0 = (size_t)row.e * a.M * a.K, b0 = (size_t)row.r0 * a.K;
-      MidOperand<T::PA> A;
-      MidOperand<T::PB> B;
-      if constexpr (ATR) {
-        mid_along<T::BM>(A, a.w + e0, a.M, m0, a.K);
-        if (a.w2) {
-          A.q = reinterpret_cast<const char*>(a.w2 + e0 + m0);
-          A.kq = a.K;
-        }
-      } else {
-        mid_rows(A, a.w + e0 + (size_t)m0 * a.K, a.K, min(T::BM, a.M - m0), a.K);
-      }
-      mid_rows(B, a.b + b0, a.K, row.valid, a.K);
-      if (ATR && a.w2) {
-        B.q = reinterpret_cast<const char*>(a.b2 + b0);
-        B.kq = a.K;
-      }
-      core.run(A, B, a.K / BK * (ATR && a.w2 ? 2 : 1), acc);
-    }
-#pragma unroll
-    for (int j = 0; j < T::TN; ++j) {
-      const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
-#pragma unroll
-      for (int i = 0; i < T::TM; i += 2) {
-        const int c = m0 + core.wm * T::WM + 16 * i;
-        float v[2][4];
-#pragma unroll
-        for (int k = 0; k < 2; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) v[k][r] = acc[i + k][j][r];
-        const u32x4_t p = pack_rows(v[0], v[1]);
-        if (t < row.valid && c < a.M)
-          *reinterpret_cast<u32x4_t*>(a.out + (size_t)(row.r0 + t) * a.M + c + pack_col(core.lane)) = p;
-      }
-    }
+    core.run(at.nk, acc);
+    const At was = at;
+    if (jt + 1 < ntiles) at = begin(jt + 1);
+    store_tile(core, acc, a.out, was.r0, was.valid, was.m0, a.M);
   }
 }
 
@@ -246,38 +260,44 @@ __device__ __forceinline__ void kept4(float (&v)[4], const void* p, const uint8_
   }
 }
 
-template <bool GATED, bool PACKED, int BN, int ST>
-__global__ __launch_bounds__(256, 2) void k_expert_dact(DactArgs a) {
-  using T = MidTile<128, BN, ST, true, false>;
-  using C = MidCore<T>;
+template <class C, bool GATED, bool PACKED>
+__global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
+  using T = typename C::T;
   __shared__ __align__(16) char lds[T::LDS];
-  __shared__ int s_first[kGroupSlots + 1];
-  const C core(lds);
-  GroupTiles tiles;
-  tiles.init(s_first, a.groups, a.groups.E, BN);
+  const GroupTiles tiles(a.groups, a.groups.E, T::BN);
   TileSched S;
   int ntiles;
-  if (!S.init(tiles.total(), (a.F + T::BM - 1) / T::BM, 1, ntiles)) return;
-  for (int jt = 0; jt < ntiles; ++jt) {
+  if (!S.init(tiles.n, (a.F + T::BM - 1) / T::BM, 1, ntiles)) return;
+  C core(lds);
+  struct At {
+    int r0, valid, f0;
+  };
+  const auto begin = [&](int jt) {
     int mt, nt, sp;
     S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, BN);
+    const RowTile row(tiles, a.groups, mt, T::BN);
     const int f0 = nt * T::BM;
+    TileOperand<T::PA> A;
+    TileOperand<T::PB> B;
+    tile_along<T::BM>(A, a.w_down + (size_t)row.e * a.d * a.F, a.F, f0, a.d);
+    tile_rows(B, a.dy + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
+    core.begin(A, B);
+    return At{row.r0, row.valid, f0};
+  };
+  At at = begin(0);
+  for (int jt = 0; jt < ntiles; ++jt) {
     typename C::Acc acc;
-    C::zero(acc);
-    MidOperand<T::PA> A;
-    MidOperand<T::PB> B;
-    mid_along<T::BM>(A, a.w_down + (size_t)row.e * a.d * a.F, a.F, f0, a.d);
-    mid_rows(B, a.dy + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
-    core.run(A, B, a.d / BK, acc);
+    core.run(a.d / BK, acc);
+    const At was = at;
+    if (jt + 1 < ntiles) at = begin(jt + 1);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
       const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
 #pragma unroll
       for (int i = 0; i < T::TM; i += 2) {
-        const int c = f0 + core.wm * T::WM + 16 * i;
-        const bool in = t < row.valid && c < a.F;
-        const size_t o = (size_t)(row.r0 + t) * a.F + c;
+        const int c = was.f0 + core.wm * T::WM + 16 * i;
+        const bool in = t < was.valid && c < a.F;
+        const size_t o = (size_t)(was.r0 + t) * a.F + c;
         float va[2][4], vu[2][4], vg[2][4];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -326,21 +346,24 @@ struct WeightArgs {
   bf16_t* out[3];
 };
 
-template <int BM, int BN, int ST>
-__global__ __launch_bounds__(256, 2) void k_expert_weights(WeightArgs a) {
-  using T = MidTile<BM, BN, ST, true, true>;
-  using C = MidCore<T>;
+template <class C>
+__global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a) {
+  using T = typename C::T;
   __shared__ __align__(16) char lds[T::LDS];
-  const C core(lds);
-  TileSched S;
-  int ntiles;
   int first[4] = {0, 0, 0, 0};
 #pragma unroll
   for (int p = 0; p < 3; ++p)
-    first[p + 1] = first[p] + (p < a.n_prod ? ((a.M[p] + BM - 1) / BM) * ((a.N[p] + BN - 1) / BN) : 0);
-  if (!S.init_total(a.groups.E * first[3], 1, 1, ntiles)) return;
-  for (int jt = 0; jt < ntiles; ++jt) {
-    const int L = S.tb + S.i0 + jt * S.bx, e = L / first[3], at = L - e * first[3];
+    first[p + 1] = first[p] + (p < a.n_prod ? ((a.M[p] + T::BM - 1) / T::BM) * ((a.N[p] + T::BN - 1) / T::BN)
+                                            : 0);
+  const GroupOrder order(a.groups);
+  const GroupSched S(first[3], a.groups.E);
+  C core(lds);
+  struct At {
+    bf16_t* out;
+    int M, N, m0, n0, nk;
+  };
+  const auto begin = [&](int rank, int at) {
+    const int e = order.group(rank);
     const int p = at >= first[2] ? 2 : at >= first[1] ? 1 : 0;
     const int M = p == 0 ? a.M[0] : p == 1 ? a.M[1] : a.M[2];
     const int N = p == 0 ? a.N[0] : p == 1 ? a.N[1] : a.N[2];
@@ -348,80 +371,109 @@ __global__ __launch_bounds__(256, 2) void k_expert_weights(WeightArgs a) {
     const bf16_t* pB = p == 0 ? a.B[0] : p == 1 ? a.B[1] : a.B[2];
     bf16_t* out = p == 0 ? a.out[0] : p == 1 ? a.out[1] : a.out[2];
     TileSched P;
-    P.n_mt = (N + BN - 1) / BN;
-    P.n_nt = (M + BM - 1) / BM;
+    P.n_mt = (N + T::BN - 1) / T::BN;
+    P.n_nt = (M + T::BM - 1) / T::BM;
     int mt, nt, sp;
     P.decode_abs(at - (p == 0 ? 0 : p == 1 ? first[1] : first[2]), mt, nt, sp);
-    const int m0 = nt * BM, n0 = mt * BN;
+    const int m0 = nt * T::BM, n0 = mt * T::BN;
     const int2 r = a.groups.rows(e);
     const int r0 = uniform(r.x), k = uniform(r.y) - r0;
+    TileOperand<T::PA> A;
+    TileOperand<T::PB> B;
+    tile_along<T::BM>(A, pA + (size_t)r0 * M, M, m0, k);
+    tile_along<T::BN>(B, pB + (size_t)r0 * N, N, n0, k);
+    core.begin(A, B);
+    return At{out + (size_t)e * M * N, M, N, m0, n0, (k + BK - 1) / BK};
+  };
+  int rank, tile;
+  if (!S.decode(0, rank, tile)) return;
+  At at = begin(rank, tile);
+  for (int jt = 1;; ++jt) {
     typename C::Acc acc;
-    C::zero(acc);
-    if (k > 0) {
-      MidOperand<T::PA> A;
-      MidOperand<T::PB> B;
-      mid_along<BM>(A, pA + (size_t)r0 * M, M, m0, k);
-      mid_along<BN>(B, pB + (size_t)r0 * N, N, n0, k);
-      core.run(A, B, (k + BK - 1) / BK, acc);
-    }
-    bf16_t* o = out + (size_t)e * M * N;
-#pragma unroll
-    for (int j = 0; j < T::TN; ++j) {
-      const int t = n0 + core.wn * T::WN + 16 * j + (core.lane & 15);
-#pragma unroll
-      for (int i = 0; i < T::TM; i += 2) {
-        const int c = m0 + core.wm * T::WM + 16 * i;
-        float v[2][4];
-#pragma unroll
-        for (int q = 0; q < 2; ++q)
-#pragma unroll
-          for (int s = 0; s < 4; ++s) v[q][s] = acc[i + q][j][s];
-        const u32x4_t w = pack_rows(v[0], v[1]);
-        if (t < N && c < M)
-          *reinterpret_cast<u32x4_t*>(o + (size_t)t * M + c + pack_col(core.lane)) = w;
-      }
-    }
+    core.run(at.nk, acc);
+    const At was = at;
+    const bool more = S.decode(jt, rank, tile);
+    if (more) at = begin(rank, tile);
+    store_tile(core, acc, was.out, was.n0, was.N - was.n0, was.m0, was.M);
+    if (!more) break;
   }
 }
 
 // --------------------------------------------------------------- launching --
-// blocks of a launch over at most `tiles` tiles
-unsigned grid_of(long tiles) { return (unsigned)std::min<long>(std::max<long>(tiles, 1), 65536); }
+// How the rows are cut: kFew 32-row tiles (groups of up to that many rows on average),
+// kMid 128-row tiles, kLarge the large-group core's 256.
+enum Rows { kFew, kMid, kLarge };
+Rows rows_kind(const Groups& g) {
+  if ((long)g.n <= 32l * g.E) return kFew;
+  return (long)g.n >= 512l * g.E ? kLarge : kMid;
+}
 
-// rows a tile: no more than the groups have on average
-bool few_rows(const Groups& g) { return (long)g.n <= 32l * g.E; }
+template <int KIND, bool ATR, bool BTR, bool PAIR = false>
+using CoreOf = std::conditional_t<
+    KIND == kLarge, BigCore<BigTile<ATR, BTR, PAIR>>,
+    std::conditional_t<KIND == kMid, MidCore<MidTile<128, 128, 2, ATR, BTR, PAIR>>,
+                       MidCore<MidTile<128, 32, 3, ATR, BTR, PAIR>>>>;
 
-// f(integral constant of the rows a tile, ... of its stages)
+// f(integral constant of the kind)
 template <typename F>
-hipError_t with_rows(const Groups& g, F f) {
-  if (few_rows(g))
-    f(std::integral_constant<int, 32>(), std::integral_constant<int, 3>());
+hipError_t with_kind(Rows kind, F f) {
+  if (kind == kFew)
+    f(std::integral_constant<int, kFew>());
+  else if (kind == kMid)
+    f(std::integral_constant<int, kMid>());
   else
-    f(std::integral_constant<int, 128>(), std::integral_constant<int, 2>());
+    f(std::integral_constant<int, kLarge>());
   return hipGetLastError();
 }
 
+// blocks of a launch over at most `tiles` tiles: one for each (which the hardware deals
+// out as others end), or one a CU that stays (the large-group core)
+template <class C>
+dim3 grid_of(long tiles, int n_cu) {
+  const long most = C::T::OCC == 1 ? n_cu : 1l << 20;
+  return dim3((unsigned)std::min(std::max(tiles, 1l), most));
+}
+template <class C>
+dim3 rows_grid(const Groups& g, int cols, int n_cu) {
+  return grid_of<C>(row_tiles_most(g.n, g.E, C::T::BN) * cdiv(cols, C::T::ROWS_A), n_cu);
+}
+
 template <bool GATED, int KEEP>
-hipError_t launch_up(const UpArgs& a, hipStream_t st) {
-  return with_rows(a.groups, [&](auto bn, auto stages) {
-    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.F, GATED ? 64 : 128);
-    hipLaunchKernelGGL((k_expert_up<GATED, bn, stages, KEEP>), dim3(grid_of(n)), dim3(256), 0, st, a);
+hipError_t launch_up(const UpArgs& a, int n_cu, hipStream_t st) {
+  return with_kind(rows_kind(a.groups), [&](auto kind) {
+    using C = CoreOf<kind, false, false, GATED>;
+    hipLaunchKernelGGL((k_expert_up<C, GATED, KEEP>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st, a);
   });
 }
 
 template <bool ATR>
-hipError_t launch_rows(const RowsArgs& a, hipStream_t st) {
-  return with_rows(a.groups, [&](auto bn, auto stages) {
-    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.M, 128);
-    hipLaunchKernelGGL((k_expert_rows<ATR, bn, stages>), dim3(grid_of(n)), dim3(256), 0, st, a);
+hipError_t launch_rows(const RowsArgs& a, int n_cu, hipStream_t st) {
+  return with_kind(rows_kind(a.groups), [&](auto kind) {
+    using C = CoreOf<kind, ATR, false>;
+    hipLaunchKernelGGL((k_expert_rows<C>), rows_grid<C>(a.groups, a.M, n_cu), dim3(256), 0, st, a);
   });
 }
 
 template <bool GATED, bool PACKED>
-hipError_t launch_dact(const DactArgs& a, hipStream_t st) {
-  return with_rows(a.groups, [&](auto bn, auto stages) {
-    const long n = row_tiles_most(a.groups.n, a.groups.E, bn) * cdiv(a.F, 128);
-    hipLaunchKernelGGL((k_expert_dact<GATED, PACKED, bn, stages>), dim3(grid_of(n)), dim3(256), 0, st, a);
+hipError_t launch_dact(const DactArgs& a, int n_cu, hipStream_t st) {
+  return with_kind(rows_kind(a.groups), [&](auto kind) {
+    using C = CoreOf<kind, true, false>;
+    hipLaunchKernelGGL((k_expert_dact<C, GATED, PACKED>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st,
+                       a);
+  });
+}
+
+hipError_t launch_weights(const WeightArgs& a, int n_cu, hipStream_t st) {
+  const Rows kind = rows_kind(a.groups) == kLarge ? kLarge : kMid;
+  return with_kind(kind, [&](auto k) {
+    if constexpr (k != kFew) {
+      using C = CoreOf<k, true, true>;
+      long tiles = 0;
+      for (int p = 0; p < a.n_prod; ++p) tiles += (long)cdiv(a.M[p], C::T::BM) * cdiv(a.N[p], C::T::BN);
+      // (every XCD's blocks take its tiles of all groups)
+      hipLaunchKernelGGL((k_expert_weights<C>), grid_of<C>((tiles * a.groups.E + 7) / 8 * 8, n_cu), dim3(256),
+                         0, st, a);
+    }
   });
 }
 
@@ -458,13 +510,13 @@ hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
   u.gate_scale = a.gate_scale;
   hipError_t e;
   if (a.gated)
-    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<true, TRIMMOE_KEEP_FULL>(u, st)
-        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<true, TRIMMOE_KEEP_PACKED>(u, st)
-                                        : launch_up<true, TRIMMOE_KEEP_NONE>(u, st);
+    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<true, TRIMMOE_KEEP_FULL>(u, a.n_cu, st)
+        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<true, TRIMMOE_KEEP_PACKED>(u, a.n_cu, st)
+                                        : launch_up<true, TRIMMOE_KEEP_NONE>(u, a.n_cu, st);
   else
-    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<false, TRIMMOE_KEEP_FULL>(u, st)
-        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<false, TRIMMOE_KEEP_PACKED>(u, st)
-                                        : launch_up<false, TRIMMOE_KEEP_NONE>(u, st);
+    e = a.keep == TRIMMOE_KEEP_FULL     ? launch_up<false, TRIMMOE_KEEP_FULL>(u, a.n_cu, st)
+        : a.keep == TRIMMOE_KEEP_PACKED ? launch_up<false, TRIMMOE_KEEP_PACKED>(u, a.n_cu, st)
+                                        : launch_up<false, TRIMMOE_KEEP_NONE>(u, a.n_cu, st);
   if (e != hipSuccess) return e;
   RowsArgs r{};
   r.groups = a.groups;
@@ -473,7 +525,7 @@ hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
   r.M = a.d;
   r.K = a.F;
   r.out = static_cast<bf16_t*>(a.y);
-  return launch_rows<false>(r, st);
+  return launch_rows<false>(r, a.n_cu, st);
 }
 
 hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
@@ -497,10 +549,10 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
   const bf16_t* x = as_bf16(a.x);
   if (n > 0) {
     if (a.gated)
-      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<true, true>(t, st) : launch_dact<true, false>(t, st);
+      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<true, true>(t, a.n_cu, st) : launch_dact<true, false>(t, a.n_cu, st);
     else
-      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<false, true>(t, st)
-                                        : launch_dact<false, false>(t, st);
+      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<false, true>(t, a.n_cu, st)
+                                        : launch_dact<false, false>(t, a.n_cu, st);
     if (e != hipSuccess) return e;
     if (a.x_scale && (a.dw_up || a.dw_gate)) {
       bf16_t* to = reinterpret_cast<bf16_t*>(a.ws + (a.gated ? 3 : 2) * act);
@@ -518,12 +570,11 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
       r.M = a.d;
       r.K = a.F;
       r.out = static_cast<bf16_t*>(a.dx);
-      if ((e = launch_rows<true>(r, st)) != hipSuccess) return e;
+      if ((e = launch_rows<true>(r, a.n_cu, st)) != hipSuccess) return e;
     }
   }
   WeightArgs w{};
   w.groups = a.groups;
-  long tiles = 0;
   const auto add = [&](const bf16_t* A, const bf16_t* B, int M, int N, void* out) {
     if (!out) return;
     const int p = w.n_prod++;
@@ -532,15 +583,12 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
     w.M[p] = M;
     w.N[p] = N;
     w.out[p] = static_cast<bf16_t*>(out);
-    tiles += (long)cdiv(M, 128) * cdiv(N, 128);
   };
   add(t.a, t.dy, a.F, a.d, a.dw_down);
   add(x, t.du, a.d, a.F, a.dw_up);
   if (a.gated) add(x, t.dg, a.d, a.F, a.dw_gate);
   if (w.n_prod == 0) return hipSuccess;
-  hipLaunchKernelGGL((k_expert_weights<128, 128, 2>), dim3(grid_of(tiles * a.groups.E)), dim3(256), 0, st,
-                     w);
-  return hipGetLastError();
+  return launch_weights(w, a.n_cu, st);
 }
 
 }  // namespace trimmoe

@@ -21,16 +21,16 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 struct F32At {
   int e, r0, end, m0;
   // false: no such tile
-  __device__ __forceinline__ bool init(const Groups& g, int slots, int M, int* lds) {
-    GroupTiles t;
-    t.init(lds, g, slots, F32S::B);
+  __device__ __forceinline__ bool init(const Groups& g, int slots, int M) {
+    const GroupTiles t(g, slots, F32S::B);
     const int n_m = (M + F32S::A - 1) / F32S::A;
     const int mt = blockIdx.x / n_m;
-    if (mt >= t.total()) return false;
+    if (mt >= t.n) return false;
     m0 = (int)(blockIdx.x % n_m) * F32S::A;
-    e = t.group(mt);
+    int within;
+    e = t.group(mt, within);
     const int2 r = g.rows(e);
-    r0 = uniform(r.x + (mt - t.first[e]) * F32S::B);
+    r0 = uniform(r.x + within * F32S::B);
     end = uniform(r.y);
     return true;
   }
@@ -77,9 +77,8 @@ struct F32Up {
 template <bool GATED>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_up_f32(F32Up a) {
   __shared__ __align__(16) float lds[F32S::FLOATS];
-  __shared__ int s_first[kGroupSlots + 1];
   F32At at;
-  if (!at.init(a.groups, a.groups.E + 2, a.F, s_first)) return;
+  if (!at.init(a.groups, a.groups.E + 2, a.F)) return;
   F32T u(at.m0, a.F, at.r0, at.end), g(at.m0, a.F, at.r0, at.end);
   zero_tile(u);
   zero_tile(g);
@@ -122,9 +121,8 @@ struct F32Rows {
 template <bool AK, bool TWO>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a) {
   __shared__ __align__(16) float lds[F32S::FLOATS];
-  __shared__ int s_first[kGroupSlots + 1];
   F32At at;
-  if (!at.init(a.groups, a.groups.E + 2, a.M, s_first)) return;
+  if (!at.init(a.groups, a.groups.E + 2, a.M)) return;
   F32T t(at.m0, a.M, at.r0, at.end), t2(at.m0, a.M, at.r0, at.end);
   zero_tile(t);
   zero_tile(t2);
@@ -167,9 +165,8 @@ __device__ __forceinline__ float kept(const void* p, const uint8_t* scale, int b
 template <bool GATED, bool PACKED>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_dact_f32(F32Dact a) {
   __shared__ __align__(16) float lds[F32S::FLOATS];
-  __shared__ int s_first[kGroupSlots + 1];
   F32At at;
-  if (!at.init(a.groups, a.groups.E, a.F, s_first)) return;
+  if (!at.init(a.groups, a.groups.E, a.F)) return;
   F32T t(at.m0, a.F, at.r0, at.end);
   f32_tile<f32p::kSquare>(
       Operand<false>{a.w_down + (size_t)at.e * a.d * a.F, (size_t)a.F, a.F, a.d},

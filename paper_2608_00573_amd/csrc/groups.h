@@ -22,52 +22,116 @@ struct Groups {
     return make_int2(a, max(a, min(max(offsets[e + 1], 0), n)));
   }
 };
-constexpr int kGroupSlots = TRIMMOE_MAX_EXPERTS + 2;
 
-// The groups' row tiles: how many there are up to each group, in LDS
+constexpr int kGroupChunks = (TRIMMOE_MAX_EXPERTS + 2 + 63) / 64;
+
+// The groups' row tiles: lane l holds how many there are before groups l, 64 + l, ...
+// (in registers: the large tiles leave no LDS)
 struct GroupTiles {
-  int* first;  // [slots + 1]
-  int slots;
-  // by all threads of the block, which then may use it
-  __device__ __forceinline__ void init(int* lds, const Groups& g, int n_slots, int tile) {
-    first = lds;
-    slots = n_slots;
-    if (threadIdx.x < 64) {
-      int sum = 0;
-      for (int e0 = 0; e0 < n_slots; e0 += 64) {
-        const int e = e0 + (int)threadIdx.x;
-        int t = 0;
-        if (e < n_slots) {
-          const int2 r = g.rows(e);
-          t = (r.y - r.x + tile - 1) / tile;
-        }
-        int s = t;
+  int first[kGroupChunks], n;
+  __device__ __forceinline__ GroupTiles(const Groups& g, int slots, int tile) {
+    const int lane = threadIdx.x & 63;
+    n = 0;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const int up = __shfl_up(s, o);
-          if ((int)threadIdx.x >= o) s += up;
-        }
-        if (e < n_slots) first[e] = sum + s - t;
-        sum += __shfl(s, 63);
+    for (int c = 0; c < kGroupChunks; ++c) {
+      first[c] = INT32_MAX;
+      if (64 * c >= slots) continue;
+      const int e = 64 * c + lane;
+      int t = 0;
+      if (e < slots) {
+        const int2 r = g.rows(e);
+        t = (r.y - r.x + tile - 1) / tile;
       }
-      if (threadIdx.x == 0) first[n_slots] = sum;
+      int s = t;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(s, o);
+        if (lane >= o) s += up;
+      }
+      if (e < slots) first[c] = n + s - t;
+      n += __builtin_amdgcn_readlane(s, 63);
     }
-    __syncthreads();
   }
-  __device__ __forceinline__ int total() const {
-    return __builtin_amdgcn_readfirstlane(first[slots]);
+  // group of row tile t < n, and the tile's number within it
+  __device__ __forceinline__ int group(int t, int& within) const {
+    int e = -1;
+#pragma unroll
+    for (int c = 0; c < kGroupChunks; ++c) e += (int)__popcll(__ballot(first[c] <= t));
+    int f = 0;
+#pragma unroll
+    for (int c = 0; c < kGroupChunks; ++c)
+      if (e >> 6 == c) f = __builtin_amdgcn_readlane(first[c], e & 63);
+    within = t - f;
+    return e;
   }
-  // group of row tile t < total()
-  __device__ __forceinline__ int group(int t) const {
-    int lo = 0, hi = slots;  // first[lo] <= t < first[hi]
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (first[mid] <= t)
-        lo = mid;
-      else
-        hi = mid;
+};
+
+// The groups by their rows, most first (ties: the lower one): a launch whose tiles take
+// their group's rows as K then ends on its shortest tiles
+struct GroupOrder {
+  int rank[kGroupChunks];
+  __device__ __forceinline__ explicit GroupOrder(const Groups& g) {
+    const int lane = threadIdx.x & 63;
+    int rows[kGroupChunks];
+#pragma unroll
+    for (int c = 0; c < kGroupChunks; ++c) {
+      rank[c] = INT32_MAX;
+      if (64 * c >= g.E) continue;
+      rows[c] = -1;
+      if (64 * c + lane < g.E) {
+        const int2 r = g.rows(64 * c + lane);
+        rows[c] = r.y - r.x;
+        rank[c] = 0;
+      }
     }
-    return __builtin_amdgcn_readfirstlane(lo);
+#pragma unroll
+    for (int c = 0; c < kGroupChunks; ++c)
+      for (int l = 0; l < 64 && 64 * c + l < g.E; ++l) {
+        const int other = __builtin_amdgcn_readlane(rows[c], l);
+#pragma unroll
+        for (int k = 0; k < kGroupChunks; ++k)
+          if (64 * k < g.E && 64 * k + lane < g.E)
+            rank[k] += other > rows[k] || (other == rows[k] && 64 * c + l < 64 * k + lane) ? 1 : 0;
+      }
+  }
+  __device__ __forceinline__ int group(int r) const {
+    int e = 0;
+#pragma unroll
+    for (int c = 0; c < kGroupChunks; ++c) {
+      const unsigned long long m = __ballot(rank[c] == r);
+      if (m) e = 64 * c + __ffsll(m) - 1;
+    }
+    return __builtin_amdgcn_readfirstlane(e);
+  }
+};
+
+// Tiles of E groups, `per` each, dealt to a grid: every group's tiles are cut into one
+// run per XCD (block b runs on XCD b % 8), the groups in order, the longer runs passed
+// on from XCD to XCD.  Block i of an XCD takes every bx-th of its tiles from i on.
+struct GroupSched {
+  int per, E, nx, x, i0, bx, q, r;
+  __device__ __forceinline__ GroupSched(int per_, int E_) : per(per_), E(E_) {
+    nx = min(8, (int)gridDim.x);
+    x = blockIdx.x % nx;
+    i0 = blockIdx.x / nx;
+    bx = ((int)gridDim.x - x + nx - 1) / nx;
+    q = per / nx;
+    r = per % nx;
+  }
+  // the block's j-th tile: its group's rank and its number among the group's; false: none
+  __device__ __forceinline__ bool decode(int j, int& rank, int& at) const {
+    const int k = i0 + j * bx;
+    rank = k / per * nx;  // nx groups in a row hold `per` tiles of every XCD
+    int left = k % per;
+    for (;;) {
+      const int p = (x + rank) % nx, n = q + (p < r ? 1 : 0);
+      if (left < n) {
+        at = p * q + min(p, r) + left;
+        return rank < E;
+      }
+      left -= n;
+      if (++rank >= E) return false;
+    }
   }
 };
 

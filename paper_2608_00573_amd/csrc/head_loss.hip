@@ -374,79 +374,6 @@ __global__ __launch_bounds__(256) void k_row_parts(const int32_t* target, const 
 
 }  // namespace
 
-__device__ __forceinline__ int cdiv_d(int a, int b) { return (a + b - 1) / b; }
-
-// the block's lane constants on the large-group core: LDS offsets of fragments
-// of a K-contiguous (a, b) and of a transposed operand (at, bt), fetch rows
-struct BigLane {
-  int lane, wave, wm, wn, r0, cc;
-  __device__ __forceinline__ BigLane() {
-    const int tid = threadIdx.x;
-    lane = tid & 63;
-    wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    wm = wave >> 1;
-    wn = wave & 1;
-    r0 = tid >> 3;
-    cc = 8 * ((tid & 7) ^ swz16(r0));
-  }
-  // fragment offsets of the operand whose half `half` of the tile this wavefront reads
-  __device__ __forceinline__ void rows(uint32_t (&o)[2], int half) const {
-    const int fr = lane & 15, hk = lane >> 4;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      o[ks] = (half * 128 + fr) * big::RB + (((4 * ks + hk) ^ swz16(fr)) << 4);
-  }
-  __device__ __forceinline__ void cols(uint32_t (&o)[2], int half) const {
-    const int i = lane & 15, hk = lane >> 4, k = 8 * hk + (i >> 2);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-      o[ks] = (32 * ks + k) * 512 + half * 256 + (tr_swz(k) << 5) + 8 * (i & 3);
-  }
-  // A TR operand of `rows` rows of ld elements along K, from row k0 (k1: the end of
-  // the tile's run) and column c0
-  __device__ __forceinline__ BigOperand<true> along(const bf16_t* p, int ld, int rows, int k0, int k1,
-                                                    int c0) const {
-    BigOperand<true> o;
-    o.p = reinterpret_cast<const char*>(p + ((size_t)k0 * ld + c0));
-    o.left = min(rows, k1) - k0;
-    o.row = (uint32_t)ld * 2;
-    o.cut = (uint32_t)c0 * 2;
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int k = 2 * wave + 8 * u + (lane >> 5), c = lane & 31;
-      o.off[u] = (uint32_t)((k * ld + 16 * ((c >> 1) ^ tr_swz(k)) + 8 * (c & 1)) * 2);
-    }
-    return o;
-  }
-  // ... that lies in panels of 256 columns
-  __device__ __forceinline__ BigOperand<true> along_panel(const bf16_t* p, int rows, int k0, int k1,
-                                                          int c0) const {
-    return along(p + (size_t)c0 * rows, 256, rows, k0, k1, 0);
-  }
-  // a K-contiguous operand of ld elements a row, `valid` rows from p on, nk slices
-  // from slice k0 on; panel: bytes from one panel of 256 to the next, or 0
-  __device__ __forceinline__ BigOperand<false> across(const bf16_t* p, int ld, int valid, int k0,
-                                                      int nk, uint32_t panel) const {
-    BigOperand<false> o;
-    o.p = reinterpret_cast<const char*>(p);
-    o.left = nk;
-    o.panel = panel ? panel - 512 : 0;
-    o.ko = panel ? (uint32_t)(k0 >> 2) * panel + (uint32_t)(k0 & 3) * big::RB
-                 : (uint32_t)k0 * big::RB;
-#pragma unroll
-    for (int u = 0; u < 8; ++u)
-      o.off[u] = ((uint32_t)min(r0 + big::RPP * u, valid - 1) * ld + cc) * 2;
-    return o;
-  }
-};
-
-__device__ __forceinline__ void big_zero(AccBig& acc) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) acc[i][j] = f32x4_t{};
-}
-
 struct DzArgs {
   const bf16_t* w;    // the piece's first row
   const bf16_t* h;

@@ -16,7 +16,7 @@ namespace trimmoe {
 
 // K slices of an operand as a tile takes them.  Everything but off is wave-uniform.
 template <int NP>  // DMAs a thread and slice
-struct MidOperand {
+struct TileOperand {
   const char* p;     // not TR: row 0 at the slice; TR: the slice's first row, column 0 of the tile
   const char* p1;    // the second operand of a pair (see MidTile::PAIR)
   const char* q;     // where the second array begins (kq of it), or anything (kq 0)
@@ -32,15 +32,22 @@ struct MidOperand {
       // (a select of constants would be made in a vector register)
       return __builtin_amdgcn_readfirstlane(k > 0 ? 0xffffffffu : 0u);
   }
-  __device__ __forceinline__ void step() {
+  // to the next slice: on, and over to the next array at the end
+  __device__ __forceinline__ void go() {
     p += inc;
     p1 += inc;
     k -= BK;
+  }
+  __device__ __forceinline__ void turn() {
     if (k <= 0) {
       p = q;
       k = kq;
       kq = 0;
     }
+  }
+  __device__ __forceinline__ void step() {
+    go();
+    turn();
   }
 };
 
@@ -48,6 +55,7 @@ struct MidOperand {
 // fragments 0 .. TM / 2 - 1 are rows of the first and the rest the same rows of the second.
 template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false>
 struct MidTile {
+  static constexpr int OCC = 2, SPAN = PAIR_ ? 32 : 0;
   static constexpr int BM = BM_, BN = BN_, ST = ST_;
   static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
   static constexpr int THREADS = 256, GM = 2, GN = 2;
@@ -69,10 +77,10 @@ __device__ __forceinline__ int mid_swz(int k) {
 }
 
 // this thread's DMA offsets: of a K-contiguous operand's rows (ld elements each, rows
-// past `valid` repeat the last one) ...
+// past `valid` repeat the last one; span: rows of a pair's turns, or 0) ...
 template <int NP>
-__device__ __forceinline__ void mid_rows(MidOperand<NP>& o, const bf16_t* p, int ld, int valid, int k,
-                                         bool pair = false) {
+__device__ __forceinline__ void tile_rows(TileOperand<NP>& o, const bf16_t* p, int ld, int valid, int k,
+                                         int span = 0) {
   const int r0 = threadIdx.x >> 3;
   o.p = reinterpret_cast<const char*>(p);
   o.inc = 2 * BK;
@@ -82,13 +90,14 @@ __device__ __forceinline__ void mid_rows(MidOperand<NP>& o, const bf16_t* p, int
   o.q = o.p1 = o.p;
 #pragma unroll
   for (int u = 0; u < NP; ++u) {
-    const int r = pair ? r0 + 32 * (u >> 1) : r0 + 32 * u;
+    const int r = span == 32 ? r0 + 32 * (u >> 1) : span == 64 ? r0 + 32 * (u & 1) + 64 * (u >> 2)
+                                                               : r0 + 32 * u;
     o.off[u] = ((uint32_t)min(r, valid - 1) * (uint32_t)ld + 8 * ((threadIdx.x & 7) ^ swz16(r0))) * 2;
   }
 }
 // ... and of one along K, k rows of it from row 0 at p, from column c0 on
 template <int COLS, int NP>
-__device__ __forceinline__ void mid_along(MidOperand<NP>& o, const bf16_t* p, int ld, int c0, int k) {
+__device__ __forceinline__ void tile_along(TileOperand<NP>& o, const bf16_t* p, int ld, int c0, int k) {
   o.p = reinterpret_cast<const char*>(p + c0);
   o.row = 2 * (uint32_t)ld;
   o.cut = 2 * (uint32_t)c0;
@@ -103,8 +112,9 @@ __device__ __forceinline__ void mid_along(MidOperand<NP>& o, const bf16_t* p, in
   }
 }
 
-template <class T>
+template <class T_>
 struct MidCore {
+  using T = T_;
   using Acc = f32x4_t[T::TM][T::TN];
   struct Frags {
     bf16x8_t a[T::TM], b[T::TN];
@@ -113,6 +123,8 @@ struct MidCore {
   static constexpr int OPS = T::TM * (T::ATR ? 2 : 1) + T::TN * (T::BTR ? 2 : 1);  // LDS reads a k-step
   int lane, wave, wm, wn;
   uint32_t s0, la[2], lb[2];
+  TileOperand<T::PA> a;
+  TileOperand<T::PB> b;
 
   __device__ __forceinline__ explicit MidCore(char* lds) {
     lane = threadIdx.x & 63;
@@ -174,7 +186,7 @@ struct MidCore {
         acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
   }
   template <bool TR, bool PAIR, int NP>
-  __device__ __forceinline__ void issue1(uint32_t dst, const MidOperand<NP>& o) const {
+  __device__ __forceinline__ void issue1(uint32_t dst, const TileOperand<NP>& o) const {
     const uint32_t n = o.template bytes<TR>();
     const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p), (short)0, (int)n, 0x00020000);
     const auto r1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(PAIR ? o.p1 : o.p), (short)0,
@@ -185,30 +197,31 @@ struct MidCore {
           PAIR && (u & 1) ? r1 : rs, (lds_byte*)(uintptr_t)(dst + (uint32_t)(u * 4096 + wave * 1024)), 16,
           o.off[u], 0, 0, 0);
   }
-  template <class A, class B>
-  __device__ __forceinline__ void issue(int stage, A& a, B& b) const {
+  __device__ __forceinline__ void issue(int stage) {
     const uint32_t s = s0 + stage * T::STAGE;
     issue1<T::ATR, T::PAIR>(s, a);
     issue1<T::BTR, false>(s + T::A_BYTES, b);
     a.step();
     b.step();
   }
-  static __device__ __forceinline__ void zero(Acc& acc) {
+  // a tile's first loads; LDS is free from the end of the tile before it
+  __device__ __forceinline__ void begin(const TileOperand<T::PA>& a_, const TileOperand<T::PB>& b_) {
+    a = a_;
+    b = b_;
+#pragma unroll
+    for (int s = 0; s < T::ST - 1; ++s) issue(s);
+  }
+  // acc = the tile's product over nk slices; afterwards LDS is free.  Loads past the
+  // last slice bring zeros into stages that nobody reads.
+  __device__ __forceinline__ void run(int nk, Acc& acc) {
 #pragma unroll
     for (int i = 0; i < T::TM; ++i)
 #pragma unroll
       for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4_t{};
-  }
-  // acc += the tile's product over nk slices; afterwards LDS is free.  Loads past the
-  // last slice bring zeros into stages that nobody reads.
-  __device__ __forceinline__ void run(MidOperand<T::PA>& a, MidOperand<T::PB>& b, int nk, Acc& acc) const {
-    if (nk <= 0) return;
-#pragma unroll
-    for (int s = 0; s < T::ST - 1; ++s) issue(s, a, b);
     int st = 0, in = T::ST - 1;
     for (int g = 0; g < nk; ++g) {
       asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NDMA * (T::ST - 2)) : "memory");
-      issue(in, a, b);
+      issue(in);
       in = in + 1 == T::ST ? 0 : in + 1;
       const uint32_t s = s0 + st * T::STAGE;
       st = st + 1 == T::ST ? 0 : st + 1;

@@ -175,6 +175,10 @@ BLOCKS = [
     (BF16, True, 192, 128, [129, 200], 0, 1),      # more than a tile of 128 rows
     (BF16, False, 320, 448, [300], 2, 0),
     (BF16, True, 512, 704, [257, 128, 0, 390], 0, 7),
+    (BF16, True, 64, 64, [513], 0, 0),             # groups of many rows: the large tiles
+    (BF16, False, 320, 192, [1, 1300, 0, 800], 2, 3),
+    (BF16, True, 128, 448, [256, 1031], 0, 0),
+    (BF16, True, 576, 320, [1025], 1, 0),
     (BF16, True, 64, 64, [0, 0], 0, 4),            # no rows at all
     (F32, True, 64, 256, [5, 0, 9, 1, 0, 17, 3, 2], 0, 0),
     (F32, False, 64, 256, [8] * 8, 0, 0),
