@@ -10,7 +10,7 @@ namespace trimmoe {
 template <bool ATR_, bool BTR_, bool PAIR_ = false>
 struct BigTile {
   static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
-  static constexpr int BM = big::BM, BN = big::BN, OCC = 1, SPAN = PAIR ? 64 : 0;
+  static constexpr int BM = big::BM, BN = big::BN, KS = BK, OCC = 1, SPAN = PAIR ? 64 : 0;
   static constexpr int THREADS = big::THREADS, WM = 128, WN = 128, TM = 8, TN = 8, PA = 8, PB = 8;
   static constexpr int LDS = big::LDS, ROWS_A = PAIR ? BM / 2 : BM;
 };
@@ -24,12 +24,9 @@ struct RunFeed {
   TileOperand<8> a, b;
   __amdgpu_buffer_rsrc_t a1, a2, b2, g1, g2;
   uint32_t n;
-  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const char* p, uint32_t bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, (int)bytes, 0x00020000);
-  }
   __device__ __forceinline__ void take_a() {
-    a2 = rsrc(a.p, n);
-    if constexpr (T::PAIR) g2 = rsrc(a.p1, n);
+    a2 = uniform_rsrc(a.p, n);
+    if constexpr (T::PAIR) g2 = uniform_rsrc(a.p1, n);
   }
   __device__ __forceinline__ void pass_a() {
     a1 = a2;
@@ -45,7 +42,7 @@ struct RunFeed {
     if constexpr (S == 13) b.go();
     if constexpr (S == 14) b.turn();
     if constexpr (S == 15) n = b.template bytes<BTR>();
-    if constexpr (S == 16) b2 = rsrc(b.p, n);
+    if constexpr (S == 16) b2 = uniform_rsrc(b.p, n);
     if constexpr (S >= 8 && S <= 16) sched_fence();
   }
   __device__ __forceinline__ void dma_a(uint32_t stage, int wave, bool next, int u) const {
@@ -64,6 +61,8 @@ struct BigCore {
   int lane, wave, wm, wn;
   uint32_t la[2], lb[2];
   RunFeed<T> f;
+  TileOperand<8> a, b;  // of the tile that load() has made ready
+  int left;
   __device__ __forceinline__ explicit BigCore(char* lds_) : lds(lds_) {
     const BigLane L;
     lane = L.lane;
@@ -79,8 +78,15 @@ struct BigCore {
     else
       L.rows(lb, wn);
   }
-  // a tile's first loads: slice 0, B of slice 1 and the first half of its A
-  __device__ __forceinline__ void begin(const TileOperand<8>& a, const TileOperand<8>& b) {
+  // Every tile runs through its own slices; the next one's first loads (slice 0, B of
+  // slice 1 and the first half of its A) go out before a tile leaves its registers.
+  template <class Load>
+  __device__ __forceinline__ void first(Load& load) {
+    ahead(load);
+  }
+  template <class Load>
+  __device__ __forceinline__ void ahead(Load& load) {
+    if (!load()) return;
     f.a = a;
     f.b = b;
     const BigLds L{lds_addr(lds)};
@@ -88,7 +94,7 @@ struct BigCore {
       f.n = f.a.template bytes<T::ATR>();
       f.take_a();
       f.n = f.b.template bytes<T::BTR>();
-      f.b2 = RunFeed<T>::rsrc(f.b.p, f.n);
+      f.b2 = uniform_rsrc(f.b.p, f.n);
     };
     take();
 #pragma unroll
@@ -117,8 +123,8 @@ struct BigCore {
   }
   // acc = the tile's product over nk slices (see big_run).  NEWER: vector-memory
   // operations that every wavefront has issued since begin, at least
-  template <int NEWER = 0>
-  __device__ __forceinline__ void run(int nk, Acc& acc) {
+  template <int NEWER = 0, class Load>
+  __device__ __forceinline__ void run(int nk, Acc& acc, Load&) {
     big_zero(acc);
     big_wait<NEWER>();
     BigStages L{BigLds{lds_addr(lds)}};
@@ -142,6 +148,7 @@ struct BigCore {
     big_close(fa, fb0, acc);
     sched_fence();
   }
+  __device__ __forceinline__ void last() {}
 };
 
 }  // namespace trimmoe

@@ -21,15 +21,34 @@ namespace {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
-// a tile of rows: its group (E and above: rows of no group, which have no product)
+// a tile of rows times columns from c0 on; its group e (E and above: rows of no group,
+// which have no product)
 struct RowTile {
-  int e, r0, valid;
-  __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, int mt, int tile) {
-    int within;
+  int e, r0, valid, c0;
+  RowTile() = default;
+  __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, const TileSched& S, int j,
+                                     int rows, int cols) {
+    int mt, nt, sp, within;
+    S.decode(j, mt, nt, sp);
     e = t.group(mt, within);
     const int2 r = g.rows(e);
-    r0 = uniform(r.x + within * tile);
-    valid = uniform(min(tile, r.y - r0));
+    r0 = uniform(r.x + within * rows);
+    valid = uniform(min(rows, r.y - r0));
+    c0 = uniform(nt * cols);
+  }
+};
+struct RowQueue {
+  TileQueue<4> q;
+  __device__ __forceinline__ int left() const { return q.n; }
+  __device__ __forceinline__ void push(const RowTile& t) { q.push({{t.e, t.r0, t.valid, t.c0}}); }
+  __device__ __forceinline__ RowTile pop() {
+    const auto v = q.pop();
+    RowTile t;
+    t.e = v.v[0];
+    t.r0 = v.v[1];
+    t.valid = v.v[2];
+    t.c0 = v.v[3];
+    return t;
   }
 };
 
@@ -88,36 +107,33 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
   int ntiles;
   if (!S.init(tiles.n, (a.F + T::ROWS_A - 1) / T::ROWS_A, 1, ntiles)) return;
   C core(lds);
-  struct At {
-    int r0, valid, f0, nk;
-  };
-  const auto begin = [&](int jt) {
-    int mt, nt, sp;
-    S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, T::BN);
-    const int f0 = nt * T::ROWS_A, k = row.e < a.groups.E ? a.d : 0;
-    const size_t w0 = ((size_t)(k ? row.e : 0) * a.F + f0) * a.d;
-    TileOperand<T::PA> A;
-    TileOperand<T::PB> B;
-    tile_rows(A, a.w_up + w0, a.d, min(T::ROWS_A, a.F - f0), k, T::SPAN);
-    if constexpr (GATED) A.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
-    tile_rows(B, a.x + (size_t)row.r0 * a.d, a.d, row.valid, k);
-    core.begin(A, B);
-    return At{row.r0, row.valid, f0, k / BK};
+  int jl = 0;
+  RowQueue queue;
+  auto load = [&] {
+    if (jl == ntiles) return false;
+    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    queue.push(at);
+    const int k = at.e < a.groups.E ? a.d : 0;
+    const size_t w0 = ((size_t)(k ? at.e : 0) * a.F + at.c0) * a.d;
+    tile_rows(core.a, a.w_up + w0, a.d, min(T::ROWS_A, a.F - at.c0), k, T::SPAN);
+    if constexpr (GATED) core.a.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
+    tile_rows(core.b, a.x + (size_t)at.r0 * a.d, a.d, at.valid, k);
+    core.left = max(k / BK, 1);
+    return true;
   };
   constexpr int TMO = GATED ? T::TM / 2 : T::TM;  // 16-column groups of a wavefront
-  At at = begin(0);
-  for (int jt = 0; jt < ntiles; ++jt) {
+  core.first(load);
+  while (queue.left()) {
+    const RowTile was = queue.pop();
     typename C::Acc acc;
-    core.run(at.nk, acc);
-    const At was = at;
-    if (jt + 1 < ntiles) at = begin(jt + 1);
+    core.run(was.e < a.groups.E ? a.d / BK : 1, acc, load);
+    core.ahead(load);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
       const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
 #pragma unroll
       for (int i = 0; i < TMO; i += 2) {
-        const int c = was.f0 + core.wm * 16 * TMO + 16 * i;  // 32 columns, all of them or none in F
+        const int c = was.c0 + core.wm * 16 * TMO + 16 * i;  // 32 columns, all of them or none in F
         const bool in = t < was.valid && c < a.F;
         const size_t o = (size_t)(was.r0 + t) * a.F + c;
         float u[2][4], g[2][4], v[2][4];
@@ -153,6 +169,7 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
       }
     }
   }
+  core.last();
 }
 
 // out [n, M] = rows times weights: y = a Wd^T (Wd K-contiguous) or, ATR, dx = du Wu (+
@@ -166,25 +183,37 @@ struct RowsArgs {
   bf16_t* out;
 };
 
-// a tile's results: bf16, 16 bytes a lane
+// A tile's results, bf16, 16 bytes a lane.  Rows past `valid` lie behind the buffer's
+// end and are dropped, as are columns past M by their offset (M is a multiple of 64:
+// blocks of 32 are valid or not as a whole), so that every wavefront issues STORES<C>
+// stores.
+template <class C>
+constexpr int STORES = C::T::TM * C::T::TN / 2;
 template <class C>
 __device__ __forceinline__ void store_tile(const C& core, const typename C::Acc& acc, bf16_t* out, size_t row0,
                                            int valid, int m0, int M) {
   using T = typename C::T;
+  m0 = uniform(m0);
+  M = uniform(M);
+  asm volatile("" : "+s"(M));  // per-tile value: keeps the offsets below inside the tile loop
+  const __amdgpu_buffer_rsrc_t ro =
+      uniform_rsrc(reinterpret_cast<const char*>(out + row0 * M + m0),
+                   uniform((int)((uint32_t)min(valid, T::BN) * M * 2 - m0 * 2)));
+  const uint32_t cw = core.wm * T::WM;
 #pragma unroll
   for (int j = 0; j < T::TN; ++j) {
-    const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+    const uint32_t off =
+        ((uint32_t)(core.wn * T::WN + 16 * j + (core.lane & 15)) * M + cw + pack_col(core.lane)) * 2;
 #pragma unroll
     for (int i = 0; i < T::TM; i += 2) {
-      const int c = m0 + core.wm * T::WM + 16 * i;
       float v[2][4];
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int r = 0; r < 4; ++r) v[k][r] = acc[i + k][j][r];
-      const u32x4_t p = pack_rows(v[0], v[1]);
-      if (t < valid && c < M)
-        *reinterpret_cast<u32x4_t*>(out + (row0 + t) * M + c + pack_col(core.lane)) = p;
+      // (no scalar offset: see pack_rows)
+      __builtin_amdgcn_raw_buffer_store_b128(
+          pack_rows(v[0], v[1]), ro, ((int)(m0 + cw + 16 * i) < M ? off : 0xffff0000u) + 32 * i, 0, 0);
     }
   }
 }
@@ -198,39 +227,41 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
   int ntiles;
   if (!S.init(tiles.n, (a.M + T::BM - 1) / T::BM, 1, ntiles)) return;
   C core(lds);
-  struct At {
-    int r0, valid, m0, nk;
-  };
-  const auto begin = [&](int jt) {
-    int mt, nt, sp;
-    S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, T::BN);
-    const int m0 = nt * T::BM, K = row.e < a.groups.E ? a.K : 0;
-    const size_t e0 = K ? (size_t)row.e * a.M * a.K : 0, b0 = (size_t)row.r0 * a.K;
-    TileOperand<T::PA> A;
-    TileOperand<T::PB> B;
+  const int slices = a.K / BK * (T::ATR && a.w2 ? 2 : 1);
+  int jl = 0;
+  RowQueue queue;
+  auto load = [&] {
+    if (jl == ntiles) return false;
+    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    queue.push(at);
+    const int K = at.e < a.groups.E ? a.K : 0;
+    const size_t e0 = K ? (size_t)at.e * a.M * a.K : 0, b0 = (size_t)at.r0 * a.K;
     if constexpr (T::ATR)
-      tile_along<T::BM>(A, a.w + e0, a.M, m0, K);
+      tile_along<T::BM>(core.a, a.w + e0, a.M, at.c0, K);
     else
-      tile_rows(A, a.w + e0 + (size_t)m0 * a.K, a.K, min(T::BM, a.M - m0), K);
-    tile_rows(B, a.b + b0, a.K, row.valid, K);
-    const bool two = T::ATR && a.w2 && K;
-    if (two) {
-      A.q = reinterpret_cast<const char*>(a.w2 + e0 + m0);
-      B.q = reinterpret_cast<const char*>(a.b2 + b0);
-      A.kq = B.kq = K;
+      tile_rows(core.a, a.w + e0 + (size_t)at.c0 * a.K, a.K, min(T::BM, a.M - at.c0), K);
+    tile_rows(core.b, a.b + b0, a.K, at.valid, K);
+    if (T::ATR && a.w2) {
+      core.a.q = reinterpret_cast<const char*>(a.w2 + e0 + at.c0);
+      core.b.q = reinterpret_cast<const char*>(a.b2 + b0);
+      core.a.kq = core.b.kq = K;
     }
-    core.begin(A, B);
-    return At{row.r0, row.valid, m0, K / BK * (two ? 2 : 1)};
+    core.left = K ? slices : 1;
+    return true;
   };
-  At at = begin(0);
-  for (int jt = 0; jt < ntiles; ++jt) {
+  core.first(load);
+  for (bool stored = false; queue.left(); stored = true) {
+    const RowTile was = queue.pop();
     typename C::Acc acc;
-    core.run(at.nk, acc);
-    const At was = at;
-    if (jt + 1 < ntiles) at = begin(jt + 1);
-    store_tile(core, acc, a.out, was.r0, was.valid, was.m0, a.M);
+    const int nk = was.e < a.groups.E ? slices : 1;
+    if (stored)
+      core.template run<STORES<C>>(nk, acc, load);
+    else
+      core.run(nk, acc, load);
+    core.ahead(load);
+    store_tile(core, acc, a.out, was.r0, was.valid, was.c0, a.M);
   }
+  core.last();
 }
 
 // --------------------------------------------------------------- backward --
@@ -269,33 +300,29 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
   int ntiles;
   if (!S.init(tiles.n, (a.F + T::BM - 1) / T::BM, 1, ntiles)) return;
   C core(lds);
-  struct At {
-    int r0, valid, f0;
+  int jl = 0;
+  RowQueue queue;
+  auto load = [&] {
+    if (jl == ntiles) return false;
+    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    queue.push(at);
+    tile_along<T::BM>(core.a, a.w_down + (size_t)at.e * a.d * a.F, a.F, at.c0, a.d);
+    tile_rows(core.b, a.dy + (size_t)at.r0 * a.d, a.d, at.valid, a.d);
+    core.left = a.d / BK;
+    return true;
   };
-  const auto begin = [&](int jt) {
-    int mt, nt, sp;
-    S.decode(jt, mt, nt, sp);
-    const RowTile row(tiles, a.groups, mt, T::BN);
-    const int f0 = nt * T::BM;
-    TileOperand<T::PA> A;
-    TileOperand<T::PB> B;
-    tile_along<T::BM>(A, a.w_down + (size_t)row.e * a.d * a.F, a.F, f0, a.d);
-    tile_rows(B, a.dy + (size_t)row.r0 * a.d, a.d, row.valid, a.d);
-    core.begin(A, B);
-    return At{row.r0, row.valid, f0};
-  };
-  At at = begin(0);
-  for (int jt = 0; jt < ntiles; ++jt) {
+  core.first(load);
+  while (queue.left()) {
+    const RowTile was = queue.pop();
     typename C::Acc acc;
-    core.run(a.d / BK, acc);
-    const At was = at;
-    if (jt + 1 < ntiles) at = begin(jt + 1);
+    core.run(a.d / BK, acc, load);
+    core.ahead(load);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
       const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
 #pragma unroll
       for (int i = 0; i < T::TM; i += 2) {
-        const int c = was.f0 + core.wm * T::WM + 16 * i;
+        const int c = was.c0 + core.wm * T::WM + 16 * i;
         const bool in = t < was.valid && c < a.F;
         const size_t o = (size_t)(was.r0 + t) * a.F + c;
         float va[2][4], vu[2][4], vg[2][4];
@@ -334,6 +361,7 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
       }
     }
   }
+  core.last();
 }
 
 // Weight gradients: of group e and product p, out [N, M] = B^T A over the group's rows
@@ -356,47 +384,50 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a)
     first[p + 1] = first[p] + (p < a.n_prod ? ((a.M[p] + T::BM - 1) / T::BM) * ((a.N[p] + T::BN - 1) / T::BN)
                                             : 0);
   const GroupOrder order(a.groups);
-  const GroupSched S(first[3], a.groups.E);
+  GroupWalk walk(first[3], a.groups.E);
   C core(lds);
-  struct At {
-    bf16_t* out;
-    int M, N, m0, n0, nk;
+  TileQueue<5> queue;  // group, product, first column and row of the result, K
+  const auto of = [](const auto (&v)[3], int p) { return p == 0 ? v[0] : p == 1 ? v[1] : v[2]; };
+  int rank = -1, e = 0, r0 = 0, k = 0;  // the group of the tile before
+  auto load = [&] {
+    if (!walk.more()) return false;
+    if (walk.rank != rank) {
+      rank = walk.rank;
+      e = order.group(rank);
+      const int2 r = a.groups.rows(e);
+      r0 = uniform(r.x);
+      k = uniform(r.y) - r0;
+    }
+    int L = uniform(walk.tile());
+    walk.next();
+    const int p = L >= first[2] ? 2 : L >= first[1] ? 1 : 0;
+    const int M = of(a.M, p), N = of(a.N, p);
+    L -= p == 0 ? 0 : p == 1 ? first[1] : first[2];
+    // patches of 8 column tiles of the result
+    const int n_mt = (N + T::BN - 1) / T::BN, n_nt = (M + T::BM - 1) / T::BM;
+    const int g = uniform((int)((unsigned)L / (unsigned)(8 * n_nt))), w = L - g * 8 * n_nt, gm = min(8, n_mt - 8 * g);
+    const int nt = gm == 8 ? w >> 3 : uniform((int)((unsigned)w / (unsigned)gm)), mt = 8 * g + w - nt * gm;
+    const int m0 = uniform(nt * T::BM), n0 = uniform(mt * T::BN);
+    queue.push({{e, p, m0, n0, k}});
+    tile_along<T::BM, T::KS>(core.a, of(a.A, p) + (size_t)r0 * M, M, m0, k);
+    tile_along<T::BN, T::KS>(core.b, of(a.B, p) + (size_t)r0 * N, N, n0, k);
+    core.left = max((k + T::KS - 1) / T::KS, 1);
+    return true;
   };
-  const auto begin = [&](int rank, int at) {
-    const int e = order.group(rank);
-    const int p = at >= first[2] ? 2 : at >= first[1] ? 1 : 0;
-    const int M = p == 0 ? a.M[0] : p == 1 ? a.M[1] : a.M[2];
-    const int N = p == 0 ? a.N[0] : p == 1 ? a.N[1] : a.N[2];
-    const bf16_t* pA = p == 0 ? a.A[0] : p == 1 ? a.A[1] : a.A[2];
-    const bf16_t* pB = p == 0 ? a.B[0] : p == 1 ? a.B[1] : a.B[2];
-    bf16_t* out = p == 0 ? a.out[0] : p == 1 ? a.out[1] : a.out[2];
-    TileSched P;
-    P.n_mt = (N + T::BN - 1) / T::BN;
-    P.n_nt = (M + T::BM - 1) / T::BM;
-    int mt, nt, sp;
-    P.decode_abs(at - (p == 0 ? 0 : p == 1 ? first[1] : first[2]), mt, nt, sp);
-    const int m0 = nt * T::BM, n0 = mt * T::BN;
-    const int2 r = a.groups.rows(e);
-    const int r0 = uniform(r.x), k = uniform(r.y) - r0;
-    TileOperand<T::PA> A;
-    TileOperand<T::PB> B;
-    tile_along<T::BM>(A, pA + (size_t)r0 * M, M, m0, k);
-    tile_along<T::BN>(B, pB + (size_t)r0 * N, N, n0, k);
-    core.begin(A, B);
-    return At{out + (size_t)e * M * N, M, N, m0, n0, (k + BK - 1) / BK};
-  };
-  int rank, tile;
-  if (!S.decode(0, rank, tile)) return;
-  At at = begin(rank, tile);
-  for (int jt = 1;; ++jt) {
+  core.first(load);
+  for (bool stored = false; queue.n; stored = true) {
+    const auto at = queue.pop();
+    const int(&was)[5] = at.v;
+    const int p = was[1], M = of(a.M, p), N = of(a.N, p), nk = max((was[4] + T::KS - 1) / T::KS, 1);
     typename C::Acc acc;
-    core.run(at.nk, acc);
-    const At was = at;
-    const bool more = S.decode(jt, rank, tile);
-    if (more) at = begin(rank, tile);
-    store_tile(core, acc, was.out, was.n0, was.N - was.n0, was.m0, was.M);
-    if (!more) break;
+    if (stored)
+      core.template run<STORES<C>>(nk, acc, load);
+    else
+      core.run(nk, acc, load);
+    core.ahead(load);
+    store_tile(core, acc, of(a.out, p) + (size_t)was[0] * M * N, was[3], N - was[3], was[2], M);
   }
+  core.last();
 }
 
 // --------------------------------------------------------------- launching --
@@ -426,12 +457,10 @@ hipError_t with_kind(Rows kind, F f) {
   return hipGetLastError();
 }
 
-// blocks of a launch over at most `tiles` tiles: one for each (which the hardware deals
-// out as others end), or one a CU that stays (the large-group core)
+// blocks of a launch over at most `tiles` tiles: as many as the CUs hold
 template <class C>
 dim3 grid_of(long tiles, int n_cu) {
-  const long most = C::T::OCC == 1 ? n_cu : 1l << 20;
-  return dim3((unsigned)std::min(std::max(tiles, 1l), most));
+  return dim3((unsigned)std::min(std::max(tiles, 1l), (long)n_cu * C::T::OCC));
 }
 template <class C>
 dim3 rows_grid(const Groups& g, int cols, int n_cu) {
@@ -467,12 +496,11 @@ hipError_t launch_weights(const WeightArgs& a, int n_cu, hipStream_t st) {
   const Rows kind = rows_kind(a.groups) == kLarge ? kLarge : kMid;
   return with_kind(kind, [&](auto k) {
     if constexpr (k != kFew) {
-      using C = CoreOf<k, true, true>;
+      using C = std::conditional_t<k == kLarge, CoreOf<k, true, true>,
+                                   MidCore<MidTile<256, 128, 3, true, true, false, 32, 2>>>;
       long tiles = 0;
       for (int p = 0; p < a.n_prod; ++p) tiles += (long)cdiv(a.M[p], C::T::BM) * cdiv(a.N[p], C::T::BN);
-      // (every XCD's blocks take its tiles of all groups)
-      hipLaunchKernelGGL((k_expert_weights<C>), grid_of<C>((tiles * a.groups.E + 7) / 8 * 8, n_cu), dim3(256),
-                         0, st, a);
+      hipLaunchKernelGGL((k_expert_weights<C>), grid_of<C>(tiles * a.groups.E, n_cu), dim3(256), 0, st, a);
     }
   });
 }

@@ -108,30 +108,35 @@ struct GroupOrder {
 // Tiles of E groups, `per` each, dealt to a grid: every group's tiles are cut into one
 // run per XCD (block b runs on XCD b % 8), the groups in order, the longer runs passed
 // on from XCD to XCD.  Block i of an XCD takes every bx-th of its tiles from i on.
-struct GroupSched {
-  int per, E, nx, x, i0, bx, q, r;
-  __device__ __forceinline__ GroupSched(int per_, int E_) : per(per_), E(E_) {
+struct GroupWalk {
+  int E, nx, bx, q, r;
+  int rank, run, left;  // the next tile: its group's rank, the XCD's run there, its place in it
+  __device__ __forceinline__ GroupWalk(int per, int E_) : E(E_), rank(0) {
     nx = min(8, (int)gridDim.x);
-    x = blockIdx.x % nx;
-    i0 = blockIdx.x / nx;
-    bx = ((int)gridDim.x - x + nx - 1) / nx;
-    q = per / nx;
-    r = per % nx;
+    run = blockIdx.x % nx;
+    left = blockIdx.x / nx;
+    bx = ((int)gridDim.x - run + nx - 1) / nx;
+    // (the compiler divides in vector registers)
+    run = __builtin_amdgcn_readfirstlane(run);
+    left = __builtin_amdgcn_readfirstlane(left);
+    bx = __builtin_amdgcn_readfirstlane(bx);
+    q = __builtin_amdgcn_readfirstlane(per / nx);
+    r = per - q * nx;
+    settle();
   }
-  // the block's j-th tile: its group's rank and its number among the group's; false: none
-  __device__ __forceinline__ bool decode(int j, int& rank, int& at) const {
-    const int k = i0 + j * bx;
-    rank = k / per * nx;  // nx groups in a row hold `per` tiles of every XCD
-    int left = k % per;
-    for (;;) {
-      const int p = (x + rank) % nx, n = q + (p < r ? 1 : 0);
-      if (left < n) {
-        at = p * q + min(p, r) + left;
-        return rank < E;
-      }
-      left -= n;
-      if (++rank >= E) return false;
+  __device__ __forceinline__ int length() const { return q + (run < r ? 1 : 0); }
+  __device__ __forceinline__ void settle() {
+    while (rank < E && left >= length()) {
+      left -= length();
+      run = run + 1 == nx ? 0 : run + 1;
+      ++rank;
     }
+  }
+  __device__ __forceinline__ bool more() const { return rank < E; }
+  __device__ __forceinline__ int tile() const { return run * q + min(run, r) + left; }  // of the group's
+  __device__ __forceinline__ void next() {
+    left += bx;
+    settle();
   }
 };
 

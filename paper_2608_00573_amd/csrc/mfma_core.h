@@ -999,6 +999,10 @@ __device__ __forceinline__ void big_tile(char* lds, const R& q, int nk, AccBig& 
 // Two accumulators' values of one row (columns 16 i .. and 16 (i + 1) ..; a lane
 // holds 4 consecutive ones) as bf16, 8 consecutive columns a lane: lanes of even
 // groups of 16 get the first block's pieces, those of odd groups the second's
+// (A 16-byte buffer store of them takes its offset in the vector register and the
+// instruction: with a scalar offset register, a VALU write to the data registers right
+// behind the store reached its data, 4 bytes of a quarter of the lanes now and then, and
+// the compiler keeps the distance only for stores without one.)
 __device__ __forceinline__ u32x4_t pack_rows(const float (&x)[4], const float (&y)[4]) {
   const unsigned x0 = pack_bf16x2(x[0], x[1]), x1 = pack_bf16x2(x[2], x[3]);
   const unsigned y0 = pack_bf16x2(y[0], y[1]), y1 = pack_bf16x2(y[2], y[3]);

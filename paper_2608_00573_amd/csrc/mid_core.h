@@ -14,6 +14,16 @@
 
 namespace trimmoe {
 
+// a buffer at p, which is the same in every lane (the compiler does not always see it,
+// and would turn every fetch into a loop over lanes)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const char* p, uint32_t bytes) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<char*>((uint64_t)hi << 32 | lo), (short)0,
+                                           (int)bytes, 0x00020000);
+}
+
 // K slices of an operand as a tile takes them.  Everything but off is wave-uniform.
 template <int NP>  // DMAs a thread and slice
 struct TileOperand {
@@ -24,19 +34,17 @@ struct TileOperand {
   uint32_t row, cut; // TR: bytes of a row, and of a row before the tile's columns
   int k, kq;         // K left from the slice on, in this array and in the next
   uint32_t off[NP];
-  template <bool TR>
+  template <bool TR, int KS = BK>
   __device__ __forceinline__ uint32_t bytes() const {
-    if constexpr (TR)
-      return k > 0 ? (uint32_t)min(k, BK) * row - cut : 0u;
-    else
-      // (a select of constants would be made in a vector register)
-      return __builtin_amdgcn_readfirstlane(k > 0 ? 0xffffffffu : 0u);
+    return __builtin_amdgcn_readfirstlane(k <= 0 ? 0u : TR ? (uint32_t)min(k, KS) * row - cut
+                                                             : 0xffffffffu);
   }
   // to the next slice: on, and over to the next array at the end
+  template <int KS = BK>
   __device__ __forceinline__ void go() {
     p += inc;
     p1 += inc;
-    k -= BK;
+    k -= KS;
   }
   __device__ __forceinline__ void turn() {
     if (k <= 0) {
@@ -45,24 +53,27 @@ struct TileOperand {
       kq = 0;
     }
   }
+  template <int KS = BK>
   __device__ __forceinline__ void step() {
-    go();
+    go<KS>();
     turn();
   }
 };
 
 // PAIR: A holds two K-contiguous operands in turns of 32 rows, so that a wavefront's
 // fragments 0 .. TM / 2 - 1 are rows of the first and the rest the same rows of the second.
-template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false>
+// KS: elements of K a slice (operands along K may take 32).  OCC: blocks a CU.
+template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false, int KS_ = BK, int OCC_ = 2>
 struct MidTile {
-  static constexpr int OCC = 2, SPAN = PAIR_ ? 32 : 0;
+  static constexpr int KS = KS_, OCC = OCC_, SPAN = PAIR_ ? 32 : 0;
   static constexpr int BM = BM_, BN = BN_, ST = ST_;
   static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
   static constexpr int THREADS = 256, GM = 2, GN = 2;
   static constexpr int WM = BM / GM, WN = BN / GN, TM = WM / 16, TN = WN / 16;
-  static constexpr int PA = BM / 32, PB = BN / 32;  // DMAs a thread
-  static constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128, LDS = ST * STAGE;
+  static constexpr int PA = BM * KS / 2048, PB = BN * KS / 2048;  // DMAs a thread
+  static constexpr int A_BYTES = BM * KS * 2, STAGE = (BM + BN) * KS * 2, LDS = ST * STAGE;
   static constexpr int ROWS_A = PAIR ? BM / 2 : BM;  // rows of C's A side
+  static_assert(KS == BK || (KS == 32 && ATR && BTR), "rows come in 128-byte slices");
   static_assert(!PAIR || (WM == 64 && !ATR), "pairs go by 32 rows");
   static_assert(ST >= 2 && (PA + PB) * (ST - 2) < 64, "waits");
 };
@@ -96,12 +107,12 @@ __device__ __forceinline__ void tile_rows(TileOperand<NP>& o, const bf16_t* p, i
   }
 }
 // ... and of one along K, k rows of it from row 0 at p, from column c0 on
-template <int COLS, int NP>
+template <int COLS, int KS = BK, int NP>
 __device__ __forceinline__ void tile_along(TileOperand<NP>& o, const bf16_t* p, int ld, int c0, int k) {
   o.p = reinterpret_cast<const char*>(p + c0);
   o.row = 2 * (uint32_t)ld;
   o.cut = 2 * (uint32_t)c0;
-  o.inc = o.row * BK;
+  o.inc = o.row * KS;
   o.k = k;
   o.kq = 0;
   o.q = o.p1 = o.p;
@@ -111,6 +122,36 @@ __device__ __forceinline__ void tile_along(TileOperand<NP>& o, const bf16_t* p, 
     o.off[u] = ((uint32_t)kr * (uint32_t)ld + 16 * ((c >> 1) ^ mid_swz<COLS>(kr)) + 8 * (c & 1)) * 2;
   }
 }
+
+// Up to three tiles (N numbers each) whose loads have begun, first in first out, in
+// registers: selected number by number, for an indexed copy would lie in memory
+template <int N>
+struct TileQueue {
+  struct At {
+    int v[N];
+  };
+  int q0[N], q1[N], q2[N], n = 0;
+  __device__ __forceinline__ void push(const At& at) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      q0[i] = n == 0 ? at.v[i] : q0[i];
+      q1[i] = n == 1 ? at.v[i] : q1[i];
+      q2[i] = n == 2 ? at.v[i] : q2[i];
+    }
+    ++n;
+  }
+  __device__ __forceinline__ At pop() {
+    At at;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      at.v[i] = q0[i];
+      q0[i] = q1[i];
+      q1[i] = q2[i];
+    }
+    --n;
+    return at;
+  }
+};
 
 template <class T_>
 struct MidCore {
@@ -187,10 +228,8 @@ struct MidCore {
   }
   template <bool TR, bool PAIR, int NP>
   __device__ __forceinline__ void issue1(uint32_t dst, const TileOperand<NP>& o) const {
-    const uint32_t n = o.template bytes<TR>();
-    const auto rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(o.p), (short)0, (int)n, 0x00020000);
-    const auto r1 = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(PAIR ? o.p1 : o.p), (short)0,
-                                                      (int)n, 0x00020000);
+    const uint32_t n = o.template bytes<TR, T::KS>();
+    const auto rs = uniform_rsrc(o.p, n), r1 = uniform_rsrc(PAIR ? o.p1 : o.p, n);
 #pragma unroll
     for (int u = 0; u < NP; ++u)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -201,40 +240,71 @@ struct MidCore {
     const uint32_t s = s0 + stage * T::STAGE;
     issue1<T::ATR, T::PAIR>(s, a);
     issue1<T::BTR, false>(s + T::A_BYTES, b);
-    a.step();
-    b.step();
+    a.template step<T::KS>();
+    b.template step<T::KS>();
   }
-  // a tile's first loads; LDS is free from the end of the tile before it
-  __device__ __forceinline__ void begin(const TileOperand<T::PA>& a_, const TileOperand<T::PB>& b_) {
-    a = a_;
-    b = b_;
-#pragma unroll
-    for (int s = 0; s < T::ST - 1; ++s) issue(s);
+  // The operands' slices of all of a block's tiles are one stream through the ring: the
+  // next tiles' loads are in flight while a tile leaves its registers.  load() makes a,
+  // b and left (at least 1) those of the next tile of the block (false: there is none;
+  // the slices that follow are zeros).  Up to ST tiles have been loaded and not run.
+  static_assert(T::ST <= 3, "TileQueue");
+  int left, st, in;  // slices of the loading tile to come; stages of the next reads and loads
+  template <class Load>
+  __device__ __forceinline__ void next(Load& load) {
+    if (left == 0 && !load()) left = INT32_MAX;
+    issue(in);
+    in = in + 1 == T::ST ? 0 : in + 1;
+    --left;
   }
-  // acc = the tile's product over nk slices; afterwards LDS is free.  Loads past the
-  // last slice bring zeros into stages that nobody reads.
-  __device__ __forceinline__ void run(int nk, Acc& acc) {
+  template <class Load>
+  __device__ __forceinline__ void first(Load& load) {
+    left = st = in = 0;
+    a.k = a.kq = b.k = b.kq = 0;
 #pragma unroll
-    for (int i = 0; i < T::TM; ++i)
-#pragma unroll
-      for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4_t{};
-    int st = 0, in = T::ST - 1;
-    for (int g = 0; g < nk; ++g) {
-      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(NDMA * (T::ST - 2)) : "memory");
-      issue(in);
-      in = in + 1 == T::ST ? 0 : in + 1;
-      const uint32_t s = s0 + st * T::STAGE;
-      st = st + 1 == T::ST ? 0 : st + 1;
-      Frags f0, f1;
-      read(f0, s, 0);
+    for (int s = 0; s < T::ST - 1; ++s) next(load);
+  }
+  template <class Load>
+  __device__ __forceinline__ void ahead(Load&) {}
+  __device__ __forceinline__ void slice(Acc& acc) {
+    const uint32_t s = s0 + st * T::STAGE;
+    st = st + 1 == T::ST ? 0 : st + 1;
+    Frags f0, f1;
+    read(f0, s, 0);
+    if constexpr (T::KS == BK) {
       read(f1, s, 1);
       wait<OPS>(f0);
       mma(f0, acc);
       wait<0>(f1);
       mma(f1, acc);
+    } else {
+      wait<0>(f0);
+      mma(f0, acc);
     }
-    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
   }
+  // acc = the tile's product over its nk slices.  NEWER: vector-memory operations that
+  // every wavefront has issued since the last run, at least.
+  template <int NEWER = 0, class Load>
+  __device__ __forceinline__ void run(int nk, Acc& acc, Load& load) {
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < T::TN; ++j) acc[i][j] = f32x4_t{};
+    constexpr int W = NDMA * (T::ST - 2);
+    int g = 0;
+    // (the first ST - 1 slices were loaded before those operations)
+    for (; g < min(nk, T::ST - 1); ++g) {
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(W + NEWER < 63 ? W + NEWER : 63) : "memory");
+      next(load);
+      slice(acc);
+    }
+    for (; g < nk; ++g) {
+      asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(W) : "memory");
+      next(load);
+      slice(acc);
+    }
+  }
+  // before the block ends: no load may land in LDS that is no longer its own
+  __device__ __forceinline__ void last() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 };
 
 }  // namespace trimmoe

@@ -52,3 +52,42 @@ def test_no_copy_into_lds_waits_for_one_lane_at_a_time(kernels):
         for i, b in enumerate(body):
             if b.startswith("buffer_load") and b.endswith("lds"):
                 assert not any(x.startswith("s_cbranch_execnz") for x in body[i:i + 4]), (name, b)
+
+
+def _registers(operand):
+    m = re.match(r"v\[(\d+):(\d+)\]$", operand)
+    if m:
+        return set(range(int(m.group(1)), int(m.group(2)) + 1))
+    m = re.match(r"v(\d+)$", operand)
+    return {int(m.group(1))} if m else set()
+
+
+def _store_hazards(body):
+    """16-byte buffer stores with a scalar offset register whose data registers the next
+    instruction writes: the compiler takes such a pair as safe, and it is not."""
+    bad = []
+    for store, after in zip(body, body[1:]):
+        m = re.match(r"buffer_store_dwordx[34] (\S+), \S+, s\[\S+\], s\d+", store)
+        if not m or not after.startswith("v_"):
+            continue
+        operands = [x.strip() for x in after.split(None, 1)[1].split(",")]
+        written = _registers(operands[0]) | (_registers(operands[1]) if "swap" in after else set())
+        if written & _registers(m.group(1)):
+            bad.append((store, after))
+    return bad
+
+
+def test_the_hazard_check_finds_one():
+    pair = ["buffer_store_dwordx4 v[76:79], v60, s[8:11], s13 offen", "v_add_u32_e32 v76, s6, v156"]
+    assert _store_hazards(pair)
+    assert not _store_hazards([pair[0], "s_nop 0", pair[1]])
+    assert not _store_hazards([pair[0], "v_add_u32_e32 v75, s6, v76"])
+    assert not _store_hazards([pair[0].replace("s13", "0"), pair[1]])
+
+
+@pytest.mark.parametrize("source", ["expert_ffn.hip", "gemm.hip"])
+def test_stored_registers_are_not_written_at_once(source, tmp_path_factory):
+    text = _compile(tmp_path_factory, source)
+    body = [x.split(";")[0].strip() for x in text.splitlines()]
+    assert any(x.startswith("buffer_store") for x in body)
+    assert not _store_hazards([x for x in body if x])
