@@ -484,7 +484,8 @@ __global__ __launch_bounds__(big::THREADS) void k_dz_big(DzArgs a) {
             x[k][r] = p * m;
             if constexpr (BIAS) sum[i + k][r] = fmaf(g, p, sum[i + k][r]);
           }
-        __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, off, 32 * i, 0);
+        // (no scalar offset: see mfma_core.h, pack_rows)
+        __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, off + 32 * i, 0, 0);
       }
     }
     if constexpr (BIAS) {
@@ -697,14 +698,14 @@ __global__ __launch_bounds__(big::THREADS) void k_prod_big(BigProdArgs a) {
           for (int k = 0; k < 2; ++k)
 #pragma unroll
             for (int r = 0; r < 4; ++r) x[k][r] = acc[i + k][j][r] * g;
-          __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, at_i, 32 * i, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(pack_rows(x[0], x[1]), ro, at_i + 32 * i, 0, 0);
         } else {
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             f32x4_t x = acc[i + k][j];
             asm volatile("" : "+v"(x));  // through VGPRs (see big_store_partial_rows)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), ro, at_i,
-                                                   64 * (i + k), 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), ro,
+                                                   at_i + 64 * (i + k), 0, 0);
           }
         }
       }

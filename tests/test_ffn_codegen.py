@@ -85,7 +85,7 @@ def test_the_hazard_check_finds_one():
     assert not _store_hazards([pair[0].replace("s13", "0"), pair[1]])
 
 
-@pytest.mark.parametrize("source", ["expert_ffn.hip", "gemm.hip"])
+@pytest.mark.parametrize("source", ["expert_ffn.hip", "head_loss.hip", "gemm.hip"])
 def test_stored_registers_are_not_written_at_once(source, tmp_path_factory):
     text = _compile(tmp_path_factory, source)
     body = [x.split(";")[0].strip() for x in text.splitlines()]
