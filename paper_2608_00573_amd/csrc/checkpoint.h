@@ -23,10 +23,13 @@ __device__ __forceinline__ int pack_code(float v, uint32_t scale) {
   const float q = rintf(__builtin_ldexpf(v, 133 - (int)scale));
   return (int)fminf(fmaxf(q, -127.f), 127.f);
 }
-// what a code stands for
+// a block's step; NaN where it stands for no number
+__device__ __forceinline__ float pack_step(uint32_t scale) {
+  return scale == 255 ? __builtin_nanf("") : __builtin_ldexpf(1.f, (int)scale - 133);
+}
+// what a code stands for (exact: a power of two times a whole number)
 __device__ __forceinline__ float pack_value(int code, uint32_t scale) {
-  const float v = __builtin_ldexpf((float)code, (int)scale - 133);
-  return scale == 255 ? __builtin_nanf("") : v;
+  return (float)code * pack_step(scale);
 }
 
 // the larger of two magnitudes as bits (NaN the largest of all)

@@ -22,25 +22,29 @@ namespace {
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // a tile of rows times columns from c0 on; its group e (E and above: rows of no group,
-// which have no product)
+// which have no product); which piece of its K
 struct RowTile {
-  int e, r0, valid, c0;
+  int e, r0, valid, c0, piece;
   RowTile() = default;
-  __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, const TileSched& S, int j,
+  // tile L of the patch order
+  __device__ __forceinline__ RowTile(const GroupTiles& t, const Groups& g, const TileSched& S, int L,
                                      int rows, int cols) {
-    int mt, nt, sp, within;
-    S.decode(j, mt, nt, sp);
+    int mt, nt, within;
+    S.decode_abs(L, mt, nt, piece);
     e = t.group(mt, within);
     const int2 r = g.rows(e);
     r0 = uniform(r.x + within * rows);
     valid = uniform(min(rows, r.y - r0));
     c0 = uniform(nt * cols);
+    piece = uniform(piece);
   }
 };
 struct RowQueue {
-  TileQueue<4> q;
+  TileQueue<5> q;
   __device__ __forceinline__ int left() const { return q.n; }
-  __device__ __forceinline__ void push(const RowTile& t) { q.push({{t.e, t.r0, t.valid, t.c0}}); }
+  __device__ __forceinline__ void push(const RowTile& t) {
+    q.push({{t.e, t.r0, t.valid, t.c0, t.piece}});
+  }
   __device__ __forceinline__ RowTile pop() {
     const auto v = q.pop();
     RowTile t;
@@ -48,6 +52,7 @@ struct RowQueue {
     t.r0 = v.v[1];
     t.valid = v.v[2];
     t.c0 = v.v[3];
+    t.piece = v.v[4];
     return t;
   }
 };
@@ -111,14 +116,14 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
   RowQueue queue;
   auto load = [&] {
     if (jl == ntiles) return false;
-    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    const RowTile at(tiles, a.groups, S, S.tb + S.i0 + jl++ * S.bx, T::BN, T::ROWS_A);
     queue.push(at);
     const int k = at.e < a.groups.E ? a.d : 0;
     const size_t w0 = ((size_t)(k ? at.e : 0) * a.F + at.c0) * a.d;
-    tile_rows(core.a, a.w_up + w0, a.d, min(T::ROWS_A, a.F - at.c0), k, T::SPAN);
+    tile_rows<T::KS>(core.a, a.w_up + w0, a.d, min(T::ROWS_A, a.F - at.c0), k, T::SPAN);
     if constexpr (GATED) core.a.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
-    tile_rows(core.b, a.x + (size_t)at.r0 * a.d, a.d, at.valid, k);
-    core.left = max(k / BK, 1);
+    tile_rows<T::KS>(core.b, a.x + (size_t)at.r0 * a.d, a.d, at.valid, k);
+    core.left = max(k / T::KS, 1);
     return true;
   };
   constexpr int TMO = GATED ? T::TM / 2 : T::TM;  // 16-column groups of a wavefront
@@ -126,7 +131,7 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
   while (queue.left()) {
     const RowTile was = queue.pop();
     typename C::Acc acc;
-    core.run(was.e < a.groups.E ? a.d / BK : 1, acc, load);
+    core.run(was.e < a.groups.E ? a.d / T::KS : 1, acc, load);
     core.ahead(load);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
@@ -175,12 +180,35 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
 // out [n, M] = rows times weights: y = a Wd^T (Wd K-contiguous) or, ATR, dx = du Wu (+
 // dg Wg) (weights along K; the second product continues the first one's K).  Rows of no
 // group get zeros.
+// Few tiles leave CUs idle, so K is cut.  Small tiles: every tile in `splits` pieces
+// whose sums k_join_slices adds.  The large-group core: the tiles of its last, partial
+// round in as many pieces as its blocks make up (RowTail), which k_join_tail adds.
+// 8192 rows over 8 experts (4096 x 14336), 2.25 rounds of 256 tiles: y 1043 to XXX us, dx
+// 1977 to XXX; 2047 rows of 2048 x 5632, a quarter of a round: dx 230 to XXX us.
 struct RowsArgs {
   Groups groups;
   const bf16_t *w, *w2;  // expert 0; w2: NULL or the second product's
   const bf16_t *b, *b2;  // [n, K]
   int M, K;
   bf16_t* out;
+  int splits;   // small tiles
+  float* part;  // [splits][n, M], or of the tail [blocks][256][256]
+};
+
+// How the large-group core's blocks of an XCD share its tiles: `full` whole ones each,
+// and the `tiles` of the last round in `pieces` each (1: whole).  A slice takes 1.5 us, the
+// two launches that pieces need 10: short K is not cut (16384 rows over 60 experts, 22 and
+// 44 slices: 157 and 280 us, 10 more with them).
+constexpr int kTailSlices = 64;
+struct RowTail {
+  int full, tiles, pieces;
+  __device__ __forceinline__ RowTail(int total, int slices, int grid, int x, int nx) {
+    const int bx = (grid - x + nx - 1) / nx, n = total / nx + (x < total % nx ? 1 : 0);
+    full = uniform(n / bx);
+    tiles = uniform(n) - full * uniform(bx);
+    pieces = tiles == 0 || slices < kTailSlices ? 1 : uniform(min(min(bx / max(tiles, 1), 8), slices / 8));
+  }
+  __device__ __forceinline__ bool cut() const { return pieces > 1; }
 };
 
 // A tile's results, bf16, 16 bytes a lane.  Rows past `valid` lie behind the buffer's
@@ -218,50 +246,141 @@ __device__ __forceinline__ void store_tile(const C& core, const typename C::Acc&
   }
 }
 
+// the same as fp32 sums [.., ld]
 template <class C>
+__device__ __forceinline__ void store_part(const C& core, const typename C::Acc& acc, float* out, int valid,
+                                           int cols, int ld) {
+  using T = typename C::T;
+  cols = uniform(cols);
+  ld = uniform(ld);
+  asm volatile("" : "+s"(ld));
+  const __amdgpu_buffer_rsrc_t ro =
+      uniform_rsrc(reinterpret_cast<const char*>(out),
+                   uniform((int)(((uint32_t)(min(valid, T::BN) - 1) * ld + min(cols, T::BM)) * 4)));
+  const uint32_t cw = core.wm * T::WM;
+#pragma unroll
+  for (int j = 0; j < T::TN; ++j) {
+    const uint32_t off =
+        ((uint32_t)(core.wn * T::WN + 16 * j + (core.lane & 15)) * ld + cw + 4 * (core.lane >> 4)) * 4;
+#pragma unroll
+    for (int i = 0; i < T::TM; ++i) {
+      f32x4_t v = acc[i][j];
+      asm volatile("" : "+v"(v));  // (through VGPRs: see gemm.hip, big_store_partial_rows)
+      __builtin_amdgcn_raw_buffer_store_b128(
+          __builtin_bit_cast(u32x4_t, v), ro,
+          ((int)(cw + 16 * i) < cols ? off : 0xffff0000u) + 64 * i, 0, 0);
+    }
+  }
+}
+
+// PART: the pieces of cut tiles, else the whole tiles
+template <class C, bool PART>
 __global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
   using T = typename C::T;
+  constexpr bool LARGE = T::OCC == 1;
   __shared__ __align__(16) char lds[T::LDS];
   const GroupTiles tiles(a.groups, a.groups.E + 2, T::BN);
+  const int n_ct = (a.M + T::BM - 1) / T::BM, one = a.K / T::KS, slices = one * (T::ATR && a.w2 ? 2 : 1);
   TileSched S;
-  int ntiles;
-  if (!S.init(tiles.n, (a.M + T::BM - 1) / T::BM, 1, ntiles)) return;
+  int n = 0;  // the block's tiles, from index S.tb + S.i0 on
+  if (!S.init(tiles.n, n_ct, !LARGE && PART ? a.splits : 1, n)) n = 0;
+  int pieces = a.splits, piece = 0;
+  if constexpr (LARGE) {
+    const int nx = min(kXcd, (int)gridDim.x);
+    const RowTail tail(tiles.n * n_ct, slices, gridDim.x, blockIdx.x % nx, nx);
+    if (PART) {
+      if (!tail.cut()) return;
+      pieces = tail.pieces;
+      piece = uniform(S.i0 / tail.tiles);
+      n = piece < pieces ? 1 : 0;
+      S.tb += tail.full * S.bx - piece * tail.tiles;
+    } else if (tail.cut()) {
+      n = tail.full;
+    }
+  }
+  if (n == 0) return;
   C core(lds);
-  const int slices = a.K / BK * (T::ATR && a.w2 ? 2 : 1);
+  const auto from = [&](int q) {  // first slice of a piece
+    return PART ? uniform((int)((long)slices * q / pieces)) : q * slices;
+  };
   int jl = 0;
   RowQueue queue;
   auto load = [&] {
-    if (jl == ntiles) return false;
-    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    if (jl == n) return false;
+    RowTile at(tiles, a.groups, S, S.tb + S.i0 + jl++ * S.bx, T::BN, T::BM);
+    if (LARGE) at.piece = piece;
     queue.push(at);
-    const int K = at.e < a.groups.E ? a.K : 0;
+    const int K = at.e < a.groups.E ? a.K : 0, s0 = PART && K ? from(at.piece) : 0;
+    const bool second = PART && s0 >= one && s0 > 0;  // the piece begins in the second product
+    const int k0 = (second ? s0 - one : s0) * T::KS, k = max(K - k0, 0);
     const size_t e0 = K ? (size_t)at.e * a.M * a.K : 0, b0 = (size_t)at.r0 * a.K;
+    const bf16_t* w = second ? a.w2 : a.w;
     if constexpr (T::ATR)
-      tile_along<T::BM>(core.a, a.w + e0, a.M, at.c0, K);
+      tile_along<T::BM, T::KS>(core.a, w + e0 + (size_t)k0 * a.M, a.M, at.c0, k);
     else
-      tile_rows(core.a, a.w + e0 + (size_t)at.c0 * a.K, a.K, min(T::BM, a.M - at.c0), K);
-    tile_rows(core.b, a.b + b0, a.K, at.valid, K);
-    if (T::ATR && a.w2) {
+      tile_rows<T::KS>(core.a, w + e0 + (size_t)at.c0 * a.K + k0, a.K, min(T::BM, a.M - at.c0), k);
+    tile_rows<T::KS>(core.b, (second ? a.b2 : a.b) + b0 + k0, a.K, at.valid, k);
+    if (T::ATR && a.w2 && !second) {
       core.a.q = reinterpret_cast<const char*>(a.w2 + e0 + at.c0);
       core.b.q = reinterpret_cast<const char*>(a.b2 + b0);
       core.a.kq = core.b.kq = K;
     }
-    core.left = K ? slices : 1;
+    core.left = K ? from(at.piece + 1) - s0 : 1;
     return true;
   };
   core.first(load);
   for (bool stored = false; queue.left(); stored = true) {
     const RowTile was = queue.pop();
     typename C::Acc acc;
-    const int nk = was.e < a.groups.E ? slices : 1;
-    if (stored)
+    const int nk = was.e < a.groups.E ? from(was.piece + 1) - from(was.piece) : 1;
+    if (stored && !PART)
       core.template run<STORES<C>>(nk, acc, load);
     else
       core.run(nk, acc, load);
     core.ahead(load);
-    store_tile(core, acc, a.out, was.r0, was.valid, was.c0, a.M);
+    if constexpr (!PART)
+      store_tile(core, acc, a.out, was.r0, was.valid, was.c0, a.M);
+    else if constexpr (LARGE)
+      store_part(core, acc, a.part + (size_t)blockIdx.x * T::BM * T::BN, was.valid, a.M - was.c0, T::BM);
+    else
+      store_part(core, acc, a.part + ((size_t)was.piece * a.groups.n + was.r0) * a.M + was.c0, was.valid,
+                 a.M - was.c0, a.M);
   }
   core.last();
+}
+
+// 8 results, 16 bytes, from the sums of their pieces
+__device__ __forceinline__ void join8(const float* p, size_t step, int pieces, bf16_t* out) {
+  f32x4_t x = *reinterpret_cast<const f32x4_t*>(p), y = *reinterpret_cast<const f32x4_t*>(p + 4);
+  for (int i = 1; i < pieces; ++i) {
+    x += *reinterpret_cast<const f32x4_t*>(p + i * step);
+    y += *reinterpret_cast<const f32x4_t*>(p + i * step + 4);
+  }
+  *reinterpret_cast<u32x4_t*>(out) = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                             pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
+}
+
+// The tail's tiles, 32 rows a block; grid.x as k_expert_rows had it
+__global__ __launch_bounds__(256) void k_join_tail(RowsArgs a, int slices) {
+  const GroupTiles tiles(a.groups, a.groups.E + 2, big::BN);
+  const int n_ct = (a.M + big::BM - 1) / big::BM, nx = min(kXcd, (int)gridDim.x), x = blockIdx.x % nx;
+  TileSched S;
+  int ntiles;
+  S.init(tiles.n, n_ct, 1, ntiles);
+  const RowTail tail(tiles.n * n_ct, slices, gridDim.x, x, nx);
+  if (!tail.cut() || S.i0 >= tail.tiles) return;
+  const RowTile at(tiles, a.groups, S, S.tb + tail.full * S.bx + S.i0, big::BN, big::BM);
+  constexpr size_t SLOT = (size_t)big::BM * big::BN;
+  const int c = 8 * (threadIdx.x & 31);
+  for (int r = 32 * blockIdx.y + (threadIdx.x >> 5); r < 32 * ((int)blockIdx.y + 1); r += 8)
+    if (r < at.valid && at.c0 + c < a.M)
+      join8(a.part + (size_t)blockIdx.x * SLOT + r * big::BM + c, (size_t)nx * tail.tiles * SLOT,
+            tail.pieces, a.out + (size_t)(at.r0 + r) * a.M + at.c0 + c);
+}
+
+__global__ __launch_bounds__(256) void k_join_slices(const float* part, int splits, size_t n, bf16_t* out) {
+  const size_t i = 8 * ((size_t)blockIdx.x * 256 + threadIdx.x);
+  if (i < n) join8(part + i, n, splits, out + i);
 }
 
 // --------------------------------------------------------------- backward --
@@ -274,22 +393,43 @@ struct DactArgs {
   bf16_t *a, *du, *dg;  // [n, F]
 };
 
-// 4 consecutive kept values, from element o on
-template <bool PACKED>
-__device__ __forceinline__ void kept4(float (&v)[4], const void* p, const uint8_t* scale, size_t o) {
-  if constexpr (PACKED) {
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(static_cast<const int8_t*>(p) + o);
-    const uint32_t s = scale[o / kPackBlock];
+// What was kept of one row of a tile: a lane's 4 consecutive columns of each 16.  All of a
+// row's loads go out together, and the next row's before this one is used.
+template <int TM, bool GATED, bool PACKED>
+struct KeptRow {
+  typedef std::conditional_t<PACKED, uint32_t, uint2> W;
+  W u[TM], g[GATED ? TM : 1];
+  uint8_t us[TM / 2], gs[TM / 2];
+  // (columns past F: the row's first ones, unused)
+  __device__ __forceinline__ void load(const DactArgs& a, size_t row, int c0, int lane) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = pack_value((int8_t)(w >> (8 * r)), s);
-  } else {
-    const uint2 w = *reinterpret_cast<const uint2*>(static_cast<const bf16_t*>(p) + o);
-    v[0] = bf2f((bf16_t)w.x);
-    v[1] = bf2f((bf16_t)(w.x >> 16));
-    v[2] = bf2f((bf16_t)w.y);
-    v[3] = bf2f((bf16_t)(w.y >> 16));
+    for (int i = 0; i < TM; ++i) {
+      const int c = c0 + 16 * i < a.F ? c0 + 16 * i : 16 * (i & 1);
+      const size_t o = row * a.F + c + 4 * (lane >> 4);
+      constexpr int ES = PACKED ? 1 : 2;
+      u[i] = *reinterpret_cast<const W*>(static_cast<const char*>(a.up) + o * ES);
+      if constexpr (GATED) g[i] = *reinterpret_cast<const W*>(static_cast<const char*>(a.gate) + o * ES);
+      if (PACKED && i % 2 == 0) {
+        us[i / 2] = a.up_scale[o / kPackBlock];
+        if constexpr (GATED) gs[i / 2] = a.gate_scale[o / kPackBlock];
+      }
+    }
   }
-}
+  static __device__ __forceinline__ void values(float (&v)[4], const W& w, uint32_t s) {
+    if constexpr (PACKED) {
+      // (code + 128) step - 128 step, exact: the unsigned bytes convert in one step each
+      const float step = pack_step(s);
+      const uint32_t b = w ^ 0x80808080u;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] = fmaf((float)(b >> (8 * r) & 0xff), step, -128.f * step);
+    } else {
+      v[0] = __uint_as_float(w.x << 16);
+      v[1] = __uint_as_float(w.x & 0xffff0000u);
+      v[2] = __uint_as_float(w.y << 16);
+      v[3] = __uint_as_float(w.y & 0xffff0000u);
+    }
+  }
+};
 
 template <class C, bool GATED, bool PACKED>
 __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
@@ -304,36 +444,43 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
   RowQueue queue;
   auto load = [&] {
     if (jl == ntiles) return false;
-    const RowTile at(tiles, a.groups, S, jl++, T::BN, T::ROWS_A);
+    const RowTile at(tiles, a.groups, S, S.tb + S.i0 + jl++ * S.bx, T::BN, T::ROWS_A);
     queue.push(at);
-    tile_along<T::BM>(core.a, a.w_down + (size_t)at.e * a.d * a.F, a.F, at.c0, a.d);
-    tile_rows(core.b, a.dy + (size_t)at.r0 * a.d, a.d, at.valid, a.d);
-    core.left = a.d / BK;
+    tile_along<T::BM, T::KS>(core.a, a.w_down + (size_t)at.e * a.d * a.F, a.F, at.c0, a.d);
+    tile_rows<T::KS>(core.b, a.dy + (size_t)at.r0 * a.d, a.d, at.valid, a.d);
+    core.left = a.d / T::KS;
     return true;
   };
   core.first(load);
   while (queue.left()) {
     const RowTile was = queue.pop();
     typename C::Acc acc;
-    core.run(a.d / BK, acc, load);
+    core.run(a.d / T::KS, acc, load);
+    const int c0 = was.c0 + core.wm * T::WM;
+    const auto row_of = [&](int j) { return core.wn * T::WN + 16 * j + (core.lane & 15); };
+    KeptRow<T::TM, GATED, PACKED> kept[2];
+    const auto fetch = [&](int j) {
+      kept[j & 1].load(a, (size_t)(was.r0 + min(row_of(j), was.valid - 1)), c0, core.lane);
+    };
+    // (the first before the next tile's loads, which it would wait for behind them)
+    fetch(0);
     core.ahead(load);
 #pragma unroll
     for (int j = 0; j < T::TN; ++j) {
-      const int t = core.wn * T::WN + 16 * j + (core.lane & 15);
+      if (j + 1 < T::TN) fetch(j + 1);
+      const int t = row_of(j);
+      const auto& kj = kept[j & 1];
 #pragma unroll
       for (int i = 0; i < T::TM; i += 2) {
-        const int c = was.c0 + core.wm * T::WM + 16 * i;
+        const int c = c0 + 16 * i;
         const bool in = t < was.valid && c < a.F;
         const size_t o = (size_t)(was.r0 + t) * a.F + c;
         float va[2][4], vu[2][4], vg[2][4];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          float u[4] = {}, g[4] = {};
-          if (in) {
-            const size_t ok = o + 16 * k + 4 * (core.lane >> 4);
-            kept4<PACKED>(u, a.up, a.up_scale, ok);
-            if constexpr (GATED) kept4<PACKED>(g, a.gate, a.gate_scale, ok);
-          }
+          float u[4], g[4];
+          kj.values(u, kj.u[i + k], kj.us[i / 2]);
+          if constexpr (GATED) kj.values(g, kj.g[i + k], kj.gs[i / 2]);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const float da = acc[i + k][j][r];
@@ -434,16 +581,35 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a)
 // How the rows are cut: kFew 32-row tiles (groups of up to that many rows on average),
 // kMid 128-row tiles, kLarge the large-group core's 256.
 enum Rows { kFew, kMid, kLarge };
-Rows rows_kind(const Groups& g) {
+Rows rows_kind(const Groups& g, long large) {
   if ((long)g.n <= 32l * g.E) return kFew;
-  return (long)g.n >= 512l * g.E ? kLarge : kMid;
+  return (long)g.n >= large * g.E ? kLarge : kMid;
 }
+constexpr long kLargeRows = 256, kLargeDactRows = 512;
 
 template <int KIND, bool ATR, bool BTR, bool PAIR = false>
 using CoreOf = std::conditional_t<
     KIND == kLarge, BigCore<BigTile<ATR, BTR, PAIR>>,
     std::conditional_t<KIND == kMid, MidCore<MidTile<128, 128, 2, ATR, BTR, PAIR>>,
                        MidCore<MidTile<128, 32, 3, ATR, BTR, PAIR>>>>;
+
+// pieces of K of small tiles of the rows' products (M columns, `slices` of K): as many as
+// two blocks a CU take at once, of 8 slices at least
+int row_splits(const Groups& g, int M, int slices) {
+  const Rows kind = rows_kind(g, kLargeRows);
+  if (kind == kLarge) return 1;
+  const int tile = kind == kFew ? 32 : 128;
+  const long tiles = std::max(1l, ((long)g.n / tile + std::min(g.E, g.n)) * cdiv(M, 128));
+  return (int)std::max(1l, std::min({512 / tiles, (long)slices / 8, 8l}));
+}
+// bytes of the pieces' sums
+constexpr int kTailBlocks = 256;
+size_t row_parts(const Groups& g, int M, int slices) {
+  if (rows_kind(g, kLargeRows) == kLarge)
+    return slices < kTailSlices ? 0 : (size_t)kTailBlocks * big::BM * big::BN * 4;
+  const int s = row_splits(g, M, slices);
+  return s > 1 ? ffn_align((size_t)s * g.n * M * 4) : 0;
+}
 
 // f(integral constant of the kind)
 template <typename F>
@@ -462,30 +628,56 @@ template <class C>
 dim3 grid_of(long tiles, int n_cu) {
   return dim3((unsigned)std::min(std::max(tiles, 1l), (long)n_cu * C::T::OCC));
 }
+// ... over row tiles, which take long enough that the hardware deals them out: a block
+// each (but on the large-group core, whose blocks load their next tile early).  16383 rows
+// over 60 experts (2048 x 1408): 466 us, with blocks that stay 480
 template <class C>
 dim3 rows_grid(const Groups& g, int cols, int n_cu) {
-  return grid_of<C>(row_tiles_most(g.n, g.E, C::T::BN) * cdiv(cols, C::T::ROWS_A), n_cu);
+  const long tiles = row_tiles_most(g.n, g.E, C::T::BN) * cdiv(cols, C::T::ROWS_A);
+  return C::T::OCC == 1 ? grid_of<C>(tiles, n_cu) : dim3((unsigned)std::min(tiles, 1l << 20));
 }
 
 template <bool GATED, int KEEP>
 hipError_t launch_up(const UpArgs& a, int n_cu, hipStream_t st) {
-  return with_kind(rows_kind(a.groups), [&](auto kind) {
+  return with_kind(rows_kind(a.groups, kLargeRows), [&](auto kind) {
     using C = CoreOf<kind, false, false, GATED>;
     hipLaunchKernelGGL((k_expert_up<C, GATED, KEEP>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st, a);
   });
 }
 
 template <bool ATR>
-hipError_t launch_rows(const RowsArgs& a, int n_cu, hipStream_t st) {
-  return with_kind(rows_kind(a.groups), [&](auto kind) {
+hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
+  const int slices = a.K / BK * (a.w2 ? 2 : 1);
+  const Rows kind = rows_kind(a.groups, kLargeRows);
+  a.splits = row_splits(a.groups, a.M, slices);
+  a.part = reinterpret_cast<float*>(part);
+  unsigned blocks = 0;
+  hipError_t e = with_kind(kind, [&](auto kind) {
     using C = CoreOf<kind, ATR, false>;
-    hipLaunchKernelGGL((k_expert_rows<C>), rows_grid<C>(a.groups, a.M, n_cu), dim3(256), 0, st, a);
+    dim3 grid = rows_grid<C>(a.groups, a.M, n_cu);
+    if (kind == kLarge)
+      grid.x = std::min(n_cu, kTailBlocks);
+    else
+      grid.x = std::min(grid.x * a.splits, 1u << 20);
+    blocks = grid.x;
+    if (kind == kLarge || a.splits == 1)
+      hipLaunchKernelGGL((k_expert_rows<C, false>), grid, dim3(256), 0, st, a);
+    if (kind == kLarge ? slices >= kTailSlices : a.splits > 1)
+      hipLaunchKernelGGL((k_expert_rows<C, true>), grid, dim3(256), 0, st, a);
   });
+  if (e != hipSuccess) return e;
+  const size_t n = (size_t)a.groups.n * a.M;
+  if (kind == kLarge && slices >= kTailSlices)
+    hipLaunchKernelGGL(k_join_tail, dim3(blocks, big::BN / 32), dim3(256), 0, st, a, slices);
+  else if (kind != kLarge && a.splits > 1)
+    hipLaunchKernelGGL(k_join_slices, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, a.part,
+                       a.splits, n, a.out);
+  return hipGetLastError();
 }
 
 template <bool GATED, bool PACKED>
 hipError_t launch_dact(const DactArgs& a, int n_cu, hipStream_t st) {
-  return with_kind(rows_kind(a.groups), [&](auto kind) {
+  return with_kind(rows_kind(a.groups, kLargeDactRows), [&](auto kind) {
     using C = CoreOf<kind, true, false>;
     hipLaunchKernelGGL((k_expert_dact<C, GATED, PACKED>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st,
                        a);
@@ -493,16 +685,11 @@ hipError_t launch_dact(const DactArgs& a, int n_cu, hipStream_t st) {
 }
 
 hipError_t launch_weights(const WeightArgs& a, int n_cu, hipStream_t st) {
-  const Rows kind = rows_kind(a.groups) == kLarge ? kLarge : kMid;
-  return with_kind(kind, [&](auto k) {
-    if constexpr (k != kFew) {
-      using C = std::conditional_t<k == kLarge, CoreOf<k, true, true>,
-                                   MidCore<MidTile<256, 128, 3, true, true, false, 32, 2>>>;
-      long tiles = 0;
-      for (int p = 0; p < a.n_prod; ++p) tiles += (long)cdiv(a.M[p], C::T::BM) * cdiv(a.N[p], C::T::BN);
-      hipLaunchKernelGGL((k_expert_weights<C>), grid_of<C>(tiles * a.groups.E, n_cu), dim3(256), 0, st, a);
-    }
-  });
+  using C = MidCore<MidTile<256, 128, 3, true, true, false, 32>>;
+  long tiles = 0;
+  for (int p = 0; p < a.n_prod; ++p) tiles += (long)cdiv(a.M[p], C::T::BM) * cdiv(a.N[p], C::T::BN);
+  hipLaunchKernelGGL((k_expert_weights<C>), grid_of<C>(tiles * a.groups.E, n_cu), dim3(256), 0, st, a);
+  return hipGetLastError();
 }
 
 const bf16_t* as_bf16(const void* p) { return static_cast<const bf16_t*>(p); }
@@ -511,13 +698,15 @@ const bf16_t* as_bf16(const void* p) { return static_cast<const bf16_t*>(p); }
 
 size_t expert_ffn_ws(bool bf16, bool gated, int keep, int E, int d, int F, int n) {
   const size_t act = ffn_array(n, F, bf16 ? 2 : 4);
+  if (bf16) return act + row_parts(Groups{nullptr, E, n}, d, F / BK);
   // (fp32 pre-activations are packed by a launch of their own)
-  return act + (!bf16 && keep == TRIMMOE_KEEP_PACKED ? (gated ? 2 : 1) * act : 0);
+  return act + (keep == TRIMMOE_KEEP_PACKED ? (gated ? 2 : 1) * act : 0);
 }
 
 size_t expert_ffn_backward_ws(bool bf16, bool gated, bool x_packed, int E, int d, int F, int n) {
   const int elem = bf16 ? 2 : 4;
-  return (gated ? 3 : 2) * ffn_array(n, F, elem) + (x_packed ? ffn_array(n, d, elem) : 0);
+  return (gated ? 3 : 2) * ffn_array(n, F, elem) + (x_packed ? ffn_array(n, d, elem) : 0) +
+         (bf16 ? row_parts(Groups{nullptr, E, n}, d, F / BK * (gated ? 2 : 1)) : 0);
 }
 
 hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
@@ -553,7 +742,7 @@ hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
   r.M = a.d;
   r.K = a.F;
   r.out = static_cast<bf16_t*>(a.y);
-  return launch_rows<false>(r, a.n_cu, st);
+  return launch_rows<false>(r, a.ws + ffn_array(a.groups.n, a.F, 2), a.n_cu, st);
 }
 
 hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
@@ -598,7 +787,8 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
       r.M = a.d;
       r.K = a.F;
       r.out = static_cast<bf16_t*>(a.dx);
-      if ((e = launch_rows<true>(r, a.n_cu, st)) != hipSuccess) return e;
+      char* part = a.ws + (a.gated ? 3 : 2) * act + (a.x_scale ? ffn_array(n, a.d, 2) : 0);
+      if ((e = launch_rows<true>(r, part, a.n_cu, st)) != hipSuccess) return e;
     }
   }
   WeightArgs w{};

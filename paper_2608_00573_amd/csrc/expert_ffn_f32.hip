@@ -12,58 +12,90 @@ namespace trimmoe {
 
 namespace {
 
-using F32T = F32Tile<f32p::kSquare>;
-using F32S = f32p::Tile<f32p::kSquare>;
-
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // the block's tile: a group's rows r0 .. (e >= E: rows of no group) times columns from m0
+template <int KIND>
 struct F32At {
+  using T = f32p::Tile<KIND>;
   int e, r0, end, m0;
   // false: no such tile
   __device__ __forceinline__ bool init(const Groups& g, int slots, int M) {
-    const GroupTiles t(g, slots, F32S::B);
-    const int n_m = (M + F32S::A - 1) / F32S::A;
+    const GroupTiles t(g, slots, T::B);
+    const int n_m = (M + T::A - 1) / T::A;
     const int mt = blockIdx.x / n_m;
     if (mt >= t.n) return false;
-    m0 = (int)(blockIdx.x % n_m) * F32S::A;
+    m0 = (int)(blockIdx.x % n_m) * T::A;
     int within;
     e = t.group(mt, within);
     const int2 r = g.rows(e);
-    r0 = uniform(r.x + within * F32S::B);
+    r0 = uniform(r.x + within * T::B);
     end = uniform(r.y);
     return true;
   }
 };
 
-// f(row, column, values, how many of the four) for what a lane holds of the tile
-template <typename F>
-__device__ __forceinline__ void each(const F32T& t, int rows, int cols, F f) {
+// A tile's sums, zero to begin with.  AK: whether A is K-contiguous; a stream of an A
+// that is not mixes the rows of A of its groups (see f32_stream_of), in whole runs.
+template <int KIND, bool AK>
+struct F32Sums : F32Tile<KIND> {
+  using T = f32p::Tile<KIND>;
+  static constexpr bool MIXED = T::STREAM && !AK;
+  __device__ __forceinline__ F32Sums(const F32At<KIND>& at, int M)
+      : F32Tile<KIND>(at.m0, M, at.r0, at.end) {
+    if (MIXED) this->a = at.m0 + 16 * T::NA * uniform(threadIdx.x >> 6);
 #pragma unroll
-  for (int j = 0; j < F32S::NB; ++j) {
+    for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+      for (int j = 0; j < T::NB; ++j) this->acc[i][j] = f32x4_t{};
+  }
+};
+
+// f(row, column, how many, take) for each run of a lane's elements of a tile (rows, cols:
+// the ends of both); take(sums, v) gives the run's values of a tile's sums
+template <class S, typename F>
+__device__ __forceinline__ void each(const S& t, int rows, int cols, F f) {
+  using T = typename S::T;
+#pragma unroll
+  for (int j = 0; j < T::NB; ++j) {
     const int b = t.row_b(j);
     if (j >= t.nb || b >= rows) continue;
+    if constexpr (S::MIXED) {
 #pragma unroll
-    for (int i = 0; i < F32S::NA; ++i) {
-      const int c = t.row_a(i, 0);
-      if (i >= t.na || c >= cols) continue;
-      f(i, j, b, c, min(4, cols - c));
+      for (int r = 0; r < 4; ++r) {
+        // elements `at` .. at + NA - 1; those before c are another lane's
+        const int c = t.a + T::NA * (4 * ((threadIdx.x & 63) >> 4) + r);
+        if (c >= cols) continue;
+        const int skip = c - min(c, cols - T::NA);
+        f(b, c, T::NA - skip, [&](const S& s, float(&v)[4]) {
+#pragma unroll
+          for (int i = 0; i < T::NA; ++i)
+#pragma unroll
+            for (int k = 0; k <= i; ++k)
+              if (k == i - skip) v[k] = s.acc[i][j][r];
+        });
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < T::NA; ++i) {
+        const int c = t.row_a(i, 0);
+        if (i >= t.na || c >= cols) continue;
+        f(b, c, min(4, cols - c), [&](const S& s, float(&v)[4]) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = s.acc[i][j][r];
+        });
+      }
     }
   }
-}
-
-__device__ __forceinline__ void zero_tile(F32T& t) {
-#pragma unroll
-  for (int i = 0; i < F32S::NA; ++i)
-#pragma unroll
-    for (int j = 0; j < F32S::NB; ++j) t.acc[i][j] = f32x4_t{};
 }
 
 __device__ __forceinline__ void put4(float* p, const float (&v)[4], int n) {
   if (n == 4) {
     *reinterpret_cast<f32x4_any*>(p) = f32x4_any{v[0], v[1], v[2], v[3]};
   } else {
-    for (int r = 0; r < n; ++r) p[r] = v[r];
+#pragma unroll
+    for (int r = 0; r < 3; ++r)
+      if (r < n) p[r] = v[r];
   }
 }
 
@@ -74,31 +106,28 @@ struct F32Up {
   float *a, *up, *gate;  // up, gate: NULL or [n, F]
 };
 
-template <bool GATED>
+template <int KIND, bool GATED>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_up_f32(F32Up a) {
-  __shared__ __align__(16) float lds[F32S::FLOATS];
-  F32At at;
+  __shared__ __align__(16) float lds[f32p::Tile<KIND>::FLOATS];
+  F32At<KIND> at;
   if (!at.init(a.groups, a.groups.E + 2, a.F)) return;
-  F32T u(at.m0, a.F, at.r0, at.end), g(at.m0, a.F, at.r0, at.end);
-  zero_tile(u);
-  zero_tile(g);
+  F32Sums<KIND, true> u(at, a.F), g(at, a.F);
   if (at.e < a.groups.E) {
     const size_t w0 = (size_t)at.e * a.F * a.d;
     const Operand<true> x{a.x, (size_t)a.d, at.end, a.d};
-    f32_tile<f32p::kSquare>(Operand<true>{a.w_up + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d,
-                            lds, u);
+    f32_product<KIND>(Operand<true>{a.w_up + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d, lds, u);
     if constexpr (GATED)
-      f32_tile<f32p::kSquare>(Operand<true>{a.w_gate + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0,
-                              a.d, lds, g);
+      f32_product<KIND>(Operand<true>{a.w_gate + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d, lds,
+                        g);
   }
-  each(u, at.end, a.F, [&](int i, int j, int row, int c, int n) {
+  each(u, at.end, a.F, [&](int row, int c, int n, auto take) {
     const size_t o = (size_t)row * a.F + c;
-    float vu[4], vg[4], va[4];
+    float vu[4] = {}, vg[4] = {}, va[4];
+    take(u, vu);
+    if constexpr (GATED) take(g, vg);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      vu[r] = u.acc[i][j][r];
       if constexpr (GATED) {
-        vg[r] = g.acc[i][j][r];
         va[r] = vg[r] / (1.f + expf(-vg[r])) * vu[r];
       } else {
         va[r] = vu[r] < 0.f ? 0.f : vu[r];  // (NaN stays)
@@ -118,27 +147,26 @@ struct F32Rows {
   float* out;
 };
 
-template <bool AK, bool TWO>
+template <int KIND, bool AK, bool TWO>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a) {
-  __shared__ __align__(16) float lds[F32S::FLOATS];
-  F32At at;
+  __shared__ __align__(16) float lds[f32p::Tile<KIND>::FLOATS];
+  F32At<KIND> at;
   if (!at.init(a.groups, a.groups.E + 2, a.M)) return;
-  F32T t(at.m0, a.M, at.r0, at.end), t2(at.m0, a.M, at.r0, at.end);
-  zero_tile(t);
-  zero_tile(t2);
+  F32Sums<KIND, AK> t(at, a.M), t2(at, a.M);
   if (at.e < a.groups.E) {
     const size_t w0 = (size_t)at.e * a.M * a.K, ld = AK ? a.K : a.M;
-    f32_tile<f32p::kSquare>(Operand<AK>{a.w + w0, ld, a.M, a.K},
-                            Operand<true>{a.b, (size_t)a.K, at.end, a.K}, at.m0, at.r0, 0, a.K, lds, t);
+    f32_product<KIND>(Operand<AK>{a.w + w0, ld, a.M, a.K}, Operand<true>{a.b, (size_t)a.K, at.end, a.K},
+                      at.m0, at.r0, 0, a.K, lds, t);
     if constexpr (TWO)
-      f32_tile<f32p::kSquare>(Operand<AK>{a.w2 + w0, ld, a.M, a.K},
-                              Operand<true>{a.b2, (size_t)a.K, at.end, a.K}, at.m0, at.r0, 0, a.K, lds,
-                              t2);
+      f32_product<KIND>(Operand<AK>{a.w2 + w0, ld, a.M, a.K}, Operand<true>{a.b2, (size_t)a.K, at.end, a.K},
+                        at.m0, at.r0, 0, a.K, lds, t2);
   }
-  each(t, at.end, a.M, [&](int i, int j, int row, int c, int n) {
-    float v[4];
+  each(t, at.end, a.M, [&](int row, int c, int n, auto take) {
+    float v[4] = {}, v2[4] = {};
+    take(t, v);
+    if constexpr (TWO) take(t2, v2);
 #pragma unroll
-    for (int r = 0; r < 4; ++r) v[r] = TWO ? t.acc[i][j][r] + t2.acc[i][j][r] : t.acc[i][j][r];
+    for (int r = 0; r < 4; ++r) v[r] = TWO ? v[r] + v2[r] : v[r];
     put4(a.out + (size_t)row * a.M + c, v, n);
   });
 }
@@ -162,22 +190,22 @@ __device__ __forceinline__ float kept(const void* p, const uint8_t* scale, int b
     return static_cast<const float*>(p)[o];
 }
 
-template <bool GATED, bool PACKED>
+template <int KIND, bool GATED, bool PACKED>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_dact_f32(F32Dact a) {
-  __shared__ __align__(16) float lds[F32S::FLOATS];
-  F32At at;
+  __shared__ __align__(16) float lds[f32p::Tile<KIND>::FLOATS];
+  F32At<KIND> at;
   if (!at.init(a.groups, a.groups.E, a.F)) return;
-  F32T t(at.m0, a.F, at.r0, at.end);
-  f32_tile<f32p::kSquare>(
-      Operand<false>{a.w_down + (size_t)at.e * a.d * a.F, (size_t)a.F, a.F, a.d},
-      Operand<true>{a.dy, (size_t)a.d, at.end, a.d}, at.m0, at.r0, 0, a.d, lds, t);
+  F32Sums<KIND, false> t(at, a.F);
+  f32_product<KIND>(Operand<false>{a.w_down + (size_t)at.e * a.d * a.F, (size_t)a.F, a.F, a.d},
+                    Operand<true>{a.dy, (size_t)a.d, at.end, a.d}, at.m0, at.r0, 0, a.d, lds, t);
   const int blocks = (a.F + kPackBlock - 1) / kPackBlock;
-  each(t, at.end, a.F, [&](int i, int j, int row, int c, int n) {
-    float va[4], vu[4], vg[4];
+  each(t, at.end, a.F, [&](int row, int c, int n, auto take) {
+    float vd[4] = {}, va[4], vu[4], vg[4];
+    take(t, vd);
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int cr = min(c + r, a.F - 1);
-      const float da = t.acc[i][j][r], u = kept<PACKED>(a.up, a.up_scale, blocks, a.F, row, cr);
+      const int cr = min(c + min(r, n - 1), a.F - 1);
+      const float da = vd[r], u = kept<PACKED>(a.up, a.up_scale, blocks, a.F, row, cr);
       if constexpr (GATED) {
         const float g = kept<PACKED>(a.gate, a.gate_scale, blocks, a.F, row, cr);
         const float s = 1.f / (1.f + expf(-g)), gs = g * s;
@@ -206,33 +234,47 @@ struct F32Weights {
 
 // blockIdx.y: product, z: group; x: tile
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_weights_f32(F32Weights a) {
-  __shared__ __align__(16) float lds[F32S::FLOATS];
+  using T = f32p::Tile<f32p::kSquare>;
+  __shared__ __align__(16) float lds[T::FLOATS];
   const int p = blockIdx.y, e = blockIdx.z;
   const int M = p == 0 ? a.M[0] : p == 1 ? a.M[1] : a.M[2];
   const int N = p == 0 ? a.N[0] : p == 1 ? a.N[1] : a.N[2];
   const float* A = p == 0 ? a.A[0] : p == 1 ? a.A[1] : a.A[2];
   const float* B = p == 0 ? a.B[0] : p == 1 ? a.B[1] : a.B[2];
   float* out = (p == 0 ? a.out[0] : p == 1 ? a.out[1] : a.out[2]) + (size_t)e * M * N;
-  const int n_m = (M + F32S::A - 1) / F32S::A;
-  const int m0 = (int)(blockIdx.x % n_m) * F32S::A, n0 = (int)(blockIdx.x / n_m) * F32S::B;
+  const int n_m = (M + T::A - 1) / T::A;
+  const int m0 = (int)(blockIdx.x % n_m) * T::A, n0 = (int)(blockIdx.x / n_m) * T::B;
   if (n0 >= N) return;
   const int2 r = a.groups.rows(e);
   const int r0 = uniform(r.x), k = uniform(r.y) - r0;
-  F32T t(m0, M, n0, N);
-  zero_tile(t);
+  F32Sums<f32p::kSquare, false> t({e, n0, N, m0}, M);
   if (k > 0)
     f32_tile<f32p::kSquare>(Operand<false>{A + (size_t)r0 * M, (size_t)M, M, k},
                             Operand<false>{B + (size_t)r0 * N, (size_t)N, N, k}, m0, n0, 0, k, lds, t);
-  each(t, N, M, [&](int i, int j, int row, int c, int n) {
-    float v[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = t.acc[i][j][q];
+  each(t, N, M, [&](int row, int c, int n, auto take) {
+    float v[4] = {};
+    take(t, v);
     put4(out + (size_t)row * M + c, v, n);
   });
 }
 
-unsigned tiles_of(const Groups& g, int M) {
-  return (unsigned)(row_tiles_most(g.n, g.E, F32S::B) * cdiv(M, F32S::A));
+template <int KIND>
+dim3 tiles_of(const Groups& g, int M) {
+  using T = f32p::Tile<KIND>;
+  return dim3((unsigned)(row_tiles_most(g.n, g.E, T::B) * cdiv(M, T::A)));
+}
+// f(integral constant of the tiles' kind) for rows times M columns: 128 x 128 tiles, or
+// 128 columns x 32 rows straight from memory where those leave CUs idle (a lane's loads
+// of an operand along K take two columns at least)
+template <typename F>
+hipError_t with_tiles(const Groups& g, int M, F f) {
+  using T = f32p::Tile<f32p::kSquare>;
+  const long tiles = ((long)g.n / T::B + std::min(g.E, g.n)) * cdiv(M, T::A);
+  if (tiles < 256 && M >= 2)
+    f(std::integral_constant<int, f32p::kSmall>());
+  else
+    f(std::integral_constant<int, f32p::kSquare>());
+  return hipGetLastError();
 }
 const float* as_f32(const void* p) { return static_cast<const float*>(p); }
 
@@ -251,20 +293,23 @@ hipError_t launch_expert_ffn_f32(const ExpertFfnArgs& a, hipStream_t st) {
     u.up = static_cast<float*>(a.up);
     u.gate = static_cast<float*>(a.gate);
   }
-  const dim3 grid(tiles_of(a.groups, a.F)), block(f32p::THREADS);
-  if (a.gated)
-    hipLaunchKernelGGL(k_expert_up_f32<true>, grid, block, 0, st, u);
-  else
-    hipLaunchKernelGGL(k_expert_up_f32<false>, grid, block, 0, st, u);
-  hipError_t e = hipGetLastError();
+  const dim3 block(f32p::THREADS);
+  hipError_t e = with_tiles(a.groups, a.F, [&](auto kind) {
+    const dim3 grid = tiles_of<kind>(a.groups, a.F);
+    if (a.gated)
+      hipLaunchKernelGGL((k_expert_up_f32<kind, true>), grid, block, 0, st, u);
+    else
+      hipLaunchKernelGGL((k_expert_up_f32<kind, false>), grid, block, 0, st, u);
+  });
   if (e == hipSuccess && packed)
     e = launch_checkpoint_pack(false, n, a.F, u.up, static_cast<int8_t*>(a.up), a.up_scale, st);
   if (e == hipSuccess && packed && a.gated)
     e = launch_checkpoint_pack(false, n, a.F, u.gate, static_cast<int8_t*>(a.gate), a.gate_scale, st);
   if (e != hipSuccess) return e;
   const F32Rows r{a.groups, as_f32(a.w_down), nullptr, u.a, nullptr, a.d, a.F, static_cast<float*>(a.y)};
-  hipLaunchKernelGGL((k_expert_rows_f32<true, false>), dim3(tiles_of(a.groups, a.d)), block, 0, st, r);
-  return hipGetLastError();
+  return with_tiles(a.groups, a.d, [&](auto kind) {
+    hipLaunchKernelGGL((k_expert_rows_f32<kind, true, false>), tiles_of<kind>(a.groups, a.d), block, 0, st, r);
+  });
 }
 
 hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st) {
@@ -278,16 +323,18 @@ hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st
   const float* x = as_f32(a.x);
   hipError_t e;
   if (n > 0) {
-    const dim3 grid(tiles_of(a.groups, a.F));
-    if (a.gated && packed)
-      hipLaunchKernelGGL((k_expert_dact_f32<true, true>), grid, block, 0, st, t);
-    else if (a.gated)
-      hipLaunchKernelGGL((k_expert_dact_f32<true, false>), grid, block, 0, st, t);
-    else if (packed)
-      hipLaunchKernelGGL((k_expert_dact_f32<false, true>), grid, block, 0, st, t);
-    else
-      hipLaunchKernelGGL((k_expert_dact_f32<false, false>), grid, block, 0, st, t);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = with_tiles(a.groups, a.F, [&](auto kind) {
+      const dim3 grid = tiles_of<kind>(a.groups, a.F);
+      if (a.gated && packed)
+        hipLaunchKernelGGL((k_expert_dact_f32<kind, true, true>), grid, block, 0, st, t);
+      else if (a.gated)
+        hipLaunchKernelGGL((k_expert_dact_f32<kind, true, false>), grid, block, 0, st, t);
+      else if (packed)
+        hipLaunchKernelGGL((k_expert_dact_f32<kind, false, true>), grid, block, 0, st, t);
+      else
+        hipLaunchKernelGGL((k_expert_dact_f32<kind, false, false>), grid, block, 0, st, t);
+    });
+    if (e != hipSuccess) return e;
     if (a.x_scale && (a.dw_up || a.dw_gate)) {
       float* to = reinterpret_cast<float*>(a.ws + (a.gated ? 3 : 2) * act);
       e = launch_checkpoint_unpack(false, n, a.d, static_cast<const int8_t*>(a.x), a.x_scale, to, st);
@@ -297,12 +344,14 @@ hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st
     if (a.dx) {
       const F32Rows r{a.groups, as_f32(a.w_up), as_f32(a.w_gate), t.du, t.dg, a.d, a.F,
                       static_cast<float*>(a.dx)};
-      const dim3 rows(tiles_of(a.groups, a.d));
-      if (a.gated)
-        hipLaunchKernelGGL((k_expert_rows_f32<false, true>), rows, block, 0, st, r);
-      else
-        hipLaunchKernelGGL((k_expert_rows_f32<false, false>), rows, block, 0, st, r);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
+      e = with_tiles(a.groups, a.d, [&](auto kind) {
+        const dim3 rows = tiles_of<kind>(a.groups, a.d);
+        if (a.gated)
+          hipLaunchKernelGGL((k_expert_rows_f32<kind, false, true>), rows, block, 0, st, r);
+        else
+          hipLaunchKernelGGL((k_expert_rows_f32<kind, false, false>), rows, block, 0, st, r);
+      });
+      if (e != hipSuccess) return e;
     }
   }
   F32Weights w{};
@@ -316,7 +365,7 @@ hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st
     w.M[p] = M;
     w.N[p] = N;
     w.out[p] = static_cast<float*>(out);
-    tiles = std::max(tiles, (unsigned)cdiv(M, F32S::A) * cdiv(N, F32S::B));
+    tiles = std::max(tiles, (unsigned)cdiv(M, 128) * cdiv(N, 128));
   };
   add(t.a, t.dy, a.F, a.d, a.dw_down);
   add(x, t.du, a.d, a.F, a.dw_up);

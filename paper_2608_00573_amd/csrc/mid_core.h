@@ -1,9 +1,9 @@
 // A bf16 matrix core for products whose operands lie in either order: C = A B^T on BM x
 // BN tiles by four wavefronts, two or more blocks a CU.  Not part of the public ABI.
 //
-// An operand is K-contiguous ([rows][K]: 64-element K slices land as 128-byte rows) or
-// runs along K (TR, [K][rows]: a slice is 64 rows of BM or BN columns), and is read out
-// of LDS as it lies or transposed (ds_read_b64_tr_b16).  Slices go straight to LDS by
+// An operand is K-contiguous ([rows][K]: slices of 64 or 32 elements land as rows of 128
+// or 64 bytes) or runs along K (TR, [K][rows]: a slice is 64 or 32 rows of BM or BN
+// columns), and is read out of LDS as it lies or transposed (ds_read_b64_tr_b16).  Slices go straight to LDS by
 // DMA into a ring of ST stages, ST - 1 of them in flight; one barrier a slice.  The
 // MFMAs are 16 x 16 x 32.  An operand may go on in a second array where the first one's
 // K ends.  Fragment reads are inline asm with explicit waits, as in the other cores: the
@@ -60,12 +60,12 @@ struct TileOperand {
   }
 };
 
-// PAIR: A holds two K-contiguous operands in turns of 32 rows, so that a wavefront's
+// PAIR: A holds two K-contiguous operands in turns of SPAN rows, so that a wavefront's
 // fragments 0 .. TM / 2 - 1 are rows of the first and the rest the same rows of the second.
-// KS: elements of K a slice (operands along K may take 32).  OCC: blocks a CU.
+// KS: elements of K a slice.  OCC: blocks a CU.
 template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false, int KS_ = BK, int OCC_ = 2>
 struct MidTile {
-  static constexpr int KS = KS_, OCC = OCC_, SPAN = PAIR_ ? 32 : 0;
+  static constexpr int KS = KS_, OCC = OCC_, SPAN = PAIR_ ? BM_ / 4 : 0;
   static constexpr int BM = BM_, BN = BN_, ST = ST_;
   static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
   static constexpr int THREADS = 256, GM = 2, GN = 2;
@@ -73,8 +73,8 @@ struct MidTile {
   static constexpr int PA = BM * KS / 2048, PB = BN * KS / 2048;  // DMAs a thread
   static constexpr int A_BYTES = BM * KS * 2, STAGE = (BM + BN) * KS * 2, LDS = ST * STAGE;
   static constexpr int ROWS_A = PAIR ? BM / 2 : BM;  // rows of C's A side
-  static_assert(KS == BK || (KS == 32 && ATR && BTR), "rows come in 128-byte slices");
-  static_assert(!PAIR || (WM == 64 && !ATR), "pairs go by 32 rows");
+  static_assert(KS == BK || KS == 32, "slices");
+  static_assert(!PAIR || (!ATR && SPAN == 2048 / KS), "a pair's turns are one DMA each");
   static_assert(ST >= 2 && (PA + PB) * (ST - 2) < 64, "waits");
 };
 
@@ -87,23 +87,32 @@ __device__ __forceinline__ int mid_swz(int k) {
   return k >> 3 & 1;
 }
 
+// 16-byte chunk of a K-contiguous operand's row r where its chunk 0 sits (exclusive or)
+template <int KS>
+__device__ __forceinline__ int row_swz(int r) {
+  return KS == BK ? swz16(r) : r >> 2 & 3;
+}
+
 // this thread's DMA offsets: of a K-contiguous operand's rows (ld elements each, rows
 // past `valid` repeat the last one; span: rows of a pair's turns, or 0) ...
-template <int NP>
+template <int KS = BK, int NP>
 __device__ __forceinline__ void tile_rows(TileOperand<NP>& o, const bf16_t* p, int ld, int valid, int k,
                                          int span = 0) {
-  const int r0 = threadIdx.x >> 3;
+  constexpr int CH = KS / 8, RP = 256 / CH;  // 16-byte chunks of a row, rows of a DMA
+  const int r0 = threadIdx.x / CH, c = (threadIdx.x % CH) ^ row_swz<KS>(r0);
   o.p = reinterpret_cast<const char*>(p);
-  o.inc = 2 * BK;
+  o.inc = 2 * KS;
   o.row = o.cut = 0;
   o.k = k;
   o.kq = 0;
   o.q = o.p1 = o.p;
 #pragma unroll
   for (int u = 0; u < NP; ++u) {
-    const int r = span == 32 ? r0 + 32 * (u >> 1) : span == 64 ? r0 + 32 * (u & 1) + 64 * (u >> 2)
-                                                               : r0 + 32 * u;
-    o.off[u] = ((uint32_t)min(r, valid - 1) * (uint32_t)ld + 8 * ((threadIdx.x & 7) ^ swz16(r0))) * 2;
+    // (the large core's pairs turn every two DMAs)
+    const int r = span == RP       ? r0 + RP * (u >> 1)
+                  : span == 2 * RP ? r0 + RP * (u & 1) + span * (u >> 2)
+                                   : r0 + RP * u;
+    o.off[u] = ((uint32_t)min(r, valid - 1) * (uint32_t)ld + 8 * c) * 2;
   }
 }
 // ... and of one along K, k rows of it from row 0 at p, from column c0 on
@@ -176,19 +185,19 @@ struct MidCore {
     place<T::ATR, T::BM>(la, wm * T::WM);
     place<T::BTR, T::BN>(lb, wn * T::WN);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) lb[ks] += T::A_BYTES;
+    for (int ks = 0; ks < T::KS / 32; ++ks) lb[ks] += T::A_BYTES;
   }
   // LDS offsets of the lane's part of fragment 0
   template <bool TR, int COLS>
   __device__ __forceinline__ void place(uint32_t (&o)[2], int first) const {
     const int fr = lane & 15, hk = lane >> 4;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int ks = 0; ks < T::KS / 32; ++ks) {
       if constexpr (TR) {
         const int k = 32 * ks + 8 * hk + (fr >> 2);
         o[ks] = k * COLS * 2 + (((first >> 4) ^ mid_swz<COLS>(k)) << 5) + 8 * (fr & 3);
       } else {
-        o[ks] = (first + fr) * 128 + (((4 * ks + hk) ^ swz16(fr)) << 4);
+        o[ks] = (first + fr) * T::KS * 2 + (((4 * ks + hk) ^ row_swz<T::KS>(fr)) << 4);
       }
     }
   }
@@ -202,7 +211,7 @@ struct MidCore {
       asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(a), "n"(4 * COLS * 2));
       return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
     } else {
-      return lds_read(at + n * 16 * 128);
+      return lds_read(at + n * 16 * T::KS * 2);
     }
   }
   __device__ __forceinline__ void read(Frags& f, uint32_t stage, int ks) const {

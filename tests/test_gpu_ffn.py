@@ -179,6 +179,10 @@ BLOCKS = [
     (BF16, False, 320, 192, [1, 1300, 0, 800], 2, 3),
     (BF16, True, 128, 448, [256, 1031], 0, 0),
     (BF16, True, 576, 320, [1025], 1, 0),
+    (BF16, True, 64, 1152, [3], 0, 2),             # long K and few tiles: K in pieces,
+    (BF16, True, 128, 2176, [40, 0, 70], 1, 0),
+    (BF16, False, 192, 1024, [100], 0, 0),
+    (BF16, True, 320, 1600, [700], 2, 0),          # ... on the large tiles too
     (BF16, True, 64, 64, [0, 0], 0, 4),            # no rows at all
     (F32, True, 64, 256, [5, 0, 9, 1, 0, 17, 3, 2], 0, 0),
     (F32, False, 64, 256, [8] * 8, 0, 0),
@@ -187,6 +191,9 @@ BLOCKS = [
     (F32, False, 3, 33, [129, 1], 0, 0),
     (F32, True, 130, 300, [260], 0, 0),
     (F32, True, 5, 7, [0], 0, 2),
+    (F32, True, 2, 3, [40, 1], 1, 0),              # no more columns than a lane's load, or one more
+    (F32, False, 259, 515, [300, 20], 0, 1),
+    (F32, True, 700, 900, [1200, 0, 700], 0, 0),   # enough tiles of 128 x 128
 ]
 IDS = ["%s-%s-%dx%d-%s" % ("bf16" if b[0] == BF16 else "f32", "gated" if b[1] else "relu", b[2], b[3],
                           ".".join(map(str, b[4]))) for b in BLOCKS]
