@@ -18,10 +18,15 @@ constexpr int kPackBlock = 32;
 // the scale byte of a block from the bits of its largest magnitude
 __device__ __forceinline__ uint32_t pack_scale(uint32_t max_bits) { return max_bits >> 23; }
 
-// code of v (a block without NaN or infinity: scale < 255).  The step is 2^(scale - 133)
-__device__ __forceinline__ int pack_code(float v, uint32_t scale) {
-  const float q = rintf(__builtin_ldexpf(v, 133 - (int)scale));
-  return (int)fminf(fmaxf(q, -127.f), 127.f);
+// code of v (a block without NaN or infinity: scale < 255) in the lowest byte.  The step
+// is 2^(scale - 133); adding 1.5 2^23 leaves the nearest whole number, ties to even, in
+// the last bits (held to 127 before: that rounds to itself)
+__device__ __forceinline__ uint32_t pack_code_bits(float v, uint32_t scale) {
+  const float q = __builtin_amdgcn_fmed3f(__builtin_ldexpf(v, 133 - (int)scale), -127.f, 127.f);
+  return __float_as_uint(q + 12582912.f);
+}
+__device__ __forceinline__ int8_t pack_code(float v, uint32_t scale) {
+  return (int8_t)pack_code_bits(v, scale);
 }
 // a block's step; NaN where it stands for no number
 __device__ __forceinline__ float pack_step(uint32_t scale) {

@@ -43,7 +43,7 @@ __global__ __launch_bounds__(kThreads) void k_pack_vec(const T* x, int c, long n
       uint2 w;
     } o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.q[i] = s == 255 ? 0 : (int8_t)pack_code(to_f32<T>(v.e[i]), s);
+    for (int i = 0; i < 8; ++i) o.q[i] = s == 255 ? 0 : pack_code(to_f32<T>(v.e[i]), s);
     if (in) *reinterpret_cast<uint2*>(codes + row * c + col) = o.w;
     if ((threadIdx.x & 3) == 0) scale[b] = (uint8_t)s;
   }
@@ -64,7 +64,7 @@ __global__ __launch_bounds__(kThreads) void k_pack_any(const T* x, int c, long n
 #pragma unroll
     for (int o = kPackBlock / 2; o > 0; o >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, o));
     const uint32_t s = pack_scale(top);
-    if (col < c) codes[row * c + col] = s == 255 ? 0 : (int8_t)pack_code(v, s);
+    if (col < c) codes[row * c + col] = s == 255 ? 0 : pack_code(v, s);
     if (threadIdx.x % kPackBlock == 0) scale[b] = (uint8_t)s;
   }
 }

@@ -79,9 +79,12 @@ __device__ __forceinline__ void store_codes(const float (&x)[2][4], bool in, int
   uint32_t w[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    w[k] = 0;
+    uint32_t b[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) w[k] |= (uint32_t)(pack_code(x[k][r], s) & 0xff) << (8 * r);
+    for (int r = 0; r < 4; ++r) b[r] = pack_code_bits(x[k][r], s);
+    // the lowest byte of each
+    w[k] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400u),
+                                 __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400u), 0x05040100u);
     w[k] = s == 255 ? 0u : w[k];
   }
   const auto q = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
