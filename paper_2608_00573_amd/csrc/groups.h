@@ -7,7 +7,7 @@
 namespace trimmoe {
 
 // offsets [E + 1] ascending (NULL: one group of all n rows).  Borders are held to
-// [0, n] and each group to a non-empty range, so no border can lead out of the rows.
+// [0, n] and a group's end to its begin or more, so no border can lead out of the rows.
 // Rows of no group lie before the first border (slot E + 1) and behind the last (slot
 // E); `slots` counts them as groups where a kernel writes zeros there.
 struct Groups {
@@ -51,6 +51,8 @@ struct GroupTiles {
       if (e < slots) first[c] = n + s - t;
       n += __builtin_amdgcn_readlane(s, 63);
     }
+    // (borders that do not ascend could make more of them)
+    n = min(n, g.n / tile + slots);
   }
   // group of row tile t < n, and the tile's number within it
   __device__ __forceinline__ int group(int t, int& within) const {

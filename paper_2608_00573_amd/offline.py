@@ -148,3 +148,42 @@ def balance_routers(routers, hs, targets, epochs: int, lr: float):
         out.append((w32.to(h.dtype), b, losses, counts))
     torch.cuda.synchronize()
     return out
+
+
+def expert_rows(target: torch.Tensor, n_experts: int):
+    """Rows sorted by expert from the routed experts target [Q, k] of a record
+    (an entry outside [0, n_experts): no slot): (row int64 [Q k], the row of
+    target behind each sorted slot, and offsets int32 [n_experts + 1], the borders
+    of the experts' slots; slots of no expert come last)."""
+    e = target.reshape(-1).long()
+    e = torch.where((e >= 0) & (e < n_experts), e, n_experts)
+    e, slot = torch.sort(e, stable=True)
+    borders = torch.arange(n_experts + 1, device=e.device)
+    return slot // target.shape[1], torch.searchsorted(e, borders).to(torch.int32)
+
+
+def fit_experts(w_up, w_gate, w_down, x, y, offsets, epochs: int, lr: float, keep="packed"):
+    """Gradient descent of the experts (weights [E, F, d], [E, F, d] or None, [E, d,
+    F]) on half the mean squared distance of their outputs from y [n, d] over the
+    rows x [n, d] sorted by expert (offsets: see trimmoe_expert_ffn), as of a
+    substitute that is to answer like the expert it stands in for.  Weights are
+    kept in fp32 and used in the rows' dtype; keep: the form in which a step
+    keeps its activations.  Returns ([w_up, w_gate, w_down], losses fp32
+    [epochs]: the loss that each step starts from)."""
+    w32 = [None if w is None else w.float().clone() for w in (w_up, w_gate, w_down)]
+    row = torch.arange(x.shape[0], device=x.device)
+    live = ((row >= offsets[0]) & (row < offsets[-1])).unsqueeze(1)
+    n = live.sum().clamp_min(1)
+    losses = torch.zeros(epochs, dtype=torch.float32, device=x.device)
+    for e in range(epochs):
+        w = [None if v is None else v.to(x.dtype) for v in w32]
+        out, kept = abi.trimmoe_expert_ffn(*w, x, offsets, keep=keep)
+        off = torch.where(live, out.float() - y.float(), 0.0)
+        losses[e] = 0.5 * off.square().sum() / n
+        _, *dw = abi.trimmoe_expert_ffn_backward(*w, x, (off / n).to(x.dtype), kept, offsets,
+                                                 want_dx=False)
+        for v, g in zip(w32, dw):
+            if v is not None:
+                v.add_(g, alpha=-lr)
+    torch.cuda.synchronize()
+    return [None if v is None else v.to(x.dtype) for v in w32], losses

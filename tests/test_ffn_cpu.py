@@ -9,7 +9,7 @@ import pytest
 import torch
 
 from oracle import ffn as X
-from paper_2608_00573_amd import abi
+from paper_2608_00573_amd import abi, offline
 
 NULL, SHAPE, DTYPE, WORKSPACE = -1, -2, -3, -6
 RELU, SWIGLU = abi.ACT_RELU, abi.ACT_SWIGLU
@@ -202,3 +202,12 @@ def test_binding_refuses_cpu_tensors_and_other_types():
         abi.trimmoe_checkpoint_pack(_t(64))
     with pytest.raises(ValueError):
         abi.trimmoe_checkpoint_unpack(_t(2, 32, dtype=torch.int8), _t(2, 2, dtype=torch.uint8))
+
+
+def test_rows_by_expert():
+    target = torch.tensor([[2, 0], [-1, 2], [0, 5], [3, 2]], dtype=torch.int16)
+    row, offsets = offline.expert_rows(target, 4)
+    assert offsets.tolist() == [0, 2, 2, 5, 6] and offsets.dtype == torch.int32
+    assert row.tolist() == [0, 2, 0, 1, 3, 3, 1, 2]  # experts 0, 2, 3; then no expert
+    row, offsets = offline.expert_rows(torch.full((3, 1), -1, dtype=torch.int16), 2)
+    assert offsets.tolist() == [0, 0, 0] and sorted(row.tolist()) == [0, 1, 2]

@@ -13,7 +13,7 @@ import pytest
 import torch
 
 from oracle import ffn as X
-from paper_2608_00573_amd import abi
+from paper_2608_00573_amd import abi, offline
 from synthgen.rng import normal_f32
 
 pytestmark = pytest.mark.gpu
@@ -222,6 +222,43 @@ def test_rows_in_8_bits(dtype):
     x8 = abi.trimmoe_checkpoint_pack(b.xd)
     x = X.unpack(x8.codes.cpu().numpy(), x8.scale.cpu().numpy())
     b.check_backward(b.backward(kept, x=x8), _kept_np(kept), x=x)
+
+
+@pytest.mark.parametrize("dtype,E", [(BF16, 65), (BF16, 200), (BF16, 256), (F32, 130)])
+def test_many_experts(dtype, E):
+    """More experts than a wavefront has lanes, with and without rows, loads of all sizes."""
+    r = np.random.default_rng(E)
+    sizes = r.integers(0, 9, size=E) * (r.random(E) < 0.7)
+    sizes[[3, E - 2]] = 150, 70
+    b = Block(50 + E, dtype, True, 64, 64, sizes.tolist(), 2, 3)
+    y, kept = b.forward("packed")
+    b.check_forward(y, kept, "packed")
+    b.check_backward(b.backward(kept), _kept_np(kept))
+
+
+def test_many_rows_of_many_experts():
+    """... on the large tiles."""
+    r = np.random.default_rng(9)
+    sizes = r.integers(0, 700, size=70)
+    sizes[r.random(70) < 0.2] = 0
+    sizes[5] = 70 * 260  # (260 rows an expert on average and more)
+    b = Block(51, BF16, False, 64, 64, sizes.tolist(), 1, 2)
+    assert b.n >= 256 * 70
+    y, kept = b.forward("full")
+    b.check_forward(y, kept, "full")
+    b.check_backward(b.backward(kept), _kept_np(kept))
+
+
+def test_borders_that_do_not_ascend_stay_within_the_rows():
+    """Unspecified results, but no row outside x is touched and the call ends."""
+    b = Block(52, BF16, True, 64, 128, [200, 300, 100])
+    b.offd.copy_(torch.tensor([500, -7, 600, 2 ** 31 - 1], dtype=torch.int32))
+    y, kept = b.forward("packed")
+    got = b.backward(kept)
+    b.offd.copy_(torch.tensor([600, 400, 300, 0], dtype=torch.int32))
+    b.forward(None)
+    torch.cuda.synchronize()
+    assert y.shape == (600, 64) and got[0].shape == (600, 64)
 
 
 def test_one_expert_without_borders():
@@ -495,3 +532,55 @@ def test_checkpoint_past_32_bit_offsets(c):
         assert np.array_equal(p.codes[rows].cpu().numpy(), codes)
         assert np.array_equal(p.scale[rows].cpu().numpy(), scale)
         assert np.array_equal(_np(back[rows]), X.unpack(codes, scale))
+
+
+# ------------------------------------------------------------- together --
+def test_experts_fitted_to_rows_of_a_record():
+    """Rows sorted from a record, a step of the descent against the oracle's
+    gradient, and the loss that it reports."""
+    Q, k, E, d, F = 60, 2, 5, 41, 97
+    r = np.random.default_rng(7)
+    target = torch.from_numpy(r.integers(-1, E - 1, size=(Q, k)).astype(np.int16)).to(DEV)
+    h, _ = _mat(31, 1, (Q, d), 1.0, F32)
+    row, offsets = offline.expert_rows(target, E)
+    x = h.to(DEV)[row].contiguous()
+    w = [_mat(31, 2 + i, s, s[2] ** -0.5, F32) for i, s in enumerate(((E, F, d), (E, F, d), (E, d, F)))]
+    y, yn = _mat(31, 9, (Q * k, d), 1.0, F32)
+    wd = [v[0].to(DEV) for v in w]
+    lr = 0.5
+    got, losses = offline.fit_experts(*wd, x, y.to(DEV), offsets, 1, lr, keep="full")
+    off, xn = offsets.cpu().numpy(), _np(x)
+    out, u, g = X.forward(w[0][1], w[1][1], w[2][1], xn, off)
+    n = int(off[-1])
+    err = np.where(np.arange(Q * k)[:, None] < n, out - yn, 0.0)
+    want = X.backward(w[0][1], w[1][1], w[2][1], xn, err / n, u, g, off)
+    # every chain of fp32 operations here has fewer than 2000 terms and factors of
+    # size 1 or less on average: 2^11 u of the largest entry is their worst case
+    for a, b, dw in zip(got, w, want[1:]):
+        np.testing.assert_allclose(_np(a), b[1] - lr * dw, rtol=0, atol=2 ** 11 * U * np.abs(b[1]).max())
+    assert abs(float(losses[0]) - 0.5 * (err ** 2).sum() / n) <= 2 ** 11 * U * 0.5 * (err ** 2).sum() / n
+    assert torch.equal(got[0][E - 1], wd[0][E - 1])  # an expert without rows stays
+    runs = [offline.fit_experts(*[v.to(BF16) for v in wd_], xx.to(BF16), yy, offsets, 3, lr)
+            for wd_, xx, yy in [([v.new_zeros(E, 64, 64) + 0.01 for v in wd],
+                                 torch.ones(Q * k, 64, device=DEV), torch.ones(Q * k, 64, device=DEV))] * 2]
+    for p, q in zip(runs[0][0], runs[1][0]):
+        assert torch.equal(p, q) and torch.isfinite(p.float()).all()
+
+
+def test_activations_of_a_stack_put_away_between_forward_and_backward():
+    """Two blocks in a row: forward keeping everything in 8 bits (rows too), then
+    backward in turn; both gradients are the oracle's of the kept values."""
+    blocks = [Block(40 + i, BF16, True, 128, 192, [33, 0, 64], 0, 4) for i in range(2)]
+    kept, rows, x = [], [], blocks[0].xd
+    for b in blocks:
+        b.xd = x
+        rows.append(abi.trimmoe_checkpoint_pack(x))
+        y, k = b.forward("packed")
+        kept.append(k)
+        x = x + y
+    dy = blocks[1].dyd
+    for b, k, r8 in reversed(list(zip(blocks, kept, rows))):
+        b.dyd, b.dy = dy, (dy, _np(dy))
+        got = b.backward(k, x=r8)
+        b.check_backward(got, _kept_np(k), x=X.unpack(r8.codes.cpu().numpy(), r8.scale.cpu().numpy()))
+        dy = dy + got[0]
