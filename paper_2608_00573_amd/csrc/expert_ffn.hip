@@ -9,6 +9,14 @@
 // the products), then dx, then all weight gradients in one kernel.
 // A tile's A side is the contiguous side of its result, so that a lane holds 4
 // consecutive elements of a row and results leave the registers in 16-byte pieces.
+//
+// Rows are cut in tiles of 32, 128 or 256 by their number a group (rows_kind): the large-
+// group core has the least LDS and L2 traffic an MFMA, but its tiles waste half a tile of
+// rows a group and leave their registers with nothing else on the CU.  16384 rows over 60
+// experts (2048 x 1408), 128-row tiles and 256: up and gate 350 and 330 us, y 170 and 157,
+// dx 313 and 280, da 233 and 345 (its epilogue reads and writes 5 values an element); 8192
+// rows over 8 experts (4096 x 14336), 128 and 256: da 1368 and 1225 us, and in 256 x 128
+// tiles of 32-deep slices and 256: up and gate 2400 and 1890, y 1480 and 1040, dx 2620 and 1980.
 #include "expert_ffn.h"
 
 #include <algorithm>
@@ -105,7 +113,11 @@ struct UpArgs {
   uint8_t *up_scale, *gate_scale;
 };
 
-// A tile's first loads go out before the tile before it leaves its registers.
+// A tile's first loads go out before the tile before it leaves its registers.  Bound by
+// the MFMAs at the clock that the power limit leaves and, beside them, the activation and
+// the codes of kept values (8192 rows, 4096 x 14336, kept in 8 bits: 1.89 ms, 1.02 PFLOP/s, a
+// fifth of it the epilogue), with few rows by reading the weights (64 rows over 8 experts:
+// 1.88 GB in 320 us, 5.9 TB/s).
 template <class C, bool GATED, int KEEP>
 __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
   using T = typename C::T;
@@ -435,6 +447,9 @@ struct KeptRow {
   }
 };
 
+// Bound by the MFMAs and by memory in turns (8192 rows, 4096 x 14336: 1.22 ms, of which 705
+// MB written and 240 read take 0.2 to 0.4), with few rows by reading w_down (48 rows over
+// 8 experts: 0.94 GB in 240 us, 3.9 TB/s: the columns of a tile are 256 bytes of each row).
 template <class C, bool GATED, bool PACKED>
 __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
   using T = typename C::T;
@@ -517,6 +532,14 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
 
 // Weight gradients: of group e and product p, out [N, M] = B^T A over the group's rows
 // (dWd: A = a, B = dy; dWu, dWg: A = x, B = du, dg).  A group without rows gets zeros.
+// K is a group's rows, few slices a tile, so what is between two tiles decides: the next
+// tiles' loads are in flight throughout, two blocks a CU fill in for each other, and
+// finding the next tile takes no division.  Tiles of 256 x 128 in 32-deep slices read the
+// least LDS an MFMA that two blocks a CU leave room for.  16384 rows over 60 experts (2048
+// x 1408): 540 us (128 x 128 tiles, 64-deep, a block a tile 984, blocks that stay 680, in
+// 32-deep slices 690; the large-group core 665 to 740); 8192 rows over 8 experts (4096 x
+// 14336): 2.87 ms (1.0 PFLOP/s; the large-group core 2.98); 48 rows: 600 us, 2.8 GB written
+// at 4.7 TB/s (the 128 x 128 tiles 818 to 1025).
 struct WeightArgs {
   Groups groups;
   int n_prod;
@@ -770,7 +793,8 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st) {
   const bf16_t* x = as_bf16(a.x);
   if (n > 0) {
     if (a.gated)
-      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<true, true>(t, a.n_cu, st) : launch_dact<true, false>(t, a.n_cu, st);
+      e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<true, true>(t, a.n_cu, st)
+                                        : launch_dact<true, false>(t, a.n_cu, st);
     else
       e = a.keep == TRIMMOE_KEEP_PACKED ? launch_dact<false, true>(t, a.n_cu, st)
                                         : launch_dact<false, false>(t, a.n_cu, st);

@@ -8,6 +8,12 @@
 // MFMAs are 16 x 16 x 32.  An operand may go on in a second array where the first one's
 // K ends.  Fragment reads are inline asm with explicit waits, as in the other cores: the
 // compiler would wait for every DMA before each of them.
+//
+// Its bound is LDS: a 128 x 128 tile moves 96 KB in and out (768 cycles) for a 64-deep
+// slice of 512 cycles of MFMAs a SIMD, a 256 x 128 tile 72 KB (576 cycles) for a 32-deep
+// one of 512.  64-byte rows of K-contiguous operands cost more than that saves (up and
+// gate of 16384 rows over 60 experts: 350 us in 128 x 128 tiles, 378 in 256 x 128), so the
+// larger tiles are for operands along K.
 #pragma once
 
 #include "mfma_core.h"
