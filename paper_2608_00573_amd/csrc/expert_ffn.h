@@ -35,7 +35,8 @@ hipError_t launch_expert_ffn_backward(const ExpertFfnArgs& a, hipStream_t st);
 inline size_t ffn_align(size_t x) { return (x + 255) & ~(size_t)255; }
 inline size_t ffn_array(int n, int cols, int elem) { return ffn_align((size_t)n * cols * elem); }
 
-// the fp32 side
+// the fp32 side; bytes of the sums of K's pieces of n rows times M columns over K
+size_t row_parts_f32(const Groups& g, int M, long K);
 hipError_t launch_expert_ffn_f32(const ExpertFfnArgs& a, hipStream_t st);
 hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st);
 

@@ -727,13 +727,15 @@ size_t expert_ffn_ws(bool bf16, bool gated, int keep, int E, int d, int F, int n
   const size_t act = ffn_array(n, F, bf16 ? 2 : 4);
   if (bf16) return act + row_parts(Groups{nullptr, E, n}, d, F / BK);
   // (fp32 pre-activations are packed by a launch of their own)
-  return act + (keep == TRIMMOE_KEEP_PACKED ? (gated ? 2 : 1) * act : 0);
+  return act + (keep == TRIMMOE_KEEP_PACKED ? (gated ? 2 : 1) * act : 0) +
+         row_parts_f32(Groups{nullptr, E, n}, d, F);
 }
 
 size_t expert_ffn_backward_ws(bool bf16, bool gated, bool x_packed, int E, int d, int F, int n) {
   const int elem = bf16 ? 2 : 4;
   return (gated ? 3 : 2) * ffn_array(n, F, elem) + (x_packed ? ffn_array(n, d, elem) : 0) +
-         (bf16 ? row_parts(Groups{nullptr, E, n}, d, F / BK * (gated ? 2 : 1)) : 0);
+         (bf16 ? row_parts(Groups{nullptr, E, n}, d, F / BK * (gated ? 2 : 1))
+               : row_parts_f32(Groups{nullptr, E, n}, d, (gated ? 2l : 1l) * F));
 }
 
 hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {

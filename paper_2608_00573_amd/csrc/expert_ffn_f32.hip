@@ -142,13 +142,20 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_up_f32(F32Up a) {
   });
 }
 
-// out [n, M]: y = a Wd^T (AK: Wd K-contiguous) or dx = du Wu + dg Wg
+// out [n, M]: y = a Wd^T (AK: Wd K-contiguous) or dx = du Wu + dg Wg.  Grid y: pieces of
+// K (of both products in a row) into slices of their own, where tiles are few (forward of
+// 1 row of 2048 x 5632, 16 tiles of y: 174 us, 89 with y in 16 pieces).
 struct F32Rows {
   Groups groups;
   const float *w, *w2, *b, *b2;
   int M, K;
-  float* out;
+  float* out;  // [pieces][n, M]
 };
+
+// K of a piece
+__host__ __device__ inline long piece_of(long K, int pieces) {
+  return ((K + pieces - 1) / pieces + f32p::KS - 1) / f32p::KS * f32p::KS;
+}
 
 template <int KIND, bool AK, bool TWO>
 __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a) {
@@ -158,11 +165,14 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a)
   F32Sums<KIND, AK> t(at, a.M), t2(at, a.M);
   if (at.e < a.groups.E) {
     const size_t w0 = (size_t)at.e * a.M * a.K, ld = AK ? a.K : a.M;
-    f32_product<KIND>(Operand<AK>{a.w + w0, ld, a.M, a.K}, Operand<true>{a.b, (size_t)a.K, at.end, a.K},
-                      at.m0, at.r0, 0, a.K, lds, t);
-    if constexpr (TWO)
+    const long all = (TWO ? 2l : 1l) * a.K, per = piece_of(all, gridDim.y);
+    const long k0 = min(per * blockIdx.y, all), k1 = min(k0 + per, all);
+    if (k0 < a.K)
+      f32_product<KIND>(Operand<AK>{a.w + w0, ld, a.M, a.K}, Operand<true>{a.b, (size_t)a.K, at.end, a.K},
+                        at.m0, at.r0, (int)k0, (int)min(k1, (long)a.K), lds, t);
+    if (TWO && k1 > a.K)
       f32_product<KIND>(Operand<AK>{a.w2 + w0, ld, a.M, a.K}, Operand<true>{a.b2, (size_t)a.K, at.end, a.K},
-                        at.m0, at.r0, 0, a.K, lds, t2);
+                        at.m0, at.r0, (int)max(k0 - a.K, 0l), (int)(k1 - a.K), lds, t2);
   }
   each(t, at.end, a.M, [&](int row, int c, int n, auto take) {
     float v[4] = {}, v2[4] = {};
@@ -170,7 +180,7 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a)
     if constexpr (TWO) take(t2, v2);
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = TWO ? v[r] + v2[r] : v[r];
-    put4(a.out + (size_t)row * a.M + c, v, n);
+    put4(a.out + ((size_t)blockIdx.y * a.groups.n + row) * a.M + c, v, n);
   });
 }
 
@@ -266,22 +276,55 @@ dim3 tiles_of(const Groups& g, int M) {
   using T = f32p::Tile<KIND>;
   return dim3((unsigned)(row_tiles_most(g.n, g.E, T::B) * cdiv(M, T::A)));
 }
+// tiles of A x B of rows times M columns, about
+long tiles_about(const Groups& g, int M, int A, int B) {
+  return std::max(1l, ((long)g.n / B + std::min(g.E, g.n)) * cdiv(M, A));
+}
+bool small_tiles(const Groups& g, int M) {
+  using T = f32p::Tile<f32p::kSquare>;
+  return M >= 2 && (g.n <= 64l * g.E || tiles_about(g, M, T::A, T::B) < 256);
+}
 // f(integral constant of the tiles' kind) for rows times M columns: 128 x 128 tiles, or
-// 128 columns x 32 rows straight from memory where those leave CUs idle (a lane's loads
-// of an operand along K take two columns at least)
+// 128 columns x 32 rows straight from memory for few rows an expert and where the others
+// leave CUs idle (a lane's loads of an operand along K take two columns at least).  56 rows
+// over 8 experts of 4096 x 14336: 1672 us in 128 x 128 tiles, 1167 in these
 template <typename F>
 hipError_t with_tiles(const Groups& g, int M, F f) {
-  using T = f32p::Tile<f32p::kSquare>;
-  const long tiles = ((long)g.n / T::B + std::min(g.E, g.n)) * cdiv(M, T::A);
-  if (tiles < 256 && M >= 2)
+  if (small_tiles(g, M))
     f(std::integral_constant<int, f32p::kSmall>());
   else
     f(std::integral_constant<int, f32p::kSquare>());
   return hipGetLastError();
 }
+// pieces of K of small tiles: a block a CU, 256 of K each at least
+int pieces_f32(const Groups& g, int M, long K) {
+  using T = f32p::Tile<f32p::kSmall>;
+  if (!small_tiles(g, M)) return 1;
+  return (int)std::max(1l, std::min({256 / tiles_about(g, M, T::A, T::B), K / 256, 16l}));
+}
+// y or dx
+template <bool AK, bool TWO>
+hipError_t launch_rows_f32(F32Rows r, float* part, hipStream_t st) {
+  const int pieces = pieces_f32(r.groups, r.M, (TWO ? 2l : 1l) * r.K);
+  float* out = r.out;
+  if (pieces > 1) r.out = part;
+  hipError_t e = with_tiles(r.groups, r.M, [&](auto kind) {
+    dim3 grid = tiles_of<kind>(r.groups, r.M);
+    grid.y = pieces;
+    hipLaunchKernelGGL((k_expert_rows_f32<kind, AK, TWO>), grid, dim3(f32p::THREADS), 0, st, r);
+  });
+  if (e == hipSuccess && pieces > 1)
+    e = launch_sum_parts(part, pieces, (size_t)r.groups.n * r.M, out, st);
+  return e;
+}
 const float* as_f32(const void* p) { return static_cast<const float*>(p); }
 
 }  // namespace
+
+size_t row_parts_f32(const Groups& g, int M, long K) {
+  const int p = pieces_f32(g, M, K);
+  return p > 1 ? ffn_align((size_t)p * g.n * M * 4) : 0;
+}
 
 hipError_t launch_expert_ffn_f32(const ExpertFfnArgs& a, hipStream_t st) {
   const int n = a.groups.n;
@@ -310,9 +353,8 @@ hipError_t launch_expert_ffn_f32(const ExpertFfnArgs& a, hipStream_t st) {
     e = launch_checkpoint_pack(false, n, a.F, u.gate, static_cast<int8_t*>(a.gate), a.gate_scale, st);
   if (e != hipSuccess) return e;
   const F32Rows r{a.groups, as_f32(a.w_down), nullptr, u.a, nullptr, a.d, a.F, static_cast<float*>(a.y)};
-  return with_tiles(a.groups, a.d, [&](auto kind) {
-    hipLaunchKernelGGL((k_expert_rows_f32<kind, true, false>), tiles_of<kind>(a.groups, a.d), block, 0, st, r);
-  });
+  return launch_rows_f32<true, false>(
+      r, reinterpret_cast<float*>(a.ws + (packed ? (a.gated ? 3 : 2) : 1) * act), st);
 }
 
 hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st) {
@@ -347,13 +389,9 @@ hipError_t launch_expert_ffn_backward_f32(const ExpertFfnArgs& a, hipStream_t st
     if (a.dx) {
       const F32Rows r{a.groups, as_f32(a.w_up), as_f32(a.w_gate), t.du, t.dg, a.d, a.F,
                       static_cast<float*>(a.dx)};
-      e = with_tiles(a.groups, a.d, [&](auto kind) {
-        const dim3 rows = tiles_of<kind>(a.groups, a.d);
-        if (a.gated)
-          hipLaunchKernelGGL((k_expert_rows_f32<kind, false, true>), rows, block, 0, st, r);
-        else
-          hipLaunchKernelGGL((k_expert_rows_f32<kind, false, false>), rows, block, 0, st, r);
-      });
+      float* part = reinterpret_cast<float*>(a.ws + (a.gated ? 3 : 2) * act +
+                                             (a.x_scale ? ffn_array(n, a.d, 4) : 0));
+      e = a.gated ? launch_rows_f32<false, true>(r, part, st) : launch_rows_f32<false, false>(r, part, st);
       if (e != hipSuccess) return e;
     }
   }

@@ -404,7 +404,10 @@ __device__ __forceinline__ void f32_stream(const Operand<AK>& A, const Operand<t
     else
       f32_stream_of<2, 4>(A, B, k0, k_end, t);
   } else if constexpr (KIND == f32p::kSmall) {
-    f32_stream_of<2, 6>(A, B, k0, k_end, t);
+    if (t.nb == 1)
+      f32_stream_of<1, 6>(A, B, k0, k_end, t);
+    else
+      f32_stream_of<2, 6>(A, B, k0, k_end, t);
   } else {
     if (t.nb == 3)
       f32_stream_of<3, 4>(A, B, k0, k_end, t);

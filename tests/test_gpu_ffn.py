@@ -194,6 +194,8 @@ BLOCKS = [
     (F32, True, 2, 3, [40, 1], 1, 0),              # no more columns than a lane's load, or one more
     (F32, False, 259, 515, [300, 20], 0, 1),
     (F32, True, 700, 900, [1200, 0, 700], 0, 0),   # enough tiles of 128 x 128
+    (F32, True, 33, 1500, [3], 1, 2),              # long K and few tiles: K in pieces
+    (F32, False, 130, 1111, [17, 0, 40], 0, 0),
 ]
 IDS = ["%s-%s-%dx%d-%s" % ("bf16" if b[0] == BF16 else "f32", "gated" if b[1] else "relu", b[2], b[3],
                           ".".join(map(str, b[4]))) for b in BLOCKS]
