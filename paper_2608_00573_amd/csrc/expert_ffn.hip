@@ -367,16 +367,28 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
 
 // 8 results, 16 bytes, from the sums of their pieces
 __device__ __forceinline__ void join8(const float* p, size_t step, int pieces, bf16_t* out) {
-  f32x4_t x = *reinterpret_cast<const f32x4_t*>(p), y = *reinterpret_cast<const f32x4_t*>(p + 4);
-  for (int i = 1; i < pieces; ++i) {
-    x += *reinterpret_cast<const f32x4_t*>(p + i * step);
-    y += *reinterpret_cast<const f32x4_t*>(p + i * step + 4);
+  // (8 pieces at most, all loads in flight; one that is missing: the first again, unused)
+  f32x4_t v[8], w[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float* q = p + (i < pieces ? i : 0) * step;
+    v[i] = *reinterpret_cast<const f32x4_t*>(q);
+    w[i] = *reinterpret_cast<const f32x4_t*>(q + 4);
   }
+  f32x4_t x = v[0], y = w[0];
+#pragma unroll
+  for (int i = 1; i < 8; ++i)
+    if (i < pieces) {
+      x += v[i];
+      y += w[i];
+    }
   *reinterpret_cast<u32x4_t*>(out) = u32x4_t{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
                                              pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
 }
 
-// The tail's tiles, 32 rows a block; grid.x as k_expert_rows had it
+// The tail's tiles, 8 rows a block (32 of them: 29 us for 24 tiles in 8 pieces); grid.x as
+// k_expert_rows had it
+constexpr int kJoinRows = 8;
 __global__ __launch_bounds__(256) void k_join_tail(RowsArgs a, int slices) {
   const GroupTiles tiles(a.groups, a.groups.E + 2, big::BN);
   const int n_ct = (a.M + big::BM - 1) / big::BM, nx = min(kXcd, (int)gridDim.x), x = blockIdx.x % nx;
@@ -387,11 +399,10 @@ __global__ __launch_bounds__(256) void k_join_tail(RowsArgs a, int slices) {
   if (!tail.cut() || S.i0 >= tail.tiles) return;
   const RowTile at(tiles, a.groups, S, S.tb + tail.full * S.bx + S.i0, big::BN, big::BM);
   constexpr size_t SLOT = (size_t)big::BM * big::BN;
-  const int c = 8 * (threadIdx.x & 31);
-  for (int r = 32 * blockIdx.y + (threadIdx.x >> 5); r < 32 * ((int)blockIdx.y + 1); r += 8)
-    if (r < at.valid && at.c0 + c < a.M)
-      join8(a.part + (size_t)blockIdx.x * SLOT + r * big::BM + c, (size_t)nx * tail.tiles * SLOT,
-            tail.pieces, a.out + (size_t)(at.r0 + r) * a.M + at.c0 + c);
+  const int c = 8 * (threadIdx.x & 31), r = kJoinRows * blockIdx.y + (threadIdx.x >> 5);
+  if (r < at.valid && at.c0 + c < a.M)
+    join8(a.part + (size_t)blockIdx.x * SLOT + r * big::BM + c, (size_t)nx * tail.tiles * SLOT, tail.pieces,
+          a.out + (size_t)(at.r0 + r) * a.M + at.c0 + c);
 }
 
 __global__ __launch_bounds__(256) void k_join_slices(const float* part, int splits, size_t n, bf16_t* out) {
@@ -605,12 +616,21 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a)
 }
 
 // --------------------------------------------------------------- launching --
-// How the rows are cut: kFew 32-row tiles (groups of up to that many rows on average),
-// kMid 128-row tiles, kLarge the large-group core's 256.
+// How the rows are cut: kFew 32-row tiles (groups of up to that many rows on average, or
+// too few larger tiles), kMid 128-row tiles, kLarge the large-group core's 256 (groups of
+// `large` rows on average, and tiles for most CUs; fewer where their K can be cut).  cols:
+// columns of the tiles' A side.  us, by the rows alone and so (d 2048, F 5632, forward
+// and gradient): 64 rows 43 and 28, 71 and 50; 110 rows 45 and 35, 78 and 59; 1736 rows over
+// 4 experts of 640 x 192: 35 and 19, 57 and 41; 959 over 2 of 448 x 3264: 85 and 30.
 enum Rows { kFew, kMid, kLarge };
-Rows rows_kind(const Groups& g, long large) {
+constexpr long kLargeTiles = 160, kLargeCutTiles = 32, kMidTiles = 192;
+Rows rows_kind(const Groups& g, long large, int cols, bool cut) {
+  const auto tiles = [&](int rows, int width) {
+    return ((long)g.n / rows + std::min(g.E, g.n)) * cdiv(cols, width);
+  };
   if ((long)g.n <= 32l * g.E) return kFew;
-  return (long)g.n >= large * g.E ? kLarge : kMid;
+  if ((long)g.n >= large * g.E && tiles(256, 256) >= (cut ? kLargeCutTiles : kLargeTiles)) return kLarge;
+  return tiles(128, 128) >= (cut ? kMidTiles / 8 : kMidTiles) ? kMid : kFew;
 }
 constexpr long kLargeRows = 256, kLargeDactRows = 512;
 
@@ -623,7 +643,7 @@ using CoreOf = std::conditional_t<
 // pieces of K of small tiles of the rows' products (M columns, `slices` of K): as many as
 // two blocks a CU take at once, of 8 slices at least
 int row_splits(const Groups& g, int M, int slices) {
-  const Rows kind = rows_kind(g, kLargeRows);
+  const Rows kind = rows_kind(g, kLargeRows, M, slices >= kTailSlices);
   if (kind == kLarge) return 1;
   const int tile = kind == kFew ? 32 : 128;
   const long tiles = std::max(1l, ((long)g.n / tile + std::min(g.E, g.n)) * cdiv(M, 128));
@@ -632,7 +652,7 @@ int row_splits(const Groups& g, int M, int slices) {
 // bytes of the pieces' sums
 constexpr int kTailBlocks = 256;
 size_t row_parts(const Groups& g, int M, int slices) {
-  if (rows_kind(g, kLargeRows) == kLarge)
+  if (rows_kind(g, kLargeRows, M, slices >= kTailSlices) == kLarge)
     return slices < kTailSlices ? 0 : (size_t)kTailBlocks * big::BM * big::BN * 4;
   const int s = row_splits(g, M, slices);
   return s > 1 ? ffn_align((size_t)s * g.n * M * 4) : 0;
@@ -666,7 +686,7 @@ dim3 rows_grid(const Groups& g, int cols, int n_cu) {
 
 template <bool GATED, int KEEP>
 hipError_t launch_up(const UpArgs& a, int n_cu, hipStream_t st) {
-  return with_kind(rows_kind(a.groups, kLargeRows), [&](auto kind) {
+  return with_kind(rows_kind(a.groups, kLargeRows, GATED ? 2 * a.F : a.F, false), [&](auto kind) {
     using C = CoreOf<kind, false, false, GATED>;
     hipLaunchKernelGGL((k_expert_up<C, GATED, KEEP>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st, a);
   });
@@ -675,7 +695,7 @@ hipError_t launch_up(const UpArgs& a, int n_cu, hipStream_t st) {
 template <bool ATR>
 hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
   const int slices = a.K / BK * (a.w2 ? 2 : 1);
-  const Rows kind = rows_kind(a.groups, kLargeRows);
+  const Rows kind = rows_kind(a.groups, kLargeRows, a.M, slices >= kTailSlices);
   a.splits = row_splits(a.groups, a.M, slices);
   a.part = reinterpret_cast<float*>(part);
   unsigned blocks = 0;
@@ -695,7 +715,7 @@ hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
   if (e != hipSuccess) return e;
   const size_t n = (size_t)a.groups.n * a.M;
   if (kind == kLarge && slices >= kTailSlices)
-    hipLaunchKernelGGL(k_join_tail, dim3(blocks, big::BN / 32), dim3(256), 0, st, a, slices);
+    hipLaunchKernelGGL(k_join_tail, dim3(blocks, big::BN / kJoinRows), dim3(256), 0, st, a, slices);
   else if (kind != kLarge && a.splits > 1)
     hipLaunchKernelGGL(k_join_slices, dim3((unsigned)((n / 8 + 255) / 256)), dim3(256), 0, st, a.part,
                        a.splits, n, a.out);
@@ -704,7 +724,7 @@ hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
 
 template <bool GATED, bool PACKED>
 hipError_t launch_dact(const DactArgs& a, int n_cu, hipStream_t st) {
-  return with_kind(rows_kind(a.groups, kLargeDactRows), [&](auto kind) {
+  return with_kind(rows_kind(a.groups, kLargeDactRows, a.F, false), [&](auto kind) {
     using C = CoreOf<kind, true, false>;
     hipLaunchKernelGGL((k_expert_dact<C, GATED, PACKED>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st,
                        a);

@@ -175,14 +175,17 @@ BLOCKS = [
     (BF16, True, 192, 128, [129, 200], 0, 1),      # more than a tile of 128 rows
     (BF16, False, 320, 448, [300], 2, 0),
     (BF16, True, 512, 704, [257, 128, 0, 390], 0, 7),
-    (BF16, True, 64, 64, [513], 0, 0),             # groups of many rows: the large tiles
+    (BF16, True, 64, 64, [513], 0, 0),             # groups of many rows
     (BF16, False, 320, 192, [1, 1300, 0, 800], 2, 3),
     (BF16, True, 128, 448, [256, 1031], 0, 0),
     (BF16, True, 576, 320, [1025], 1, 0),
     (BF16, True, 64, 1152, [3], 0, 2),             # long K and few tiles: K in pieces,
     (BF16, True, 128, 2176, [40, 0, 70], 1, 0),
     (BF16, False, 192, 1024, [100], 0, 0),
-    (BF16, True, 320, 1600, [700], 2, 0),          # ... on the large tiles too
+    (BF16, True, 320, 1600, [700], 2, 0),          # ... and more rows
+    (BF16, True, 64, 4096, [2700, 0, 2301], 1, 2),  # enough large tiles: up, da,
+    (BF16, False, 4096, 128, [3000, 2001], 0, 3),  # ... y and dx,
+    (BF16, True, 2048, 2112, [1300], 0, 0),        # ... and those in pieces of K
     (BF16, True, 64, 64, [0, 0], 0, 4),            # no rows at all
     (F32, True, 64, 256, [5, 0, 9, 1, 0, 17, 3, 2], 0, 0),
     (F32, False, 64, 256, [8] * 8, 0, 0),
