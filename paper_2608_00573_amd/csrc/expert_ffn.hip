@@ -107,7 +107,7 @@ __device__ __forceinline__ void store_codes(const float (&x)[2][4], bool in, int
 struct UpArgs {
   Groups groups;
   const bf16_t *w_up, *w_gate, *x;
-  int d, F, keep;
+  int d, F;
   bf16_t* a;  // [n, F]
   void *up, *gate;
   uint8_t *up_scale, *gate_scale;
@@ -296,7 +296,8 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
   constexpr bool LARGE = T::OCC == 1;
   __shared__ __align__(16) char lds[T::LDS];
   const GroupTiles tiles(a.groups, a.groups.E + 2, T::BN);
-  const int n_ct = (a.M + T::BM - 1) / T::BM, one = a.K / T::KS, slices = one * (T::ATR && a.w2 ? 2 : 1);
+  const int n_ct = (a.M + T::BM - 1) / T::BM, one = a.K / T::KS;
+  const int slices = one * (T::ATR && a.w2 ? 2 : 1);
   TileSched S;
   int n = 0;  // the block's tiles, from index S.tb + S.i0 on
   if (!S.init(tiles.n, n_ct, !LARGE && PART ? a.splits : 1, n)) n = 0;
@@ -391,7 +392,8 @@ __device__ __forceinline__ void join8(const float* p, size_t step, int pieces, b
 constexpr int kJoinRows = 8;
 __global__ __launch_bounds__(256) void k_join_tail(RowsArgs a, int slices) {
   const GroupTiles tiles(a.groups, a.groups.E + 2, big::BN);
-  const int n_ct = (a.M + big::BM - 1) / big::BM, nx = min(kXcd, (int)gridDim.x), x = blockIdx.x % nx;
+  const int n_ct = (a.M + big::BM - 1) / big::BM;
+  const int nx = min(kXcd, (int)gridDim.x), x = blockIdx.x % nx;
   TileSched S;
   int ntiles;
   S.init(tiles.n, n_ct, 1, ntiles);
@@ -590,8 +592,10 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a)
     L -= p == 0 ? 0 : p == 1 ? first[1] : first[2];
     // patches of 8 column tiles of the result
     const int n_mt = (N + T::BN - 1) / T::BN, n_nt = (M + T::BM - 1) / T::BM;
-    const int g = uniform((int)((unsigned)L / (unsigned)(8 * n_nt))), w = L - g * 8 * n_nt, gm = min(8, n_mt - 8 * g);
-    const int nt = gm == 8 ? w >> 3 : uniform((int)((unsigned)w / (unsigned)gm)), mt = 8 * g + w - nt * gm;
+    const int g = uniform((int)((unsigned)L / (unsigned)(8 * n_nt))), w = L - g * 8 * n_nt;
+    const int gm = min(8, n_mt - 8 * g);
+    const int nt = gm == 8 ? w >> 3 : uniform((int)((unsigned)w / (unsigned)gm));
+    const int mt = 8 * g + w - nt * gm;
     const int m0 = uniform(nt * T::BM), n0 = uniform(mt * T::BN);
     queue.push({{e, p, m0, n0, k}});
     tile_along<T::BM, T::KS>(core.a, of(a.A, p) + (size_t)r0 * M, M, m0, k);
@@ -768,7 +772,6 @@ hipError_t launch_expert_ffn(const ExpertFfnArgs& a, hipStream_t st) {
   u.x = as_bf16(a.x);
   u.d = a.d;
   u.F = a.F;
-  u.keep = a.keep;
   u.a = reinterpret_cast<bf16_t*>(a.ws);
   u.up = a.up;
   u.gate = a.gate;
