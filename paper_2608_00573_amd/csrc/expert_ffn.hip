@@ -446,11 +446,11 @@ struct KeptRow {
   }
   static __device__ __forceinline__ void values(float (&v)[4], const W& w, uint32_t s) {
     if constexpr (PACKED) {
-      // (code + 128) step - 128 step, exact: the unsigned bytes convert in one step each
+      // (exact at every scale: the whole number before the power of two.  An offset would
+      // be scaled too, and 128 steps of the largest scale are past the range of fp32)
       const float step = pack_step(s);
-      const uint32_t b = w ^ 0x80808080u;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = fmaf((float)(b >> (8 * r) & 0xff), step, -128.f * step);
+      for (int r = 0; r < 4; ++r) v[r] = (float)(int8_t)(w >> (8 * r)) * step;
     } else {
       v[0] = __uint_as_float(w.x << 16);
       v[1] = __uint_as_float(w.x & 0xffff0000u);
