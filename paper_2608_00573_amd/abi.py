@@ -681,6 +681,8 @@ def trimmoe_expert_ffn(w_up: torch.Tensor, w_gate, w_down: torch.Tensor, x: torc
     without w_gate, or None."""
     if keep not in KEEP:
         raise ValueError(f"keep is one of {list(KEEP)}")
+    if not isinstance(x, torch.Tensor):
+        raise ValueError("x: a tensor [n, d] is needed (the gradient alone takes Packed rows)")
     dims = _ffn_args(w_up, w_gate, w_down, x, offsets)
     code, act, E, d, F, n = dims
     dev = w_up.device
@@ -714,6 +716,8 @@ def trimmoe_expert_ffn_backward(w_up: torch.Tensor, w_gate, w_down: torch.Tensor
     dtype) of sum(dy * y) with kept from trimmoe_expert_ffn (tensors or Packed, both
     alike); x: the rows, or their Packed form.  None for one that is not wanted
     (dw_gate: without w_gate)."""
+    if not isinstance(dy, torch.Tensor):
+        raise ValueError("dy: a tensor [n, d] is needed")
     code, act, E, d, F, n = _ffn_args(w_up, w_gate, w_down, dy, offsets)
     dev = w_up.device
     _take("dy", dy, (n, d), w_up.dtype, dev)

@@ -1,0 +1,30 @@
+"""Calls of the feed-forward block's binding that it refuses, with what it says (no call
+below reaches the GPU)."""
+import pytest
+import torch
+
+from paper_2608_00573_amd import abi
+
+
+def _t(*shape, dtype=torch.float32):
+    return torch.zeros(*shape, dtype=dtype)
+
+
+def _packed(n, c):
+    return abi.Packed(_t(n, c, dtype=torch.int8), _t(n, -(-c // 32), dtype=torch.uint8))
+
+
+W = dict(w_up=_t(2, 8, 4), w_gate=_t(2, 8, 4), w_down=_t(2, 4, 8))
+OFFSETS = _t(3, dtype=torch.int32)
+
+
+@pytest.mark.parametrize("x", [_packed(3, 4), tuple(_packed(3, 4)), None])
+def test_the_forward_takes_rows_as_a_tensor_only(x):
+    with pytest.raises(ValueError, match="x.*gradient alone"):
+        abi.trimmoe_expert_ffn(**W, x=x, offsets=OFFSETS)
+
+
+def test_the_gradient_takes_dy_as_a_tensor_only():
+    with pytest.raises(ValueError, match="dy"):
+        abi.trimmoe_expert_ffn_backward(**W, x=_t(3, 4), dy=_packed(3, 4), kept=(_t(3, 8), _t(3, 8)),
+                                        offsets=OFFSETS)
