@@ -165,17 +165,19 @@ def expert_rows(target: torch.Tensor, n_experts: int):
 def fit_experts(w_up, w_gate, w_down, x, y, offsets, epochs: int, lr: float, keep=None):
     """Gradient descent of the experts (weights [E, F, d], [E, F, d] or None, [E, d,
     F]) on half the mean squared distance of their outputs from y [n, d] over the
-    rows x [n, d] sorted by expert (offsets: see trimmoe_expert_ffn), as of a
-    substitute that is to answer like the expert it stands in for.  Weights are
-    kept in fp32 and used in the rows' dtype; keep: the form in which a step
-    keeps its activations, "full" or "packed" (None: packed for bf16 rows, full
-    for fp32, whose precision 8 bits would take).  Returns ([w_up, w_gate,
-    w_down], losses fp32 [epochs]: the loss that each step starts from)."""
+    rows x [n, d] sorted by expert (offsets: see trimmoe_expert_ffn; None: all
+    rows are one expert's), as of a substitute that is to answer like the expert
+    it stands in for.  Weights are kept in fp32 and used in the rows' dtype;
+    keep: the form in which a step keeps its activations, "full" or "packed"
+    (None: packed for bf16 rows, full for fp32, whose precision 8 bits would
+    take).  Returns ([w_up, w_gate, w_down], losses fp32 [epochs]: the loss that
+    each step starts from)."""
     if keep is None:
         keep = "packed" if x.dtype == torch.bfloat16 else "full"
     w32 = [None if w is None else w.float().clone() for w in (w_up, w_gate, w_down)]
     row = torch.arange(x.shape[0], device=x.device)
-    live = ((row >= offsets[0]) & (row < offsets[-1])).unsqueeze(1)
+    live = row >= 0 if offsets is None else (row >= offsets[0]) & (row < offsets[-1])
+    live = live.unsqueeze(1)
     n = live.sum().clamp_min(1)
     losses = torch.zeros(epochs, dtype=torch.float32, device=x.device)
     for e in range(epochs):
