@@ -449,7 +449,7 @@ def _on_stream(t: torch.Tensor, stream):
     """Context in which outputs and workspaces belong to the stream that the
     call runs on (`stream`, or the current one of t's device)."""
     if not t.is_cuda:
-        raise ValueError("the training losses run on GPU tensors")
+        raise ValueError(f"tensors on the GPU are needed, not on {t.device}")
     if stream is not None:
         if stream.device != t.device:
             raise ValueError(f"a stream of {stream.device} for tensors on {t.device}")

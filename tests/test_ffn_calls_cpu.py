@@ -28,3 +28,17 @@ def test_the_gradient_takes_dy_as_a_tensor_only():
     with pytest.raises(ValueError, match="dy"):
         abi.trimmoe_expert_ffn_backward(**W, x=_t(3, 4), dy=_packed(3, 4), kept=(_t(3, 8), _t(3, 8)),
                                         offsets=OFFSETS)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: abi.trimmoe_expert_ffn(**W, x=_t(3, 4), offsets=OFFSETS),
+    lambda: abi.trimmoe_expert_ffn_backward(**W, x=_t(3, 4), dy=_t(3, 4), kept=(_t(3, 8), _t(3, 8)),
+                                            offsets=OFFSETS),
+    lambda: abi.trimmoe_checkpoint_pack(_t(2, 32)),
+    lambda: abi.trimmoe_checkpoint_unpack(*_packed(2, 32)),
+    lambda: abi.trimmoe_head_cross_entropy(_t(5, 4), _t(3, 4), _t(3, dtype=torch.int32)),
+])
+def test_host_tensors_are_refused_by_where_they_are(call):
+    with pytest.raises(ValueError, match="GPU.* not on cpu") as e:
+        call()
+    assert "loss" not in str(e.value)
