@@ -24,6 +24,7 @@ ABI_VERSION = 6   # TRIMMOE_ABI_VERSION this binding is written for
 STATIC_SCRATCH_BYTES = 64 << 20  # TRIMMOE_STATIC_SCRATCH_BYTES
 N_COUNTERS = 16   # per-layer trace counters (row stride of trimmoe_trace.counters)
 TRIMMOE_OK = 0
+TRIMMOE_ERR_SHAPE = -2
 STATUS = {0: "OK", -1: "ERR_NULL", -2: "ERR_SHAPE", -3: "ERR_DTYPE", -4: "ERR_POLICY",
           -5: "ERR_LAYER", -6: "ERR_WORKSPACE", -7: "ERR_HIP"}
 F32, BF16 = 0, 1
@@ -195,6 +196,12 @@ class TrimmoeError(RuntimeError):
 def _check(fn: str, rc: int):
     if rc != TRIMMOE_OK:
         raise TrimmoeError(fn, rc)
+
+
+def _check_sizes(fn: str, dims):
+    """The library takes sizes of 32 bits (ctypes would pass the lower ones of more)."""
+    if max(dims) > 2 ** 31 - 1:
+        raise TrimmoeError(fn, TRIMMOE_ERR_SHAPE)
 
 
 def _ptr(t):
@@ -478,6 +485,7 @@ def _rows_and_weights(w: torch.Tensor, h: torch.Tensor):
 
 @functools.lru_cache(maxsize=1024)
 def _loss_ws_bytes(name: str, dims) -> int:
+    _check_sizes(name, dims)
     n = C.c_size_t(0)
     _check(name + "_workspace_size", getattr(lib(), name + "_workspace_size")(*dims, C.byref(n)))
     return max(n.value, 256)
@@ -620,6 +628,7 @@ def trimmoe_checkpoint_pack(x: torch.Tensor, stream=None) -> Packed:
     if x.dim() != 2 or x.shape[1] < 1 or not x.is_contiguous():
         raise ValueError("a contiguous tensor [n, c] is needed")
     n, c = x.shape
+    _check_sizes("trimmoe_checkpoint_pack", (n, c))
     with _on_stream(x, stream):
         out = _packed_like(n, c, x.device)
         _check("trimmoe_checkpoint_pack",
@@ -635,6 +644,7 @@ def trimmoe_checkpoint_unpack(codes: torch.Tensor, scale: torch.Tensor,
     if codes.dim() != 2 or codes.shape[1] < 1:
         raise ValueError("codes are [n, c]")
     n, c = codes.shape
+    _check_sizes("trimmoe_checkpoint_unpack", (n, c))
     _take_packed("checkpoint", (codes, scale), n, c, codes.device)
     with _on_stream(codes, stream):
         x = torch.empty(n, c, dtype=dtype, device=codes.device)

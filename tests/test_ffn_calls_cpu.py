@@ -42,3 +42,17 @@ def test_host_tensors_are_refused_by_where_they_are(call):
     with pytest.raises(ValueError, match="GPU.* not on cpu") as e:
         call()
     assert "loss" not in str(e.value)
+
+
+@pytest.mark.parametrize("name,dims", [
+    ("trimmoe_expert_ffn", (abi.BF16, abi.ACT_SWIGLU, 4, 64, 128, 2 ** 32 + 10, 0)),
+    ("trimmoe_expert_ffn", (abi.F32, abi.ACT_RELU, 1, 2 ** 32 + 1, 3, 10, 0)),
+    ("trimmoe_expert_ffn_backward", (abi.F32, abi.ACT_RELU, 1, 3, 2 ** 40 + 1, 10, 0)),
+    ("trimmoe_expert_ffn_backward", (abi.F32, abi.ACT_RELU, 2 ** 32 + 1, 3, 4, 10, 0)),
+    ("trimmoe_head_cross_entropy", (abi.F32, 2 ** 32 + 7, 4, 8)),
+    ("trimmoe_balance_loss", (abi.F32, 8, 2, 4, 2 ** 32 + 8)),
+])
+def test_sizes_past_32_bits_are_refused(name, dims):
+    """... and not taken by their lower bits."""
+    with pytest.raises(abi.TrimmoeError, match=name):
+        abi._loss_ws_bytes(name, dims)
