@@ -1,15 +1,15 @@
-// The large-group core (mfma_core.h) on the operands of mid_core.h: either order, a
-// second array where the first one's K ends, and pairs of operands that share their
-// rows.  Not part of the public ABI.
+// The large-group core (mfma_core.h) on the operands of mid_core.h: A in either order, B
+// K-contiguous, a second array where the first one's K ends, and pairs of operands that
+// share their rows.  Not part of the public ABI.
 #pragma once
 
 #include "mid_core.h"
 
 namespace trimmoe {
 
-template <bool ATR_, bool BTR_, bool PAIR_ = false>
+template <bool ATR_, bool PAIR_ = false>
 struct BigTile {
-  static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
+  static constexpr bool ATR = ATR_, BTR = false, PAIR = PAIR_;
   static constexpr int BM = big::BM, BN = big::BN, KS = BK, OCC = 1, SPAN = PAIR ? 64 : 0;
   static constexpr int THREADS = big::THREADS, WM = 128, WN = 128, TM = 8, TN = 8, PA = 8, PB = 8;
   static constexpr int LDS = big::LDS, ROWS_A = PAIR ? BM / 2 : BM;
@@ -73,10 +73,7 @@ struct BigCore {
       L.cols(la, wm);
     else
       L.rows(la, wm);
-    if constexpr (T::BTR)
-      L.cols(lb, wn);
-    else
-      L.rows(lb, wn);
+    L.rows(lb, wn);
   }
   // Every tile runs through its own slices; the next one's first loads (slice 0, B of
   // slice 1 and the first half of its A) go out before a tile leaves its registers.

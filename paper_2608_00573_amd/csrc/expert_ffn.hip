@@ -135,9 +135,9 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_up(UpArgs a) {
     queue.push(at);
     const int k = at.e < a.groups.E ? a.d : 0;
     const size_t w0 = ((size_t)(k ? at.e : 0) * a.F + at.c0) * a.d;
-    tile_rows<T::KS>(core.a, a.w_up + w0, a.d, min(T::ROWS_A, a.F - at.c0), k, T::SPAN);
+    tile_rows(core.a, a.w_up + w0, a.d, min(T::ROWS_A, a.F - at.c0), k, T::SPAN);
     if constexpr (GATED) core.a.p1 = reinterpret_cast<const char*>(a.w_gate + w0);
-    tile_rows<T::KS>(core.b, a.x + (size_t)at.r0 * a.d, a.d, at.valid, k);
+    tile_rows(core.b, a.x + (size_t)at.r0 * a.d, a.d, at.valid, k);
     core.left = max(k / T::KS, 1);
     return true;
   };
@@ -335,8 +335,8 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_rows(RowsArgs a) {
     if constexpr (T::ATR)
       tile_along<T::BM, T::KS>(core.a, w + e0 + (size_t)k0 * a.M, a.M, at.c0, k);
     else
-      tile_rows<T::KS>(core.a, w + e0 + (size_t)at.c0 * a.K + k0, a.K, min(T::BM, a.M - at.c0), k);
-    tile_rows<T::KS>(core.b, (second ? a.b2 : a.b) + b0 + k0, a.K, at.valid, k);
+      tile_rows(core.a, w + e0 + (size_t)at.c0 * a.K + k0, a.K, min(T::BM, a.M - at.c0), k);
+    tile_rows(core.b, (second ? a.b2 : a.b) + b0 + k0, a.K, at.valid, k);
     if (T::ATR && a.w2 && !second) {
       core.a.q = reinterpret_cast<const char*>(a.w2 + e0 + at.c0);
       core.b.q = reinterpret_cast<const char*>(a.b2 + b0);
@@ -479,7 +479,7 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
     const RowTile at(tiles, a.groups, S, S.tb + S.i0 + jl++ * S.bx, T::BN, T::ROWS_A);
     queue.push(at);
     tile_along<T::BM, T::KS>(core.a, a.w_down + (size_t)at.e * a.d * a.F, a.F, at.c0, a.d);
-    tile_rows<T::KS>(core.b, a.dy + (size_t)at.r0 * a.d, a.d, at.valid, a.d);
+    tile_rows(core.b, a.dy + (size_t)at.r0 * a.d, a.d, at.valid, a.d);
     core.left = a.d / T::KS;
     return true;
   };
@@ -638,11 +638,11 @@ Rows rows_kind(const Groups& g, long large, int cols, bool cut) {
 }
 constexpr long kLargeRows = 256, kLargeDactRows = 512;
 
-template <int KIND, bool ATR, bool BTR, bool PAIR = false>
+template <int KIND, bool ATR, bool PAIR = false>
 using CoreOf = std::conditional_t<
-    KIND == kLarge, BigCore<BigTile<ATR, BTR, PAIR>>,
-    std::conditional_t<KIND == kMid, MidCore<MidTile<128, 128, 2, ATR, BTR, PAIR>>,
-                       MidCore<MidTile<128, 32, 3, ATR, BTR, PAIR>>>>;
+    KIND == kLarge, BigCore<BigTile<ATR, PAIR>>,
+    std::conditional_t<KIND == kMid, MidCore<MidTile<128, 128, 2, ATR, false, PAIR>>,
+                       MidCore<MidTile<128, 32, 3, ATR, false, PAIR>>>>;
 
 // pieces of K of small tiles of the rows' products (M columns, `slices` of K): as many as
 // two blocks a CU take at once, of 8 slices at least
@@ -691,7 +691,7 @@ dim3 rows_grid(const Groups& g, int cols, int n_cu) {
 template <bool GATED, int KEEP>
 hipError_t launch_up(const UpArgs& a, int n_cu, hipStream_t st) {
   return with_kind(rows_kind(a.groups, kLargeRows, GATED ? 2 * a.F : a.F, false), [&](auto kind) {
-    using C = CoreOf<kind, false, false, GATED>;
+    using C = CoreOf<kind, false, GATED>;
     hipLaunchKernelGGL((k_expert_up<C, GATED, KEEP>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st, a);
   });
 }
@@ -704,7 +704,7 @@ hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
   a.part = reinterpret_cast<float*>(part);
   unsigned blocks = 0;
   hipError_t e = with_kind(kind, [&](auto kind) {
-    using C = CoreOf<kind, ATR, false>;
+    using C = CoreOf<kind, ATR>;
     dim3 grid = rows_grid<C>(a.groups, a.M, n_cu);
     if (kind == kLarge)
       grid.x = std::min(n_cu, kTailBlocks);
@@ -729,7 +729,7 @@ hipError_t launch_rows(RowsArgs a, char* part, int n_cu, hipStream_t st) {
 template <bool GATED, bool PACKED>
 hipError_t launch_dact(const DactArgs& a, int n_cu, hipStream_t st) {
   return with_kind(rows_kind(a.groups, kLargeDactRows, a.F, false), [&](auto kind) {
-    using C = CoreOf<kind, true, false>;
+    using C = CoreOf<kind, true>;
     hipLaunchKernelGGL((k_expert_dact<C, GATED, PACKED>), rows_grid<C>(a.groups, a.F, n_cu), dim3(256), 0, st,
                        a);
   });

@@ -1,9 +1,9 @@
 // A bf16 matrix core for products whose operands lie in either order: C = A B^T on BM x
 // BN tiles by four wavefronts, two or more blocks a CU.  Not part of the public ABI.
 //
-// An operand is K-contiguous ([rows][K]: slices of 64 or 32 elements land as rows of 128
-// or 64 bytes) or runs along K (TR, [K][rows]: a slice is 64 or 32 rows of BM or BN
-// columns), and is read out of LDS as it lies or transposed (ds_read_b64_tr_b16).  Slices go straight to LDS by
+// An operand is K-contiguous ([rows][K]: slices of 64 elements land as rows of 128 bytes)
+// or runs along K (TR, [K][rows]: a slice is 64 or 32 rows of BM or BN columns), and is read
+// out of LDS as it lies or transposed (ds_read_b64_tr_b16).  Slices go straight to LDS by
 // DMA into a ring of ST stages, ST - 1 of them in flight; one barrier a slice.  The
 // MFMAs are 16 x 16 x 32.  An operand may go on in a second array where the first one's
 // K ends.  Fragment reads are inline asm with explicit waits, as in the other cores: the
@@ -68,10 +68,10 @@ struct TileOperand {
 
 // PAIR: A holds two K-contiguous operands in turns of SPAN rows, so that a wavefront's
 // fragments 0 .. TM / 2 - 1 are rows of the first and the rest the same rows of the second.
-// KS: elements of K a slice.  OCC: blocks a CU.
-template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false, int KS_ = BK, int OCC_ = 2>
+// KS: elements of K a slice (32 where both operands are along K).  OCC: blocks a CU.
+template <int BM_, int BN_, int ST_, bool ATR_, bool BTR_, bool PAIR_ = false, int KS_ = BK>
 struct MidTile {
-  static constexpr int KS = KS_, OCC = OCC_, SPAN = PAIR_ ? BM_ / 4 : 0;
+  static constexpr int KS = KS_, OCC = 2, SPAN = PAIR_ ? BM_ / 4 : 0;
   static constexpr int BM = BM_, BN = BN_, ST = ST_;
   static constexpr bool ATR = ATR_, BTR = BTR_, PAIR = PAIR_;
   static constexpr int THREADS = 256, GM = 2, GN = 2;
@@ -79,7 +79,7 @@ struct MidTile {
   static constexpr int PA = BM * KS / 2048, PB = BN * KS / 2048;  // DMAs a thread
   static constexpr int A_BYTES = BM * KS * 2, STAGE = (BM + BN) * KS * 2, LDS = ST * STAGE;
   static constexpr int ROWS_A = PAIR ? BM / 2 : BM;  // rows of C's A side
-  static_assert(KS == BK || KS == 32, "slices");
+  static_assert(KS == BK || (KS == 32 && ATR && BTR), "slices");
   static_assert(!PAIR || (!ATR && SPAN == 2048 / KS), "a pair's turns are one DMA each");
   static_assert(ST >= 2 && (PA + PB) * (ST - 2) < 64, "waits");
 };
@@ -88,26 +88,19 @@ struct MidTile {
 // the eight rows that 32 lanes read together then touch distinct banks
 template <int COLS>
 __device__ __forceinline__ int mid_swz(int k) {
-  if constexpr (COLS >= 128) return (k & 3) | ((k >> 3 & 1) << 2);
-  if constexpr (COLS == 64) return (k >> 1 & 1) | ((k >> 3 & 1) << 1);
-  return k >> 3 & 1;
-}
-
-// 16-byte chunk of a K-contiguous operand's row r where its chunk 0 sits (exclusive or)
-template <int KS>
-__device__ __forceinline__ int row_swz(int r) {
-  return KS == BK ? swz16(r) : r >> 2 & 3;
+  static_assert(COLS >= 128, "a row of fewer pieces needs another order");
+  return (k & 3) | ((k >> 3 & 1) << 2);
 }
 
 // this thread's DMA offsets: of a K-contiguous operand's rows (ld elements each, rows
 // past `valid` repeat the last one; span: rows of a pair's turns, or 0) ...
-template <int KS = BK, int NP>
+template <int NP>
 __device__ __forceinline__ void tile_rows(TileOperand<NP>& o, const bf16_t* p, int ld, int valid, int k,
                                          int span = 0) {
-  constexpr int CH = KS / 8, RP = 256 / CH;  // 16-byte chunks of a row, rows of a DMA
-  const int r0 = threadIdx.x / CH, c = (threadIdx.x % CH) ^ row_swz<KS>(r0);
+  constexpr int CH = BK / 8, RP = 256 / CH;  // 16-byte chunks of a row, rows of a DMA
+  const int r0 = threadIdx.x / CH, c = (threadIdx.x % CH) ^ swz16(r0);
   o.p = reinterpret_cast<const char*>(p);
-  o.inc = 2 * KS;
+  o.inc = 2 * BK;
   o.row = o.cut = 0;
   o.k = k;
   o.kq = 0;
@@ -203,7 +196,7 @@ struct MidCore {
         const int k = 32 * ks + 8 * hk + (fr >> 2);
         o[ks] = k * COLS * 2 + (((first >> 4) ^ mid_swz<COLS>(k)) << 5) + 8 * (fr & 3);
       } else {
-        o[ks] = (first + fr) * T::KS * 2 + (((4 * ks + hk) ^ row_swz<T::KS>(fr)) << 4);
+        o[ks] = (first + fr) * BK * 2 + (((4 * ks + hk) ^ swz16(fr)) << 4);
       }
     }
   }
@@ -217,7 +210,7 @@ struct MidCore {
       asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(hi) : "v"(a), "n"(4 * COLS * 2));
       return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3));
     } else {
-      return lds_read(at + n * 16 * T::KS * 2);
+      return lds_read(at + n * 16 * BK * 2);
     }
   }
   __device__ __forceinline__ void read(Frags& f, uint32_t stage, int ks) const {
