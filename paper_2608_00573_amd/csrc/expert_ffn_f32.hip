@@ -3,7 +3,11 @@
 // through LDS, or 128 columns x 32 rows straight from memory where those are few.  Bound by
 // the fp32 matrix rate, with few tiles by the chain of a tile's loads (777 rows over 4
 // experts of 768 x 1000: da 38 us, 80 in 128 x 128 tiles; dx 52 and 163; the weights'
-// gradients, 128 x 128 tiles of all experts in one launch, 55).
+// gradients, 128 x 128 tiles of all experts in one launch, 55).  The 32-row tiles sum K in
+// four chains, whose registers are free (one chain and four: forward of 1 row of 2048 x
+// 5632 93 and 95 us, gradient of 9 rows of 3769 x 2870 156 and 146, forward of 3800 rows over
+// 60 experts of 2048 x 1408 1284 and 1264): sums of random signs off by half as much,
+// 5.5e-7 of their norm over K = 4096 (1.1e-6).
 #include <math.h>
 
 #include <algorithm>
@@ -16,6 +20,8 @@ namespace trimmoe {
 namespace {
 
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+constexpr int kChains = 4;
 
 // the block's tile: a group's rows r0 .. (e >= E: rows of no group) times columns from m0
 template <int KIND>
@@ -118,10 +124,11 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_up_f32(F32Up a) {
   if (at.e < a.groups.E) {
     const size_t w0 = (size_t)at.e * a.F * a.d;
     const Operand<true> x{a.x, (size_t)a.d, at.end, a.d};
-    f32_product<KIND>(Operand<true>{a.w_up + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d, lds, u);
+    f32_product<KIND, kChains>(Operand<true>{a.w_up + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d,
+                               lds, u);
     if constexpr (GATED)
-      f32_product<KIND>(Operand<true>{a.w_gate + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0, a.d, lds,
-                        g);
+      f32_product<KIND, kChains>(Operand<true>{a.w_gate + w0, (size_t)a.d, a.F, a.d}, x, at.m0, at.r0, 0,
+                                 a.d, lds, g);
   }
   each(u, at.end, a.F, [&](int row, int c, int n, auto take) {
     const size_t o = (size_t)row * a.F + c;
@@ -168,11 +175,13 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_rows_f32(F32Rows a)
     const long all = (TWO ? 2l : 1l) * a.K, per = piece_of(all, gridDim.y);
     const long k0 = min(per * blockIdx.y, all), k1 = min(k0 + per, all);
     if (k0 < a.K)
-      f32_product<KIND>(Operand<AK>{a.w + w0, ld, a.M, a.K}, Operand<true>{a.b, (size_t)a.K, at.end, a.K},
-                        at.m0, at.r0, (int)k0, (int)min(k1, (long)a.K), lds, t);
+      f32_product<KIND, kChains>(Operand<AK>{a.w + w0, ld, a.M, a.K},
+                                 Operand<true>{a.b, (size_t)a.K, at.end, a.K}, at.m0, at.r0, (int)k0,
+                                 (int)min(k1, (long)a.K), lds, t);
     if (TWO && k1 > a.K)
-      f32_product<KIND>(Operand<AK>{a.w2 + w0, ld, a.M, a.K}, Operand<true>{a.b2, (size_t)a.K, at.end, a.K},
-                        at.m0, at.r0, (int)max(k0 - a.K, 0l), (int)(k1 - a.K), lds, t2);
+      f32_product<KIND, kChains>(Operand<AK>{a.w2 + w0, ld, a.M, a.K},
+                                 Operand<true>{a.b2, (size_t)a.K, at.end, a.K}, at.m0, at.r0,
+                                 (int)max(k0 - a.K, 0l), (int)(k1 - a.K), lds, t2);
   }
   each(t, at.end, a.M, [&](int row, int c, int n, auto take) {
     float v[4] = {}, v2[4] = {};
@@ -209,8 +218,8 @@ __global__ __launch_bounds__(f32p::THREADS, 2) void k_expert_dact_f32(F32Dact a)
   F32At<KIND> at;
   if (!at.init(a.groups, a.groups.E, a.F)) return;
   F32Sums<KIND, false> t(at, a.F);
-  f32_product<KIND>(Operand<false>{a.w_down + (size_t)at.e * a.d * a.F, (size_t)a.F, a.F, a.d},
-                    Operand<true>{a.dy, (size_t)a.d, at.end, a.d}, at.m0, at.r0, 0, a.d, lds, t);
+  f32_product<KIND, kChains>(Operand<false>{a.w_down + (size_t)at.e * a.d * a.F, (size_t)a.F, a.F, a.d},
+                             Operand<true>{a.dy, (size_t)a.d, at.end, a.d}, at.m0, at.r0, 0, a.d, lds, t);
   const int blocks = (a.F + kPackBlock - 1) / kPackBlock;
   each(t, at.end, a.F, [&](int row, int c, int n, auto take) {
     float vd[4] = {}, va[4], vu[4], vg[4];

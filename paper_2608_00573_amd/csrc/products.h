@@ -300,7 +300,10 @@ __device__ __forceinline__ void f32_tile(const Operand<AK>& A, const Operand<BKC
 // otherwise be read from the same few memory channels at a time.  1.2 GB of w (rows of
 // 8 KB) against 7 rows of h: 298 us (4.2 TB/s), 328 without that, 365 through LDS;
 // against 20: 336 and 415 through LDS.
-template <int NB, int DEPTH, int KIND, bool AK>
+// CHAINS: accumulators of an element, for a slice's k in turns, added at the end: an
+// element's rounding errors are those of K / CHAINS additions (a random sum's error goes
+// with their square root).
+template <int NB, int DEPTH, int CHAINS, int KIND, bool AK>
 __device__ __forceinline__ void f32_stream_of(const Operand<AK>& A, const Operand<true>& B, int k0,
                                               int k_end, F32Tile<KIND>& t) {
   constexpr int KS = f32p::KS, NA = f32p::Tile<KIND>::NA;
@@ -348,15 +351,24 @@ __device__ __forceinline__ void f32_stream_of(const Operand<AK>& A, const Operan
       for (int u = 0; u < 4; ++u) x.b[j][u] = v[u];
     }
   };
+  [[maybe_unused]] f32x4_t more[CHAINS][NA][NB];  // (the first chain is t.acc)
+  if constexpr (CHAINS > 1)
+#pragma unroll
+    for (int c = 1; c < CHAINS; ++c)
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) more[c][i][j] = f32x4_t{};
   const auto mma = [&](const Regs& x) {
 #pragma unroll
     for (int u = 0; u < 4; ++u)
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
-        for (int i = 0; i < NA; ++i)
-          t.acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(AK ? x.a[i][u] : x.a[u][i], x.b[j][u],
-                                                             t.acc[i][j], 0, 0, 0);
+        for (int i = 0; i < NA; ++i) {
+          f32x4_t& acc = u % CHAINS ? more[u % CHAINS][i][j] : t.acc[i][j];
+          acc = __builtin_amdgcn_mfma_f32_16x16x4f32(AK ? x.a[i][u] : x.a[u][i], x.b[j][u], acc, 0, 0, 0);
+        }
   };
   if (n > 0) {
     Regs x[DEPTH];
@@ -388,9 +400,15 @@ __device__ __forceinline__ void f32_stream_of(const Operand<AK>& A, const Operan
       for (int u = 0; u < 4; ++u) x.b[j][u] = 4 * q + u < rest ? qb[ob[j] + u] : 0.f;
     mma(x);
   }
+#pragma unroll
+  for (int c = 1; c < CHAINS; ++c)
+#pragma unroll
+    for (int i = 0; i < NA; ++i)
+#pragma unroll
+      for (int j = 0; j < NB; ++j) t.acc[i][j] += more[c][i][j];
 }
 // (as many slices in flight as 168 registers hold)
-template <int KIND, bool AK>
+template <int CHAINS, int KIND, bool AK>
 __device__ __forceinline__ void f32_stream(const Operand<AK>& A, const Operand<true>& B, int k0,
                                            int k_end, F32Tile<KIND>& t) {
   using T = f32p::Tile<KIND>;
@@ -400,29 +418,29 @@ __device__ __forceinline__ void f32_stream(const Operand<AK>& A, const Operand<t
     for (int j = 0; j < T::NB; ++j) t.acc[i][j] = f32x4_t{};
   if constexpr (KIND == f32p::kFewer) {
     if (t.nb == 1)
-      f32_stream_of<1, 4>(A, B, k0, k_end, t);
+      f32_stream_of<1, 4, CHAINS>(A, B, k0, k_end, t);
     else
-      f32_stream_of<2, 4>(A, B, k0, k_end, t);
+      f32_stream_of<2, 4, CHAINS>(A, B, k0, k_end, t);
   } else if constexpr (KIND == f32p::kSmall) {
     if (t.nb == 1)
-      f32_stream_of<1, 6>(A, B, k0, k_end, t);
+      f32_stream_of<1, 6, CHAINS>(A, B, k0, k_end, t);
     else
-      f32_stream_of<2, 6>(A, B, k0, k_end, t);
+      f32_stream_of<2, 6, CHAINS>(A, B, k0, k_end, t);
   } else {
     if (t.nb == 3)
-      f32_stream_of<3, 4>(A, B, k0, k_end, t);
+      f32_stream_of<3, 4, CHAINS>(A, B, k0, k_end, t);
     else
-      f32_stream_of<4, 3>(A, B, k0, k_end, t);
+      f32_stream_of<4, 3, CHAINS>(A, B, k0, k_end, t);
   }
 }
 
 // the product of a tile in the way of its kind
-template <int KIND, bool AK, bool BKC>
+template <int KIND, int CHAINS = 1, bool AK, bool BKC>
 __device__ __forceinline__ void f32_product(const Operand<AK>& A, const Operand<BKC>& B, int r0,
                                             int n0, int k0, int k_end, float* lds,
                                             F32Tile<KIND>& t) {
   if constexpr (f32p::Tile<KIND>::STREAM)
-    f32_stream(A, B, k0, k_end, t);
+    f32_stream<CHAINS>(A, B, k0, k_end, t);
   else
     f32_tile<KIND>(A, B, r0, n0, k0, k_end, lds, t);
 }
