@@ -12,11 +12,8 @@
 //
 // Rows are cut in tiles of 32, 128 or 256 by their number a group (rows_kind): the large-
 // group core has the least LDS and L2 traffic an MFMA, but its tiles waste half a tile of
-// rows a group and leave their registers with nothing else on the CU.  16384 rows over 60
-// experts (2048 x 1408), 128-row tiles and 256: up and gate 350 and 330 us, y 170 and 157,
-// dx 313 and 280, da 233 and 345 (its epilogue reads and writes 5 values an element); 8192
-// rows over 8 experts (4096 x 14336), 128 and 256: da 1368 and 1225 us, and in 256 x 128
-// tiles of 32-deep slices and 256: up and gate 2400 and 1890, y 1480 and 1040, dx 2620 and 1980.
+// rows a group and leave their registers with nothing else on the CU (da's epilogue reads
+// and writes 5 values an element).  Traces of both sides: rows_kind.
 #include "expert_ffn.h"
 
 #include <algorithm>
@@ -549,7 +546,7 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_dact(DactArgs a) {
 // tiles' loads are in flight throughout, two blocks a CU fill in for each other, and
 // finding the next tile takes no division.  Tiles of 256 x 128 in 32-deep slices read the
 // least LDS an MFMA that two blocks a CU leave room for.  16384 rows over 60 experts (2048
-// x 1408): 540 us (128 x 128 tiles, 64-deep, a block a tile 984, blocks that stay 680, in
+// x 1408): 510 to 580 us (128 x 128 tiles, 64-deep, a block a tile 984, blocks that stay 680, in
 // 32-deep slices 690; the large-group core 665 to 740); 8192 rows over 8 experts (4096 x
 // 14336): 2.87 ms (1.0 PFLOP/s; the large-group core 2.98); 48 rows: 600 us, 2.8 GB written
 // at 4.7 TB/s (the 128 x 128 tiles 818 to 1025).
@@ -626,6 +623,25 @@ __global__ __launch_bounds__(256, C::T::OCC) void k_expert_weights(WeightArgs a)
 // columns of the tiles' A side.  us, by the rows alone and so (d 2048, F 5632, forward
 // and gradient): 64 rows 43 and 28, 71 and 50; 110 rows 45 and 35, 78 and 59; 1736 rows over
 // 4 experts of 640 x 192: 35 and 19, 57 and 41; 959 over 2 of 448 x 3264: 85 and 30.
+// 128-row tiles and the large-group core (kernels' us with equal loads; in pieces of K
+// with their sum):
+//   rows an expert           up, gate       y             dx            da
+//   60 x (2048 x 1408)  100  217   255      87   102      165   177     107   164
+//                       150  283   263      121  107      216   180     161   170
+//                       200  293   289      126  110      223   189     167   184
+//                       273  363   392      177  171      318   311     219   265
+//                       400  434   395      218  183      379   327     289   283
+//                       500  447   424      233  189      406   339     312   298
+//   8 x (4096 x 14336)  200  592   555      274  251      535   426     350   305
+//                       400  1022  827      476  371      953   733     606   566
+//                       1024 2057  1625     1041 709      2015  1371    1275  1066
+//   1 x (2048 x 5632)   600  39    57       32   54       46    70      37    72
+//                       1000 68    61       41   67       61    81      46    75
+//                       2047 118   126      74   82       107   113     88    87
+//                       4000 226   190      101  112      185   175     154   174
+// The limits lie where up and gate change over, and da.  What they cost: y and dx of 150 to
+// 255 rows an expert up to a quarter, y and dx of one expert of 1000 rows 26 and 20 us, da
+// of 4000 rows of one expert 20.
 enum Rows { kFew, kMid, kLarge };
 constexpr long kLargeTiles = 160, kLargeCutTiles = 32, kMidTiles = 192;
 Rows rows_kind(const Groups& g, long large, int cols, bool cut) {
@@ -680,8 +696,9 @@ dim3 grid_of(long tiles, int n_cu) {
   return dim3((unsigned)std::min(std::max(tiles, 1l), (long)n_cu * C::T::OCC));
 }
 // ... over row tiles, which take long enough that the hardware deals them out: a block
-// each (but on the large-group core, whose blocks load their next tile early).  16383 rows
-// over 60 experts (2048 x 1408): 466 us, with blocks that stay 480
+// each (but on the large-group core, whose blocks load their next tile early).  60 experts of
+// 2048 x 1408, 100 rows each: up and gate 217 to 229 us, with blocks that stay 233, dx 164 to
+// 174 and 174; 273 rows each: da 222 and 229
 template <class C>
 dim3 rows_grid(const Groups& g, int cols, int n_cu) {
   const long tiles = row_tiles_most(g.n, g.E, C::T::BN) * cdiv(cols, C::T::ROWS_A);
